@@ -189,6 +189,100 @@ ppas_status ppas_rope_kv_append(const ppas_shape* shape, float rope_theta, void*
                                 const int32_t* block_table_host, void* hip_stream);
 
 /*
+ * Rotary positions in their general form (the paper does not describe positional
+ * encoding; the operation is the library's own offer to models that need more than
+ * ppas_rope_kv_append). Pair j < rotary_dim / 2 of a head at position p turns by
+ * a = p w_j, and both results are multiplied by the magnitude m:
+ *   x_a <- m (x_a cos a - x_b sin a),  x_b <- m (x_b cos a + x_a sin a)
+ * with (x_a, x_b) features (j, j + rotary_dim / 2) in the half layout and
+ * (2j, 2j + 1) in the interleaved one. Features from rotary_dim on are copied bit for
+ * bit. With u_j = theta^(-2j / rotary_dim):
+ *   PLAIN   w_j = u_j
+ *   LINEAR  w_j = u_j / factor (positions squeezed into the learned length)
+ *   BASE    w_j = (theta factor^(R / (R - 2)))^(-2j / R), R = rotary_dim (a larger base,
+ *           which leaves the first pair as it is and divides the last by factor; R = 2: u_j)
+ *   BANDS   by turns over the learned length, n_j = original_len u_j / (2 pi): pairs of at
+ *           least `high` turns keep u_j, those of at most `low` get u_j / factor, and
+ *           between them w_j = u_j (s + (1 - s) / factor), s = (n_j - low) / (high - low)
+ *   RAMP    by pair numbers: with d(b) = R ln(original_len / (2 pi b)) / (2 ln theta), the
+ *           pair of b turns, first = max(floor d(high), 0), last = min(ceil d(low), R - 1):
+ *           w_j = u_j (1 - t + t / factor), t = (j - first) / (last - first) kept within
+ *           0..1 (t = 0 up to `first` where last <= first, 1 behind it)
+ * Frequencies and angles are computed in fp64 (whole turns removed), cos and sin in
+ * fp32, the turn in fp32, and results rounded to bf16 nearest-even.
+ */
+enum { PPAS_ROPE_HALF = 0, PPAS_ROPE_INTERLEAVED = 1 };
+enum { PPAS_ROPE_PLAIN = 0, PPAS_ROPE_LINEAR = 1, PPAS_ROPE_BASE = 2, PPAS_ROPE_BANDS = 3, PPAS_ROPE_RAMP = 4 };
+
+typedef struct ppas_rope {
+  int32_t layout;       /* PPAS_ROPE_HALF or PPAS_ROPE_INTERLEAVED */
+  int32_t rotary_dim;   /* features that turn: even, 2..head_dim */
+  int32_t scaling;      /* PPAS_ROPE_PLAIN .. PPAS_ROPE_RAMP */
+  int32_t original_len; /* BANDS, RAMP: the learned length in positions, >= 1 */
+  double theta;         /* finite, > 0 (RAMP: > 1) */
+  double factor;        /* unless PLAIN: finite, > 0 */
+  double low, high;     /* BANDS, RAMP: turns over original_len, 0 < low < high, finite */
+  double magnitude;     /* m, finite and > 0; 0 selects 1 */
+} ppas_rope;
+
+/* w_j in radians per position for every pair of a ppas_rope, to rotary_dim / 2 doubles
+ * (host only, no HIP call). PPAS_EINVAL for a field out of range. */
+ppas_status ppas_rope_frequencies(const ppas_rope* rope, int32_t head_dim, double* out);
+
+/*
+ * Rows of heads turned by given positions: row r < n_rows of x (n_heads heads of
+ * head_dim features each, one after the other, at x + r * x_stride elements) to the
+ * same row of y (y_stride), at position positions_dev[r] (device int32, any value,
+ * negative ones included). bf16. `transposed` turns by -a instead: the gradient of the
+ * turn, and for m = 1 its inverse. x == y with equal strides turns in place; otherwise
+ * the two must not overlap. head_dim is even, 2..256; n_heads 1..65536; strides are at
+ * least n_heads * head_dim (PPAS_EINVAL otherwise; PPAS_EUNSUPPORTED for a larger
+ * head_dim). Pointers need their element's alignment only; bases and strides on 16
+ * bytes, and a rotary_dim that is a multiple of 16 in the half layout, are faster.
+ * n_rows == 0 is a no-op. One launch; it allocates nothing, keeps nothing, and may be
+ * captured into a HIP graph. events may be NULL.
+ */
+ppas_status ppas_rope_rows(const ppas_rope* rope, const void* x, int64_t x_stride, void* y, int64_t y_stride,
+                           const int32_t* positions_dev, int32_t n_rows, int32_t n_heads, int32_t head_dim,
+                           int32_t transposed, const ppas_events* events, void* hip_stream);
+
+/*
+ * A step's new rows as the projection left them: bf16 rows of n_q_heads (q) or
+ * n_kv_heads (k, v) heads of 128 features, at base + row * stride elements. Fused
+ * QKV rows are three pointers into one buffer with one stride.
+ */
+typedef struct ppas_qkv {
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t q_stride, k_stride, v_stride;   /* elements between rows, at least a row's features */
+} ppas_qkv;
+
+/*
+ * As ppas_rope_kv_append, with any ppas_rope and rows at any stride: the queries are
+ * rotated to q_out [T][n_q_heads][128] (the layout ppas_attn_step reads), the rotated
+ * keys and the values go to the pages; the rows themselves are not modified. q_out may
+ * be rows->q where q_stride is n_q_heads * 128 (in place); otherwise it must not overlap
+ * the rows (PPAS_EINVAL, as for strides below a row's features or pools off 16 bytes).
+ * Validation, ownership, streams and errors otherwise as ppas_rope_kv_append.
+ */
+ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope, const ppas_qkv* rows, void* q_out,
+                                 void* k_pages, void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
+                                 const int32_t* block_table_dev, int32_t bt_stride,
+                                 const int32_t* block_table_host, void* hip_stream);
+
+/*
+ * Requests first_seq .. first_seq + n_seqs - 1 of a step hold the same first `len`
+ * positions in the same pages (a system prompt, a document, sampled continuations):
+ * their block-table rows start with the same len / 16 entries. len is a multiple of 16
+ * (whole pages) and at most every member's cached_len; 0 shares nothing. Prefixes of a
+ * step are given in request order and do not overlap.
+ */
+typedef struct ppas_prefix {
+  int32_t first_seq, n_seqs, len;
+} ppas_prefix;
+
+/*
  * Device workspace that ppas_attn_step needs for this step description on the
  * current device, with the automatic planning choices. This sizing call is the
  * library's own (the paper describes no workspace): the workspace holds the
@@ -253,6 +347,38 @@ ppas_status ppas_step_plan_create(const ppas_shape* shape, const ppas_seq* seqs,
                                   const int32_t* block_table_host, int32_t bt_stride,
                                   const ppas_plan_opts* opts, ppas_step_plan** plan);
 
+/*
+ * As ppas_step_plan_create, for a step some of whose requests share prefixes (the
+ * library's own; the paper's requests share nothing). The plan's attention reads a
+ * shared prefix once for all rows of its group, in tiles of matrix instructions that
+ * hold rows of several requests, then each request's own keys, and merges the two by
+ * their log-sum-exp: the results are those of ppas_attn_step but for the order of the
+ * sums. Used are whole blocks of 64 keys of a prefix; requests of more than 64 new
+ * tokens fill tiles of their own and read it for themselves. The pages of a prefix are
+ * taken from its first member's table row. PPAS_EINVAL for a prefix out of range, out of
+ * order, of a length that is no multiple of 16 or longer than a member's cached_len, or,
+ * when block_table_host is not NULL, whose members' entries differ. n_prefixes == 0
+ * (prefixes may be NULL) is ppas_step_plan_create. Used and destroyed like any plan.
+ */
+ppas_status ppas_step_plan_create_shared(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,
+                                         const ppas_prefix* prefixes, int32_t n_prefixes,
+                                         const int32_t* block_table_host, int32_t bt_stride,
+                                         const ppas_plan_opts* opts, ppas_step_plan** plan);
+
+/* As ppas_attn_step and ppas_attn_workspace_bytes, for a step with shared prefixes:
+ * equivalent to ppas_step_plan_create_shared with default options,
+ * ppas_attn_step_planned, and destroying the plan. */
+ppas_status ppas_attn_step_shared(const ppas_shape* shape, void* out, const void* q,
+                                  const void* k_pages, const void* v_pages,
+                                  const ppas_seq* seqs, int32_t n_seqs,
+                                  const ppas_prefix* prefixes, int32_t n_prefixes,
+                                  const int32_t* block_table_dev, int32_t bt_stride,
+                                  const int32_t* block_table_host,
+                                  void* workspace, size_t workspace_bytes, void* hip_stream);
+
+size_t ppas_attn_shared_workspace_bytes(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,
+                                        const ppas_prefix* prefixes, int32_t n_prefixes);
+
 /* What a plan launches (host only). */
 typedef struct ppas_plan_info {
   int32_t n_items;          /* workgroups of the packed attention launch */
@@ -276,6 +402,12 @@ ppas_status ppas_rope_kv_append_planned(const ppas_step_plan* plan, float rope_t
                                         const void* k_new, const void* v_new,
                                         const int32_t* block_table_dev, const ppas_events* events,
                                         void* hip_stream);
+
+/* As ppas_rope_qkv_append, with the plan's descriptors and validation; events may be NULL. */
+ppas_status ppas_rope_qkv_append_planned(const ppas_step_plan* plan, const ppas_rope* rope, const ppas_qkv* rows,
+                                         void* q_out, void* k_pages, void* v_pages,
+                                         const int32_t* block_table_dev, const ppas_events* events,
+                                         void* hip_stream);
 
 /*
  * As ppas_attn_step, with the plan's descriptors, validation and work list
@@ -371,6 +503,51 @@ ppas_status ppas_gateup_act(const void* x, const void* w, void* y, int32_t n_tok
  * (0 when it does not split the reduction, or for an invalid shape). The library's
  * own sizing call. */
 size_t ppas_gateup_act_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t n_inter);
+
+/*
+ * 8-bit integers for the projections (the library's own; the paper's models run in
+ * bf16). Rows of activations (one per token) or weights (one per output channel) to
+ * 8-bit integers and a scale: for row r < n_rows of x (bf16, x_stride elements apart,
+ * `hidden` of them), with m its largest magnitude,
+ *   scale[r] = m / 127 (fp32),  xq[r][i] = 127 x[r][i] / m to the nearest integer, ties
+ * to even, in -127..127. xq [n_rows][hidden] int8, scale [n_rows] fp32. A row whose m is
+ * below 2^-110 gives zeros and scale 0; a row that holds an infinity or a NaN gives zeros
+ * and a NaN scale, which makes every product with it NaN. hidden is any positive size;
+ * multiples of 8 on 16 bytes (x and x_stride) are faster. n_rows == 0 is a no-op; NULL
+ * pointers, an x_stride below hidden or non-positive sizes are PPAS_EINVAL. x and the
+ * outputs must not overlap. One launch, no workspace, no host sync.
+ */
+ppas_status ppas_quant_i8(const void* x, int64_t x_stride, void* xq, float* scale, int32_t n_rows, int32_t hidden,
+                          const ppas_events* events, void* hip_stream);
+
+/*
+ * ppas_gateup_proj and ppas_gateup_act on such rows: x [n_tokens][hidden] and w
+ * [n_out][hidden] (or [2 n_inter][hidden]) int8, -128 included, with x_scale [n_tokens]
+ * and w_scale [n_out] (or [2 n_inter]) fp32:
+ *   s[t][n] = x_scale[t] w_scale[n] sum_k x[t][k] w[n][k]
+ * written as y[t][n] = s[t][n], or as y[t][f] = silu(s[t][f]) s[t][n_inter + f], bf16
+ * nearest-even. The sums are exact int32, so that results depend neither on the number
+ * of tokens beside a token, nor on the workspace or kernel; the product of the scales,
+ * the sum and their product are each rounded to fp32. hidden is 1..131071 (the sums
+ * then fit; above: PPAS_ERANGE); multiples of 128 with x and w on 16 bytes are fast, and
+ * may be split over workgroups with int32 partial sums in the workspace (optional, as in
+ * ppas_gateup_proj; any size, 16-byte aligned). x_scale and w_scale may be any fp32
+ * values. n_tokens == 0 is a no-op. Other arguments, events, streams and errors as for
+ * ppas_gateup_proj. No call allocates or keeps anything; each may be captured into a
+ * HIP graph, and graphs that share a workspace must not run at once.
+ */
+ppas_status ppas_gateup_proj_i8(const void* x, const float* x_scale, const void* w, const float* w_scale, void* y,
+                                int32_t n_tokens, int32_t hidden, int32_t n_out, void* workspace,
+                                size_t workspace_bytes, const ppas_events* events, void* hip_stream);
+
+ppas_status ppas_gateup_act_i8(const void* x, const float* x_scale, const void* w, const float* w_scale, void* y,
+                               int32_t n_tokens, int32_t hidden, int32_t n_inter, void* workspace,
+                               size_t workspace_bytes, const ppas_events* events, void* hip_stream);
+
+/* The most workspace that such a call can use for this shape on the current device (0
+ * when it does not split the reduction, or for an invalid shape). */
+size_t ppas_gateup_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t n_out);
+size_t ppas_gateup_act_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t n_inter);
 
 /*
  * Kernel choice of a projection call, for tests (host only, no HIP call): the

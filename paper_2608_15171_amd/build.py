@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libppas.so")
 
-SOURCES = ["api.cpp", "plan.cpp", "attn_step.hip", "kv_append.hip", "rope_append.hip", "noalloc.hip", "gateup.hip", "gateup_any.hip",
+SOURCES = ["api.cpp", "plan.cpp", "attn_step.hip", "kv_append.hip", "rope_append.hip", "rope.cpp", "rope_rows.hip", "noalloc.hip", "gateup.hip", "gateup_any.hip", "gateup_i8.hip", "int8.hip",
            "stream_read.hip"]
 
 HIPCC_FLAGS = [

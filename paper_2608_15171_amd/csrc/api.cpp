@@ -13,6 +13,7 @@
 #include "device.h"
 #include "plan.h"
 #include "ppas.h"
+#include "rope.h"
 
 namespace ppas {
 
@@ -230,6 +231,7 @@ struct ppas_step_plan {
   ppas_shape shape{};
   int32_t bt_stride = 0;
   int32_t n_seqs = 0;
+  int64_t n_rows = 0;
   Plan plan;
   int32_t n_append = 0;
   size_t off_append = 0;
@@ -243,20 +245,24 @@ enum : int { kWantAttn = 1, kWantAppend = 2 };
 // Validate, plan and stage. On success p.buf holds the lists (nullptr for an empty step).
 ppas_status build_plan(ppas_step_plan& p, const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,
                        const int32_t* bt_host, int32_t bt_stride, const ppas_plan_opts* opts, int want,
-                       bool check_overlap) {
+                       bool check_overlap, const ppas_prefix* prefixes = nullptr, int32_t n_prefixes = 0) {
   ppas_status st = check_opts(opts);
   if (st != PPAS_OK) return st;
   st = validate(shape, seqs, n_seqs, bt_host, bt_stride, check_overlap);
+  if (st != PPAS_OK) return st;
+  st = validate_prefixes(seqs, n_seqs, bt_host, bt_stride, prefixes, n_prefixes);
   if (st != PPAS_OK) return st;
   p.shape = *shape;
   p.bt_stride = bt_stride;
   p.n_seqs = n_seqs;
   if (n_seqs == 0) return PPAS_OK;
+  p.n_rows = int64_t(seqs[n_seqs - 1].query_start) + seqs[n_seqs - 1].n_query;
   const DeviceInfo dev = current_device();
   if (!dev.gfx950) return PPAS_EUNSUPPORTED;
   std::vector<AppendItem> app;
   if (want & kWantAttn)
-    make_plan(*shape, seqs, n_seqs, (opts && opts->num_cus > 0) ? opts->num_cus : dev.cus, to_opts(opts), p.plan);
+    make_plan(*shape, seqs, n_seqs, (opts && opts->num_cus > 0) ? opts->num_cus : dev.cus, to_opts(opts), p.plan,
+              prefixes, n_prefixes);
   if (want & kWantAppend) make_append_items(seqs, n_seqs, app);
   if (!plan_fits(p.plan, app.size())) return PPAS_ERANGE;
   p.n_append = int32_t(app.size());
@@ -297,6 +303,67 @@ ppas_status run_append(const ppas_step_plan& p, bool rope, float theta, void* q,
   return (e == hipSuccess && noted) ? PPAS_OK : PPAS_EHIP;
 }
 
+// Bytes that T rows of `row` elements, `stride` apart, span.
+uint64_t span_bytes(int64_t T, int64_t stride, int64_t row) { return 2 * (uint64_t(T - 1) * uint64_t(stride) + uint64_t(row)); }
+
+bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
+  const uint64_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y ? y - x < a_bytes : x - y < b_bytes;
+}
+
+bool off(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
+// T: the step's token rows.
+ppas_status check_qkv(const ppas_shape& s, const ppas_rope* rope, const ppas_qkv* r, const void* q_out,
+                      const void* k_pages, const void* v_pages, const int32_t* bt_dev, int64_t T) {
+  const ppas_status st = check_rope(rope, s.head_dim);
+  if (st != PPAS_OK) return st;
+  if (!r || !r->q || !r->k || !r->v || !q_out || !k_pages || !v_pages || !bt_dev) return PPAS_EINVAL;
+  const int64_t q_row = int64_t(s.n_q_heads) * s.head_dim, kv_row = int64_t(s.n_kv_heads) * s.head_dim;
+  if (r->q_stride < q_row || r->k_stride < kv_row || r->v_stride < kv_row) return PPAS_EINVAL;
+  // a step's last row has to lie within 2^62 bytes, far past any device's memory
+  const int64_t most = (int64_t(1) << 61) / T;
+  if (r->q_stride > most || r->k_stride > most || r->v_stride > most) return PPAS_ERANGE;
+  if (off(r->q, 2) || off(r->k, 2) || off(r->v, 2) || off(q_out, 2) || off(k_pages, 16) || off(v_pages, 16) ||
+      off(bt_dev, 4))
+    return PPAS_EINVAL;
+  const uint64_t out_bytes = span_bytes(T, q_row, q_row);
+  const bool in_place = q_out == r->q && r->q_stride == q_row;
+  if ((!in_place && overlap(q_out, out_bytes, r->q, span_bytes(T, r->q_stride, q_row))) ||
+      overlap(q_out, out_bytes, r->k, span_bytes(T, r->k_stride, kv_row)) ||
+      overlap(q_out, out_bytes, r->v, span_bytes(T, r->v_stride, kv_row)))
+    return PPAS_EINVAL;
+  return PPAS_OK;
+}
+
+ppas_status run_qkv_append(const ppas_step_plan& p, const ppas_rope& rope, const ppas_qkv& rows, void* q_out,
+                           void* k_pages, void* v_pages, const int32_t* bt_dev, const ppas_events* ev,
+                           void* hip_stream) {
+  if (!p.buf || p.n_append == 0) return PPAS_EINVAL;   // a plan made without the page-write list
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  RopeTable table;
+  make_rope_table(rope, table);
+  RopeAppend r;
+  r.q = static_cast<const uint16_t*>(rows.q);
+  r.k = static_cast<const uint16_t*>(rows.k);
+  r.v = static_cast<const uint16_t*>(rows.v);
+  r.q_stride = rows.q_stride;
+  r.k_stride = rows.k_stride;
+  r.v_stride = rows.v_stride;
+  r.q_out = static_cast<uint16_t*>(q_out);
+  r.k_pages = static_cast<uint16_t*>(k_pages);
+  r.v_pages = static_cast<uint16_t*>(v_pages);
+  r.items = reinterpret_cast<const AppendItem*>(p.buf->dev + p.off_append);
+  r.bt = bt_dev;
+  r.n_items = p.n_append;
+  r.bt_stride = p.bt_stride;
+  r.hq = p.shape.n_q_heads;
+  r.hkv = p.shape.n_kv_heads;
+  const hipError_t e = launch_rope_qkv_append(r, table, stream, ev_of(ev, 0), ev_of(ev, 1));
+  const bool noted = note_use(p.buf, stream);
+  return (e == hipSuccess && noted) ? PPAS_OK : PPAS_EHIP;
+}
+
 ppas_status run_attn(const ppas_step_plan& p, void* out, const void* q, const void* k_pages, const void* v_pages,
                      const int32_t* bt_dev, void* workspace, size_t workspace_bytes, const ppas_events* ev,
                      void* hip_stream) {
@@ -312,7 +379,7 @@ ppas_status run_attn(const ppas_step_plan& p, void* out, const void* q, const vo
       static_cast<const uint16_t*>(v_pages), bt_dev, p.bt_stride, p.shape.n_q_heads, p.shape.n_kv_heads,
       p.shape.scale, reinterpret_cast<const WorkItem*>(p.buf->dev), int(plan.items.size()),
       reinterpret_cast<const CombineItem*>(p.buf->dev + plan.off_combine), int(plan.combine.size()),
-      reinterpret_cast<float2*>(ws + plan.off_ml), reinterpret_cast<float*>(ws + plan.off_acc), plan.tile_pos,
+      plan.combine_pos, reinterpret_cast<float2*>(ws + plan.off_ml), reinterpret_cast<float*>(ws + plan.off_acc), plan.tile_pos,
       stream, ev_of(ev, 0), ev_of(ev, 1), ev_of(ev, 2), ev_of(ev, 3));
   const bool noted = note_use(p.buf, stream);
   return (e == hipSuccess && noted) ? PPAS_OK : PPAS_EHIP;
@@ -388,13 +455,21 @@ size_t ppas_attn_workspace_bytes(const ppas_shape* shape, const ppas_seq* seqs, 
 ppas_status ppas_step_plan_create(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,
                                   const int32_t* block_table_host, int32_t bt_stride, const ppas_plan_opts* opts,
                                   ppas_step_plan** plan) {
+  return ppas_step_plan_create_shared(shape, seqs, n_seqs, nullptr, 0, block_table_host, bt_stride, opts, plan);
+}
+
+ppas_status ppas_step_plan_create_shared(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,
+                                         const ppas_prefix* prefixes, int32_t n_prefixes,
+                                         const int32_t* block_table_host, int32_t bt_stride,
+                                         const ppas_plan_opts* opts, ppas_step_plan** plan) {
   if (!plan) return PPAS_EINVAL;
   *plan = nullptr;
   ppas_step_plan* p = nullptr;
   try {
     p = new ppas_step_plan;
     const ppas_status st =
-        build_plan(*p, shape, seqs, n_seqs, block_table_host, bt_stride, opts, kWantAttn | kWantAppend, true);
+        build_plan(*p, shape, seqs, n_seqs, block_table_host, bt_stride, opts, kWantAttn | kWantAppend, true, prefixes,
+                   n_prefixes);
     if (st != PPAS_OK) {
       release(p->buf);
       delete p;
@@ -452,6 +527,22 @@ ppas_status ppas_rope_kv_append_planned(const ppas_step_plan* plan, float rope_t
   try {
     return run_append(*plan, true, rope_theta, q, k_pages, v_pages, k_new, v_new, block_table_dev, events,
                       hip_stream);
+  } catch (...) {
+    return PPAS_EINVAL;
+  }
+}
+
+ppas_status ppas_rope_qkv_append_planned(const ppas_step_plan* plan, const ppas_rope* rope, const ppas_qkv* rows,
+                                         void* q_out, void* k_pages, void* v_pages, const int32_t* block_table_dev,
+                                         const ppas_events* events, void* hip_stream) {
+  if (!plan) return PPAS_EINVAL;
+  ppas_status st = check_events(events);
+  if (st != PPAS_OK) return st;
+  try {
+    if (plan->n_seqs == 0) return check_rope(rope, kHeadDim);
+    st = check_qkv(plan->shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, plan->n_rows);
+    if (st != PPAS_OK) return st;
+    return run_qkv_append(*plan, *rope, *rows, q_out, k_pages, v_pages, block_table_dev, events, hip_stream);
   } catch (...) {
     return PPAS_EINVAL;
   }
@@ -568,6 +659,106 @@ ppas_status ppas_gateup_choice(int32_t n_tokens, int32_t hidden, int32_t n_out, 
   return PPAS_OK;
 }
 
+namespace {
+
+// 8-bit rows: sums of up to 131,071 products of at most 128 x 128 fit int32.
+constexpr int32_t kMaxHiddenI8 = 131071;
+
+ppas_status check_gateup_i8(int32_t n_tokens, int32_t hidden, int32_t n_out, bool act) {
+  if (n_tokens < 0 || hidden <= 0 || n_out <= 0) return PPAS_EINVAL;
+  if (hidden > kMaxHiddenI8 || n_tokens > INT32_MAX - 512 || n_out > INT32_MAX - 512) return PPAS_ERANGE;
+  if (gateup_tiles(n_tokens, n_out) > INT32_MAX || gateup_i8_any_tiles(n_tokens, n_out, act) > INT32_MAX)
+    return PPAS_ERANGE;
+  return PPAS_OK;
+}
+
+// The most splits of a call in whole 128-feature stages (1: the general kernel takes it).
+int splits_i8(int32_t n_tokens, int32_t hidden, int32_t n_out, int cus) {
+  return hidden % 128 ? 1 : gateup_splits(n_tokens, hidden / 2, n_out, cus);
+}
+
+ppas_status gateup_i8_call(const void* x, const float* sx, const void* w, const float* sw, void* y, int32_t n_tokens,
+                           int32_t hidden, int32_t n_out, bool act, void* workspace, size_t workspace_bytes,
+                           const ppas_events* events, void* hip_stream) {
+  ppas_status st = check_gateup_i8(n_tokens, hidden, n_out, act);
+  if (st != PPAS_OK) return st;
+  st = check_events(events);
+  if (st != PPAS_OK) return st;
+  if (n_tokens == 0) return PPAS_OK;
+  if (!x || !sx || !w || !sw || !y || (workspace_bytes > 0 && !workspace)) return PPAS_EINVAL;
+  if (off(sx, 4) || off(sw, 4) || off(y, 2) || off(workspace, 16)) return PPAS_EINVAL;
+  const DeviceInfo dev = current_device();
+  if (!dev.gfx950) return PPAS_EUNSUPPORTED;
+  int splits = splits_i8(n_tokens, hidden, n_out, dev.cus);
+  while (splits > 1 && gateup_workspace_bytes(n_tokens, n_out, splits) > workspace_bytes) --splits;
+  if (gateup_tiles(n_tokens, n_out) * splits > INT32_MAX) splits = 1;
+  const Int8Product p{static_cast<const int8_t*>(x), sx, static_cast<const int8_t*>(w), sw,
+                      static_cast<uint16_t*>(y), n_tokens, hidden, n_out};
+  const hipError_t e = launch_gateup_i8(p, act, splits, workspace, dev.cus, static_cast<hipStream_t>(hip_stream),
+                                        ev_of(events, 0), ev_of(events, 1));
+  return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
+}
+
+}  // namespace
+
+ppas_status ppas_quant_i8(const void* x, int64_t x_stride, void* xq, float* scale, int32_t n_rows, int32_t hidden,
+                          const ppas_events* events, void* hip_stream) {
+  try {
+    if (n_rows < 0 || hidden <= 0) return PPAS_EINVAL;
+    const ppas_status st = check_events(events);
+    if (st != PPAS_OK) return st;
+    if (n_rows == 0) return PPAS_OK;
+    if (!x || !xq || !scale || x_stride < hidden || off(x, 2) || off(scale, 4)) return PPAS_EINVAL;
+    if (x_stride > (int64_t(1) << 61) / n_rows) return PPAS_ERANGE;
+    if (!current_device().gfx950) return PPAS_EUNSUPPORTED;
+    const hipError_t e = launch_quant_i8(static_cast<const uint16_t*>(x), x_stride, static_cast<int8_t*>(xq), scale,
+                                         n_rows, hidden, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
+                                         ev_of(events, 1));
+    return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
+  } catch (...) {
+    return PPAS_EINVAL;
+  }
+}
+
+ppas_status ppas_gateup_proj_i8(const void* x, const float* x_scale, const void* w, const float* w_scale, void* y,
+                                int32_t n_tokens, int32_t hidden, int32_t n_out, void* workspace,
+                                size_t workspace_bytes, const ppas_events* events, void* hip_stream) {
+  try {
+    return gateup_i8_call(x, x_scale, w, w_scale, y, n_tokens, hidden, n_out, false, workspace, workspace_bytes,
+                          events, hip_stream);
+  } catch (...) {
+    return PPAS_EINVAL;
+  }
+}
+
+ppas_status ppas_gateup_act_i8(const void* x, const float* x_scale, const void* w, const float* w_scale, void* y,
+                               int32_t n_tokens, int32_t hidden, int32_t n_inter, void* workspace,
+                               size_t workspace_bytes, const ppas_events* events, void* hip_stream) {
+  try {
+    if (n_inter > (INT32_MAX - 512) / 2) return PPAS_ERANGE;
+    const int32_t n_out = act_rows(n_inter);
+    if (n_out < 0) return PPAS_EINVAL;
+    return gateup_i8_call(x, x_scale, w, w_scale, y, n_tokens, hidden, n_out, true, workspace, workspace_bytes,
+                          events, hip_stream);
+  } catch (...) {
+    return PPAS_EINVAL;
+  }
+}
+
+size_t ppas_gateup_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t n_out) {
+  try {
+    if (check_gateup_i8(n_tokens, hidden, n_out, false) != PPAS_OK || n_tokens == 0) return 0;
+    return gateup_workspace_bytes(n_tokens, n_out, splits_i8(n_tokens, hidden, n_out, current_device().cus));
+  } catch (...) {
+    return 0;
+  }
+}
+
+size_t ppas_gateup_act_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t n_inter) {
+  const int32_t n_out = act_rows(n_inter);
+  return n_out < 0 ? 0 : ppas_gateup_i8_workspace_bytes(n_tokens, hidden, n_out);
+}
+
 ppas_status ppas_stream_read(const void* buf, size_t bytes, void* sink, const ppas_events* events,
                              void* hip_stream) {
   try {
@@ -632,17 +823,105 @@ ppas_status ppas_rope_kv_append(const ppas_shape* shape, float rope_theta, void*
   }
 }
 
+ppas_status ppas_rope_frequencies(const ppas_rope* rope, int32_t head_dim, double* out) {
+  const ppas_status st = check_rope(rope, head_dim);
+  if (st != PPAS_OK) return st;
+  if (!out) return PPAS_EINVAL;
+  for (int32_t j = 0; j < rope->rotary_dim / 2; ++j) out[j] = rope_frequency(*rope, j);
+  return PPAS_OK;
+}
+
+ppas_status ppas_rope_rows(const ppas_rope* rope, const void* x, int64_t x_stride, void* y, int64_t y_stride,
+                           const int32_t* positions_dev, int32_t n_rows, int32_t n_heads, int32_t head_dim,
+                           int32_t transposed, const ppas_events* events, void* hip_stream) {
+  try {
+    if (n_rows < 0 || n_heads < 1 || n_heads > 65536 || head_dim < 2 || head_dim % 2 != 0) return PPAS_EINVAL;
+    if (head_dim > 2 * kRopeMaxPairs) return PPAS_EUNSUPPORTED;
+    ppas_status st = check_rope(rope, head_dim);
+    if (st != PPAS_OK) return st;
+    st = check_events(events);
+    if (st != PPAS_OK) return st;
+    if (n_rows == 0) return PPAS_OK;
+    const int64_t row = int64_t(n_heads) * head_dim, most = (int64_t(1) << 61) / n_rows;
+    if (!x || !y || !positions_dev || x_stride < row || y_stride < row) return PPAS_EINVAL;
+    if (x_stride > most || y_stride > most) return PPAS_ERANGE;
+    if (off(x, 2) || off(y, 2) || off(positions_dev, 4)) return PPAS_EINVAL;
+    if (!(x == y && x_stride == y_stride) &&
+        overlap(x, span_bytes(n_rows, x_stride, row), y, span_bytes(n_rows, y_stride, row)))
+      return PPAS_EINVAL;
+    if (!current_device().gfx950) return PPAS_EUNSUPPORTED;
+    RopeTable table;
+    make_rope_table(*rope, table);
+    const RopeRows r{static_cast<const uint16_t*>(x), static_cast<uint16_t*>(y), x_stride, y_stride, positions_dev,
+                     n_rows, n_heads, head_dim, transposed != 0};
+    const hipError_t e = launch_rope_rows(r, table, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
+                                          ev_of(events, 1));
+    return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
+  } catch (...) {
+    return PPAS_EINVAL;
+  }
+}
+
+ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope, const ppas_qkv* rows, void* q_out,
+                                 void* k_pages, void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
+                                 const int32_t* block_table_dev, int32_t bt_stride,
+                                 const int32_t* block_table_host, void* hip_stream) {
+  ppas_step_plan p;
+  try {
+    ppas_status st = validate(shape, seqs, n_seqs, block_table_host, bt_stride, true);
+    if (st != PPAS_OK) return st;
+    if (n_seqs == 0) return check_rope(rope, kHeadDim);
+    const int64_t T = int64_t(seqs[n_seqs - 1].query_start) + seqs[n_seqs - 1].n_query;
+    st = check_qkv(*shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, T);
+    if (st != PPAS_OK) return st;
+    // validated above; build only the page-write list
+    st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantAppend, false);
+    if (st == PPAS_OK)
+      st = run_qkv_append(p, *rope, *rows, q_out, k_pages, v_pages, block_table_dev, nullptr, hip_stream);
+    release(p.buf);
+    return st;
+  } catch (...) {
+    release(p.buf);
+    return PPAS_EINVAL;
+  }
+}
+
+size_t ppas_attn_shared_workspace_bytes(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,
+                                        const ppas_prefix* prefixes, int32_t n_prefixes) {
+  try {
+    if (validate(shape, seqs, n_seqs, nullptr, INT32_MAX, false) != PPAS_OK ||
+        validate_prefixes(seqs, n_seqs, nullptr, INT32_MAX, prefixes, n_prefixes) != PPAS_OK)
+      return 0;
+    Plan plan;
+    make_plan(*shape, seqs, n_seqs, current_device().cus, PlanOpts{}, plan, prefixes, n_prefixes);
+    return plan_fits(plan, 0) ? plan.total : 0;
+  } catch (...) {
+    return 0;
+  }
+}
+
 ppas_status ppas_attn_step(const ppas_shape* shape, void* out, const void* q, const void* k_pages,
                            const void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
                            const int32_t* block_table_dev, int32_t bt_stride, const int32_t* block_table_host,
                            void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return ppas_attn_step_shared(shape, out, q, k_pages, v_pages, seqs, n_seqs, nullptr, 0, block_table_dev, bt_stride,
+                               block_table_host, workspace, workspace_bytes, hip_stream);
+}
+
+ppas_status ppas_attn_step_shared(const ppas_shape* shape, void* out, const void* q, const void* k_pages,
+                                  const void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
+                                  const ppas_prefix* prefixes, int32_t n_prefixes, const int32_t* block_table_dev,
+                                  int32_t bt_stride, const int32_t* block_table_host, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream) {
   ppas_step_plan p;
   try {
     ppas_status st = validate(shape, seqs, n_seqs, block_table_host, bt_stride, false);
     if (st != PPAS_OK) return st;
+    st = validate_prefixes(seqs, n_seqs, block_table_host, bt_stride, prefixes, n_prefixes);
+    if (st != PPAS_OK) return st;
     if (n_seqs == 0) return PPAS_OK;
     if (!out || !q || !k_pages || !v_pages || !block_table_dev || !workspace) return PPAS_EINVAL;
-    st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantAttn, false);
+    st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantAttn, false, prefixes, n_prefixes);
     if (st == PPAS_OK)
       st = run_attn(p, out, q, k_pages, v_pages, block_table_dev, workspace, workspace_bytes, nullptr, hip_stream);
     release(p.buf);

@@ -1016,14 +1016,12 @@ constexpr int kCombineThreads = 32 * kCombineRowsPerBlock;
 // issued before any is used (one memory round trip per batch); the result does not
 // depend on kBatch. Absent splits of a group enter with m = -inf and weigh 0. Every
 // split gives each of its rows at least one key, so a real split's m is finite.
+// M, L and acc hold what is merged already (M = -inf: nothing).
 constexpr int kMergeGroup = 4;
 template <int kBatch>
 __device__ __forceinline__ void merge_splits(const float2* ml_row, const float* acc_row, int rows, int nsplit,
-                                             float& L, f32x4& acc) {
+                                             float& M, float& L, f32x4& acc) {
   static_assert(kBatch % kMergeGroup == 0, "whole groups");
-  float M = kNegInf;
-  L = 0.f;
-  acc = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < nsplit; s0 += kBatch) {
     float2 ml[kBatch];
     f32x4 pa[kBatch];
@@ -1062,18 +1060,22 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const CombineI
   const int r = blockIdx.y * kCombineRowsPerBlock + (threadIdx.x >> 5);
   if (r >= rows) return;
   const int d0 = (threadIdx.x & 31) * 4;
-  const size_t slot = size_t(ci.part) + r;
-  const float2* ml_row = part_ml + slot;
-  const float* acc_row = part_acc + slot * kHeadDim + d0;
-  float L;
-  f32x4 acc;
+  float M = kNegInf, L = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   // rows in many pieces (a few long decode rows) wait for a quarter of the round trips
   // (one row's 96 pieces: 13.2 -> 11.7 us, 38 pieces 7.5 -> 6.9); the others don't load
   // splits that are not there
-  if (ci.nsplit > 8)
-    merge_splits<16>(ml_row, acc_row, rows, ci.nsplit, L, acc);
-  else
-    merge_splits<4>(ml_row, acc_row, rows, ci.nsplit, L, acc);
+  auto merge = [&](int part, int stride, int nsplit) {
+    const size_t slot = size_t(part) + r;
+    const float2* ml_row = part_ml + slot;
+    const float* acc_row = part_acc + slot * kHeadDim + d0;
+    if (nsplit > 8)
+      merge_splits<16>(ml_row, acc_row, stride, nsplit, M, L, acc);
+    else
+      merge_splits<4>(ml_row, acc_row, stride, nsplit, M, L, acc);
+  };
+  if (ci.pre_nsplit > 0) merge(ci.pre_part, ci.strides >> 16, ci.pre_nsplit);
+  merge(ci.part, ci.strides & 0xffff, ci.nsplit);
   const float inv = 1.f / L;
   uint16_t* orow = out + (size_t(ci.row0 + r / kGroup) * hq + ci.kvh * kGroup + r % kGroup) * kHeadDim + d0;
   u32x2 v;
@@ -1085,7 +1087,7 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const CombineI
 hipError_t launch_attn_step(const uint16_t* q, uint16_t* out, const uint16_t* kp, const uint16_t* vp,
                             const int32_t* bt, int32_t bt_stride, int32_t hq, int32_t hkv, float scale,
                             const WorkItem* items, int n_items, const CombineItem* comb, int n_comb,
-                            float2* part_ml, float* part_acc, int tile_pos, hipStream_t stream,
+                            int comb_pos, float2* part_ml, float* part_acc, int tile_pos, hipStream_t stream,
                             hipEvent_t ev_start, hipEvent_t ev_stop, hipEvent_t ev_merge_start,
                             hipEvent_t ev_merge_stop) {
   if (tile_pos != kTilePosSmall && tile_pos != kTilePosLarge) return hipErrorInvalidValue;
@@ -1116,7 +1118,7 @@ hipError_t launch_attn_step(const uint16_t* q, uint16_t* out, const uint16_t* kp
     if (e != hipSuccess) return e;
   }
   if (n_comb > 0) {
-    const int ymax = tile_pos * kGroup / kCombineRowsPerBlock;
+    const int ymax = comb_pos * kGroup / kCombineRowsPerBlock;
     hipExtLaunchKernelGGL(combine_kernel, dim3(n_comb, ymax), dim3(kCombineThreads), 0, stream, ev_merge_start,
                           ev_merge_stop, 0, comb, part_ml, part_acc, out, hq);
     hipError_t e = hipGetLastError();

@@ -20,11 +20,12 @@ struct DeviceInfo {
 // Without a usable device: 256 CUs, not gfx950.
 DeviceInfo current_device();
 
-// The packed attention launch and, when n_comb > 0, the split-merge launch.
+// The packed attention launch and, when n_comb > 0, the split-merge launch (of items of
+// at most comb_pos positions).
 hipError_t launch_attn_step(const uint16_t* q, uint16_t* out, const uint16_t* kp, const uint16_t* vp,
                             const int32_t* bt, int32_t bt_stride, int32_t hq, int32_t hkv, float scale,
                             const WorkItem* items, int n_items, const CombineItem* comb, int n_comb,
-                            float2* part_ml, float* part_acc, int tile_pos, hipStream_t stream,
+                            int comb_pos, float2* part_ml, float* part_acc, int tile_pos, hipStream_t stream,
                             hipEvent_t ev_start, hipEvent_t ev_stop, hipEvent_t ev_merge_start,
                             hipEvent_t ev_merge_stop);
 
@@ -34,7 +35,8 @@ hipError_t launch_attn_step(const uint16_t* q, uint16_t* out, const uint16_t* kp
 // workgroups per output tile, as many as pay, whose fp32 partial sums
 // (gateup_workspace_bytes of `part`, columns in weight-row order) a second launch
 // adds in order. `cus` is the device's compute-unit count. gateup_choose (host
-// only) is the kernel that such a call takes; `aligned`: x and w on 16 bytes.
+// only) is the kernel that such a call takes; `aligned`: x and w on 16 bytes;
+// `int_sums`: 8-bit rows of 2 H features, whose sums are exact in any order.
 struct GateupChoice {
   enum Kernel { kTiles = 0, kRows = 1, kGeneral = 2 };
   Kernel kernel = kGeneral;
@@ -44,7 +46,8 @@ struct GateupChoice {
   int32_t main_m = 0, tail_m = 0;           // tiles: main ones along the token rows, 64-row ones after them
   int32_t light = 0, grid = 0, block = 8;   // tiles: see GemmArgs
 };
-GateupChoice gateup_choose(int32_t T, int32_t H, int32_t N2, bool act, bool aligned, int max_splits, int cus);
+GateupChoice gateup_choose(int32_t T, int32_t H, int32_t N2, bool act, bool aligned, int max_splits, int cus,
+                           bool int_sums = false);
 hipError_t launch_gateup(const uint16_t* x, const uint16_t* w, uint16_t* y, int32_t T, int32_t H, int32_t N2,
                          bool act, int max_splits, float* part, int cus, hipStream_t stream, hipEvent_t ev_start,
                          hipEvent_t ev_stop);
@@ -53,6 +56,25 @@ hipError_t launch_gateup(const uint16_t* x, const uint16_t* w, uint16_t* y, int3
 hipError_t launch_gateup_any(const uint16_t* x, const uint16_t* w, uint16_t* y, int32_t T, int32_t H, int32_t N2,
                              bool act, int splits, float* part, int cus, hipStream_t stream, hipEvent_t ev_start,
                              hipEvent_t ev_stop);
+// The same product of 8-bit integers, x [T][H] and w [N2][H], with a scale per token
+// and per weight row; int32 partial sums (gateup_workspace_bytes). launch_gateup_i8_any
+// takes any H and alignment, without splits, up to 2^31 - 1 tiles of its own.
+struct Int8Product {
+  const int8_t* x;
+  const float* sx;
+  const int8_t* w;
+  const float* sw;
+  uint16_t* y;
+  int32_t T, H, N2;
+};
+hipError_t launch_gateup_i8(const Int8Product& p, bool act, int max_splits, void* part, int cus, hipStream_t stream,
+                            hipEvent_t ev_start, hipEvent_t ev_stop);
+hipError_t launch_gateup_i8_any(const Int8Product& p, bool act, hipStream_t stream, hipEvent_t ev_start,
+                                hipEvent_t ev_stop);
+int64_t gateup_i8_any_tiles(int32_t T, int32_t N2, bool act);
+// Rows of bf16 to 8-bit integers and a scale each (x_stride elements between rows).
+hipError_t launch_quant_i8(const uint16_t* x, int64_t x_stride, int8_t* xq, float* scale, int32_t T, int32_t H,
+                           hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop);
 // Output tiles of a call: 256 x 256, plus 64 x 256 for the last T % 256 token rows.
 int64_t gateup_tiles(int32_t T, int32_t N2);
 // The most reduction splits a call on a device with `cus` compute units uses (1: none).

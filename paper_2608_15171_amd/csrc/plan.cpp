@@ -91,7 +91,42 @@ ppas_status validate(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_se
   return PPAS_OK;
 }
 
+ppas_status validate_prefixes(const ppas_seq* seqs, int32_t n_seqs, const int32_t* bt_host, int32_t bt_stride,
+                              const ppas_prefix* prefixes, int32_t n_prefixes) {
+  if (n_prefixes < 0 || (n_prefixes > 0 && !prefixes)) return PPAS_EINVAL;
+  int32_t at = 0;   // requests before this one belong to earlier prefixes
+  for (int32_t k = 0; k < n_prefixes; ++k) {
+    const ppas_prefix& p = prefixes[k];
+    if (p.first_seq < at || p.n_seqs < 1 || p.first_seq >= n_seqs || p.n_seqs > n_seqs - p.first_seq) return PPAS_EINVAL;
+    if (p.len < 0 || p.len % kPage != 0) return PPAS_EINVAL;
+    at = p.first_seq + p.n_seqs;
+    for (int32_t s = p.first_seq; s < at; ++s)
+      if (p.len > seqs[s].cached_len) return PPAS_EINVAL;
+    if (!bt_host) continue;
+    const int32_t* first = bt_host + int64_t(p.first_seq) * bt_stride;
+    for (int32_t s = p.first_seq + 1; s < at; ++s)
+      if (!std::equal(first, first + p.len / kPage, bt_host + int64_t(s) * bt_stride)) return PPAS_EINVAL;
+  }
+  return PPAS_OK;
+}
+
 namespace {
+
+// Most new tokens of a request whose rows share their prefix's tiles with other
+// requests' rows; the rows of longer chunks fill tiles of their own.
+constexpr int32_t kShareMaxRows = 64;
+
+// Consecutive rows (of requests first_seq..end_seq-1) over keys [0, len) of table row
+// `seq`, and their tiles, KV head after KV head, each with nsplit partials from slot
+// `part` on.
+struct SharedTile {
+  int32_t row0, npos, part, nsplit;
+};
+struct SharedRun {
+  int32_t seq, first_seq, end_seq, row0, rows;
+  int64_t len;
+  std::vector<SharedTile> tiles;
+};
 
 struct Job {
   WorkItem item;
@@ -102,12 +137,36 @@ struct Job {
 }  // namespace
 
 void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, int num_cus, const PlanOpts& opts,
-               Plan& plan) {
+               Plan& plan, const ppas_prefix* prefixes, int32_t n_prefixes) {
   plan.items.clear();
   plan.combine.clear();
+  plan.combine_pos = 0;
   plan.part_slots = 0;
   const int hkv = shape.n_kv_heads;
   if (num_cus <= 0) num_cus = 256;
+
+  // Shared prefixes: runs of consecutive rows whose first keys are attended by tiles
+  // of all of them together, over whole 64-key blocks, so that their items need no
+  // mask and own key ranges start on a block; the rest of the prefix is read by every
+  // request for itself. own[s] is the first key of request s's own range.
+  std::vector<int32_t> own(size_t(n_seqs), 0);
+  std::vector<SharedRun> runs;
+  for (int32_t k = 0; k < n_prefixes; ++k) {
+    const ppas_prefix& p = prefixes[k];
+    const int32_t len = p.len / kPrefillBlock * kPrefillBlock;
+    if (len == 0) continue;
+    const int32_t end = p.first_seq + p.n_seqs;
+    for (int32_t s = p.first_seq; s < end;) {
+      int32_t e = s;
+      while (e < end && seqs[e].n_query <= kShareMaxRows) ++e;
+      if (e - s > 1) {
+        const int32_t row0 = seqs[s].query_start;
+        runs.push_back(SharedRun{p.first_seq, s, e, row0, seqs[e - 1].query_start + seqs[e - 1].n_query - row0, len, {}});
+        for (int32_t i = s; i < e; ++i) own[size_t(i)] = len;
+      }
+      s = std::max(e, s + 1);
+    }
+  }
 
   // Total work, to size the key splits so that the launch has several
   // workgroups per compute unit: keys summed over prefill tiles (of either
@@ -117,15 +176,17 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
     for (int32_t s = 0; s < n_seqs; ++s) {
       const ppas_seq& q = seqs[s];
       if (q.n_query == 1) continue;
-      for (int32_t t0 = 0; t0 < q.n_query; t0 += tile) keys += int64_t(q.cached_len) + std::min(q.n_query, t0 + tile);
+      for (int32_t t0 = 0; t0 < q.n_query; t0 += tile)
+        keys += int64_t(q.cached_len) + std::min(q.n_query, t0 + tile) - own[size_t(s)];
     }
+    for (const SharedRun& r : runs) keys += ceil_div(r.rows, tile) * r.len;
     return keys * hkv;
   };
   int64_t decode_keys = 0, large_tiles = 0;
   for (int32_t s = 0; s < n_seqs; ++s) {
     const ppas_seq& q = seqs[s];
     if (q.n_query == 1)
-      decode_keys += int64_t(q.cached_len + 1) * hkv;
+      decode_keys += int64_t(q.cached_len + 1 - own[size_t(s)]) * hkv;
     else
       large_tiles += ceil_div(q.n_query, kTilePosLarge) * hkv;
   }
@@ -187,35 +248,36 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
   // rounded. Against 64 bits that row's error would go from 2.12e-3 to 2.31e-3 in ten
   // pieces, that of 500 keys left whole from 2.01e-3 to 2.25e-3.
   const bool decode_even = prefill_keys == 0 && decode_keys > 0 && opts.decode_split <= 0;
-  auto piece_bounds = [&](int64_t kend, int64_t pos0, int kind) {
-    std::vector<int64_t> b{0};
+  // lo: the first key, a multiple of 64
+  auto piece_bounds = [&](int64_t lo, int64_t hi, int64_t pos0, int kind) {
+    std::vector<int64_t> b{lo};
+    const int64_t kend = hi - lo;
     if (kind == kKindDecode && decode_even) {
       const int64_t n = std::max<int64_t>(ceil_div(kend, int64_t(kDecodeMaxKeys - kDecodeBlock)),
                                           (kend * num_cus + decode_keys / 2) / decode_keys);
-      for (int64_t k = 1; k < n; ++k) b.push_back(kend * k / n / kDecodeBlock * kDecodeBlock);
+      for (int64_t k = 1; k < n; ++k) b.push_back(lo + kend * k / n / kDecodeBlock * kDecodeBlock);
     } else if (kind == kKindDecode) {
-      for (int64_t k = 1; k * ksd < kend; ++k) b.push_back(k * ksd);
+      for (int64_t k = 1; k * ksd < kend; ++k) b.push_back(lo + k * ksd);
     } else if (interleave) {
-      for (int64_t k = 1; k * ksp <= pos0; ++k) b.push_back(k * ksp);
+      for (int64_t k = 1; lo + k * ksp <= pos0; ++k) b.push_back(lo + k * ksp);
     } else {
       const int64_t n = std::max<int64_t>(1, (kend + ksp / 2) / ksp);
       const int64_t top = pos0 / kPrefillBlock * kPrefillBlock;
-      for (int64_t k = 1; k < n; ++k) b.push_back(std::min(top, kend * k / n / kPrefillBlock * kPrefillBlock));
+      for (int64_t k = 1; k < n; ++k) b.push_back(std::min(top, lo + kend * k / n / kPrefillBlock * kPrefillBlock));
     }
-    b.push_back(kend);
+    b.push_back(hi);
     b.erase(std::unique(b.begin(), b.end()), b.end());
     return b;
   };
 
   std::vector<Job> jobs;
-  auto add_unit = [&](int32_t s, int32_t g, int32_t row0, int32_t pos0, int32_t npos, int kind) {
-    const int64_t kend = int64_t(pos0) + npos;        // keys 0..kend-1 are visible to some row
-    const std::vector<int64_t> bounds = piece_bounds(kend, pos0, kind);
+  // One item per piece of `bounds`; the partials' first slot, or -1 where rows are written whole.
+  auto add_items = [&](int32_t s, int32_t g, int32_t row0, int32_t pos0, int32_t npos, int kind,
+                       const std::vector<int64_t>& bounds, bool partial) {
     const int64_t nsplit = int64_t(bounds.size()) - 1;
     int32_t part = -1;
-    if (nsplit > 1) {
+    if (partial) {
       part = int32_t(plan.part_slots);
-      plan.combine.push_back(CombineItem{row0, g, npos, int32_t(nsplit), part, 0, 0, 0});
       plan.part_slots += nsplit * int64_t(npos) * kGroup;
     }
     for (int64_t k = 0; k < nsplit; ++k) {
@@ -233,15 +295,54 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
       j.order_key[3] = int32_t(k);
       jobs.push_back(j);
     }
+    return part;
   };
+  auto merge = [&](int32_t g, int32_t row0, int32_t npos, int32_t part, int32_t nsplit, int32_t stride,
+                   const SharedTile* t) {
+    plan.combine.push_back(CombineItem{row0, g, npos, nsplit, part, t ? t->part + (row0 - t->row0) * kGroup : 0,
+                                       t ? t->nsplit : 0, stride | (t ? t->npos * kGroup << 16 : 0)});
+    plan.combine_pos = std::max(plan.combine_pos, npos);
+  };
+  // Rows row0.. of request s with its own keys, and with the tiles of its run (no shared prefix: null).
+  auto add_unit = [&](int32_t s, int32_t g, int32_t row0, int32_t pos0, int32_t npos, int kind,
+                      const SharedRun* pre) {
+    const int64_t kend = int64_t(pos0) + npos;        // keys own..kend-1 are visible to some row
+    const std::vector<int64_t> bounds = piece_bounds(own[size_t(s)], kend, pos0, kind);
+    const int32_t nsplit = int32_t(bounds.size()) - 1;
+    const int32_t part = add_items(s, g, row0, pos0, npos, kind, bounds, nsplit > 1 || pre);
+    if (!pre) {
+      if (nsplit > 1) merge(g, row0, npos, part, nsplit, npos * kGroup, nullptr);
+      return;
+    }
+    const size_t per_head = pre->tiles.size() / size_t(hkv);
+    for (int32_t lo = row0; lo < row0 + npos;) {
+      const SharedTile& t = pre->tiles[size_t(g) * per_head + size_t((lo - pre->row0) / tile)];
+      const int32_t hi = std::min(row0 + npos, t.row0 + t.npos);
+      merge(g, lo, hi - lo, part + (lo - row0) * kGroup, nsplit, npos * kGroup, &t);
+      lo = hi;
+    }
+  };
+  // A run's tiles see every key of their pieces: their position is the first one behind the prefix.
+  for (SharedRun& r : runs) {
+    const std::vector<int64_t> bounds = piece_bounds(0, r.len, r.len, kKindPrefill);
+    for (int32_t g = 0; g < hkv; ++g)
+      for (int32_t t0 = 0; t0 < r.rows; t0 += tile) {
+        const int32_t npos = std::min(tile, r.rows - t0);
+        const int32_t part = add_items(r.seq, g, r.row0 + t0, int32_t(r.len), npos, kKindPrefill, bounds, true);
+        r.tiles.push_back(SharedTile{r.row0 + t0, npos, part, int32_t(bounds.size()) - 1});
+      }
+  }
+  size_t run = 0;   // the first one that ends behind the request
   for (int32_t s = 0; s < n_seqs; ++s) {
     const ppas_seq& q = seqs[s];
     for (int32_t g = 0; g < hkv; ++g) {
+      while (run < runs.size() && runs[run].end_seq <= s) ++run;
+      const SharedRun* pre = own[size_t(s)] ? &runs[run] : nullptr;
       if (q.n_query == 1) {
-        add_unit(s, g, q.query_start, q.cached_len, 1, kKindDecode);
+        add_unit(s, g, q.query_start, q.cached_len, 1, kKindDecode, pre);
       } else {
         for (int32_t t0 = 0; t0 < q.n_query; t0 += tile)
-          add_unit(s, g, q.query_start + t0, q.cached_len + t0, std::min(tile, q.n_query - t0), kKindPrefill);
+          add_unit(s, g, q.query_start + t0, q.cached_len + t0, std::min(tile, q.n_query - t0), kKindPrefill, pre);
       }
     }
   }

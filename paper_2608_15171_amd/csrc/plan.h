@@ -35,9 +35,11 @@ struct WorkItem {
 };
 static_assert(sizeof(WorkItem) == 32, "WorkItem is 32 bytes");
 
-// Rows split over nsplit items: split s of local row r sits at slot part + s*npos*8 + r.
+// Rows split over nsplit items: split s of local row r sits at slot part + s*stride + r
+// (stride: the low half of `strides`). Rows of a shared prefix come with its pre_nsplit
+// splits before them, at pre_part + s*pre_stride + r (pre_stride: the high half).
 struct CombineItem {
-  int32_t row0, kvh, npos, nsplit, part, pad0, pad1, pad2;
+  int32_t row0, kvh, npos, nsplit, part, pre_part, pre_nsplit, strides;
 };
 static_assert(sizeof(CombineItem) == 32, "CombineItem is 32 bytes");
 
@@ -61,6 +63,7 @@ struct Plan {
   int tile_pos = kTilePosSmall;    // prefill tile positions, selects the kernel shape
   std::vector<WorkItem> items;     // in launch order
   std::vector<CombineItem> combine;
+  int32_t combine_pos = 0;         // most positions of a merge item
   int64_t part_slots = 0;
   // work list as the kernels read it (bytes): items from 0, combine items at off_combine
   size_t off_combine = 0, list_bytes = 0;
@@ -71,9 +74,14 @@ struct Plan {
 ppas_status validate(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,
                      const int32_t* bt_host, int32_t bt_stride, bool check_overlap);
 
-// Builds the plan for a device with num_cus compute units. The step must already be valid.
+// The shared prefixes of a valid step: PPAS_OK, or PPAS_EINVAL.
+ppas_status validate_prefixes(const ppas_seq* seqs, int32_t n_seqs, const int32_t* bt_host, int32_t bt_stride,
+                              const ppas_prefix* prefixes, int32_t n_prefixes);
+
+// Builds the plan for a device with num_cus compute units. The step and its shared
+// prefixes must already be valid.
 void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, int num_cus, const PlanOpts& opts,
-               Plan& plan);
+               Plan& plan, const ppas_prefix* prefixes = nullptr, int32_t n_prefixes = 0);
 
 // The page-write work of a valid step: one item per (request, touched logical page).
 void make_append_items(const ppas_seq* seqs, int32_t n_seqs, std::vector<AppendItem>& items);

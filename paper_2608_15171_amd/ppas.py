@@ -73,7 +73,24 @@ class PlanInfo(ctypes.Structure):
                 ("n_append", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64)]
 
 
+class Rope(ctypes.Structure):
+    """Rotary positions in their general form: see ppas_rope in include/ppas.h, and rope() below."""
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("original_len", ctypes.c_int32), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class Qkv(ctypes.Structure):
+    """A step's new rows where the projection left them: see ppas_qkv."""
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
 _vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+_i64, _R = ctypes.c_int64, ctypes.POINTER(Rope)
 _P = ctypes.POINTER(Shape)
 _O = ctypes.POINTER(PlanOpts)
 _E = ctypes.POINTER(Events)
@@ -117,6 +134,30 @@ _lib.ppas_rope_kv_append_planned.restype = ctypes.c_int
 _lib.ppas_rope_kv_append_planned.argtypes = [_vp, ctypes.c_float, _vp, _vp, _vp, _vp, _vp, _vp, _E, _vp]
 _lib.ppas_attn_step_planned.restype = ctypes.c_int
 _lib.ppas_attn_step_planned.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _E, _vp]
+
+
+_lib.ppas_rope_frequencies.restype = ctypes.c_int
+_lib.ppas_rope_frequencies.argtypes = [_R, _i32, _vp]
+_lib.ppas_rope_rows.restype = ctypes.c_int
+_lib.ppas_rope_rows.argtypes = [_R, _vp, _i64, _vp, _i64, _vp, _i32, _i32, _i32, _i32, _E, _vp]
+_lib.ppas_rope_qkv_append.restype = ctypes.c_int
+_lib.ppas_rope_qkv_append.argtypes = [_P, _R, ctypes.POINTER(Qkv), _vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp]
+_lib.ppas_rope_qkv_append_planned.restype = ctypes.c_int
+_lib.ppas_rope_qkv_append_planned.argtypes = [_vp, _R, ctypes.POINTER(Qkv), _vp, _vp, _vp, _vp, _E, _vp]
+_lib.ppas_step_plan_create_shared.restype = ctypes.c_int
+_lib.ppas_step_plan_create_shared.argtypes = [_P, _vp, _i32, _vp, _i32, _vp, _i32, _O, ctypes.POINTER(ctypes.c_void_p)]
+_lib.ppas_attn_step_shared.restype = ctypes.c_int
+_lib.ppas_attn_step_shared.argtypes = [_P, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _sz, _vp]
+_lib.ppas_attn_shared_workspace_bytes.restype = _sz
+_lib.ppas_attn_shared_workspace_bytes.argtypes = [_P, _vp, _i32, _vp, _i32]
+_lib.ppas_quant_i8.restype = ctypes.c_int
+_lib.ppas_quant_i8.argtypes = [_vp, _i64, _vp, _vp, _i32, _i32, _E, _vp]
+for _f in (_lib.ppas_gateup_proj_i8, _lib.ppas_gateup_act_i8):
+    _f.restype = ctypes.c_int
+    _f.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _sz, _E, _vp]
+for _f in (_lib.ppas_gateup_i8_workspace_bytes, _lib.ppas_gateup_act_i8_workspace_bytes):
+    _f.restype = _sz
+    _f.argtypes = [_i32, _i32, _i32]
 
 
 def status_string(status: int) -> str:
@@ -247,6 +288,107 @@ def rope_kv_append(shape: Shape, theta: float, q, k_pages, v_pages, k_new, v_new
     _check(st, "ppas_rope_kv_append")
 
 
+def rope(layout: str = "half", rotary_dim: int = 128, theta: float = 1e6, scaling: str = "none", factor: float = 1.0,
+         original_len: int = 0, low: float = 0.0, high: float = 0.0, magnitude: float = 1.0) -> Rope:
+    """Rotary positions: `layout` "half" or "interleaved", the first `rotary_dim` features of a head, frequencies
+    scaled for long contexts by "linear", "base", "bands" or "ramp" (ppas_rope in include/ppas.h has the formulas)."""
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        raise ValueError(f"layout is one of {sorted(ROPE_LAYOUTS)}, scaling one of {sorted(ROPE_SCALINGS)}")
+    return Rope(ROPE_LAYOUTS[layout], int(rotary_dim), ROPE_SCALINGS[scaling], int(original_len), float(theta),
+                float(factor), float(low), float(high), float(magnitude))
+
+
+def rope_frequencies(rope: Rope, head_dim: int = 128) -> np.ndarray:
+    """Radians per position of every pair (host only)."""
+    out = np.zeros(max(int(rope.rotary_dim) // 2, 1), dtype=np.float64)
+    _check(_lib.ppas_rope_frequencies(ctypes.byref(rope), int(head_dim), _host_ptr(out)), "ppas_rope_frequencies")
+    return out[:int(rope.rotary_dim) // 2]
+
+
+def _heads(t, name, elem: int = 2):
+    """A device tensor [rows, heads, features] of packed heads (any row stride):
+    its data pointer and row stride."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dim() != 3 or t.element_size() != elem:
+        raise ValueError(f"{name} must be [rows, heads, features] of {elem}-byte elements, got {tuple(t.shape)} {t.dtype}")
+    n, h, d = t.shape
+    row, head, one = t.stride()
+    if (d > 1 and one != 1) or (h > 1 and head != d):
+        raise ValueError(f"the heads of {name} must follow each other")
+    return t.data_ptr(), row if n > 1 else max(row, h * d)
+
+
+def rope_rows(rope: Rope, x, positions, y, transposed: bool = False, events: Events | None = None, stream=None) -> None:
+    """y[r] = the heads of x[r] turned by positions[r] (x, y [rows, heads, features] bf16 with any row stride,
+    positions int32). y may be x. `transposed` turns the other way: the gradient, and without a magnitude the inverse."""
+    xp, xs = _heads(x, "x")
+    yp, ys = _heads(y, "y")
+    if x.shape != y.shape or positions.dim() != 1 or positions.shape[0] != x.shape[0]:
+        raise ValueError(f"shapes x {tuple(x.shape)}, y {tuple(y.shape)}, positions {tuple(positions.shape)} do not match")
+    if positions.element_size() != 4 or positions.is_floating_point():
+        raise ValueError("positions must be int32")
+    n, h, d = x.shape
+    st = _lib.ppas_rope_rows(ctypes.byref(rope), xp, xs, yp, ys, _dev(positions, "positions"), n, h, d,
+                             int(bool(transposed)), None if events is None else ctypes.byref(events), _stream(stream))
+    _check(st, "ppas_rope_rows")
+
+
+def _qkv(shape: Shape, q, k, v, rows: int) -> Qkv:
+    """The step's rows as ppas_qkv; each tensor holds at least `rows` of them."""
+    D = shape.head_dim
+    for t, name, heads in ((q, "q_new", shape.n_q_heads), (k, "k_new", shape.n_kv_heads), (v, "v_new", shape.n_kv_heads)):
+        if t.dim() != 3 or tuple(t.shape[1:]) != (heads, D) or t.shape[0] < rows:
+            raise ValueError(f"{name} must be [{rows} rows or more, {heads}, {D}], got {tuple(t.shape)}")
+    (qp, qs), (kp, ks), (vp, vs) = _heads(q, "q_new"), _heads(k, "k_new"), _heads(v, "v_new")
+    return Qkv(qp, kp, vp, qs, ks, vs)
+
+
+def rope_qkv_append(shape: Shape, rope: Rope, q, k_pages, v_pages, q_new, k_new, v_new, desc, bt_dev, bt_host=None,
+                    stream=None) -> None:
+    """Rotate the rows q_new into q and k_new into the pages at their positions, and copy v_new into the pages. The
+    rows are [T, heads, 128] at any row stride, as a fused QKV projection leaves them."""
+    d = _desc(desc)
+    bt = _bt_host(bt_host, bt_dev)
+    rows = _rows(d)
+    _check_buffers(shape, d, q=q, k_pages=k_pages, v_pages=v_pages, bt_dev=bt_dev, rows=rows)
+    x = _qkv(shape, q_new, k_new, v_new, rows)
+    st = _lib.ppas_rope_qkv_append(ctypes.byref(shape), ctypes.byref(rope), ctypes.byref(x), _dev(q, "q"),
+                                   _dev(k_pages, "k_pages"), _dev(v_pages, "v_pages"), _host_ptr(d), len(d),
+                                   _dev(bt_dev, "block_table"), bt_dev.shape[1], _host_ptr(bt), _stream(stream))
+    _check(st, "ppas_rope_qkv_append")
+
+
+def _prefixes(prefixes):
+    """Shared prefixes as int32 [P, 3] rows of (first request, requests, positions), or None."""
+    if prefixes is None or len(prefixes) == 0:
+        return None
+    p = np.ascontiguousarray(prefixes, dtype=np.int32)
+    if p.ndim != 2 or p.shape[1] != 3:
+        raise ValueError("prefixes must be int32 [P, 3] (first_seq, n_seqs, len)")
+    return p
+
+
+def attn_shared_workspace_bytes(shape: Shape, desc, prefixes) -> int:
+    d, p = _desc(desc), _prefixes(prefixes)
+    return int(_lib.ppas_attn_shared_workspace_bytes(ctypes.byref(shape), _host_ptr(d), len(d), _host_ptr(p),
+                                                     0 if p is None else len(p)))
+
+
+def attn_step_shared(shape: Shape, out, q, k_pages, v_pages, desc, prefixes, bt_dev, workspace, bt_host=None,
+                     stream=None) -> None:
+    """attn_step for a step whose requests share prefixes: rows (first request, requests, shared positions)."""
+    d, p = _desc(desc), _prefixes(prefixes)
+    bt = _bt_host(bt_host, bt_dev)
+    _check_buffers(shape, d, q=q, out=out, k_pages=k_pages, v_pages=v_pages, bt_dev=bt_dev)
+    st = _lib.ppas_attn_step_shared(ctypes.byref(shape), _dev(out, "out"), _dev(q, "q"), _dev(k_pages, "k_pages"),
+                                    _dev(v_pages, "v_pages"), _host_ptr(d), len(d), _host_ptr(p),
+                                    0 if p is None else len(p), _dev(bt_dev, "block_table"), bt_dev.shape[1],
+                                    _host_ptr(bt), _dev(workspace, "workspace"),
+                                    workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "ppas_attn_step_shared")
+
+
 def attn_workspace_bytes(shape: Shape, desc) -> int:
     d = _desc(desc)
     return int(_lib.ppas_attn_workspace_bytes(ctypes.byref(shape), _host_ptr(d), len(d)))
@@ -334,6 +476,59 @@ def gateup_act(x, w, y, workspace=None, events: Events | None = None, stream=Non
     _check(st, "ppas_gateup_act")
 
 
+def quant_i8(x, xq, scale, events: Events | None = None, stream=None) -> None:
+    """The rows of x [R, H] (bf16, any row stride) as 8-bit integers xq [R, H] (int8) and a scale each (fp32 [R]):
+    token rows of activations, or output channels of weights."""
+    if x.dim() != 2 or x.element_size() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("x must be a 2-D bf16 tensor of packed rows")
+    R, H = x.shape
+    if tuple(xq.shape) != (R, H) or xq.element_size() != 1 or tuple(scale.shape) != (R,) or scale.element_size() != 4:
+        raise ValueError(f"xq must be int8 {(R, H)} and scale fp32 {(R,)}, got {tuple(xq.shape)} {tuple(scale.shape)}")
+    if not x.is_cuda:
+        raise ValueError("x must be a device tensor")
+    st = _lib.ppas_quant_i8(x.data_ptr(), x.stride(0) if R > 1 else max(x.stride(0), H), _dev(xq, "xq"),
+                            _dev(scale, "scale"), R, H, None if events is None else ctypes.byref(events),
+                            _stream(stream))
+    _check(st, "ppas_quant_i8")
+
+
+def gateup_i8_workspace_bytes(n_tokens: int, hidden: int, n_out: int) -> int:
+    return int(_lib.ppas_gateup_i8_workspace_bytes(int(n_tokens), int(hidden), int(n_out)))
+
+
+def gateup_act_i8_workspace_bytes(n_tokens: int, hidden: int, n_inter: int) -> int:
+    return int(_lib.ppas_gateup_act_i8_workspace_bytes(int(n_tokens), int(hidden), int(n_inter)))
+
+
+def _gateup_i8(fn, what, x, x_scale, w, w_scale, y, per, workspace, events, stream):
+    for t, name, size in ((x, "x", 1), (w, "w", 1), (y, "y", 2)):
+        if t.dim() != 2 or t.element_size() != size:
+            raise ValueError(f"{name} must be a 2-D tensor of {size}-byte elements")
+    T, H = x.shape
+    N = w.shape[0]
+    if N % per or w.shape[1] != H or tuple(y.shape) != (T, N // per):
+        raise ValueError(f"shapes x {tuple(x.shape)}, w {tuple(w.shape)}, y {tuple(y.shape)} do not match")
+    for t, name, n in ((x_scale, "x_scale", T), (w_scale, "w_scale", N)):
+        if t.numel() != n or t.element_size() != 4 or not t.is_floating_point():
+            raise ValueError(f"{name} must hold {n} fp32 values")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = fn(_dev(x, "x"), _dev(x_scale, "x_scale"), _dev(w, "w"), _dev(w_scale, "w_scale"), _dev(y, "y"), T, H, N // per,
+            _dev(workspace, "workspace"), ws_bytes, None if events is None else ctypes.byref(events), _stream(stream))
+    _check(st, what)
+
+
+def gateup_proj_i8(x, x_scale, w, w_scale, y, workspace=None, events: Events | None = None, stream=None) -> None:
+    """y = (x x_scale) (w w_scale)^T for 8-bit rows x [T, H] and w [N, H] with fp32 scales per row; y [T, N] bf16.
+    workspace: a device buffer for split reductions (see gateup_i8_workspace_bytes), or None."""
+    _gateup_i8(_lib.ppas_gateup_proj_i8, "ppas_gateup_proj_i8", x, x_scale, w, w_scale, y, 1, workspace, events, stream)
+
+
+def gateup_act_i8(x, x_scale, w, w_scale, y, workspace=None, events: Events | None = None, stream=None) -> None:
+    """The gated activation of such products, as gateup_act (w [2I, H], y [T, I]).
+    workspace: see gateup_act_i8_workspace_bytes, or None."""
+    _gateup_i8(_lib.ppas_gateup_act_i8, "ppas_gateup_act_i8", x, x_scale, w, w_scale, y, 2, workspace, events, stream)
+
+
 def stream_read(buf, sink, events: Events | None = None, stream=None) -> None:
     """A plain streaming read of the whole of `buf` (a contiguous device tensor, a multiple of
     16 bytes): the XOR of its 16-byte words, as four 32-bit lanes, is XORed into `sink` (a
@@ -377,7 +572,9 @@ class StepPlan:
     """A step's validated descriptors, attention work list and page-write list, made once
     (ppas_step_plan_create) and used by any number of planned calls, e.g. one per layer."""
 
-    def __init__(self, shape: Shape, desc, bt_host=None, bt_stride: int | None = None, opts: PlanOpts | None = None):
+    def __init__(self, shape: Shape, desc, bt_host=None, bt_stride: int | None = None, opts: PlanOpts | None = None,
+                 prefixes=None):
+        """prefixes: rows (first request, requests, shared positions) of requests that share their first pages."""
         self.shape = Shape(shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.page_size, shape.num_pages,
                            shape.scale)
         self.desc = _desc(desc)
@@ -387,9 +584,16 @@ class StepPlan:
         if bt is not None and bt.shape[1] != self.bt_stride:
             raise ValueError("bt_stride differs from the host block table's row length")
         h = ctypes.c_void_p()
-        st = _lib.ppas_step_plan_create(ctypes.byref(self.shape), _host_ptr(self.desc), len(self.desc),
-                                        _host_ptr(bt), self.bt_stride, _opts_ptr(opts), ctypes.byref(h))
-        _check(st, "ppas_step_plan_create")
+        p = _prefixes(prefixes)
+        if p is None:
+            st = _lib.ppas_step_plan_create(ctypes.byref(self.shape), _host_ptr(self.desc), len(self.desc),
+                                            _host_ptr(bt), self.bt_stride, _opts_ptr(opts), ctypes.byref(h))
+            _check(st, "ppas_step_plan_create")
+        else:
+            st = _lib.ppas_step_plan_create_shared(ctypes.byref(self.shape), _host_ptr(self.desc), len(self.desc),
+                                                   _host_ptr(p), len(p), _host_ptr(bt), self.bt_stride,
+                                                   _opts_ptr(opts), ctypes.byref(h))
+            _check(st, "ppas_step_plan_create_shared")
         self._h = h.value
         self.info = PlanInfo()
         _check(_lib.ppas_step_plan_info(self._h, ctypes.byref(self.info)), "ppas_step_plan_info")
@@ -422,6 +626,17 @@ class StepPlan:
                                               _dev(bt_dev, "block_table"),
                                               None if events is None else ctypes.byref(events), _stream(stream))
         _check(st, "ppas_rope_kv_append_planned")
+
+    def rope_qkv_append(self, rope: Rope, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev,
+                        events: Events | None = None, stream=None) -> None:
+        _check_buffers(self.shape, self.desc, q=q, k_pages=k_pages, v_pages=v_pages, bt_dev=self._bt(bt_dev),
+                       rows=self._n_rows)
+        x = _qkv(self.shape, q_new, k_new, v_new, self._n_rows)
+        st = _lib.ppas_rope_qkv_append_planned(self._h, ctypes.byref(rope), ctypes.byref(x), _dev(q, "q"),
+                                               _dev(k_pages, "k_pages"), _dev(v_pages, "v_pages"),
+                                               _dev(bt_dev, "block_table"),
+                                               None if events is None else ctypes.byref(events), _stream(stream))
+        _check(st, "ppas_rope_qkv_append_planned")
 
     def attn_step(self, out, q, k_pages, v_pages, bt_dev, workspace, events: Events | None = None,
                   stream=None) -> None:

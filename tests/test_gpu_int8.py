@@ -1,0 +1,310 @@
+"""GPU parity of the 8-bit quantiser and products (ppas_quant_i8, ppas_gateup_proj_i8, ppas_gateup_act_i8).
+
+The quantiser's integers are exact; its scale is one fp32 division (2^-24). A product's integer sum s is exact; the
+scales' product c, float(s) and their product are rounded to fp32 (2^-24 each), and the result to bf16 (2^-8 of it):
+    |y - c s| <= (2^-8 + 2^-22) |c s|.
+With the activation, g and u are off by 3 x 2^-24 each before it; silu has slope at most 1.1, its fp32 evaluation and the
+product with u add 2^-24 (|g| + 4) |z|, and the rounding 2^-8 of the result:
+    |y - z| <= (2^-8 |z| + 3 x 2^-24 (1.1 |g u| + |z|) + 2^-24 (|g| + 4) |z|) / (1 - 2^-8).
+"""
+import numpy as np
+import pytest
+
+import oracle.int8 as Q
+from paper_2608_15171_amd import inputs as I
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2608_15171_amd import ppas, step
+    return ppas, step, torch
+
+
+# ------------------------------------------------------------------ quantiser
+
+def quant(lib, bits, stride=None, shift=0):
+    ppas, step, torch = lib
+    R, H = bits.shape
+    stride = H if stride is None else stride
+    buf = torch.full((shift + R * stride + 8,), -1, dtype=torch.int16, device="cuda")
+    x = buf.as_strided((R, H), (stride, 1), shift)
+    x.copy_(torch.from_numpy(bits.view(np.int16)))
+    xq = torch.full((R + 2, H), 99, dtype=torch.int8, device="cuda")
+    s = torch.full((R + 2,), -7.0, dtype=torch.float32, device="cuda")
+    ppas.quant_i8(x.view(torch.bfloat16), xq[:R], s[:R])
+    torch.cuda.synchronize()
+    assert bool((xq[R:] == 99).all()) and bool((s[R:] == -7.0).all())
+    return xq[:R].cpu().numpy(), s[:R].double().cpu().numpy()
+
+
+def check_quant(lib, bits, label, **kw):
+    print(f"quant {label} {bits.shape} {kw}", flush=True)
+    q, s = quant(lib, bits, **kw)
+    qr, sr = Q.quantise(bits)
+    assert np.array_equal(q, qr), f"{label}: {int((q != qr).sum())} integers differ"
+    fine = np.isfinite(sr)
+    assert np.array_equal(np.isnan(s), ~fine)
+    assert (np.abs(s[fine] - sr[fine]) <= 2.0 ** -24 * sr[fine]).all()
+
+
+@pytest.mark.parametrize("R,H", [(1, 1), (3, 7), (2, 8), (5, 100), (24, 2048), (300, 2048), (1030, 2048), (1025, 512),
+                                 (7, 11008), (1100, 2040), (9, 16384), (3, 16392), (2, 40000), (1029, 2056)])
+def test_quantiser(lib, R, H):
+    check_quant(lib, I.normal_bf16(I.rng(1, R, H), (R, H)), "sizes")
+
+
+@pytest.mark.parametrize("H,stride,shift", [(2048, 2560, 0), (2048, 2056, 8), (2048, 2049, 0), (100, 101, 3), (64, 64, 1)])
+def test_quantiser_strides(lib, H, stride, shift):
+    check_quant(lib, I.normal_bf16(I.rng(2, H, stride), (1040, H)), "strides", stride=stride, shift=shift)
+
+
+@pytest.mark.parametrize("H", [256, 4096, 2055])
+def test_quantiser_every_value(lib, H):
+    """Rows over all bf16 bit patterns: every exponent, subnormals, both zeros, infinities and NaNs."""
+    bits = np.arange(65536, dtype=np.uint16)
+    rows = np.resize(bits, (-(-65536 // H), H))
+    check_quant(lib, rows, "patterns")
+    # every mantissa against every maximum's, over twelve binades
+    m = (np.arange(12)[:, None] * 128 + np.arange(128)).reshape(-1).astype(np.uint16) + np.uint16((127 - 11) << 7)
+    for sign in (0, 0x8000):
+        rows = np.zeros((128, H), np.uint16)
+        k = min(H - 1, len(m))
+        rows[:, :k] = m[None, :k] | np.uint16(sign)
+        rows[:, k] = (128 << 7) | np.arange(128, dtype=np.uint16)
+        check_quant(lib, rows, "ratios")
+
+
+@pytest.mark.parametrize("H", [64, 2048, 33])
+def test_quantiser_special_rows(lib, H):
+    b = I.normal_bf16(I.rng(4, H), (9, H))
+    b[0] = 0
+    b[1, H // 2] = 0x7f80                              # infinity
+    b[2, H - 1] = 0xffc0                               # NaN
+    b[3] = 0x8000                                      # minus zero
+    b[4] = (127 - 110) << 7                            # 2^-110: the smallest row that counts
+    b[5] = ((127 - 110) << 7) - 1                      # just below
+    b[6] = 1                                           # the smallest subnormal
+    b[7, 0] = 0x7f7f                                   # the largest finite value
+    check_quant(lib, b, "special")
+
+
+# ------------------------------------------------------------------ products
+
+def make(lib, T, H, N, seed, extreme=False):
+    ppas, step, torch = lib
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    if extreme:
+        x = torch.full((T, H), -128, dtype=torch.int8, device="cuda")
+        w = torch.full((N, H), -128, dtype=torch.int8, device="cuda")
+    else:
+        x = torch.randint(-128, 128, (T, H), dtype=torch.int8, device="cuda", generator=g)
+        w = torch.randint(-128, 128, (N, H), dtype=torch.int8, device="cuda", generator=g)
+    sx = torch.rand(T, device="cuda", generator=g) * 0.02 + 1e-3
+    sw = torch.rand(N, device="cuda", generator=g) * 4e-4 + 1e-5
+    return x, sx, w, sw
+
+
+def call(lib, x, sx, w, sw, act, split=True):
+    ppas, step, torch = lib
+    T, H = x.shape
+    n = w.shape[0] // (2 if act else 1)
+    y = torch.full((T, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+    size = ppas.gateup_act_i8_workspace_bytes if act else ppas.gateup_i8_workspace_bytes
+    nbytes = size(T, H, n) if split is True else int(split)
+    ws = torch.full((nbytes // 4,), -1, dtype=torch.int32, device="cuda") if nbytes else None
+    (ppas.gateup_act_i8 if act else ppas.gateup_proj_i8)(x, sx, w, sw, y, ws)
+    torch.cuda.synchronize()
+    return y
+
+
+def check(lib, x, sx, w, sw, y, act, label):
+    """Every element, in double on the GPU: integer products of up to 131,071 features are exact there."""
+    ppas, step, torch = lib
+    wd, worst = w.double(), 0.0
+    for r in range(0, x.shape[0], 2048):
+        s = torch.matmul(x[r:r + 2048].double(), wd.t()) * sx[r:r + 2048].double()[:, None] * sw.double()
+        got = y[r:r + 2048].double()
+        if act:
+            n = y.shape[1]
+            gate, up = s[:, :n], s[:, n:]
+            z = torch.nn.functional.silu(gate) * up
+            bound = (2.0 ** -8 * z.abs() + 3 * 2.0 ** -24 * (1.1 * (gate * up).abs() + z.abs())
+                     + 2.0 ** -24 * (gate.abs() + 4) * z.abs()) / (1 - 2.0 ** -8)
+        else:
+            z = s
+            bound = (2.0 ** -8 + 2.0 ** -22) * z.abs()
+        bound = bound + 1e-30
+        assert bool(torch.isfinite(got).all()), label
+        worst = max(worst, float(((got - z).abs() / bound).max()))
+    print(f"{label}: err/bound={worst:.3f}", flush=True)
+    assert worst <= 1.0, label
+
+
+SHAPES = [(1, 1, 1), (1, 128, 1), (3, 5, 2), (5, 64, 150), (31, 100, 17), (257, 128, 256), (300, 384, 260),
+          (256, 256, 128), (513, 2048, 300), (700, 640, 515), (65, 63, 65), (64, 127, 33), (16, 2048, 11008),
+          (3, 2048, 1025), (100, 11008, 1280), (2048, 2048, 1024), (1125, 256, 7650), (130, 4096, 11005)]
+
+
+@pytest.mark.parametrize("T,H,N", SHAPES)
+@pytest.mark.parametrize("act", [False, True])
+@pytest.mark.parametrize("split", [True, 0])
+def test_ragged_shapes_every_element(lib, T, H, N, act, split):
+    print(f"i8 T={T} H={H} N={N} act={act} split={split}", flush=True)
+    a = make(lib, T, H, 2 * N if act else N, 3)
+    check(lib, *a, call(lib, *a, act, split), act, f"T{T} H{H} N{N} act={act}")
+
+
+# (tokens, features, columns) that reach each kernel of the bf16 projection at half the features
+ACT_VARIANTS = [(9, 22016, 1514), (13, 6016, 3836), (8, 6016, 6233), (8, 4224, 8874), (30, 7168, 1395), (21, 6016, 2375),
+                (25, 2048, 5864), (24, 4096, 11008), (208, 11008, 131), (88, 2048, 1665), (139, 1152, 1873),
+                (70, 1152, 4183), (48, 4096, 11008), (228, 640, 2056), (775, 7168, 54), (256, 256, 8197),
+                (129, 256, 10982), (1024, 22016, 133), (1136, 22016, 12), (768, 640, 5600), (611, 640, 10889),
+                (1280, 11008, 1549), (2076, 22016, 387)]
+PROJ_VARIANTS = [(1, 4096, 8192), (16, 2048, 2048), (24, 11008, 2048), (48, 22016, 512), (200, 4096, 512), (9, 4096, 200),
+                 (60, 1152, 9000), (130, 8192, 3000), (700, 2048, 2048), (2056, 11008, 2048), (520, 22016, 256),
+                 (4100, 1024, 2560), (33, 16384, 8192)]
+
+
+@pytest.mark.parametrize("T,H,N,act", [(*s, True) for s in ACT_VARIANTS] + [(*s, False) for s in PROJ_VARIANTS])
+def test_kernel_variants_every_element(lib, T, H, N, act):
+    print(f"i8 variants T={T} H={H} N={N} act={act}", flush=True)
+    a = make(lib, T, H, 2 * N if act else N, 14)
+    check(lib, *a, call(lib, *a, act), act, f"T{T} H{H} N{N} act={act}")
+
+
+@pytest.mark.parametrize("T,H,N,act", [(16384, 2048, 11008, True), (16384, 2048, 2560, False), (16384, 11008, 2048, False)])
+def test_layer_sizes_every_element(lib, T, H, N, act):
+    print(f"i8 T={T} H={H} N={N} act={act}", flush=True)
+    a = make(lib, T, H, 2 * N if act else N, 15)
+    check(lib, *a, call(lib, *a, act), act, f"T{T} H{H} N{N} act={act}")
+
+
+@pytest.mark.parametrize("T,H,N", [(2, 131071, 3), (3, 130944, 40), (70, 131072 - 128, 5)])
+def test_largest_sums(lib, T, H, N):
+    """-128 x -128 over the largest hidden size: 2,147,467,264 still fits int32."""
+    a = make(lib, T, H, N, 16, extreme=True)
+    check(lib, *a, call(lib, *a, False), False, f"extreme H{H}")
+
+
+@pytest.mark.parametrize("which", ["x", "w", "xw"])
+@pytest.mark.parametrize("act", [False, True])
+def test_operands_off_16_bytes(lib, which, act):
+    ppas, step, torch = lib
+    x, sx, w, sw = make(lib, 70, 256, 130, 17)
+
+    def off(t):
+        flat = torch.zeros(t.numel() + 16, dtype=torch.int8, device="cuda")
+        v = flat[1:1 + t.numel()].view(t.shape)
+        v.copy_(t)
+        return v
+    if "x" in which:
+        x = off(x)
+    if "w" in which:
+        w = off(w)
+    check(lib, x, sx, w, sw, call(lib, x, sx, w, sw, act), act, f"off {which}")
+
+
+@pytest.mark.parametrize("T,H,N", [(40, 11008, 2048), (2056, 11008, 512), (300, 4096, 256)])
+def test_results_depend_on_neither_workspace_nor_neighbours(lib, T, H, N):
+    ppas, step, torch = lib
+    x, sx, w, sw = make(lib, T, H, N, 18)
+    whole = call(lib, x, sx, w, sw, False).view(torch.int16)
+    full = ppas.gateup_i8_workspace_bytes(T, H, N)
+    for nbytes in (0, full // 2, max(0, full - 4)):
+        assert torch.equal(call(lib, x, sx, w, sw, False, nbytes).view(torch.int16), whole), nbytes
+    for t in (1, 17, T - 3):
+        assert torch.equal(call(lib, x[:t], sx[:t], w, sw, False).view(torch.int16), whole[:t]), t
+
+
+def test_scales_of_every_kind(lib):
+    """Zero, negative, tiny, NaN and infinite scales touch their own rows and columns only."""
+    ppas, step, torch = lib
+    x, sx, w, sw = make(lib, 40, 256, 96, 19)
+    plain = call(lib, x, sx, w, sw, False)
+    sx[3], sx[7], sw[5], sw[11] = float("nan"), 0.0, -1.0, float("inf")
+    y = call(lib, x, sx, w, sw, False)
+    rows = torch.ones(40, dtype=torch.bool)
+    rows[[3, 7]] = False
+    cols = torch.ones(96, dtype=torch.bool)
+    cols[[5, 11]] = False
+    assert torch.equal(y[rows][:, cols], plain[rows][:, cols])
+    assert bool(y[3].isnan().all()) and bool((y[7][cols] == 0).all())
+
+
+def test_no_tokens_other_stream_and_replay(lib):
+    ppas, step, torch = lib
+    T, H, N = 33, 2048, 1024
+    bf = torch.randn(T, H, device="cuda").bfloat16()
+    _, _, w, sw = make(lib, 1, H, N, 20)
+    xq, sx = torch.empty(T, H, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    nbytes = max(256, ppas.gateup_i8_workspace_bytes(T, H, N))
+    ws, y = torch.empty(nbytes, dtype=torch.uint8, device="cuda"), torch.empty(T, N, dtype=torch.bfloat16, device="cuda")
+
+    def both(stream=None):
+        ppas.quant_i8(bf, xq, sx, stream=stream)
+        ppas.gateup_proj_i8(xq, sx, w, sw, y, ws, stream=stream)
+    ppas.quant_i8(bf[:0], xq[:0], sx[:0])
+    ppas.gateup_proj_i8(xq[:0], sx[:0], w, sw, y[:0], ws)
+    both()
+    want = y.clone()
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    y.zero_()
+    torch.cuda.synchronize()
+    both(s)
+    s.synchronize()
+    assert torch.equal(y, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        both()
+    for k in range(3):
+        bf.copy_(torch.randn(T, H, device="cuda"))
+        both()
+        want = y.clone()
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want), k
+
+
+def test_weights_quantised_by_channel(lib):
+    """Weights are rows too: the quantised product is within the two quantisers' half steps of the bf16 one."""
+    ppas, step, torch = lib
+    T, H, N = 50, 2048, 300
+    x, w = torch.randn(T, H, device="cuda").bfloat16(), (torch.randn(N, H, device="cuda") * 0.02).bfloat16()
+    q = []
+    for t in (x, w):
+        a, s = torch.empty(t.shape, dtype=torch.int8, device="cuda"), torch.empty(len(t), device="cuda")
+        ppas.quant_i8(t, a, s)
+        q += [a, s]
+    y = torch.empty(T, N, dtype=torch.bfloat16, device="cuda")
+    ppas.gateup_proj_i8(*q, y)
+    xd, wd, sx, sw = x.double(), w.double(), q[1].double(), q[3].double()
+    ref = xd @ wd.t()
+    # every element is off by at most half a step of its row: |dx| <= sx / 2 (and 2^-23 of sx x 127)
+    half = 0.5 + 127 * 2.0 ** -23
+    bound = half * sx[:, None] * wd.abs().sum(1) + half * sw * xd.abs().sum(1)[:, None] + half ** 2 * H * sx[:, None] * sw
+    assert bool(((y.double() - ref).abs() <= bound + 2.0 ** -8 * y.double().abs()).all())
+    rel = float((y.double() - ref).norm() / ref.norm())
+    print(f"8-bit against bf16: relative {rel:.4f}", flush=True)
+
+
+def test_binding_refusals(lib):
+    ppas, step, torch = lib
+    x, sx, w, sw = make(lib, 4, 64, 8, 21)
+    y = torch.empty(4, 8, dtype=torch.bfloat16, device="cuda")
+    for bad in ((x.float(), sx, w, sw, y), (x, sx[:3], w, sw, y), (x, sx, w[:, :32], sw, y), (x, sx, w, sw[:7], y),
+                (x, sx, w, sw, y[:, :7]), (x, sx.double(), w, sw, y), (x.cpu(), sx, w, sw, y), (x, sx, w.t(), sw, y),
+                (x, sx, w, sw, y.float()), (x, sx.int(), w, sw, y)):
+        with pytest.raises(ValueError):
+            ppas.gateup_proj_i8(*bad)
+    with pytest.raises(ValueError):
+        ppas.gateup_act_i8(x, sx, w[:7], sw[:7], y[:, :3])
+    b = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    for bad in ((b.float(), x, sx), (b, x[:, :32], sx), (b, x, sx[:3]), (b.t(), x.t(), sx), (b.cpu(), x, sx), (b, b, sx)):
+        with pytest.raises(ValueError):
+            ppas.quant_i8(*bad)

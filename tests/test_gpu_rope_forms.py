@@ -1,0 +1,274 @@
+"""GPU parity of the rotary forms (ppas_rope_rows, ppas_rope_qkv_append) against the 64-bit oracle.
+
+Bound of a turned element, m (a cos t - b sin t): the angle is reduced in fp64 and rounded to fp32, at most pi, so it is
+off by at most 2^-24 pi; cos and sin are within two units (2^-23); the magnitude, its product with them, the two
+products and their sum round once each (2^-24). Together under 1e-6 m (|a| + |b|), and the result is rounded to bf16
+once, by at most 2^-8 of its value:
+    |gpu - exact| <= 2^-8 |exact| + 1e-6 m (|a| + |b|).
+fp64's own reduction error, 2^-53 of the turns, stays below 1e-6 radians up to 2^31 positions. Features that do not turn
+are copied bit for bit, NaNs and infinities included, and nothing else is written.
+"""
+import numpy as np
+import pytest
+
+import oracle.kv_cache as OK
+import oracle.rope as R
+import oracle.rope_forms as F
+from paper_2608_15171_amd import inputs as I
+
+pytestmark = pytest.mark.gpu
+
+BANDS = dict(scaling="bands", factor=8.0, original_len=8192, low=1.0, high=4.0)
+RAMP = dict(scaling="ramp", factor=4.0, original_len=8192, low=1.0, high=32.0)
+SENTINEL = 0xFFFF
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2608_15171_amd import ppas, step
+    return ppas, step, torch
+
+
+def check(got_bits, x_bits, positions, layout, rotary, theta, label, magnitude=1.0, transposed=False, **kw):
+    x = R.bf16_bits_to_f64(x_bits)
+    ref = F.turn(np.where(np.isfinite(x), x, 0.0), positions, layout, rotary, theta, magnitude, transposed, **kw)
+    a, b = F.pairs_of(layout, rotary)
+    tol = 2.0 ** -8 * np.abs(ref)
+    for one in (a, b):
+        tol[..., one] += 1e-6 * magnitude * (np.abs(x[..., a]) + np.abs(x[..., b]))
+    assert np.array_equal(got_bits[..., rotary:], x_bits[..., rotary:]), f"{label}: copied features changed"
+    got = R.bf16_bits_to_f64(got_bits[..., :rotary])
+    err, tol = np.abs(got - ref[..., :rotary]), tol[..., :rotary]
+    print(f"{label}: worst/tol={float((err / np.maximum(tol, 1e-300)).max()) if err.size else 0:.3f}", flush=True)
+    assert np.isfinite(got).all() and (err <= tol).all(), label
+
+
+def rows_case(lib, rows, heads, dim, layout, rotary, seed=0, pad=0, shift=0, positions=None, in_place=False, theta=1e6,
+              transposed=False, **kw):
+    """Rows `pad` elements apart from a base `shift` elements into its buffer; everything around them stays as it was."""
+    ppas, step, torch = lib
+    g = I.rng(seed, rows, heads, dim, rotary)
+    x = I.normal_bf16(g, (rows, heads, dim))
+    if rotary < dim:
+        x[..., rotary:][g.random((rows, heads, dim - rotary)) < 0.2] = 0x7f80      # infinities and NaNs are copied
+        x[0, 0, -1] = 0x7fc1
+    pos = g.integers(0, 131072, rows) if positions is None else np.asarray(positions)
+    stride = heads * dim + pad
+
+    def place(bits):
+        buf = torch.full((shift + rows * stride + 64,), -1, dtype=torch.int16, device="cuda")
+        view = buf.as_strided((rows, heads, dim), (stride, dim, 1), shift)
+        if bits is not None:
+            view.copy_(torch.from_numpy(bits.view(np.int16)))
+        return buf, view.view(torch.bfloat16)
+
+    xbuf, xv = place(x)
+    ybuf, yv = (xbuf, xv) if in_place else place(None)
+    print(f"rope rows={rows} heads={heads} dim={dim} {layout} rotary={rotary} pad={pad} shift={shift} {kw}", flush=True)
+    ppas.rope_rows(ppas.rope(layout, rotary, theta, **kw), xv, torch.from_numpy(pos.astype(np.int32)).cuda(), yv, transposed)
+    torch.cuda.synchronize()
+    check(step.bits_of(yv), x, pos, layout, rotary, theta, "rows", transposed=transposed, **kw)
+    if not in_place:
+        assert np.array_equal(step.bits_of(xv), x)
+    around = torch.ones(ybuf.numel(), dtype=torch.bool, device="cuda")
+    around.as_strided((rows, heads, dim), (stride, dim, 1), shift).fill_(False)
+    assert bool((ybuf[around] == -1).all()), "wrote outside its rows"
+    return step.bits_of(yv)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("rotary", [2, 20, 64, 96, 126, 128])
+@pytest.mark.parametrize("kw", [dict(), dict(scaling="linear", factor=3.0), dict(scaling="base", factor=4.0), BANDS,
+                                dict(magnitude=1.1386, **RAMP)])
+def test_forms(lib, layout, rotary, kw):
+    rows_case(lib, 37, 3, 128, layout, rotary, **kw)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("rows,heads,dim,rotary", [(1, 1, 2, 2), (1, 1, 128, 128), (5, 7, 6, 4), (33, 2, 80, 32),
+                                                   (3, 1, 256, 256), (17, 5, 100, 100), (2, 200, 64, 48),
+                                                   (1500, 18, 128, 128), (16385, 2, 128, 64), (40000, 1, 64, 64)])
+def test_sizes(lib, layout, rows, heads, dim, rotary):
+    rows_case(lib, rows, heads, dim, layout, rotary, seed=1)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("pad,shift", [(512, 0), (8, 8), (4, 0), (1, 0), (0, 1), (3, 5)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_strides_and_alignment(lib, layout, pad, shift, in_place):
+    rows_case(lib, 50, 5, 128, layout, 96, seed=2, pad=pad, shift=shift, in_place=in_place)
+    rows_case(lib, 50, 5, 128, layout, 44, seed=3, pad=pad, shift=shift, in_place=in_place)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_far_and_negative_positions(lib, layout):
+    far = [0, -1, -77, 1 << 20, (1 << 31) - 1, -(1 << 31), 131071, 3]
+    rows_case(lib, len(far), 2, 128, layout, 128, seed=4, positions=far)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_position_zero_is_the_row_itself(lib, layout):
+    x = I.normal_bf16(I.rng(5, 4, 2, 128, 128), (4, 2, 128))
+    assert np.array_equal(rows_case(lib, 4, 2, 128, layout, 128, seed=5, positions=[0] * 4), x)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_transposed_is_the_gradient(lib, layout):
+    """The turn is linear: its transpose is the gradient, which the oracle gives, and <T x, g> = <x, T' g>."""
+    ppas, step, torch = lib
+    kw = dict(magnitude=1.1386, **RAMP)
+    rows_case(lib, 20, 3, 128, layout, 96, seed=6, transposed=True, **kw)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, d = (torch.randn(64, 4, 128, device="cuda", generator=g).bfloat16() for _ in range(2))
+    pos = torch.arange(64, device="cuda", dtype=torch.int32) * 977
+    r, y, dx = ppas.rope(layout, 96, **kw), torch.empty_like(x), torch.empty_like(x)
+    ppas.rope_rows(r, x, pos, y)
+    ppas.rope_rows(r, d, pos, dx, transposed=True)
+    a, b = (y.double() * d.double()).sum((1, 2)), (x.double() * dx.double()).sum((1, 2))
+    # every output is rounded by at most 2^-8 (and 1e-6 of its pair before that)
+    tol = 2.01 ** -8 * ((y.double() * d.double()).abs().sum((1, 2)) + (x.double() * dx.double()).abs().sum((1, 2))) + 1e-3
+    assert bool(((a - b).abs() <= tol).all())
+    # the difference of two rows' turns is the turn of their difference, as differences of any step
+    h = torch.zeros_like(x)
+    h[:, :, 5] = 0.5
+    yh = torch.empty_like(x)
+    ppas.rope_rows(r, h, pos, yh)
+    dxh = (yh.double() * d.double()).sum((1, 2)) / 0.5
+    want = dx.double()[:, :, 5].sum(1)
+    bound = 2.01 ** -8 * ((yh.double() * d.double()).abs().sum((1, 2)) / 0.5 + dx.double()[:, :, 5].abs().sum(1)) + 1e-4
+    assert bool(((dxh - want).abs() <= bound).all())
+
+
+def test_no_rows_other_stream_and_replay(lib):
+    ppas, step, torch = lib
+    r = ppas.rope("interleaved", 64, **BANDS)
+    x = torch.randn(24, 3, 128, device="cuda").bfloat16()
+    pos = torch.arange(24, device="cuda", dtype=torch.int32) + 1000
+    want = torch.empty_like(x)
+    ppas.rope_rows(r, x[:0], pos[:0], want[:0])
+    ppas.rope_rows(r, x, pos, want)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    y = torch.zeros_like(x)
+    torch.cuda.synchronize()
+    ppas.rope_rows(r, x, pos, y, stream=s)
+    s.synchronize()
+    assert torch.equal(y.view(torch.int16), want.view(torch.int16))
+    graph = torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=s):
+        ppas.rope_rows(r, x, pos, y)
+    for k in range(3):
+        x.copy_(torch.randn(24, 3, 128, device="cuda"))
+        pos.add_(k + 1)
+        ppas.rope_rows(r, x, pos, want)
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y.view(torch.int16), want.view(torch.int16)), k
+
+
+# ------------------------------------------------------------------ a step's rows into the pages
+
+def append_case(lib, spec, seed, layout="half", rotary=128, theta=1e6, fused=True, extra=0, shift=0, in_place=False,
+                planned=True, **kw):
+    ppas, step, torch = lib
+    data = I.make_step_data(spec, seed, with_history=False)
+    bt, npages = I.make_block_table(spec, seed, spare_pages=4)
+    ds = step.DeviceStep(data, bt, npages, pool_fill=SENTINEL)
+    k0, v0 = step.bits_of(ds.k_pages), step.bits_of(ds.v_pages)
+    T, hq, hkv = spec.n_rows, spec.n_q_heads, spec.n_kv_heads
+    print(f"append rows={T} {layout} rotary={rotary} fused={fused} extra={extra} shift={shift} {kw}", flush=True)
+    if fused:
+        stride = (hq + 2 * hkv) * 128 + extra
+        buf = torch.full((shift + T * stride + 8,), -1, dtype=torch.int16, device="cuda").view(torch.bfloat16)
+        rows = buf.as_strided((T, hq + 2 * hkv, 128), (stride, 128, 1), shift)
+        q_new, k_new, v_new = rows[:, :hq], rows[:, hq:hq + hkv], rows[:, hq + hkv:]
+        q_new.copy_(ds.q), k_new.copy_(ds.k_new), v_new.copy_(ds.v_new)
+        before = buf.view(torch.int16).clone()
+    else:
+        q_new, k_new, v_new, before = ds.q, ds.k_new, ds.v_new, None
+    # rows behind the step's last one stay as they were
+    q = torch.full((T + 3, hq, 128), -1, dtype=torch.int16, device="cuda").view(torch.bfloat16)
+    out = q_new if in_place else q
+    r = ppas.rope(layout, rotary, theta, **kw)
+    if planned:
+        with ds.plan() as plan:
+            plan.rope_qkv_append(r, out, ds.k_pages, ds.v_pages, q_new, k_new, v_new, ds.bt)
+    else:
+        ppas.rope_qkv_append(ds.shape, r, out, ds.k_pages, ds.v_pages, q_new, k_new, v_new, ds.desc, ds.bt, ds.bt_host)
+    torch.cuda.synchronize()
+    pos = R.row_positions(data.desc)
+    got_q = step.bits_of(out)[:T]
+    check(got_q, data.q, pos, layout, rotary, theta, "append q", **kw)
+    if not in_place:
+        assert (step.bits_of(q)[T:] == SENTINEL).all()
+    if fused:
+        assert torch.equal(buf.view(torch.int16), before)
+    kp, vp = step.bits_of(ds.k_pages), step.bits_of(ds.v_pages)
+    kw_, vw = OK.append(k0, v0, data.k_new, data.v_new, data.desc, bt, 16)
+    assert np.array_equal(vp, vw)
+    for s, (qs, n, c) in enumerate(data.desc.tolist()):
+        kg, _ = OK.gather(kp, vp, bt[s], c + n, 16)
+        check(kg[c:], data.k_new[qs:qs + n], pos[qs:qs + n], layout, rotary, theta, f"append k seq{s}", **kw)
+    # nothing but the new positions changed: the plain rows put back give the plain append
+    assert np.array_equal(OK.append(kp, vp, data.k_new, data.v_new, data.desc, bt, 16)[0], kw_)
+    return got_q, kp
+
+
+EDGES = [I.Seq(1, 0, 0), I.Seq(1, 15, 1), I.Seq(1, 16, 2), I.Seq(3, 14, 3), I.Seq(17, 31, 4), I.Seq(40, 0, 5)]
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("rotary,kw", [(128, {}), (64, BANDS), (96, dict(magnitude=1.1386, **RAMP)),
+                                       (20, dict(scaling="linear", factor=2.0)), (2, dict(scaling="base", factor=4.0))])
+def test_append_forms(lib, layout, rotary, kw):
+    append_case(lib, I.StepSpec("edges", EDGES), 7, layout, rotary, **kw)
+
+
+@pytest.mark.parametrize("seed", range(3))
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("extra,shift", [(0, 0), (8, 8), (2, 0), (1, 3)])
+def test_append_strides(lib, seed, layout, extra, shift):
+    heads = dict(n_q_heads=8, n_kv_heads=1) if seed == 1 else {}
+    spec = I.random_small_step(seed + 40, max_seqs=6, max_n=70, max_c=300, **heads)
+    append_case(lib, spec, seed, layout, 64, extra=extra, shift=shift, **BANDS)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("planned", [True, False])
+def test_append_packed_rows_in_place(lib, layout, planned):
+    append_case(lib, I.StepSpec("edges", EDGES), 8, layout, 96, fused=False, in_place=True, planned=planned)
+
+
+def test_append_is_the_plain_rotation_append(lib):
+    """The half layout over the whole head without scaling: the bits that ppas_rope_kv_append writes."""
+    ppas, step, torch = lib
+    spec = I.StepSpec("edges", EDGES)
+    got_q, kp = append_case(lib, spec, 9)
+    data = I.make_step_data(spec, 9, with_history=False)
+    bt, npages = I.make_block_table(spec, 9, spare_pages=4)
+    ds = step.DeviceStep(data, bt, npages, pool_fill=SENTINEL)
+    ds.rope_append(1e6)
+    torch.cuda.synchronize()
+    assert np.array_equal(step.bits_of(ds.q), got_q) and np.array_equal(step.bits_of(ds.k_pages), kp)
+
+
+@pytest.mark.parametrize("cfg,layout,rotary,kw", [(2, "half", 128, dict(magnitude=1.1386, **RAMP)), (3, "interleaved", 64, BANDS)])
+def test_append_full_size_steps(lib, cfg, layout, rotary, kw):
+    append_case(lib, I.CONFIGS[cfg](0), 0, layout, rotary, **kw)
+
+
+def test_binding_refusals(lib):
+    ppas, step, torch = lib
+    x = torch.zeros(4, 2, 128, device="cuda", dtype=torch.bfloat16)
+    p = torch.zeros(4, device="cuda", dtype=torch.int32)
+    for args in ((x, p[:3], x), (x, p.long(), x), (x, p, x[:3]), (x[:, :, ::2], p, x[:, :, ::2]),
+                 (x.float(), p, x.float()), (x.cpu(), p, x), (x, p.cpu(), x), (x.flatten(1), p, x.flatten(1)),
+                 (x.transpose(0, 1)[:, :2], p[:2], x[:2])):
+        with pytest.raises(ValueError):
+            ppas.rope_rows(ppas.rope(), *args)
+    with pytest.raises(ppas.PPASError):
+        ppas.rope_rows(ppas.rope(), x[:2], p[:2], x[1:3])       # overlapping rows

@@ -1,0 +1,15 @@
+"""Order of LDS reads and refills in the 8-bit products' tile kernels (CPU only), as in test_lds_order."""
+import pytest
+
+from test_lds_order import _kernels, longest_flight
+
+
+def test_no_lds_read_is_in_flight_across_two_barriers(tmp_path):
+    bodies = _kernels(tmp_path, "gateup_i8.hip")
+    names = [n for n in bodies if "gateup_kernelILi256E" in n or "gateup_kernelILi128E" in n]
+    assert len(names) == 4
+    for n in names:
+        assert sum(l.startswith("s_barrier") for l in bodies[n]) >= 4 and \
+            sum(l.startswith("ds_read") for l in bodies[n]) >= 16, n
+        worst, where = longest_flight(bodies[n])
+        assert worst <= 1, f"{n}: an LDS read in flight across {worst} barriers ({where})"
