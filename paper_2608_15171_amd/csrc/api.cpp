@@ -235,6 +235,8 @@ struct ppas_step_plan {
   Plan plan;
   int32_t n_append = 0;
   size_t off_append = 0;
+  int32_t n_desc = 0;            // the page-write list by request, where the step has few
+  AppendDesc desc[kAppendInline];
   Pinned* buf = nullptr;
 };
 
@@ -266,6 +268,15 @@ ppas_status build_plan(ppas_step_plan& p, const ppas_shape* shape, const ppas_se
   if (want & kWantAppend) make_append_items(seqs, n_seqs, app);
   if (!plan_fits(p.plan, app.size())) return PPAS_ERANGE;
   p.n_append = int32_t(app.size());
+  if ((want & kWantAppend) && n_seqs <= kAppendInline) {
+    int32_t item = 0;
+    for (int32_t s = 0; s < n_seqs; ++s) {
+      const ppas_seq& q = seqs[s];
+      p.desc[s] = AppendDesc{item, q.query_start, q.n_query, q.cached_len};
+      item += (q.cached_len + q.n_query - 1) / kPage - q.cached_len / kPage + 1;
+    }
+    p.n_desc = n_seqs;
+  }
   const size_t list = (want & kWantAttn) ? p.plan.list_bytes : 0;
   p.off_append = (list + 255) / 256 * 256;
   const size_t bytes = p.off_append + app.size() * sizeof(AppendItem);
@@ -316,7 +327,7 @@ bool off(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p)
 // T: the step's token rows.
 ppas_status check_qkv(const ppas_shape& s, const ppas_rope* rope, const ppas_qkv* r, const void* q_out,
                       const void* k_pages, const void* v_pages, const int32_t* bt_dev, int64_t T) {
-  const ppas_status st = check_rope(rope, s.head_dim);
+  const ppas_status st = rope_table(rope, s.head_dim, nullptr);
   if (st != PPAS_OK) return st;
   if (!r || !r->q || !r->k || !r->v || !q_out || !k_pages || !v_pages || !bt_dev) return PPAS_EINVAL;
   const int64_t q_row = int64_t(s.n_q_heads) * s.head_dim, kv_row = int64_t(s.n_kv_heads) * s.head_dim;
@@ -341,8 +352,9 @@ ppas_status run_qkv_append(const ppas_step_plan& p, const ppas_rope& rope, const
                            void* hip_stream) {
   if (!p.buf || p.n_append == 0) return PPAS_EINVAL;   // a plan made without the page-write list
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  RopeTable table;
-  make_rope_table(rope, table);
+  const RopeTable* table = nullptr;
+  const ppas_status st = rope_table(&rope, p.shape.head_dim, &table);
+  if (st != PPAS_OK) return st;
   RopeAppend r;
   r.q = static_cast<const uint16_t*>(rows.q);
   r.k = static_cast<const uint16_t*>(rows.k);
@@ -355,11 +367,13 @@ ppas_status run_qkv_append(const ppas_step_plan& p, const ppas_rope& rope, const
   r.v_pages = static_cast<uint16_t*>(v_pages);
   r.items = reinterpret_cast<const AppendItem*>(p.buf->dev + p.off_append);
   r.bt = bt_dev;
+  r.desc = p.desc;
+  r.n_desc = p.n_desc;
   r.n_items = p.n_append;
   r.bt_stride = p.bt_stride;
   r.hq = p.shape.n_q_heads;
   r.hkv = p.shape.n_kv_heads;
-  const hipError_t e = launch_rope_qkv_append(r, table, stream, ev_of(ev, 0), ev_of(ev, 1));
+  const hipError_t e = launch_rope_qkv_append(r, *table, stream, ev_of(ev, 0), ev_of(ev, 1));
   const bool noted = note_use(p.buf, stream);
   return (e == hipSuccess && noted) ? PPAS_OK : PPAS_EHIP;
 }
@@ -539,7 +553,7 @@ ppas_status ppas_rope_qkv_append_planned(const ppas_step_plan* plan, const ppas_
   ppas_status st = check_events(events);
   if (st != PPAS_OK) return st;
   try {
-    if (plan->n_seqs == 0) return check_rope(rope, kHeadDim);
+    if (plan->n_seqs == 0) return rope_table(rope, kHeadDim, nullptr);
     st = check_qkv(plan->shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, plan->n_rows);
     if (st != PPAS_OK) return st;
     return run_qkv_append(*plan, *rope, *rows, q_out, k_pages, v_pages, block_table_dev, events, hip_stream);
@@ -824,7 +838,7 @@ ppas_status ppas_rope_kv_append(const ppas_shape* shape, float rope_theta, void*
 }
 
 ppas_status ppas_rope_frequencies(const ppas_rope* rope, int32_t head_dim, double* out) {
-  const ppas_status st = check_rope(rope, head_dim);
+  const ppas_status st = rope_table(rope, head_dim, nullptr);
   if (st != PPAS_OK) return st;
   if (!out) return PPAS_EINVAL;
   for (int32_t j = 0; j < rope->rotary_dim / 2; ++j) out[j] = rope_frequency(*rope, j);
@@ -837,7 +851,8 @@ ppas_status ppas_rope_rows(const ppas_rope* rope, const void* x, int64_t x_strid
   try {
     if (n_rows < 0 || n_heads < 1 || n_heads > 65536 || head_dim < 2 || head_dim % 2 != 0) return PPAS_EINVAL;
     if (head_dim > 2 * kRopeMaxPairs) return PPAS_EUNSUPPORTED;
-    ppas_status st = check_rope(rope, head_dim);
+    const RopeTable* table = nullptr;
+    ppas_status st = rope_table(rope, head_dim, &table);
     if (st != PPAS_OK) return st;
     st = check_events(events);
     if (st != PPAS_OK) return st;
@@ -850,11 +865,9 @@ ppas_status ppas_rope_rows(const ppas_rope* rope, const void* x, int64_t x_strid
         overlap(x, span_bytes(n_rows, x_stride, row), y, span_bytes(n_rows, y_stride, row)))
       return PPAS_EINVAL;
     if (!current_device().gfx950) return PPAS_EUNSUPPORTED;
-    RopeTable table;
-    make_rope_table(*rope, table);
     const RopeRows r{static_cast<const uint16_t*>(x), static_cast<uint16_t*>(y), x_stride, y_stride, positions_dev,
                      n_rows, n_heads, head_dim, transposed != 0};
-    const hipError_t e = launch_rope_rows(r, table, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
+    const hipError_t e = launch_rope_rows(r, *table, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
                                           ev_of(events, 1));
     return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
   } catch (...) {
@@ -870,7 +883,7 @@ ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope,
   try {
     ppas_status st = validate(shape, seqs, n_seqs, block_table_host, bt_stride, true);
     if (st != PPAS_OK) return st;
-    if (n_seqs == 0) return check_rope(rope, kHeadDim);
+    if (n_seqs == 0) return rope_table(rope, kHeadDim, nullptr);
     const int64_t T = int64_t(seqs[n_seqs - 1].query_start) + seqs[n_seqs - 1].n_query;
     st = check_qkv(*shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, T);
     if (st != PPAS_OK) return st;

@@ -52,6 +52,13 @@ struct AppendItem {
 };
 static_assert(sizeof(AppendItem) == 32, "AppendItem is 32 bytes");
 
+// The same by request, for steps of at most kAppendInline requests: the request's
+// pages are items first_item.. in order.
+struct AppendDesc {
+  int32_t first_item, query_start, n_query, cached_len;
+};
+constexpr int kAppendInline = 64;
+
 // Per-call planning choices; zero selects the automatic one.
 struct PlanOpts {
   int32_t prefill_split = 0;       // >0: keys per prefill work item at most (rounded up to 64)

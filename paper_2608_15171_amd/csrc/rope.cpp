@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 
 namespace ppas {
 
@@ -12,11 +13,10 @@ bool positive(double v) { return std::isfinite(v) && v > 0; }
 
 }  // namespace
 
-ppas_status check_rope(const ppas_rope* rope, int32_t head_dim) {
-  if (!rope) return PPAS_EINVAL;
-  const ppas_rope& r = *rope;
+// The fields that do not depend on the head.
+static ppas_status check_rope(const ppas_rope& r) {
   if (r.layout != PPAS_ROPE_HALF && r.layout != PPAS_ROPE_INTERLEAVED) return PPAS_EINVAL;
-  if (r.rotary_dim < 2 || r.rotary_dim % 2 != 0 || r.rotary_dim > head_dim) return PPAS_EINVAL;
+  if (r.rotary_dim < 2 || r.rotary_dim % 2 != 0 || r.rotary_dim > 2 * kRopeMaxPairs) return PPAS_EINVAL;
   if (!positive(r.theta)) return PPAS_EINVAL;
   if (!(r.magnitude == 0 || positive(r.magnitude)) || !std::isfinite(float(r.magnitude))) return PPAS_EINVAL;
   if (r.scaling < PPAS_ROPE_PLAIN || r.scaling > PPAS_ROPE_RAMP) return PPAS_EINVAL;
@@ -26,9 +26,6 @@ ppas_status check_rope(const ppas_rope* rope, int32_t head_dim) {
     if (r.original_len < 1 || !positive(r.low) || !positive(r.high) || !(r.low < r.high)) return PPAS_EINVAL;
     if (r.scaling == PPAS_ROPE_RAMP && !(r.theta > 1)) return PPAS_EINVAL;
   }
-  // every pair has to turn (a base or factor at the ends of fp64's range can leave it)
-  for (int32_t j = 0; j < r.rotary_dim / 2; ++j)
-    if (!positive(rope_frequency(r, j))) return PPAS_EINVAL;
   return PPAS_OK;
 }
 
@@ -55,11 +52,29 @@ double rope_frequency(const ppas_rope& r, int32_t j) {
   }
 }
 
-void make_rope_table(const ppas_rope& rope, RopeTable& t) {
-  t.layout = rope.layout;
-  t.pairs = rope.rotary_dim / 2;
-  t.magnitude = rope.magnitude == 0 ? 1.f : float(rope.magnitude);
-  for (int32_t j = 0; j < t.pairs; ++j) t.turns[j] = rope_frequency(rope, j) / (2.0 * M_PI);
+ppas_status rope_table(const ppas_rope* rope, int32_t head_dim, const RopeTable** table) {
+  static_assert(sizeof(ppas_rope) == 4 * sizeof(int32_t) + 5 * sizeof(double), "compared byte by byte: no padding");
+  thread_local ppas_rope last{};   // rotary_dim 0: none
+  thread_local RopeTable kept;
+  if (!rope || rope->rotary_dim > head_dim) return PPAS_EINVAL;
+  if (std::memcmp(&last, rope, sizeof(last)) != 0 || last.rotary_dim == 0) {
+    const ppas_rope r = *rope;
+    const ppas_status st = check_rope(r);
+    if (st != PPAS_OK) return st;
+    last = ppas_rope{};
+    kept.layout = r.layout;
+    kept.pairs = r.rotary_dim / 2;
+    kept.magnitude = r.magnitude == 0 ? 1.f : float(r.magnitude);
+    for (int32_t j = 0; j < kept.pairs; ++j) {
+      const double w = rope_frequency(r, j);
+      // every pair has to turn (a base or factor at the ends of fp64's range can leave it)
+      if (!positive(w)) return PPAS_EINVAL;
+      kept.turns[j] = w / (2.0 * M_PI);
+    }
+    last = r;
+  }
+  if (table) *table = &kept;
+  return PPAS_OK;
 }
 
 }  // namespace ppas

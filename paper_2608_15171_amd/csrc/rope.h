@@ -20,12 +20,12 @@ struct RopeTable {
   double turns[kRopeMaxPairs] = {};
 };
 
-// PPAS_OK, or PPAS_EINVAL for a field out of range (host only).
-ppas_status check_rope(const ppas_rope* rope, int32_t head_dim);
-// Radians per position of pair j of a valid ppas_rope, in 64 bits (host only).
+// Radians per position of pair j, in 64 bits (host only).
 double rope_frequency(const ppas_rope& rope, int32_t j);
-// The table of a valid ppas_rope.
-void make_rope_table(const ppas_rope& rope, RopeTable& table);
+// The table of a ppas_rope, or PPAS_EINVAL for a field out of range (host only). The
+// table of the thread's last values is kept: a layer's calls come with the same ones,
+// and its powers take 3 us. Valid until the thread's next call.
+ppas_status rope_table(const ppas_rope* rope, int32_t head_dim, const RopeTable** table);
 
 // Rows of heads turned by their positions; x == y is allowed.
 struct RopeRows {
@@ -49,8 +49,9 @@ struct RopeAppend {
   uint16_t* k_pages;
   uint16_t* v_pages;
   const AppendItem* items;
+  const AppendDesc* desc;       // n_desc of them (host memory) in place of the items, or none
   const int32_t* bt;
-  int32_t n_items, bt_stride, hq, hkv;
+  int32_t n_items, n_desc, bt_stride, hq, hkv;
 };
 hipError_t launch_rope_qkv_append(const RopeAppend& r, const RopeTable& t, hipStream_t stream, hipEvent_t ev_start,
                                   hipEvent_t ev_stop);

@@ -44,6 +44,15 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const f32x2 v = {a, b};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
+// Every byte is used once, so loads and stores ask the caches not to keep it: 16,384
+// rows of 18 heads from memory take 27.6 us with both, 31.5 with the loads alone, 37.7
+// with neither (a copy of as many bytes 29.7).
+__device__ __forceinline__ u32x4 load16(const uint16_t* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+}
+__device__ __forceinline__ void store16(uint16_t* p, u32x4 v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+}
 __device__ __forceinline__ float turn_a(float a, float b, float2 c) { return fmaf(a, c.x, -(b * c.y)); }
 __device__ __forceinline__ float turn_b(float a, float b, float2 c) { return fmaf(b, c.x, a * c.y); }
 
@@ -86,9 +95,9 @@ __device__ __forceinline__ Unit fetch(const uint16_t* src, const Head& h, int u)
     r.x[0] = src[first_feature<kMode>(h, u)];
     r.y[0] = src[second_feature<kMode>(h, u)];
   } else {
-    r.x = *reinterpret_cast<const u32x4*>(src + first_feature<kMode>(h, u));
+    r.x = load16(src + first_feature<kMode>(h, u));
     if (kMode == kHalf) {
-      if (u < h.pairs / 8) r.y = *reinterpret_cast<const u32x4*>(src + second_feature<kMode>(h, u));
+      if (u < h.pairs / 8) r.y = load16(src + second_feature<kMode>(h, u));
     }
   }
   return r;
@@ -119,7 +128,7 @@ __device__ __forceinline__ void put(Unit r, const Head& h, int u, const float2* 
         r.x[w] = pack2(turn_a(x0, y0, c0), turn_a(x1, y1, c1));
         r.y[w] = pack2(turn_b(x0, y0, c0), turn_b(x1, y1, c1));
       }
-      *reinterpret_cast<u32x4*>(dst(second_feature<kMode>(h, u))) = r.y;
+      store16(dst(second_feature<kMode>(h, u)), r.y);
     }
   } else {
 #pragma unroll
@@ -132,7 +141,7 @@ __device__ __forceinline__ void put(Unit r, const Head& h, int u, const float2* 
       }
     }
   }
-  *reinterpret_cast<u32x4*>(dst(first_feature<kMode>(h, u))) = r.x;
+  store16(dst(first_feature<kMode>(h, u)), r.x);
 }
 
 // Units of a head; where nothing is copied (in place), those that turn.
@@ -146,25 +155,32 @@ __device__ __forceinline__ int units_of(const Head& h, bool copies) {
 constexpr int kThreads = 256;
 constexpr int kAhead = 4;   // units a thread has in flight
 
-// Every (row, head, unit) of n_rows rows, units fastest: `ready` is called once,
-// behind the first loads, and makes the table cs[row][pair].
+// Every (row, head, unit) of n_rows rows; a thread keeps its unit and steps through the
+// heads without a division (two per task were a third of the kernel's instructions).
+// `ready` is called once, behind the first loads, and makes the table cs[row][pair].
 template <int kMode, typename Src, typename Dst, typename Ready>
 __device__ __forceinline__ void turn_rows(int n_rows, int heads, const Head& h, bool copies, const float2* cs, Src src,
                                           Dst dst, Ready ready) {
-  const int units = units_of<kMode>(h, copies);
-  const int tasks = n_rows * heads * units;
+  const int units = units_of<kMode>(h, copies), step = kThreads / units;   // at most 128 units
+  const int unit = int(threadIdx.x) % units, start = int(threadIdx.x) / units;
+  const int step_row = step / heads, step_head = step % heads;
+  // threads past the last whole head have no rows
+  int row = start < step ? start / heads : n_rows, head = start % heads;
   bool first = true;
-  for (int t0 = threadIdx.x; first || t0 < tasks; t0 += kThreads * kAhead) {
+  while (first || row < n_rows) {
     Unit r[kAhead];
-    int row[kAhead], head[kAhead], unit[kAhead];
+    int rows[kAhead], at_head[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const int t = t0 + i * kThreads;
-      unit[i] = t % units;
-      const int rest = t / units;
-      head[i] = rest % heads;
-      row[i] = rest / heads;
-      if (t < tasks) r[i] = fetch<kMode>(src(row[i], head[i]), h, unit[i]);
+      rows[i] = row;
+      at_head[i] = head;
+      if (row < n_rows) r[i] = fetch<kMode>(src(row, head), h, unit);
+      row += step_row;
+      head += step_head;
+      if (head >= heads) {
+        head -= heads;
+        ++row;
+      }
     }
     if (first) {
       ready();
@@ -173,9 +189,9 @@ __device__ __forceinline__ void turn_rows(int n_rows, int heads, const Head& h, 
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      if (t0 + i * kThreads >= tasks) continue;
-      uint16_t* base = dst(row[i], head[i]);
-      put<kMode>(r[i], h, unit[i], cs + row[i] * h.pairs, [&](int f) { return base + f; });
+      if (rows[i] >= n_rows) continue;
+      uint16_t* base = dst(rows[i], at_head[i]);
+      put<kMode>(r[i], h, unit, cs + rows[i] * h.pairs, [&](int f) { return base + f; });
     }
   }
 }
@@ -209,67 +225,119 @@ __global__ __launch_bounds__(kThreads) void rope_rows_kernel(RowsArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// A step's rows on their way into the pages: one workgroup per (request, touched
-// page), as in the append that takes packed rows.
+// A step's rows on their way into the pages. Workgroup (item, y) of a (request,
+// touched page): for y = 0 the keys and values of its slots, so that a page's stores
+// are whole runs (256 bytes of a key chunk's 16 slots, 32 of a value feature's), else
+// the queries of slots 4 (y - 1) .. + 3. Each is one batch of loads, all in flight
+// while its cos/sin are computed.
+//
+// Steps of few requests bring their descriptors in the kernel's arguments: the page
+// list in host memory costs every workgroup a read over the bus before its first load
+// (16,384 rows: 5 of 40 us).
 // ---------------------------------------------------------------------------
+constexpr int kSlots = 4;                     // query slots of a workgroup
+constexpr int kParts = kPage / kSlots + 1;    // workgroups of a page
+static_assert(kThreads == 2 * kHeadDim && kThreads == 16 * kPage, "one value task and one 16-byte run per thread");
+
 struct AppendArgs {
   RopeAppend r;
-  RopeTable t;
+  bool v_aligned;   // rows of v start on 16 bytes
+  int32_t layout, pairs;
+  float magnitude;
+  double turns[kHeadDim / 2];
+  AppendDesc desc[kAppendInline];
 };
+
+// The descriptors are sorted by their first item: item i is of the last one at or before it.
+__device__ __forceinline__ AppendItem inline_item(const AppendArgs& a, int item) {
+  const int lane = threadIdx.x & 63;
+  const bool before = lane < a.r.n_desc && a.desc[lane].first_item <= item;
+  const int s = int(__popcll(__ballot(before))) - 1;
+  const AppendDesc d = a.desc[__builtin_amdgcn_readfirstlane(s)];
+  return AppendItem{s, d.cached_len / kPage + item - d.first_item, d.cached_len, d.n_query, d.query_start, 0, 0, 0};
+}
 
 template <int kMode>
 __global__ __launch_bounds__(kThreads) void rope_qkv_append_kernel(AppendArgs a) {
   __shared__ float2 cs[kPage * kHeadDim / 2];
   const RopeAppend& r = a.r;
-  const AppendItem it = r.items[blockIdx.x];
-  const int tid = threadIdx.x;
+  const AppendItem it = r.n_desc > 0 ? inline_item(a, blockIdx.x) : r.items[blockIdx.x];
+  const int tid = threadIdx.x, part = blockIdx.y;
   const int pos_lo = it.lpage * kPage;   // position of slot 0
-  const int slot_lo = max(it.cached_len - pos_lo, 0), slot_hi = min(it.cached_len + it.n_query - pos_lo, kPage);
+  int slot_lo = max(it.cached_len - pos_lo, 0), slot_hi = min(it.cached_len + it.n_query - pos_lo, kPage);
+  if (part > 0) {
+    slot_lo = max(slot_lo, (part - 1) * kSlots);
+    slot_hi = min(slot_hi, part * kSlots);
+    if (slot_lo >= slot_hi) return;
+  }
   const int n = slot_hi - slot_lo;
   const int64_t row0 = int64_t(it.query_start) + (pos_lo + slot_lo - it.cached_len);   // the first slot's row
-  const int32_t page = r.bt[int64_t(it.seq) * r.bt_stride + it.lpage];
-  const Head h{kHeadDim, a.t.pairs, a.t.layout == PPAS_ROPE_HALF};
-
-  turn_rows<kMode>(
-      n, r.hq, h, r.q != r.q_out, cs,
-      [&](int row, int head) { return r.q + (row0 + row) * r.q_stride + head * kHeadDim; },
-      [&](int row, int head) { return r.q_out + ((row0 + row) * r.hq + head) * kHeadDim; },
-      [&]() {
-        for (int e = tid; e < n * h.pairs; e += kThreads) {
-          const int row = e / h.pairs, j = e % h.pairs;
-          cs[e] = cos_sin(double(pos_lo + slot_lo + row), a.t.turns[j], a.t.magnitude, false);
-        }
-      });
-
-  // Keys: task (head, unit, slot), slot fastest, so that the stores of a chunk are one run.
-  const int units = units_of<kMode>(h, true);
-  for (int t = tid; t < r.hkv * units * n; t += kThreads) {
-    const int s = t % n, u = (t / n) % units, g = t / (n * units);
-    const Unit x = fetch<kMode>(r.k + (row0 + s) * r.k_stride + g * kHeadDim, h, u);
-    uint16_t* dst = r.k_pages + (int64_t(page) * r.hkv + g) * kPage * kHeadDim + (slot_lo + s) * 8;
-    put<kMode>(x, h, u, cs + s * h.pairs, [&](int f) { return dst + (f >> 3) * (kPage * 8) + (f & 7); });
+  const Head h{kHeadDim, a.pairs, a.layout == PPAS_ROPE_HALF};
+  auto table = [&]() {
+    for (int e = tid; e < n * h.pairs; e += kThreads) {
+      const int row = e / h.pairs, j = e % h.pairs;
+      cs[e] = cos_sin(double(pos_lo + slot_lo + row), a.turns[j], a.magnitude, false);
+    }
+  };
+  if (part > 0) {
+    turn_rows<kMode>(
+        n, r.hq, h, r.q != r.q_out, cs,
+        [&](int row, int head) { return r.q + (row0 + row) * r.q_stride + head * kHeadDim; },
+        [&](int row, int head) { return r.q_out + ((row0 + row) * r.hq + head) * kHeadDim; }, table);
+    return;
   }
 
-  // Values: task (head, feature, eight slots), whole 16-byte stores where all eight are new.
-  for (int t = tid; t < r.hkv * kHeadDim * 2; t += kThreads) {
-    const int g = t / (2 * kHeadDim), d = (t >> 1) % kHeadDim, s0 = 8 * (t & 1);
-    if (s0 >= slot_hi || s0 + 8 <= slot_lo) continue;
-    uint16_t* dst = r.v_pages + (int64_t(page) * r.hkv + g) * kPage * kHeadDim + d * kPage + s0;
-    const uint16_t* src = r.v + (row0 - slot_lo + s0) * r.v_stride + g * kHeadDim + d;
-    const int lo = max(slot_lo - s0, 0), hi = min(slot_hi - s0, 8);
-    uint16_t v[8];
+  const int32_t page = r.bt[int64_t(it.seq) * r.bt_stride + it.lpage];
+  // Keys: task (head, unit, slot), slot fastest; a thread's first ones are fetched ahead.
+  const int units = units_of<kMode>(h, true), k_tasks = r.hkv * units * n;
+  Unit key[2];
+  auto fetch_key = [&](int t) {
+    return fetch<kMode>(r.k + (row0 + t % n) * r.k_stride + t / (n * units) * kHeadDim, h, (t / n) % units);
+  };
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e >= lo && e < hi ? src[e * r.v_stride] : uint16_t(0);
+  for (int i = 0; i < 2; ++i)
+    if (tid + i * kThreads < k_tasks) key[i] = fetch_key(tid + i * kThreads);
+  // Values, transposed through LDS a head at a time: rows in by 16 bytes (or one element),
+  // then per task (feature, eight slots) one 16-byte store where all eight are new.
+  __shared__ __attribute__((aligned(16))) uint16_t rows[kPage][kHeadDim + 8];
+  u32x4 v = {};
+  auto fetch_value = [&](int g) {
+    if (a.v_aligned && tid < n * 16) v = load16(r.v + (row0 + tid / 16) * r.v_stride + g * kHeadDim + 8 * (tid % 16));
+  };
+  fetch_value(0);
+  table();
+  __syncthreads();
+  auto put_key = [&](const Unit& x, int t) {
+    const int s = t % n, u = (t / n) % units, g = t / (n * units);
+    uint16_t* dst = r.k_pages + (int64_t(page) * r.hkv + g) * kPage * kHeadDim + (slot_lo + s) * 8;
+    put<kMode>(x, h, u, cs + s * h.pairs, [&](int f) { return dst + (f >> 3) * (kPage * 8) + (f & 7); });
+  };
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (tid + i * kThreads < k_tasks) put_key(key[i], tid + i * kThreads);
+  for (int t = tid + 2 * kThreads; t < k_tasks; t += kThreads) put_key(fetch_key(t), t);
+
+  for (int g = 0; g < r.hkv; ++g) {
+    if (a.v_aligned) {
+      if (tid < n * 16) *reinterpret_cast<u32x4*>(&rows[slot_lo + tid / 16][8 * (tid % 16)]) = v;
+    } else {
+      const uint16_t* src = r.v + row0 * r.v_stride + g * kHeadDim;
+      for (int t = tid; t < n * kHeadDim; t += kThreads)
+        rows[slot_lo + t / kHeadDim][t % kHeadDim] = src[t / kHeadDim * r.v_stride + t % kHeadDim];
+    }
+    __syncthreads();
+    if (g + 1 < r.hkv) fetch_value(g + 1);
+    const int d = tid / 2, s0 = 8 * (tid & 1), lo = max(slot_lo - s0, 0), hi = min(slot_hi - s0, 8);
+    uint16_t* dst = r.v_pages + (int64_t(page) * r.hkv + g) * kPage * kHeadDim + d * kPage + s0;
     if (hi - lo == 8) {
       u32x4 w;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = uint32_t(v[2 * e]) | (uint32_t(v[2 * e + 1]) << 16);
-      *reinterpret_cast<u32x4*>(dst) = w;
+      for (int e = 0; e < 4; ++e) w[e] = uint32_t(rows[s0 + 2 * e][d]) | (uint32_t(rows[s0 + 2 * e + 1][d]) << 16);
+      store16(dst, w);
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e >= lo && e < hi) dst[e] = v[e];
+      for (int e = lo; e < hi; ++e) dst[e] = rows[s0 + e][d];
     }
+    __syncthreads();
   }
 }
 
@@ -291,8 +359,9 @@ hipError_t launch_rope_rows(const RopeRows& r, const RopeTable& t, hipStream_t s
   RowsArgs a;
   a.r = r;
   a.t = t;
-  // about four workgroups per compute unit, then more rows each
-  a.per = std::min<int32_t>(kMaxRows, std::max<int32_t>(1, r.rows / 1024));
+  // one batch of loads per thread, but at least about four workgroups per compute unit
+  const int64_t units = int64_t(r.heads) * std::max(1, t.layout == PPAS_ROPE_HALF ? t.pairs / 8 : r.head_dim / 8);
+  a.per = int32_t(std::max<int64_t>(1, std::min<int64_t>({kMaxRows, r.rows / 1024, kThreads * kAhead / units})));
   const dim3 grid(unsigned((int64_t(r.rows) + a.per - 1) / a.per));
   const bool aligned = on16(r.x) && on16(r.y) && r.x_stride % 8 == 0 && r.y_stride % 8 == 0;
   switch (mode_of(t, r.head_dim, aligned)) {
@@ -308,10 +377,16 @@ hipError_t launch_rope_rows(const RopeRows& r, const RopeTable& t, hipStream_t s
 hipError_t launch_rope_qkv_append(const RopeAppend& r, const RopeTable& t, hipStream_t stream, hipEvent_t ev_start,
                                   hipEvent_t ev_stop) {
   if (r.n_items <= 0) return hipSuccess;
+  if (t.pairs > kHeadDim / 2 || r.n_desc > kAppendInline) return hipErrorInvalidValue;
   AppendArgs a;
   a.r = r;
-  a.t = t;
-  const dim3 grid{unsigned(r.n_items)};
+  a.layout = t.layout;
+  a.pairs = t.pairs;
+  a.magnitude = t.magnitude;
+  std::copy(t.turns, t.turns + t.pairs, a.turns);
+  std::copy(r.desc, r.desc + r.n_desc, a.desc);
+  a.v_aligned = on16(r.v) && r.v_stride % 8 == 0;
+  const dim3 grid{unsigned(r.n_items), kParts};
   const bool aligned = on16(r.q) && on16(r.k) && on16(r.q_out) && r.q_stride % 8 == 0 && r.k_stride % 8 == 0;
   switch (mode_of(t, kHeadDim, aligned)) {
     case kHalf:

@@ -179,7 +179,8 @@ def _desc(desc) -> np.ndarray:
 
 
 def _host_ptr(a):
-    return None if a is None else a.ctypes.data
+    # a third of the time of a.ctypes.data, which makes an object each time
+    return None if a is None else a.__array_interface__["data"][0]
 
 
 def _bt_host(bt_host, bt_dev=None):
@@ -246,9 +247,14 @@ def _check_buffers(shape: Shape, d, q=None, out=None, k_new=None, v_new=None, k_
             raise ValueError(f"block_table has {bt_dev.shape[0]} rows for {len(d)} requests")
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) if torch is not None else None
+
+
 def _stream(stream):
     if stream is None:
-        import torch
+        # the handle itself, without the object around it (1-2 us of a call)
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     return getattr(stream, "cuda_stream", stream)
 
@@ -334,14 +340,30 @@ def rope_rows(rope: Rope, x, positions, y, transposed: bool = False, events: Eve
     _check(st, "ppas_rope_rows")
 
 
-def _qkv(shape: Shape, q, k, v, rows: int) -> Qkv:
-    """The step's rows as ppas_qkv; each tensor holds at least `rows` of them."""
-    D = shape.head_dim
-    for t, name, heads in ((q, "q_new", shape.n_q_heads), (k, "k_new", shape.n_kv_heads), (v, "v_new", shape.n_kv_heads)):
-        if t.dim() != 3 or tuple(t.shape[1:]) != (heads, D) or t.shape[0] < rows:
-            raise ValueError(f"{name} must be [{rows} rows or more, {heads}, {D}], got {tuple(t.shape)}")
-    (qp, qs), (kp, ks), (vp, vs) = _heads(q, "q_new"), _heads(k, "k_new"), _heads(v, "v_new")
+def _step_rows(t, name, rows: int, heads: int, dim: int):
+    """_heads of at least `rows` rows of `heads` heads of `dim` features."""
+    p = _heads(t, name)
+    n, h, d = t.shape
+    if n < rows or h != heads or d != dim:
+        raise ValueError(f"{name} must be [{rows} rows or more, {heads}, {dim}], got {tuple(t.shape)}")
+    return p
+
+
+def _qkv(q, k, v, rows: int, hq: int, hkv: int, dim: int) -> Qkv:
+    """The step's rows as ppas_qkv."""
+    qp, qs = _step_rows(q, "q_new", rows, hq, dim)
+    kp, ks = _step_rows(k, "k_new", rows, hkv, dim)
+    vp, vs = _step_rows(v, "v_new", rows, hkv, dim)
     return Qkv(qp, kp, vp, qs, ks, vs)
+
+
+def _buffer(t, name, nbytes: int):
+    """_need and _dev in one: the pointer of a contiguous device buffer of 2-byte elements."""
+    size = t.element_size()
+    if size != 2 or t.numel() * size < nbytes or not t.is_cuda or not t.is_contiguous():
+        _need(t, name, nbytes)
+        _dev(t, name)
+    return t.data_ptr()
 
 
 def rope_qkv_append(shape: Shape, rope: Rope, q, k_pages, v_pages, q_new, k_new, v_new, desc, bt_dev, bt_host=None,
@@ -352,7 +374,7 @@ def rope_qkv_append(shape: Shape, rope: Rope, q, k_pages, v_pages, q_new, k_new,
     bt = _bt_host(bt_host, bt_dev)
     rows = _rows(d)
     _check_buffers(shape, d, q=q, k_pages=k_pages, v_pages=v_pages, bt_dev=bt_dev, rows=rows)
-    x = _qkv(shape, q_new, k_new, v_new, rows)
+    x = _qkv(q_new, k_new, v_new, rows, shape.n_q_heads, shape.n_kv_heads, shape.head_dim)
     st = _lib.ppas_rope_qkv_append(ctypes.byref(shape), ctypes.byref(rope), ctypes.byref(x), _dev(q, "q"),
                                    _dev(k_pages, "k_pages"), _dev(v_pages, "v_pages"), _host_ptr(d), len(d),
                                    _dev(bt_dev, "block_table"), bt_dev.shape[1], _host_ptr(bt), _stream(stream))
@@ -579,6 +601,10 @@ class StepPlan:
                            shape.scale)
         self.desc = _desc(desc)
         self._n_rows = _rows(self.desc)   # counted once: a planned call is made for every layer
+        s = self.shape
+        self._heads = s.n_q_heads, s.n_kv_heads, s.head_dim
+        self._q_bytes = self._n_rows * s.n_q_heads * s.head_dim * 2
+        self._pool_bytes = int(s.num_pages) * s.n_kv_heads * s.page_size * s.head_dim * 2
         bt = _bt_host(bt_host)
         self.bt_stride = int(bt_stride if bt_stride is not None else (bt.shape[1] if bt is not None else 1))
         if bt is not None and bt.shape[1] != self.bt_stride:
@@ -629,12 +655,14 @@ class StepPlan:
 
     def rope_qkv_append(self, rope: Rope, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev,
                         events: Events | None = None, stream=None) -> None:
-        _check_buffers(self.shape, self.desc, q=q, k_pages=k_pages, v_pages=v_pages, bt_dev=self._bt(bt_dev),
-                       rows=self._n_rows)
-        x = _qkv(self.shape, q_new, k_new, v_new, self._n_rows)
-        st = _lib.ppas_rope_qkv_append_planned(self._h, ctypes.byref(rope), ctypes.byref(x), _dev(q, "q"),
-                                               _dev(k_pages, "k_pages"), _dev(v_pages, "v_pages"),
-                                               _dev(bt_dev, "block_table"),
+        bt = self._bt(bt_dev)
+        if bt.element_size() != 4 or bt.shape[0] < len(self.desc):
+            _check_buffers(self.shape, self.desc, bt_dev=bt)
+        x = _qkv(q_new, k_new, v_new, self._n_rows, *self._heads)
+        st = _lib.ppas_rope_qkv_append_planned(self._h, ctypes.byref(rope), ctypes.byref(x),
+                                               _buffer(q, "q", self._q_bytes),
+                                               _buffer(k_pages, "k_pages", self._pool_bytes),
+                                               _buffer(v_pages, "v_pages", self._pool_bytes), _dev(bt, "block_table"),
                                                None if events is None else ctypes.byref(events), _stream(stream))
         _check(st, "ppas_rope_qkv_append_planned")
 
