@@ -18,8 +18,9 @@ hipError_t launch_gateup_i8(const Int8Product& p, bool act, int max_splits, void
                             hipEvent_t ev_start, hipEvent_t ev_stop) {
   if (p.T <= 0) return hipSuccess;
   if (max_splits < 1 || (max_splits > 1 && !part) || (act && p.N2 % 2 != 0)) return hipErrorInvalidValue;
-  // whole 128-byte stages of 16-byte aligned rows; anything else in the general kernel
-  const bool aligned = p.H % (2 * kBK) == 0 && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 &&
+  // whole 128-byte stages of 16-byte aligned rows, and at least two of them (the scales'
+  // transfer); anything else in the general kernel
+  const bool aligned = p.H % (2 * kBK) == 0 && p.H > 2 * kBK && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 &&
                        reinterpret_cast<uintptr_t>(p.w) % 16 == 0;
   GateupChoice c;
   if (aligned) c = gateup_choose(p.T, p.H / 2, p.N2, act, true, std::min(max_splits, p.H / (2 * kBK)), cus, true);

@@ -177,7 +177,7 @@ __device__ __forceinline__ void transfer(const Rows& r, char* lds, uint32_t lane
 // stage, one per pair of units, and a ring of two stages), below that one (two
 // phases, three stages). Wave (wn, wm) owns, of every unit pair, QN columns x QM
 // token rows as kNT x kMT MFMA tiles.
-template <int BM>
+template <int BM, bool kScaled = false>
 struct Tile {
   static constexpr int XH = BM == 256 ? 2 : 1;             // X units
   static constexpr int WNW = BM == 256 ? 2 : 4;            // waves along the columns
@@ -189,9 +189,12 @@ struct Tile {
   static constexpr int kStage = (kBN + BM) * kRow;
   static constexpr int kOffX = kBN * kRow;
   static constexpr int kDW = kHN / 8 / kWaves, kDX = HM / 8 / kWaves;   // transfers per wave and unit
-  static constexpr int kEpiRows = QN == 64 ? QM : 32;      // rows staged at a time in the epilogue
+  // rows staged at a time in the epilogue (scaled sums leave room for their scales)
+  static constexpr int kEpiRows = kScaled ? 16 : QN == 64 ? QM : 32;
   static constexpr int kEpi = QN * kEpiRows * 2;           // a wave's staging bytes
-  static_assert(kRing * kStage + kWaves * kEpi <= kSmem, "the ring and the staging areas fit");
+  static constexpr int kOffScales = kRing * kStage + kWaves * kEpi;
+  static constexpr int kScales = kScaled ? 2 * 512 * 4 : 0;   // two tiles' 256 column and 256 row scales
+  static_assert(kOffScales + kScales <= kSmem, "the ring, the staging areas and the scales fit");
   static_assert(kDW * 8 * kWaves == kHN && kDX * 8 * kWaves == HM && kDX >= 1, "whole transfers per wave");
   static_assert(QM % kEpiRows == 0 && kEpiRows % 16 == 0, "whole staged blocks");
 };
@@ -234,7 +237,7 @@ struct Staged {
 template <int BM, bool kAct, typename E, typename List>
 __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int m_first, int tiles_m) {
 #ifdef __HIP_DEVICE_COMPILE__
-  using C = Tile<BM>;
+  using C = Tile<BM, E::kInt>;
   constexpr int QN = C::QN, QM = C::QM, kNT = C::kNT, kMT = C::kMT;
   List todo(a);
   if (!todo.more()) return;
@@ -440,8 +443,42 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int m_f
   }
   if (late) bare_barrier();
 
+  // Scales of a tile's sums, for the epilogue: its 256 columns' (with the activation 128
+  // gate and 128 up ones') from waves 0-3, its token rows' from waves 4-7, 64 each by one
+  // transfer of four bytes per lane, into the half of the area that the tile before does
+  // not use. Its wait is another transfer's: a tile has at least two stages, so that by
+  // its last phase every wave has waited for fewer transfers to be in flight than it has
+  // issued since (loads into registers would have to drain the stream: 8 % of a tile).
+  int sc_half = 0;
+  auto issue_scales = [&](const Item& it) {
+    const int part = w & 3;
+    int first, total;
+    const float* src;
+    if (w >= kWaves / 2) {
+      src = a.sx;
+      first = it.m0 + 64 * part;
+      total = 64 * part < BM ? a.T : 0;
+    } else if (kAct) {
+      src = a.sw + (part >= 2 ? a.I : 0);
+      first = it.n0 / 2 + 64 * (part & 1);
+      total = a.I;
+    } else {
+      src = a.sw;
+      first = it.n0 + 64 * part;
+      total = a.N2;
+    }
+    const int valid = max(0, min(64, total - first));
+    const uint64_t b = reinterpret_cast<uint64_t>(src + (valid > 0 ? first : 0));
+    __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<void*>(uint64_t(uniform(uint32_t(b))) | (uint64_t(uniform(uint32_t(b >> 32))) << 32)), 0,
+        int(uniform(uint32_t(valid) * 4)), 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (lds_void*)(smem + C::kOffScales + sc_half * 2048 + w * 256), 4, 4 * lane,
+                                             0, 0, 0);
+  };
+
   for (; todo.more(); todo.next()) {
     const Item it = item_at(a, todo.at, tiles_m, BM, m_first);
+    if (E::kInt && a.splits == 1) issue_scales(it);
     // Below 256 rows the sums are kept in two levels, blocks of a.block stages added
     // to a running total: one chain over 2,048 features rounds 1.6 times as far off as
     // eight partial sums (blocks of eight stages cost 2-4 % of a tile, of four 3-9 %).
@@ -520,11 +557,10 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int m_f
                 const int row = 16 * tj + (lane & 15), col = 16 * ti + 4 * (lane >> 4);
                 f32x4 sv = {}, su = {};
                 if constexpr (E::kInt) {
-                  const int m = it.m0 + g * C::HM + wm * QM + 16 * tb + row;
-                  const int n = (kAct ? it.n0 / 2 : it.n0 + h * kHN) + wn * QN + col;
-                  const float sm = m < a.T ? a.sx[m] : 0.f;
-                  sv = scales4(a.sw, n, ncols) * sm;
-                  if (kAct) su = scales4(a.sw + a.I, n, a.I) * sm;
+                  const float* sc = reinterpret_cast<const float*>(smem + C::kOffScales + sc_half * 2048);
+                  const float sm = sc[kBN + g * C::HM + wm * QM + 16 * tb + row];
+                  sv = *reinterpret_cast<const f32x4*>(sc + h * kHN + wn * QN + col) * sm;
+                  if (kAct) su = *reinterpret_cast<const f32x4*>(sc + kHN + wn * QN + col) * sm;
                 }
                 f32x4 r;
 #pragma unroll
@@ -540,6 +576,7 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int m_f
                    (kAct ? it.n0 / 2 : it.n0 + h * kHN) + wn * QN, a.T, ncols);
           }
       __builtin_amdgcn_s_waitcnt(0xC07F);   // the reads of rows past the edge, which no store waits for
+      sc_half ^= 1;
     }
     bare_barrier();
   }
