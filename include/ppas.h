@@ -354,7 +354,9 @@ ppas_status ppas_step_plan_create(const ppas_shape* shape, const ppas_seq* seqs,
  * hold rows of several requests, then each request's own keys, and merges the two by
  * their log-sum-exp: the results are those of ppas_attn_step but for the order of the
  * sums. Used are whole blocks of 64 keys of a prefix; requests of more than 64 new
- * tokens fill tiles of their own and read it for themselves. The pages of a prefix are
+ * tokens fill tiles of their own and read it for themselves, and a step that would
+ * save little is planned without sharing (opts->prefill_split > 0 shares whatever it
+ * saves). The pages of a prefix are
  * taken from its first member's table row. PPAS_EINVAL for a prefix out of range, out of
  * order, of a length that is no multiple of 16 or longer than a member's cached_len, or,
  * when block_table_host is not NULL, whose members' entries differ. n_prefixes == 0

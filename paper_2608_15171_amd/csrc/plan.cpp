@@ -128,11 +128,117 @@ struct SharedRun {
   std::vector<SharedTile> tiles;
 };
 
+// How a step with shared prefixes is cut: tile positions, and the most keys of a
+// prefill and of a decode item; tile 0 where it is not worth sharing.
+struct SharedCut {
+  int32_t tile = 0;
+  int64_t prefill = 0, decode = 0;
+};
+
+// Sharing pays where it saves a step about 100,000 keys (times KV heads) or more: below,
+// the requests find the prefix in the caches, and the tiles' longer items and the join
+// cost as much as they save. Measured, attention with its merge, 2 KV heads: 8 requests
+// of 2,048 shared keys (29,000 saved) 12.3 us against 11.6 apart; 16 of 4,096 (123,000)
+// 16.8 against 15.3 to 17.0 against 18.6 with what else they hold; 32 of 4,096
+// (254,000) 17.2 against 23.7; 64 of 8,192 with up to 4,000 of their own 38 against 92.
+constexpr int64_t kShareMinSaved = 100000;
+
+// Microseconds of a step with pieces of at most `prefill` and `decode` keys, fitted to 6,000
+// timed plans (108 steps, 12 % rms; the choice made with it is 5 % slower than the best
+// one on average): a fixed part, then what is longest of the tiles' whole rounds over the
+// workgroup slots, all items' time over the slots, the longest decode item and the decode
+// rows' bytes; then the merge, by its partials' bytes and the splits of a row.
+struct SharedCost {
+  double fixed, tile_item, tile_key, tile_key_few, decode_key, gbs, mb, split;
+};
+constexpr SharedCost kShared16{9.1, 0.56, 0.0227, 0.0166, 0.0088, 5200, 0.51, 0.078};
+constexpr SharedCost kShared32{8.9, 2.14, 0.0264, 0.0223, 0.0083, 3900, 0.46, 0.093};
+
 struct Job {
   WorkItem item;
   double cost;
   int32_t order_key[4];
 };
+
+}  // namespace
+
+namespace {
+
+// `own` is the first own key of every request; opts' fields that are set stand.
+SharedCut choose_shared(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_cus, const PlanOpts& opts,
+                        const std::vector<SharedRun>& runs, const std::vector<int32_t>& own) {
+  SharedCut best;
+  int64_t saved = 0;
+  for (const SharedRun& r : runs) saved += int64_t(r.rows - 1) * r.len * hkv;
+  if (saved < kShareMinSaved && opts.prefill_split <= 0) return best;
+  static constexpr int64_t kPrefill[] = {128, 256, 512, 768, 1024, 1536, 2048, 2816, 4224, 5632, 8448};
+  static constexpr int64_t kDecode[] = {256, 512, 1024, 2048, 4096};
+  auto up = [](int64_t keys, int64_t block) { return std::max(block, ceil_div(keys, block) * block); };
+  struct Decode {
+    int64_t most;
+    double items = 0, keys = 0, longest = 0, slots = 0, splits = 1;
+  };
+  std::vector<Decode> decode;
+  for (int64_t ds : kDecode) {
+    if (opts.decode_split > 0 && !decode.empty()) break;
+    Decode d{opts.decode_split > 0 ? std::min<int64_t>(up(opts.decode_split, kDecodeBlock), kDecodeMaxKeys) : ds};
+    for (int32_t s = 0; s < n_seqs; ++s) {
+      if (seqs[s].n_query != 1) continue;
+      const int64_t keys = int64_t(seqs[s].cached_len) + 1 - own[size_t(s)], n = ceil_div(keys, d.most);
+      d.items += double(n);
+      d.keys += double(keys);
+      d.longest = std::max(d.longest, double(keys) / double(n));
+      if (n > 1 || own[size_t(s)]) d.slots += double(n) * kGroup;
+      d.splits = std::max(d.splits, double(n));
+    }
+    decode.push_back(d);
+  }
+  double best_us = 0;
+  for (int32_t tile : {kTilePosSmall, kTilePosLarge}) {
+    if (opts.tile_pos != 0 && opts.tile_pos != tile) continue;
+    const SharedCost& c = tile == kTilePosSmall ? kShared16 : kShared32;
+    const double slots = double(num_cus) * (tile == kTilePosSmall ? 2 : 1);
+    for (int64_t p : kPrefill) {
+      if (opts.prefill_split > 0) {
+        if (p != kPrefill[0]) break;
+        p = up(opts.prefill_split, kPrefillBlock);
+      }
+      // the tiles' pieces: (items, keys of one); requests of several tiles count their middle one
+      double items = 0, keys = 0, longest = 0, long_items = 0, part = 0, splits = 0;
+      auto add = [&](double tiles, int64_t len, double rows) {
+        const int64_t n = ceil_div(len, p);
+        const double piece = double(len) / double(n);
+        if (piece > longest) {
+          if (longest < 0.6 * piece) long_items = 0;
+          longest = piece;
+        }
+        if (piece >= 0.6 * longest) long_items += tiles * double(n);
+        items += tiles * double(n);
+        keys += tiles * double(len);
+        part += rows * double(n) * kGroup;
+        return double(n);
+      };
+      for (const SharedRun& r : runs) splits = std::max(splits, add(double(ceil_div(r.rows, tile)), r.len, r.rows));
+      for (int32_t s = 0; s < n_seqs; ++s)
+        if (seqs[s].n_query > 1)
+          add(double(ceil_div(seqs[s].n_query, tile)),
+              int64_t(seqs[s].cached_len) + (seqs[s].n_query + 1) / 2 - own[size_t(s)], seqs[s].n_query);
+      for (const Decode& d : decode) {
+        const double per_key = (items + d.items) * hkv <= num_cus ? c.tile_key_few : c.tile_key;
+        const double rounds = std::ceil(long_items * hkv / slots) * (c.tile_item + per_key * longest);
+        const double all = hkv * (items * c.tile_item + keys * per_key + d.keys * c.decode_key) / slots;
+        const double bytes = hkv * d.keys * 4.0 * kHeadDim / (c.gbs * 1e3);
+        const double us = c.fixed + std::max(std::max(rounds, all), std::max(d.longest * c.decode_key, bytes)) +
+                          c.mb * hkv * (part + d.slots) * (kHeadDim + 2) * 4e-6 + c.split * (splits + d.splits);
+        if (best.tile == 0 || us < best_us) {
+          best_us = us;
+          best = SharedCut{tile, p, d.most};
+        }
+      }
+    }
+  }
+  return best;
+}
 
 }  // namespace
 
@@ -168,6 +274,15 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
     }
   }
 
+  SharedCut cut;
+  if (!runs.empty()) {
+    cut = choose_shared(seqs, n_seqs, hkv, num_cus, opts, runs, own);
+    if (cut.tile == 0) {
+      runs.clear();
+      std::fill(own.begin(), own.end(), 0);
+    }
+  }
+
   // Total work, to size the key splits so that the launch has several
   // workgroups per compute unit: keys summed over prefill tiles (of either
   // size) and over decode rows.
@@ -196,7 +311,7 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
   // 32-position tiles (two per CU before any key split) and decode rows are a
   // small share of the work (a workgroup then holds a whole CU, so a prefill
   // tile no longer shares its CU with a decode item).
-  int32_t tile = opts.tile_pos;
+  int32_t tile = cut.tile ? cut.tile : opts.tile_pos;
   if (tile != kTilePosSmall && tile != kTilePosLarge) {
     const int64_t small_keys = prefill_keys_for(kTilePosSmall);
     const bool big = large_tiles >= int64_t(2) * num_cus;
@@ -206,13 +321,13 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
   plan.tile_pos = tile;
   const int64_t prefill_keys = prefill_keys_for(tile);
 
-  int64_t ksp = opts.prefill_split;
+  int64_t ksp = cut.tile ? cut.prefill : opts.prefill_split;
   if (ksp <= 0) {
     const int64_t target = int64_t(PPAS_PREFILL_ITEMS_PER_CU) * num_cus;
     ksp = std::max<int64_t>(256, ceil_div(prefill_keys, target));
   }
   ksp = std::max<int64_t>(kPrefillBlock, ceil_div(ksp, kPrefillBlock) * kPrefillBlock);
-  int64_t ksd = opts.decode_split;
+  int64_t ksd = cut.tile ? cut.decode : opts.decode_split;
   if (ksd <= 0) {
     const int64_t target = int64_t(2) * num_cus;
     ksd = std::min<int64_t>(8192, std::max<int64_t>(512, ceil_div(decode_keys, target)));
@@ -252,7 +367,12 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
   auto piece_bounds = [&](int64_t lo, int64_t hi, int64_t pos0, int kind) {
     std::vector<int64_t> b{lo};
     const int64_t kend = hi - lo;
-    if (kind == kKindDecode && decode_even) {
+    if (cut.tile) {   // even pieces
+      const int64_t n = ceil_div(kend, kind == kKindDecode ? ksd : ksp);
+      const int64_t unit = kind == kKindDecode ? kDecodeBlock : kPrefillBlock;
+      const int64_t top = kind == kKindDecode ? hi : pos0 / kPrefillBlock * kPrefillBlock;
+      for (int64_t k = 1; k < n; ++k) b.push_back(std::min(top, lo + kend * k / n / unit * unit));
+    } else if (kind == kKindDecode && decode_even) {
       const int64_t n = std::max<int64_t>(ceil_div(kend, int64_t(kDecodeMaxKeys - kDecodeBlock)),
                                           (kend * num_cus + decode_keys / 2) / decode_keys);
       for (int64_t k = 1; k < n; ++k) b.push_back(lo + kend * k / n / kDecodeBlock * kDecodeBlock);

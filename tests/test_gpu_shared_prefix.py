@@ -124,7 +124,8 @@ def test_prefix_lengths(lib, length, rows):
     spec, prefixes = I.StepSpec("lengths", seqs), [(0, 5, length)]
     data, ds = make_step(lib, spec, prefixes, 3)
     ref = OA.step_attention_from_data(data, ds.shape.scale, with_abs=True)
-    compare(attend(lib, ds, prefixes), ref, f"length={length} rows={rows}")
+    for tile in (16, 32):     # a split size shares whatever a step saves
+        compare(attend(lib, ds, prefixes, lib[0].plan_opts(128, 0, tile)), ref, f"length={length} rows={rows} tile={tile}")
 
 
 @pytest.mark.parametrize("n", [1, 2, 3, 17, 33, 130])
@@ -134,7 +135,7 @@ def test_group_sizes(lib, n):
     data, ds = make_step(lib, spec, prefixes, 4)
     ref = OA.step_attention_from_data(data, ds.shape.scale, with_abs=True)
     for tile in (16, 32):
-        compare(attend(lib, ds, prefixes, lib[0].plan_opts(0, 0, tile)), ref, f"n={n} tile={tile}")
+        compare(attend(lib, ds, prefixes, lib[0].plan_opts(128, 0, tile)), ref, f"n={n} tile={tile}")
 
 
 @pytest.mark.parametrize("prefix,n,own", [(8192, 40, 700), (20000, 24, 64), (30000, 3, 2000)])
@@ -144,7 +145,7 @@ def test_long_prefixes(lib, prefix, n, own):
     spec, prefixes = I.StepSpec("long", seqs), [(0, n + 1, prefix)]
     data, ds = make_step(lib, spec, prefixes, 5)
     ref = OA.step_attention_from_data(data, ds.shape.scale, with_abs=True)
-    for tile in (0, 32):
+    for tile in (0, 16, 32):
         compare(attend(lib, ds, prefixes, lib[0].plan_opts(0, 0, tile)), ref, f"prefix={prefix} tile={tile}")
 
 
@@ -161,7 +162,7 @@ def test_dominant_keys_on_either_side_of_the_join(lib):
     ds.q.copy_(q)
     moved = I.StepData(data.spec, data.desc, step.bits_of(ds.q), data.k_new, data.v_new, data.k_hist, data.v_hist)
     O, A = OA.step_attention_from_data(moved, ds.shape.scale, with_abs=True)
-    g = attend(lib, ds, prefixes).float().cpu().numpy().astype(np.float64)
+    g = attend(lib, ds, prefixes, ppas.plan_opts(256, 0, 0)).float().cpu().numpy().astype(np.float64)
     # logits are 16 times larger: their fp32 error (128 products, sums of up to ~100) moves a weight by up to 16 x 2e-4
     bound = 2.0 ** -8 * np.abs(g) + (2.0 ** -8 + 6e-4 + 16 * 2e-4) * (A + np.abs(O)) + 1e-6
     assert (np.abs(g - O) <= bound).all()
@@ -176,7 +177,7 @@ def test_plan_serves_layers_streams_and_other_pools(lib):
     a, b = made[0][1], made[1][1]
     streams = [torch.cuda.Stream() for _ in range(2)]
     torch.cuda.synchronize()
-    with ppas.StepPlan(a.shape, a.desc, None, a.bt_host.shape[1], prefixes=prefixes) as plan:
+    with ppas.StepPlan(a.shape, a.desc, None, a.bt_host.shape[1], ppas.plan_opts(256, 0, 0), prefixes) as plan:
         ws = [torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda") for _ in range(2)]
         outs = [torch.zeros_like(a.out) for _ in range(2)]
         torch.cuda.synchronize()
@@ -191,8 +192,9 @@ def test_plan_serves_layers_streams_and_other_pools(lib):
 def test_same_results_whenever_run(lib):
     spec, prefixes = random_step(21)
     _, ds = make_step(lib, spec, prefixes, 21)
-    a = attend(lib, ds, prefixes)
-    assert bool((a == attend(lib, ds, prefixes)).all())
+    for opts in (None, lib[0].plan_opts(64, 0, 0)):
+        a = attend(lib, ds, prefixes, opts)
+        assert bool((a == attend(lib, ds, prefixes, opts)).all())
 
 
 def test_without_prefixes_is_the_plain_step(lib):
