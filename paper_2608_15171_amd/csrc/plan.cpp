@@ -157,8 +157,26 @@ constexpr SharedCost kShared32{8.9, 2.14, 0.0264, 0.0223, 0.0083, 3900, 0.46, 0.
 struct Job {
   WorkItem item;
   double cost;
-  int32_t order_key[4];
+  int32_t piece;
 };
+
+// A job's place in its queue: longest first, in cost buckets of 256 keys; inside a
+// bucket items of the same request and KV head stay together, so that neighbours share
+// keys in one L2. Packed, so that the sort compares plain integers (a third of a
+// plan's time).
+struct Place {
+  uint64_t cost_seq, head_pos, piece_job;
+  bool operator<(const Place& o) const {
+    if (cost_seq != o.cost_seq) return cost_seq < o.cost_seq;
+    if (head_pos != o.head_pos) return head_pos < o.head_pos;
+    return piece_job < o.piece_job;
+  }
+};
+Place place_of(const Job& j, size_t job) {
+  const uint64_t bucket = UINT32_MAX - uint64_t(int64_t(j.cost) >> 8);   // a cost is below 2^33
+  return Place{bucket << 32 | uint32_t(j.item.seq), uint64_t(j.item.kvh) << 32 | (UINT32_MAX - uint32_t(j.item.pos0)),
+               uint64_t(j.piece) << 32 | uint64_t(job)};
+}
 
 }  // namespace
 
@@ -364,8 +382,9 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
   // pieces, that of 500 keys left whole from 2.01e-3 to 2.25e-3.
   const bool decode_even = prefill_keys == 0 && decode_keys > 0 && opts.decode_split <= 0;
   // lo: the first key, a multiple of 64
-  auto piece_bounds = [&](int64_t lo, int64_t hi, int64_t pos0, int kind) {
-    std::vector<int64_t> b{lo};
+  std::vector<int64_t> b;   // the latest bounds
+  auto piece_bounds = [&](int64_t lo, int64_t hi, int64_t pos0, int kind) -> const std::vector<int64_t>& {
+    b.assign(1, lo);
     const int64_t kend = hi - lo;
     if (cut.tile) {   // even pieces
       const int64_t n = ceil_div(kend, kind == kKindDecode ? ksd : ksp);
@@ -391,6 +410,7 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
   };
 
   std::vector<Job> jobs;
+  jobs.reserve(size_t(4) * size_t(num_cus));
   // One item per piece of `bounds`; the partials' first slot, or -1 where rows are written whole.
   auto add_items = [&](int32_t s, int32_t g, int32_t row0, int32_t pos0, int32_t npos, int kind,
                        const std::vector<int64_t>& bounds, bool partial) {
@@ -409,10 +429,7 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
       // work (twice that in a 32-position tile), a decode key ~512 bytes of HBM
       // traffic; one decode key is about two prefill keys of a 16-position tile.
       j.cost = double(hi - lo) * (kind == kKindDecode ? 2.0 : tile_cost);
-      j.order_key[0] = s;
-      j.order_key[1] = g;
-      j.order_key[2] = -pos0;
-      j.order_key[3] = int32_t(k);
+      j.piece = int32_t(k);
       jobs.push_back(j);
     }
     return part;
@@ -427,7 +444,7 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
   auto add_unit = [&](int32_t s, int32_t g, int32_t row0, int32_t pos0, int32_t npos, int kind,
                       const SharedRun* pre) {
     const int64_t kend = int64_t(pos0) + npos;        // keys own..kend-1 are visible to some row
-    const std::vector<int64_t> bounds = piece_bounds(own[size_t(s)], kend, pos0, kind);
+    const std::vector<int64_t>& bounds = piece_bounds(own[size_t(s)], kend, pos0, kind);
     const int32_t nsplit = int32_t(bounds.size()) - 1;
     const int32_t part = add_items(s, g, row0, pos0, npos, kind, bounds, nsplit > 1 || pre);
     if (!pre) {
@@ -444,7 +461,7 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
   };
   // A run's tiles see every key of their pieces: their position is the first one behind the prefix.
   for (SharedRun& r : runs) {
-    const std::vector<int64_t> bounds = piece_bounds(0, r.len, r.len, kKindPrefill);
+    const std::vector<int64_t>& bounds = piece_bounds(0, r.len, r.len, kKindPrefill);
     for (int32_t g = 0; g < hkv; ++g)
       for (int32_t t0 = 0; t0 < r.rows; t0 += tile) {
         const int32_t npos = std::min(tile, r.rows - t0);
@@ -467,55 +484,45 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
     }
   }
 
-  // Longest first within each kind, in cost buckets of 256 keys; inside a bucket
-  // keep items of the same request and KV head together so neighbours share keys
-  // in one L2.
-  auto lpt = [](const Job& a, const Job& b) {
-    const int64_t ca = int64_t(a.cost) >> 8, cb = int64_t(b.cost) >> 8;
-    if (ca != cb) return ca > cb;
-    for (int i = 0; i < 4; ++i)
-      if (a.order_key[i] != b.order_key[i]) return a.order_key[i] < b.order_key[i];
-    return false;
-  };
-  std::vector<Job> pre, dec;
-  for (const Job& j : jobs) ((j.item.npos_kind >> 16) == kKindDecode ? dec : pre).push_back(j);
-  std::stable_sort(pre.begin(), pre.end(), lpt);
-  std::stable_sort(dec.begin(), dec.end(), lpt);
+  // The two kinds' queues.
+  std::vector<Place> pre, dec;
+  double tot_p = 0, tot_d = 0;
+  for (size_t i = 0; i < jobs.size(); ++i) {
+    const bool decode = (jobs[i].item.npos_kind >> 16) == kKindDecode;
+    (decode ? dec : pre).push_back(place_of(jobs[i], i));
+    (decode ? tot_d : tot_p) += jobs[i].cost;
+  }
+  std::sort(pre.begin(), pre.end());
+  std::sort(dec.begin(), dec.end());
   // Interleaved steps merge the two queues so that both advance at the same
   // fraction of their total work and finish together (prefill tiles load the
   // matrix cores, decode items the memory system); otherwise decode goes last
   // and fills the tail of the prefill rounds.
-  double tot_p = 0, tot_d = 0;
-  for (const Job& j : pre) tot_p += j.cost;
-  for (const Job& j : dec) tot_d += j.cost;
-  jobs.clear();
+  std::vector<uint32_t> order;
+  order.reserve(jobs.size());
   size_t ip = 0, id = 0;
   double done_p = 0, done_d = 0;
   while (ip < pre.size() || id < dec.size()) {
     const bool take_p = id >= dec.size() ||
                         (ip < pre.size() && (!interleave || done_p * tot_d <= PPAS_INTERLEAVE_BIAS * done_d * tot_p));
-    if (take_p) {
-      done_p += pre[ip].cost;
-      jobs.push_back(pre[ip++]);
-    } else {
-      done_d += dec[id].cost;
-      jobs.push_back(dec[id++]);
-    }
+    const uint32_t job = uint32_t(take_p ? pre[ip++].piece_job : dec[id++].piece_job);
+    (take_p ? done_p : done_d) += jobs[job].cost;
+    order.push_back(job);
   }
 
   // Workgroup b of a launch runs on XCD b % 8. Hand each XCD runs of 8
   // consecutive items of the sorted list, with runs dealt round-robin so every XCD
   // gets the same mix of long and short items: within each block of 64 launch
   // slots, slot 8v + x takes sorted item 8x + v.
-  const size_t n = jobs.size();
+  const size_t n = order.size();
   plan.items.resize(n);
   const size_t full = n / 64 * 64;
   for (size_t b = 0; b < full; ++b) {
     const size_t x = b % 8, k = b / 8;
     const size_t src = ((k / 8) * 8 + x) * 8 + (k % 8);
-    plan.items[b] = jobs[src].item;
+    plan.items[b] = jobs[order[src]].item;
   }
-  for (size_t b = full; b < n; ++b) plan.items[b] = jobs[b].item;
+  for (size_t b = full; b < n; ++b) plan.items[b] = jobs[order[b]].item;
 
   plan.off_combine = align_up(n * sizeof(WorkItem), 256);
   plan.list_bytes = plan.off_combine + plan.combine.size() * sizeof(CombineItem);

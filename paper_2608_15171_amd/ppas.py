@@ -402,9 +402,15 @@ def attn_step_shared(shape: Shape, out, q, k_pages, v_pages, desc, prefixes, bt_
     """attn_step for a step whose requests share prefixes: rows (first request, requests, shared positions)."""
     d, p = _desc(desc), _prefixes(prefixes)
     bt = _bt_host(bt_host, bt_dev)
-    _check_buffers(shape, d, q=q, out=out, k_pages=k_pages, v_pages=v_pages, bt_dev=bt_dev)
-    st = _lib.ppas_attn_step_shared(ctypes.byref(shape), _dev(out, "out"), _dev(q, "q"), _dev(k_pages, "k_pages"),
-                                    _dev(v_pages, "v_pages"), _host_ptr(d), len(d), _host_ptr(p),
+    if len(d) == 0 or bt_dev.element_size() != 4 or bt_dev.dim() != 2 or bt_dev.shape[0] < len(d):
+        _check_buffers(shape, d, bt_dev=bt_dev)
+        rows, pool = 0, 0
+    else:
+        rows = _rows(d) * shape.n_q_heads * shape.head_dim * 2
+        pool = int(shape.num_pages) * shape.n_kv_heads * shape.page_size * shape.head_dim * 2
+    st = _lib.ppas_attn_step_shared(ctypes.byref(shape), _buffer(out, "out", rows), _buffer(q, "q", rows),
+                                    _buffer(k_pages, "k_pages", pool), _buffer(v_pages, "v_pages", pool),
+                                    _host_ptr(d), len(d), _host_ptr(p),
                                     0 if p is None else len(p), _dev(bt_dev, "block_table"), bt_dev.shape[1],
                                     _host_ptr(bt), _dev(workspace, "workspace"),
                                     workspace.numel() * workspace.element_size(), _stream(stream))
