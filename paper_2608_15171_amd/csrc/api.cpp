@@ -61,7 +61,7 @@ namespace {
 // Work-item counts and partial-slot offsets travel as int32 (and the item count
 // sets the launch grid): a step too large for that is refused.
 bool plan_fits(const Plan& plan, size_t n_append) {
-  return plan.items.size() <= size_t(INT32_MAX) && plan.combine.size() <= size_t(INT32_MAX) &&
+  return plan.items.size() + plan.rows.size() <= size_t(INT32_MAX) && plan.combine.size() <= size_t(INT32_MAX) &&
          n_append <= size_t(INT32_MAX) && plan.part_slots <= int64_t(INT32_MAX) - 64 * kGroup;
 }
 
@@ -284,6 +284,8 @@ ppas_status build_plan(ppas_step_plan& p, const ppas_shape* shape, const ppas_se
   if (st != PPAS_OK) return st;
   char* host = static_cast<char*>(p.buf->host);
   if (!p.plan.items.empty()) std::memcpy(host, p.plan.items.data(), p.plan.items.size() * sizeof(WorkItem));
+  if (!p.plan.rows.empty())
+    std::memcpy(host + p.plan.off_rows, p.plan.rows.data(), p.plan.rows.size() * sizeof(WorkItem));
   if (!p.plan.combine.empty())
     std::memcpy(host + p.plan.off_combine, p.plan.combine.data(), p.plan.combine.size() * sizeof(CombineItem));
   if (!app.empty()) std::memcpy(host + p.off_append, app.data(), app.size() * sizeof(AppendItem));
@@ -383,7 +385,7 @@ ppas_status run_attn(const ppas_step_plan& p, void* out, const void* q, const vo
                      void* hip_stream) {
   if (p.n_seqs == 0) return PPAS_OK;
   if (!out || !q || !k_pages || !v_pages || !bt_dev || !workspace) return PPAS_EINVAL;
-  if (!p.buf || p.plan.items.empty()) return PPAS_EINVAL;   // a plan made without the attention list
+  if (!p.buf || (p.plan.items.empty() && p.plan.rows.empty())) return PPAS_EINVAL;   // a plan made without the attention list
   if (workspace_bytes < p.plan.total) return PPAS_ENOSPACE;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   char* ws = static_cast<char*>(workspace);
@@ -392,6 +394,7 @@ ppas_status run_attn(const ppas_step_plan& p, void* out, const void* q, const vo
       static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), static_cast<const uint16_t*>(k_pages),
       static_cast<const uint16_t*>(v_pages), bt_dev, p.bt_stride, p.shape.n_q_heads, p.shape.n_kv_heads,
       p.shape.scale, reinterpret_cast<const WorkItem*>(p.buf->dev), int(plan.items.size()),
+      reinterpret_cast<const WorkItem*>(p.buf->dev + plan.off_rows), int(plan.rows.size()),
       reinterpret_cast<const CombineItem*>(p.buf->dev + plan.off_combine), int(plan.combine.size()),
       plan.combine_pos, reinterpret_cast<float2*>(ws + plan.off_ml), reinterpret_cast<float*>(ws + plan.off_acc), plan.tile_pos,
       stream, ev_of(ev, 0), ev_of(ev, 1), ev_of(ev, 2), ev_of(ev, 3));
@@ -502,7 +505,8 @@ ppas_status ppas_step_plan_create_shared(const ppas_shape* shape, const ppas_seq
 
 ppas_status ppas_step_plan_info(const ppas_step_plan* plan, ppas_plan_info* info) {
   if (!plan || !info) return PPAS_EINVAL;
-  info->n_items = int32_t(plan->plan.items.size());
+  const size_t waves = plan->plan.tile_pos == kTilePosLarge ? 8 : 4;
+  info->n_items = int32_t(plan->plan.items.size() + (plan->plan.rows.size() + waves - 1) / waves);
   info->n_merge = int32_t(plan->plan.combine.size());
   info->tile_positions = plan->plan.tile_pos;
   info->n_append = plan->n_append;

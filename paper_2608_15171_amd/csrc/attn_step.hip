@@ -45,6 +45,9 @@ struct StepArgs {
   int32_t bt_stride;
   int32_t hq, hkv;
   float scale_log2;     // softmax scale * log2(e)
+  int32_t n_items;      // workgroups from here on take n_rows short decode rows, one per wave
+  int32_t n_rows;
+  const WorkItem* rows;
 };
 
 // The kernel comes in two shapes, by waves per workgroup W: W = 4 (prefill tiles
@@ -770,13 +773,12 @@ __device__ __forceinline__ void prefill_pp(const StepArgs& a, const WorkItem& it
 // j) for both the Q and K operands, so lane q's K operand is chunks 4q..4q+3 of
 // its key.
 // ---------------------------------------------------------------------------
-template <int kW>
-__device__ __forceinline__ void decode_row(const StepArgs& a, const WorkItem& it, char* smem) {
-  constexpr int kWaves = kW;
-  constexpr int kThreads = threads_of<kW>();
-  const int tid = threadIdx.x;
-  // the wave index is uniform; saying so keeps per-wave control flow scalar
-  const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+//
+// decode_stream is one wave's part: wave w of the kWaves that share the row, with items
+// of at most kMaxKeys keys and its probability-regrouping slot.
+template <int kWaves, int kMaxKeys>
+__device__ __forceinline__ void decode_stream(const StepArgs& a, const WorkItem& it, const int lane, const int w,
+                                              char* pslot, f32x4 (&oacc)[8], float& m_run, float& l_run) {
   const int n = lane & 15, q = lane >> 4;
   const bool hvalid = n < kGroup;
 
@@ -802,8 +804,8 @@ __device__ __forceinline__ void decode_row(const StepArgs& a, const WorkItem& it
   // page are clamped to it, so every block's loads stay inside the item's pages.
   const int first_page = it.key_lo >> 4;
   const int last_page = (kend - 1) >> 4;
-  constexpr int kPidRegs = kDecodeMaxKeys / (kWaves * 32 * kDecodeBlock);
-  static_assert(kPidRegs * kWaves * 32 * kDecodeBlock == kDecodeMaxKeys, "whole page-id registers");
+  constexpr int kPidRegs = kMaxKeys / (kWaves * 32 * kDecodeBlock);
+  static_assert(kPidRegs * kWaves * 32 * kDecodeBlock == kMaxKeys, "whole page-id registers");
   int pid[kPidRegs];
 #pragma unroll
   for (int r = 0; r < kPidRegs; ++r) {
@@ -855,13 +857,10 @@ __device__ __forceinline__ void decode_row(const StepArgs& a, const WorkItem& it
     for (int t = 0; t < 8; ++t) B.v[t] = ldg16_nt(vb + 16 * t * kPage);
   };
 
-  f32x4 oacc[8];
 #pragma unroll
   for (int t = 0; t < 8; ++t) oacc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = kNegInf, l_run = 0.f;
-  // this wave's probability-regrouping slot, past the region the final merge uses
-  char* pslot = smem + 3 * kBlockBytes + w * 1024;
-  static_assert(kWaves * 1024 <= kBlockBytes, "regrouping slots fit in the last ring block");
+  m_run = kNegInf;
+  l_run = 0.f;
 
   // Block at keys kb..kb+31. In a ragged last block, keys >= kend get logit
   // -inf and zero V, whatever their (clamped) pages hold.
@@ -941,6 +940,22 @@ __device__ __forceinline__ void decode_row(const StepArgs& a, const WorkItem& it
     }
     wait_vmem();
   }
+}
+
+template <int kW>
+__device__ __forceinline__ void decode_row(const StepArgs& a, const WorkItem& it, char* smem) {
+  constexpr int kWaves = kW;
+  constexpr int kThreads = threads_of<kW>();
+  const int tid = threadIdx.x;
+  // the wave index is uniform; saying so keeps per-wave control flow scalar
+  const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, q = lane >> 4;
+  const bool hvalid = n < kGroup;
+  // this wave's probability-regrouping slot, past the region the final merge uses
+  static_assert(kWaves * 1024 <= kBlockBytes, "regrouping slots fit in the last ring block");
+  f32x4 oacc[8];
+  float m_run, l_run;
+  decode_stream<kWaves, kDecodeMaxKeys>(a, it, lane, w, smem + 3 * kBlockBytes + w * 1024, oacc, m_run, l_run);
 
   // Merge the waves. O^T register r of feature tile t holds feature 16t + 4q + r.
   float l_w = l_run + __shfl_xor(l_run, 16);
@@ -992,9 +1007,46 @@ __device__ __forceinline__ void decode_row(const StepArgs& a, const WorkItem& it
   }
 }
 
+// A short decode row: one wave streams all its keys, so that rows with a few hundred keys
+// of their own (behind a shared prefix) take a quarter or an eighth of the workgroups and
+// need no merge of waves: 256 rows of 16 to 512 keys behind 24,576 shared ones ran in 512
+// workgroups of 6 us each that the tiles had to wait for.
+__device__ __forceinline__ void decode_wave(const StepArgs& a, const WorkItem& it, int lane, char* pslot) {
+  const int n = lane & 15, q = lane >> 4;
+  f32x4 oacc[8];
+  float m_run, l_run;
+  decode_stream<1, kRowMaxKeys>(a, it, lane, 0, pslot, oacc, m_run, l_run);
+  float l = l_run + __shfl_xor(l_run, 16);
+  l += __shfl_xor(l, 32);
+  if (n >= kGroup) return;
+  // O^T register r of feature tile t: feature 16t + 4q + r of head n
+  if (it.part < 0) {
+    const float inv = 1.f / l;
+    uint16_t* orow = a.out + (size_t(it.row0) * a.hq + it.kvh * kGroup + n) * kHeadDim + 4 * q;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      u32x2 v;
+      v[0] = pack_bf16x2(oacc[t][0] * inv, oacc[t][1] * inv);
+      v[1] = pack_bf16x2(oacc[t][2] * inv, oacc[t][3] * inv);
+      *reinterpret_cast<u32x2*>(orow + 16 * t) = v;
+    }
+  } else {
+    float* acc = a.part_acc + size_t(it.part + n) * kHeadDim + 4 * q;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) *reinterpret_cast<f32x4*>(acc + 16 * t) = oacc[t];
+    if (q == 0) a.part_ml[it.part + n] = make_float2(m_run, l);
+  }
+}
+
 template <int kW>
 __global__ __launch_bounds__(threads_of<kW>(), kW == 4 ? 2 : 1) void attn_step_kernel(StepArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[(kW == 8 ? 2 * kPPRing : 4) * kBlockBytes];
+  if (int(blockIdx.x) >= a.n_items) {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = (int(blockIdx.x) - a.n_items) * kW + w;
+    if (row < a.n_rows) decode_wave(a, a.rows[row], threadIdx.x & 63, smem + w * 1024);
+    return;
+  }
   const WorkItem it = a.items[blockIdx.x];
   if ((it.npos_kind >> 16) == kKindDecode)
     decode_row<kW>(a, it, smem);
@@ -1086,13 +1138,18 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const CombineI
 
 hipError_t launch_attn_step(const uint16_t* q, uint16_t* out, const uint16_t* kp, const uint16_t* vp,
                             const int32_t* bt, int32_t bt_stride, int32_t hq, int32_t hkv, float scale,
-                            const WorkItem* items, int n_items, const CombineItem* comb, int n_comb,
-                            int comb_pos, float2* part_ml, float* part_acc, int tile_pos, hipStream_t stream,
+                            const WorkItem* items, int n_items, const WorkItem* rows, int n_rows,
+                            const CombineItem* comb, int n_comb, int comb_pos, float2* part_ml, float* part_acc, int tile_pos, hipStream_t stream,
                             hipEvent_t ev_start, hipEvent_t ev_stop, hipEvent_t ev_merge_start,
                             hipEvent_t ev_merge_stop) {
   if (tile_pos != kTilePosSmall && tile_pos != kTilePosLarge) return hipErrorInvalidValue;
-  if (n_items > 0) {
+  const int per_wg = tile_pos == kTilePosLarge ? 8 : 4;
+  const int blocks = n_items + (n_rows + per_wg - 1) / per_wg;
+  if (blocks > 0) {
     StepArgs a;
+    a.n_items = n_items;
+    a.n_rows = n_rows;
+    a.rows = rows;
     a.q = q;
     a.out = out;
     a.kp = kp;
@@ -1109,10 +1166,10 @@ hipError_t launch_attn_step(const uint16_t* q, uint16_t* out, const uint16_t* kp
     // start and end (events recorded as separate commands would also time the
     // gap between those commands and the dispatch).
     if (tile_pos == kTilePosLarge)
-      hipExtLaunchKernelGGL(attn_step_kernel<8>, dim3(n_items), dim3(threads_of<8>()), 0, stream, ev_start, ev_stop,
+      hipExtLaunchKernelGGL(attn_step_kernel<8>, dim3(blocks), dim3(threads_of<8>()), 0, stream, ev_start, ev_stop,
                             0, a);
     else
-      hipExtLaunchKernelGGL(attn_step_kernel<4>, dim3(n_items), dim3(threads_of<4>()), 0, stream, ev_start, ev_stop,
+      hipExtLaunchKernelGGL(attn_step_kernel<4>, dim3(blocks), dim3(threads_of<4>()), 0, stream, ev_start, ev_stop,
                             0, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

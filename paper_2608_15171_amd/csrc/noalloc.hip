@@ -83,7 +83,7 @@ ppas_status run(const ppas_shape* shape, void* out, const void* q, const void* k
   const hipError_t e = launch_attn_step(
       static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), static_cast<const uint16_t*>(k_pages),
       static_cast<const uint16_t*>(v_pages), bt_dev, bt_stride, shape->n_q_heads, shape->n_kv_heads, shape->scale,
-      reinterpret_cast<const WorkItem*>(base), int(plan.items.size()),
+      reinterpret_cast<const WorkItem*>(base), int(plan.items.size()), nullptr, 0,
       reinterpret_cast<const CombineItem*>(base + plan.off_combine), int(plan.combine.size()), plan.combine_pos,
       reinterpret_cast<float2*>(part + plan.off_ml), reinterpret_cast<float*>(part + plan.off_acc), plan.tile_pos,
       stream, nullptr, nullptr, nullptr, nullptr);

@@ -132,7 +132,7 @@ struct SharedRun {
 // prefill and of a decode item; tile 0 where it is not worth sharing.
 struct SharedCut {
   int32_t tile = 0;
-  int64_t prefill = 0, decode = 0;
+  int64_t prefill = 0, decode = 0, row_keys = 0;   // rows of at most row_keys own keys go to single waves
 };
 
 // Sharing pays where it saves a step about 100,000 keys (times KV heads) or more: below,
@@ -143,16 +143,51 @@ struct SharedCut {
 // (254,000) 17.2 against 23.7; 64 of 8,192 with up to 4,000 of their own 38 against 92.
 constexpr int64_t kShareMinSaved = 100000;
 
-// Microseconds of a step with pieces of at most `prefill` and `decode` keys, fitted to 6,000
-// timed plans (108 steps, 12 % rms; the choice made with it is 5 % slower than the best
-// one on average): a fixed part, then what is longest of the tiles' whole rounds over the
-// workgroup slots, all items' time over the slots, the longest decode item and the decode
-// rows' bytes; then the merge, by its partials' bytes and the splits of a row.
+// Most own keys of a decode row that a single wave takes (a wave streams a key in about
+// 42 ns, a workgroup in 8). Packed so, rows take a quarter or an eighth of the workgroups:
+// 256 rows of 16 to 512 own keys and 384 tile items 77 -> 70 us; where workgroups are few,
+// they only take longer (206 rows of 217 to 439 keys and 28 tiles 21.5 -> 25.5 us).
+constexpr int64_t kRowKeys = 512;
+static_assert(kRowKeys <= kRowMaxKeys, "a wave takes the row");
+
+// Microseconds of a step with pieces of at most so many keys, fitted to 24,000 timed plans
+// of 136 steps (11 to 13 % rms; the choice made with it is 4 % slower than the best of them
+// on average, which is about what two timings of one plan differ by): a fixed part; the
+// time that the items take on the workgroup slots in launch order, or their keys' bytes;
+// then the merge, by its partials' bytes and the splits of a row. A tile's key takes
+// `key` alone and `key_full` with every slot taken.
 struct SharedCost {
-  double fixed, tile_item, tile_key, tile_key_few, decode_key, gbs, mb, split;
+  double fixed, item, key, key_full, decode_item, decode_key, row, row_key, tbs, tbs_many, mb, split;
 };
-constexpr SharedCost kShared16{9.1, 0.56, 0.0227, 0.0166, 0.0088, 5200, 0.51, 0.078};
-constexpr SharedCost kShared32{8.9, 2.14, 0.0264, 0.0223, 0.0083, 3900, 0.46, 0.093};
+constexpr SharedCost kShared16{8.8, 0.08, 0.0168, 0.0251, 0.46, 0.0083, 1.23, 0.0429, 6.13, 4.55, 0.543, 0.082};
+constexpr SharedCost kShared32{4.1, 6.29, 0.0233, 0.0252, 7.76, 0.0080, 10.1, 0.0401, 4.29, 4.29, 0.384, 0.064};
+
+// Items of one length: their keys, and how many (per KV head).
+struct Lot {
+  double keys, count;
+};
+
+// When the last of the lots ends (`keys`: an item's time) that `slots` workgroup slots take
+// in order, each on the slots that are free first. Slots that are free at about the same
+// time are one entry of `free`.
+double last_end(const std::vector<Lot>& lots, double slots) {
+  std::vector<Lot> free{{0, slots}};   // time, slots
+  double end = 0;
+  for (const Lot& lot : lots) {
+    for (double left = lot.count; left > 1e-6;) {
+      auto first = std::min_element(free.begin(), free.end(), [](const Lot& x, const Lot& y) { return x.keys < y.keys; });
+      const double start = first->keys, n = std::min(first->count, left), t = start + lot.keys;
+      first->count -= n;
+      if (first->count < 1e-6) free.erase(first);
+      auto same = std::find_if(free.begin(), free.end(), [&](const Lot& f) { return std::fabs(f.keys - t) < 0.2; });
+      if (same == free.end()) free.push_back(Lot{t, n});
+      else same->count += n;
+      end = std::max(end, t);
+      left -= n;
+    }
+  }
+  return end;
+}
 
 struct Job {
   WorkItem item;
@@ -189,70 +224,131 @@ SharedCut choose_shared(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_c
   int64_t saved = 0;
   for (const SharedRun& r : runs) saved += int64_t(r.rows - 1) * r.len * hkv;
   if (saved < kShareMinSaved && opts.prefill_split <= 0) return best;
-  static constexpr int64_t kPrefill[] = {128, 256, 512, 768, 1024, 1536, 2048, 2816, 4224, 5632, 8448};
-  static constexpr int64_t kDecode[] = {256, 512, 1024, 2048, 4096};
+  static constexpr int64_t kPrefill[] = {128, 256, 512, 768, 1024, 1280, 1536, 2048, 2816, 4224, 5632, 8448};
+  static constexpr int64_t kDecode[] = {256, 512, 768, 1024, 1536, 2048, 2560, 4096};
   auto up = [](int64_t keys, int64_t block) { return std::max(block, ceil_div(keys, block) * block); };
+  auto add = [](std::vector<Lot>& lots, double keys, double count) {
+    for (Lot& l : lots)
+      if (std::fabs(l.keys - keys) < 1) {
+        l.count += count;
+        return;
+      }
+    lots.push_back(Lot{keys, count});
+  };
+  auto longest_first = [](const Lot& x, const Lot& y) { return x.keys > y.keys; };
+
+  // The decode rows' pieces by length, in steps of 128 keys: those that a wave can take apart.
   struct Decode {
-    int64_t most;
-    double items = 0, keys = 0, longest = 0, slots = 0, splits = 1;
+    int64_t most = 0;
+    std::vector<Lot> items, rows;
+    double n_items = 0, n_rows = 0, keys = 0, slots = 0, splits = 1;
   };
   std::vector<Decode> decode;
   for (int64_t ds : kDecode) {
     if (opts.decode_split > 0 && !decode.empty()) break;
-    Decode d{opts.decode_split > 0 ? std::min<int64_t>(up(opts.decode_split, kDecodeBlock), kDecodeMaxKeys) : ds};
+    Decode d;
+    d.most = opts.decode_split > 0 ? std::min<int64_t>(up(opts.decode_split, kDecodeBlock), kDecodeMaxKeys) : ds;
     for (int32_t s = 0; s < n_seqs; ++s) {
       if (seqs[s].n_query != 1) continue;
       const int64_t keys = int64_t(seqs[s].cached_len) + 1 - own[size_t(s)], n = ceil_div(keys, d.most);
-      d.items += double(n);
+      const double len = keys <= 64 * n ? 32 : 128.0 * double(ceil_div(keys, 128 * n)) - 64;
+      if (n == 1 && keys <= kRowKeys) {
+        add(d.rows, len, 1);
+        d.n_rows += 1;
+      } else {
+        add(d.items, len, double(n));
+        d.n_items += double(n);
+      }
       d.keys += double(keys);
-      d.longest = std::max(d.longest, double(keys) / double(n));
       if (n > 1 || own[size_t(s)]) d.slots += double(n) * kGroup;
       d.splits = std::max(d.splits, double(n));
     }
-    decode.push_back(d);
+    std::sort(d.items.begin(), d.items.end(), longest_first);
+    std::sort(d.rows.begin(), d.rows.end(), longest_first);
+    decode.push_back(std::move(d));
   }
-  double best_us = 0;
+  // The tiles' pieces; requests of several tiles count their middle one.
+  struct Tiles {
+    int32_t tile;
+    int64_t most;
+    std::vector<Lot> items;
+    double n = 0, keys = 0, slots = 0, splits = 0;
+  };
+  std::vector<Tiles> tiles;
   for (int32_t tile : {kTilePosSmall, kTilePosLarge}) {
     if (opts.tile_pos != 0 && opts.tile_pos != tile) continue;
-    const SharedCost& c = tile == kTilePosSmall ? kShared16 : kShared32;
-    const double slots = double(num_cus) * (tile == kTilePosSmall ? 2 : 1);
     for (int64_t p : kPrefill) {
-      if (opts.prefill_split > 0) {
-        if (p != kPrefill[0]) break;
-        p = up(opts.prefill_split, kPrefillBlock);
-      }
-      // the tiles' pieces: (items, keys of one); requests of several tiles count their middle one
-      double items = 0, keys = 0, longest = 0, long_items = 0, part = 0, splits = 0;
-      auto add = [&](double tiles, int64_t len, double rows) {
-        const int64_t n = ceil_div(len, p);
-        const double piece = double(len) / double(n);
-        if (piece > longest) {
-          if (longest < 0.6 * piece) long_items = 0;
-          longest = piece;
-        }
-        if (piece >= 0.6 * longest) long_items += tiles * double(n);
-        items += tiles * double(n);
-        keys += tiles * double(len);
-        part += rows * double(n) * kGroup;
+      if (opts.prefill_split > 0 && p != kPrefill[0]) break;
+      Tiles t{tile, opts.prefill_split > 0 ? up(opts.prefill_split, kPrefillBlock) : p, {}};
+      auto cut_tiles = [&](int64_t rows, int64_t len) {
+        const int64_t n = ceil_div(len, t.most), items = ceil_div(rows, tile) * n;
+        add(t.items, double(len) / double(n), double(items));
+        t.n += double(items);
+        t.keys += double(items) * double(len) / double(n);
+        t.slots += double(rows * n) * kGroup;
         return double(n);
       };
-      for (const SharedRun& r : runs) splits = std::max(splits, add(double(ceil_div(r.rows, tile)), r.len, r.rows));
+      for (const SharedRun& r : runs) t.splits = std::max(t.splits, cut_tiles(r.rows, r.len));
       for (int32_t s = 0; s < n_seqs; ++s)
         if (seqs[s].n_query > 1)
-          add(double(ceil_div(seqs[s].n_query, tile)),
-              int64_t(seqs[s].cached_len) + (seqs[s].n_query + 1) / 2 - own[size_t(s)], seqs[s].n_query);
-      for (const Decode& d : decode) {
-        const double per_key = (items + d.items) * hkv <= num_cus ? c.tile_key_few : c.tile_key;
-        const double rounds = std::ceil(long_items * hkv / slots) * (c.tile_item + per_key * longest);
-        const double all = hkv * (items * c.tile_item + keys * per_key + d.keys * c.decode_key) / slots;
-        const double bytes = hkv * d.keys * 4.0 * kHeadDim / (c.gbs * 1e3);
-        const double us = c.fixed + std::max(std::max(rounds, all), std::max(d.longest * c.decode_key, bytes)) +
-                          c.mb * hkv * (part + d.slots) * (kHeadDim + 2) * 4e-6 + c.split * (splits + d.splits);
-        if (best.tile == 0 || us < best_us) {
-          best_us = us;
-          best = SharedCut{tile, p, d.most};
-        }
+          cut_tiles(seqs[s].n_query, int64_t(seqs[s].cached_len) + (seqs[s].n_query + 1) / 2 - own[size_t(s)]);
+      std::sort(t.items.begin(), t.items.end(), longest_first);
+      tiles.push_back(std::move(t));
+    }
+  }
+
+  // Every combination's lower bound (no slot idle); then, from the lowest on, the time with
+  // idle slots, until no bound is below the best time.
+  struct Option {
+    const Tiles* t;
+    const Decode* d;
+    bool pack;
+    double bound, rest;   // rest: what does not depend on the slots
+  };
+  std::vector<Option> options;
+  auto waves = [](const Tiles& t) { return t.tile == kTilePosSmall ? 4.0 : 8.0; };
+  auto slots_of = [&](const Tiles& t) { return double(num_cus) * (t.tile == kTilePosSmall ? 2 : 1); };
+  auto per_key = [&](const Tiles& t, const SharedCost& c) {
+    return c.key + (c.key_full - c.key) * std::min(1.0, t.n * hkv / slots_of(t));
+  };
+  for (const Tiles& t : tiles) {
+    const SharedCost& c = t.tile == kTilePosSmall ? kShared16 : kShared32;
+    for (const Decode& d : decode)
+      for (const bool pack : {false, true}) {
+        if (pack && d.n_rows == 0) continue;
+        double work = t.n * c.item + t.keys * per_key(t, c), n = t.n + d.n_items;
+        for (const Lot& l : d.items) work += l.count * (c.decode_item + c.decode_key * l.keys);
+        for (const Lot& l : d.rows)
+          work += pack ? l.count / waves(t) * (c.row + c.row_key * l.keys) : l.count * (c.decode_item + c.decode_key * l.keys);
+        n += pack ? d.n_rows / waves(t) : d.n_rows;
+        const double bytes = hkv * d.keys * 4.0 * kHeadDim / ((n * hkv <= num_cus ? c.tbs : c.tbs_many) * 1e6);
+        const double rest = c.fixed + c.mb * hkv * (t.slots + d.slots) * (kHeadDim + 2) * 4e-6 + c.split * (t.splits + d.splits);
+        const double one = t.items.empty() ? 0 : c.item + per_key(t, c) * t.items[0].keys;
+        options.push_back(Option{&t, &d, pack, rest + std::max(std::max(work * hkv / slots_of(t), bytes), one), rest});
       }
+  }
+  std::sort(options.begin(), options.end(), [](const Option& x, const Option& y) { return x.bound < y.bound; });
+  double best_us = 0;
+  for (const Option& o : options) {
+    if (best.tile != 0 && o.bound >= best_us) break;
+    const SharedCost& c = o.t->tile == kTilePosSmall ? kShared16 : kShared32;
+    const double key = per_key(*o.t, c);
+    // lots in launch order, as their times: tiles and decode items, longest first, then the rows
+    std::vector<Lot> lots;
+    for (const Lot& l : o.t->items) lots.push_back(Lot{c.item + key * l.keys, l.count * hkv});
+    for (const Lot& l : o.d->items) lots.push_back(Lot{c.decode_item + c.decode_key * l.keys, l.count * hkv});
+    if (!o.pack)
+      for (const Lot& l : o.d->rows) lots.push_back(Lot{c.decode_item + c.decode_key * l.keys, l.count * hkv});
+    std::sort(lots.begin(), lots.end(), longest_first);
+    if (o.pack)
+      for (const Lot& l : o.d->rows) lots.push_back(Lot{c.row + c.row_key * l.keys, l.count * hkv / waves(*o.t)});
+    const double us = std::max(o.bound, o.rest + last_end(lots, slots_of(*o.t)));
+    if (best.tile == 0 || us < best_us) {
+      best_us = us;
+      best.tile = o.t->tile;
+      best.prefill = o.t->most;
+      best.decode = o.d->most;
+      best.row_keys = o.pack ? kRowKeys : 0;
     }
   }
   return best;
@@ -263,6 +359,7 @@ SharedCut choose_shared(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_c
 void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, int num_cus, const PlanOpts& opts,
                Plan& plan, const ppas_prefix* prefixes, int32_t n_prefixes) {
   plan.items.clear();
+  plan.rows.clear();
   plan.combine.clear();
   plan.combine_pos = 0;
   plan.part_slots = 0;
@@ -428,7 +525,10 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
       // relative cost: a prefill key of a 16-position tile costs 128 rows of MFMA
       // work (twice that in a 32-position tile), a decode key ~512 bytes of HBM
       // traffic; one decode key is about two prefill keys of a 16-position tile.
+      // With shared prefixes the queues are one, in nanoseconds / 8: half a decode row's
+      // items are shorter than a tile's there, and have to fill in behind the longest.
       j.cost = double(hi - lo) * (kind == kKindDecode ? 2.0 : tile_cost);
+      if (cut.tile) j.cost = (kind == kKindDecode ? 3000 + 12.0 * double(hi - lo) : 5000 + 20.0 * tile_cost * double(hi - lo)) / 8;
       j.piece = int32_t(k);
       jobs.push_back(j);
     }
@@ -446,7 +546,16 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
     const int64_t kend = int64_t(pos0) + npos;        // keys own..kend-1 are visible to some row
     const std::vector<int64_t>& bounds = piece_bounds(own[size_t(s)], kend, pos0, kind);
     const int32_t nsplit = int32_t(bounds.size()) - 1;
-    const int32_t part = add_items(s, g, row0, pos0, npos, kind, bounds, nsplit > 1 || pre);
+    int32_t part = -1;
+    if (cut.tile && kind == kKindDecode && nsplit == 1 && kend - own[size_t(s)] <= cut.row_keys) {
+      if (pre) {
+        part = int32_t(plan.part_slots);
+        plan.part_slots += kGroup;
+      }
+      plan.rows.push_back(WorkItem{s, g, row0, pos0, 1 | (kKindDecode << 16), own[size_t(s)], int32_t(kend), part});
+    } else {
+      part = add_items(s, g, row0, pos0, npos, kind, bounds, nsplit > 1 || pre);
+    }
     if (!pre) {
       if (nsplit > 1) merge(g, row0, npos, part, nsplit, npos * kGroup, nullptr);
       return;
@@ -484,11 +593,13 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
     }
   }
 
+  std::stable_sort(plan.rows.begin(), plan.rows.end(),
+                   [](const WorkItem& x, const WorkItem& y) { return x.key_hi - x.key_lo > y.key_hi - y.key_lo; });
   // The two kinds' queues.
   std::vector<Place> pre, dec;
   double tot_p = 0, tot_d = 0;
   for (size_t i = 0; i < jobs.size(); ++i) {
-    const bool decode = (jobs[i].item.npos_kind >> 16) == kKindDecode;
+    const bool decode = !cut.tile && (jobs[i].item.npos_kind >> 16) == kKindDecode;
     (decode ? dec : pre).push_back(place_of(jobs[i], i));
     (decode ? tot_d : tot_p) += jobs[i].cost;
   }
@@ -524,7 +635,8 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
   }
   for (size_t b = full; b < n; ++b) plan.items[b] = jobs[order[b]].item;
 
-  plan.off_combine = align_up(n * sizeof(WorkItem), 256);
+  plan.off_rows = align_up(n * sizeof(WorkItem), 256);
+  plan.off_combine = align_up(plan.off_rows + plan.rows.size() * sizeof(WorkItem), 256);
   plan.list_bytes = plan.off_combine + plan.combine.size() * sizeof(CombineItem);
   plan.off_ml = 0;
   plan.off_acc = align_up(size_t(plan.part_slots) * 8, 256);

@@ -20,6 +20,7 @@ constexpr int kTilePosLarge = 32;
 constexpr int kPrefillBlock = 64;  // keys per staged K/V block of a prefill tile
 constexpr int kDecodeBlock = 32;   // keys per block of a decode wave
 constexpr int kDecodeMaxKeys = 16384;  // longest key range of one decode item
+constexpr int kRowMaxKeys = 1024;      // longest key range of a decode row that one wave takes
 constexpr int kKindPrefill = 0;
 constexpr int kKindDecode = 1;
 
@@ -69,11 +70,13 @@ struct PlanOpts {
 struct Plan {
   int tile_pos = kTilePosSmall;    // prefill tile positions, selects the kernel shape
   std::vector<WorkItem> items;     // in launch order
+  std::vector<WorkItem> rows;      // short decode rows, longest first, one per wave behind the items
   std::vector<CombineItem> combine;
   int32_t combine_pos = 0;         // most positions of a merge item
   int64_t part_slots = 0;
-  // work list as the kernels read it (bytes): items from 0, combine items at off_combine
-  size_t off_combine = 0, list_bytes = 0;
+  // work list as the kernels read it (bytes): items from 0, rows at off_rows, combine
+  // items at off_combine
+  size_t off_rows = 0, off_combine = 0, list_bytes = 0;
   // caller workspace layout (bytes): the split partials (max, sum) then accumulators
   size_t off_ml = 0, off_acc = 0, total = 0;
 };

@@ -76,7 +76,14 @@ void check(const Step& st, const Plan& plan, int hkv) {
       pos_of.push_back(int64_t(st.seqs[s].cached_len) + i);
       seq_of.push_back(int64_t(s));
     }
-  for (const WorkItem& it : plan.items) {
+  std::vector<WorkItem> items = plan.items;
+  items.insert(items.end(), plan.rows.begin(), plan.rows.end());
+  for (const WorkItem& r : plan.rows)
+    CHECK(r.npos_kind == (1 | kKindDecode << 16) && r.key_hi - r.key_lo <= kRowMaxKeys && r.key_hi == r.pos0 + 1);
+  CHECK(plan.off_rows >= plan.items.size() * sizeof(WorkItem) && plan.off_rows % 256 == 0);
+  CHECK(plan.off_combine >= plan.off_rows + plan.rows.size() * sizeof(WorkItem) && plan.off_combine % 256 == 0);
+  CHECK(plan.list_bytes == plan.off_combine + plan.combine.size() * sizeof(CombineItem));
+  for (const WorkItem& it : items) {
     const int npos = it.npos_kind & 0xffff, kind = it.npos_kind >> 16;
     CHECK(it.key_lo >= 0 && it.key_lo < it.key_hi && npos >= 1 && npos <= plan.tile_pos);
     CHECK(it.row0 >= 0 && size_t(it.row0 + npos) <= pos_of.size());
