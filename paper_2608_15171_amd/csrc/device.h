@@ -45,6 +45,7 @@ struct GateupChoice {
   int32_t splits = 1;
   int32_t main_m = 0, tail_m = 0;           // tiles: main ones along the token rows, 64-row ones after them
   int32_t light = 0, grid = 0, block = 8;   // tiles: see GemmArgs
+  double cost = 0;                          // microseconds by the choice's model (not of the general kernel)
 };
 GateupChoice gateup_choose(int32_t T, int32_t H, int32_t N2, bool act, bool aligned, int max_splits, int cus,
                            bool int_sums = false);

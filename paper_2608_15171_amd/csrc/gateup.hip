@@ -37,11 +37,18 @@ struct Shape {
 // and kReduceSplit (more rows hide the chain) belong to the fit at rows_cost.
 constexpr double kStage256 = 0.92, kStage128 = 0.66, kStage64 = 0.53;
 constexpr double kTile256 = 5.3, kTile128 = 1.4, kTile64 = 0.4;
+// 64-row tiles of 8-bit rows, in 128-feature stages (3,400 timed calls of 15 projections, 1 to
+// 4,100 tokens; with kRowsInt the choice is 0.7 % slower than the best on average)
+constexpr double kStage64Int = 0.48, kTile64Int = 1.5;
 constexpr double kReduce = 4.25, kReduceSplit = 0.12, kPartBytes = 5.5e6, kLoaded = 0.186, kWeightBytes = 9.45e6;
 
 constexpr int kRowsMaxT = 256;   // the few-row kernel measured up to here; from about 64 rows the tiles win on wide outputs
+// 8-bit rows: measured up to here (154 calls of 200 to 1,500 tokens, where the model's choice
+// is 1.3 % slower than the best on average; without the few-row kernel above 256 it was
+// 19 %: 512 tokens x 4,096 x 512 15.7 us instead of 7.7)
+constexpr int kRowsMaxTInt = 1536;
 
-Shape shape_cost(int32_t T, int32_t H, int32_t N2, int grid_max, int bm, int splits) {
+Shape shape_cost(int32_t T, int32_t H, int32_t N2, int grid_max, int bm, int splits, bool int_sums) {
   Shape s;
   s.bm = bm;
   s.splits = splits;
@@ -53,7 +60,7 @@ Shape shape_cost(int32_t T, int32_t H, int32_t N2, int grid_max, int bm, int spl
   s.items = nf + ns;
   const double nk = double(H / kBK) / splits;
   const double cf = bm == 256 ? nk * kStage256 + kTile256 : nk * kStage128 + kTile128;
-  const double cs = nk * kStage64 + kTile64;
+  const double cs = int_sums ? nk * kStage64Int + kTile64Int : nk * kStage64 + kTile64;
   s.light = std::max(0, int(cf / cs));
   const int64_t grid = std::min<int64_t>(s.items, grid_max);
   const int64_t rem = nf % grid, light = grid - rem;
@@ -89,7 +96,12 @@ constexpr RowsShape kRowsShapes[] = {{1, 8, false, true}, {1, 16, false, true}, 
 // for all sizes had been: 11,008 x 512 with 48 tokens 24.2 us where that one takes 22.3
 // (now 18.9), 16,384 x 8,192 with 16 tokens 82.4 against 73.8 (now 65.2).
 constexpr double kTilesBase = 4.64;
-double rows_cost(int32_t T, int32_t H, int32_t N2, int cus, const RowsShape& v) {
+struct RowsCost {
+  double base, cu, chip, x, result, fill, tile;   // microseconds, or bytes per microsecond
+};
+constexpr RowsCost kRowsBf16{2.9, 5.57e4, 8.0e6, 9.93e4, 0.02, 2.84, 0.01};
+constexpr RowsCost kRowsInt{0.91, 12.9e4, 12.3e6, 9.04e4, 0.11, 2.18, 0.11};
+double rows_cost(int32_t T, int32_t H, int32_t N2, int cus, const RowsShape& v, const RowsCost& k) {
   const int xt = rows_tokens(T) / 16;
   const double cols = double((int64_t(N2) + v.g * v.wr - 1) / (v.g * v.wr));
   const double mt = (T + 16 * xt - 1) / (16 * xt);
@@ -99,9 +111,9 @@ double rows_cost(int32_t T, int32_t H, int32_t N2, int cus, const RowsShape& v) 
   const double wgs = cols * mt, room = double(cus) * per_cu;
   const double rounds = wgs > room ? std::ceil(wgs / room) * per_cu : std::max(1.0, wgs / cus);
   const double w = 2.0 * v.g * v.wr * H, x = 2.0 * T / mt * H;
-  const double cost = 2.9 + std::max(rounds * w / 5.57e4, mt * 2.0 * N2 * H / 8.0e6) + rounds * x / 9.93e4 +
-                      0.02 * v.g * xt + 2.84 * std::ceil(wgs / room);
-  return cost * (1 + 0.01 * (v.g - 1));
+  const double cost = k.base + std::max(rounds * w / k.cu, mt * 2.0 * N2 * H / k.chip) + rounds * x / k.x +
+                      k.result * v.g * xt + k.fill * std::ceil(wgs / room);
+  return cost * (1 + k.tile * (v.g - 1));
 }
 
 }  // namespace
@@ -149,7 +161,7 @@ GateupChoice gateup_choose(int32_t T, int32_t H, int32_t N2, bool act, bool alig
     for (int s = 1; s <= max_splits; ++s) {
       if (bm == 256 && s < max_splits && !int_sums) continue;
       if (narrow && ((s > 1 && s * 4 * kBK != H) || bm == 256)) continue;
-      const Shape c = shape_cost(T, H, N2, grid_max, bm, s);
+      const Shape c = shape_cost(T, H, N2, grid_max, bm, s, int_sums);
       if (c.items > INT32_MAX / 2) continue;
       if (best.bm == 0 || c.cost < best.cost) best = c;
     }
@@ -163,13 +175,14 @@ GateupChoice gateup_choose(int32_t T, int32_t H, int32_t N2, bool act, bool alig
   r.light = best.light;
   r.grid = int32_t(std::min<int64_t>(best.items, grid_max));
   r.block = narrow || longest < 8 ? 4 : 8;
-  if (T > kRowsMaxT) return r;
   double cost = best.cost + kTilesBase;
+  r.cost = cost;
+  if (T > (int_sums ? kRowsMaxTInt : kRowsMaxT)) return r;
   for (const RowsShape& v : kRowsShapes) {
     if (!(act ? v.with_act : v.without) || N2 / (v.g * v.wr) >= (1 << 22) || (narrow && v.g > 1)) continue;
-    const double c = rows_cost(T, H, N2, grid_max, v);
+    const double c = rows_cost(T, H, N2, grid_max, v, int_sums ? kRowsInt : kRowsBf16);
     if (c < cost) {
-      cost = c;
+      r.cost = cost = c;
       r.kernel = GateupChoice::kRows;
       r.rows = rows_tokens(T);
       r.splits = 1;

@@ -14,6 +14,27 @@
 
 namespace ppas {
 
+namespace {
+
+// One launch (two with splits) of token rows first .. first + T - 1.
+hipError_t launch_rows_of(const Int8Product& p, int32_t first, int32_t T, const GateupChoice& c, bool act, void* part,
+                          hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop) {
+  GemmArgs a{};
+  a.x = reinterpret_cast<const uint16_t*>(p.x + size_t(first) * p.H);
+  a.w = reinterpret_cast<const uint16_t*>(p.w);
+  a.y = p.y + size_t(first) * (act ? p.N2 / 2 : p.N2);
+  a.sx = p.sx + first;
+  a.sw = p.sw;
+  a.part = static_cast<float*>(part);
+  a.T = T;
+  a.H = p.H / 2;
+  a.N2 = p.N2;
+  const hipError_t e = launch_choice<Int8>(a, c, act, stream, ev_start, ev_stop);
+  return e != hipSuccess || c.splits == 1 ? e : launch_reduce<Int8>(a, act, c.splits, stream, ev_stop);
+}
+
+}  // namespace
+
 hipError_t launch_gateup_i8(const Int8Product& p, bool act, int max_splits, void* part, int cus, hipStream_t stream,
                             hipEvent_t ev_start, hipEvent_t ev_stop) {
   if (p.T <= 0) return hipSuccess;
@@ -22,21 +43,23 @@ hipError_t launch_gateup_i8(const Int8Product& p, bool act, int max_splits, void
   // transfer); anything else in the general kernel
   const bool aligned = p.H % (2 * kBK) == 0 && p.H > 2 * kBK && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 &&
                        reinterpret_cast<uintptr_t>(p.w) % 16 == 0;
-  GateupChoice c;
-  if (aligned) c = gateup_choose(p.T, p.H / 2, p.N2, act, true, std::min(max_splits, p.H / (2 * kBK)), cus, true);
+  if (!aligned) return launch_gateup_i8_any(p, act, stream, ev_start, ev_stop);
+  auto choose = [&](int32_t T, int splits) { return gateup_choose(T, p.H / 2, p.N2, act, true, splits, cus, true); };
+  const GateupChoice c = choose(p.T, max_splits);
   if (c.kernel == GateupChoice::kGeneral) return launch_gateup_i8_any(p, act, stream, ev_start, ev_stop);
-  GemmArgs a{};
-  a.x = reinterpret_cast<const uint16_t*>(p.x);
-  a.w = reinterpret_cast<const uint16_t*>(p.w);
-  a.y = p.y;
-  a.sx = p.sx;
-  a.sw = p.sw;
-  a.part = static_cast<float*>(part);
-  a.T = p.T;
-  a.H = p.H / 2;
-  a.N2 = p.N2;
-  const hipError_t e = launch_choice<Int8>(a, c, act, stream, ev_start, ev_stop);
-  return e != hipSuccess || c.splits == 1 ? e : launch_reduce<Int8>(a, act, c.splits, stream, ev_stop);
+  // The rows past the last whole 64 in a launch of their own, where they would make a
+  // round of tiles for themselves (the sums are the same): 2,056 tokens x 11,008 x 2,048,
+  // a chunk with eight decode rows, in one launch 61 us.
+  const int32_t tail = p.T % kTailBM, main = p.T - tail;
+  if (c.kernel == GateupChoice::kTiles && tail > 0 && main > 0) {
+    // both parts' partial sums fit where the whole call's do
+    const GateupChoice m = choose(main, max_splits), t = choose(tail, 1);
+    if (m.kernel != GateupChoice::kGeneral && t.kernel != GateupChoice::kGeneral && m.cost + t.cost < 0.97 * c.cost) {
+      const hipError_t e = launch_rows_of(p, 0, main, m, act, part, stream, ev_start, nullptr);
+      return e != hipSuccess ? e : launch_rows_of(p, main, tail, t, act, part, stream, nullptr, ev_stop);
+    }
+  }
+  return launch_rows_of(p, 0, p.T, c, act, part, stream, ev_start, ev_stop);
 }
 
 }  // namespace ppas
