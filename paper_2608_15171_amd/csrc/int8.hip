@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void quant_i8_kernel(QuantArgs a) {
 #pragma unroll
   for (int i = 0; i < kC; ++i) {
     const int c = t + i * kRow;
-    v[i] = c < chunks ? *reinterpret_cast<const u32x4*>(x + 8 * c) : u32x4{0, 0, 0, 0};
+    v[i] = c < chunks ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x + 8 * c)) : u32x4{0, 0, 0, 0};
   }
 #pragma unroll
   for (int i = 0; i < kC; ++i)

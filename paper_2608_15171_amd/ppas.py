@@ -320,7 +320,7 @@ def _heads(t, name, elem: int = 2):
         raise ValueError(f"{name} must be [rows, heads, features] of {elem}-byte elements, got {tuple(t.shape)} {t.dtype}")
     n, h, d = t.shape
     row, head, one = t.stride()
-    if (d > 1 and one != 1) or (h > 1 and head != d):
+    if (one != 1 and d > 1) or (head != d and h > 1):
         raise ValueError(f"the heads of {name} must follow each other")
     return t.data_ptr(), row if n > 1 else max(row, h * d)
 
@@ -329,7 +329,7 @@ def rope_rows(rope: Rope, x, positions, y, transposed: bool = False, events: Eve
     """y[r] = the heads of x[r] turned by positions[r] (x, y [rows, heads, features] bf16 with any row stride,
     positions int32). y may be x. `transposed` turns the other way: the gradient, and without a magnitude the inverse."""
     xp, xs = _heads(x, "x")
-    yp, ys = _heads(y, "y")
+    yp, ys = (xp, xs) if y is x else _heads(y, "y")
     if x.shape != y.shape or positions.dim() != 1 or positions.shape[0] != x.shape[0]:
         raise ValueError(f"shapes x {tuple(x.shape)}, y {tuple(y.shape)}, positions {tuple(positions.shape)} do not match")
     if positions.element_size() != 4 or positions.is_floating_point():
@@ -529,16 +529,15 @@ def gateup_act_i8_workspace_bytes(n_tokens: int, hidden: int, n_inter: int) -> i
 
 
 def _gateup_i8(fn, what, x, x_scale, w, w_scale, y, per, workspace, events, stream):
-    for t, name, size in ((x, "x", 1), (w, "w", 1), (y, "y", 2)):
-        if t.dim() != 2 or t.element_size() != size:
-            raise ValueError(f"{name} must be a 2-D tensor of {size}-byte elements")
+    if not (x.dim() == w.dim() == y.dim() == 2 and x.element_size() == w.element_size() == 1 and y.element_size() == 2):
+        raise ValueError(f"x and w must be 2-D int8 tensors and y a 2-D bf16 tensor, got {x.dtype}, {w.dtype}, {y.dtype}")
     T, H = x.shape
     N = w.shape[0]
     if N % per or w.shape[1] != H or tuple(y.shape) != (T, N // per):
         raise ValueError(f"shapes x {tuple(x.shape)}, w {tuple(w.shape)}, y {tuple(y.shape)} do not match")
-    for t, name, n in ((x_scale, "x_scale", T), (w_scale, "w_scale", N)):
-        if t.numel() != n or t.element_size() != 4 or not t.is_floating_point():
-            raise ValueError(f"{name} must hold {n} fp32 values")
+    if not (x_scale.numel() == T and w_scale.numel() == N and x_scale.element_size() == w_scale.element_size() == 4
+            and x_scale.is_floating_point() and w_scale.is_floating_point()):
+        raise ValueError(f"x_scale must hold {T} fp32 values and w_scale {N}")
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     st = fn(_dev(x, "x"), _dev(x_scale, "x_scale"), _dev(w, "w"), _dev(w_scale, "w_scale"), _dev(y, "y"), T, H, N // per,
             _dev(workspace, "workspace"), ws_bytes, None if events is None else ctypes.byref(events), _stream(stream))
