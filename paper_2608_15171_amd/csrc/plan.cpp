@@ -150,17 +150,23 @@ constexpr int64_t kShareMinSaved = 100000;
 constexpr int64_t kRowKeys = 512;
 static_assert(kRowKeys <= kRowMaxKeys, "a wave takes the row");
 
-// Microseconds of a step with pieces of at most so many keys, fitted to 24,000 timed plans
-// of 136 steps (11 to 13 % rms; the choice made with it is 4 % slower than the best of them
-// on average, which is about what two timings of one plan differ by): a fixed part; the
-// time that the items take on the workgroup slots in launch order, or their keys' bytes;
-// then the merge, by its partials' bytes and the splits of a row. A tile's key takes
-// `key` alone and `key_full` with every slot taken.
+// Microseconds of a step with pieces of at most so many keys, fitted to 32,000 plans of 105
+// steps, each timed over a hundred passes in a row (5 to 6 % rms; the choice made with it
+// is 3 % slower than the best of them on average): a fixed part; the time that the items
+// take on the workgroup slots in launch order, and the one that the decode rows' keys take
+// from memory (with a share of a slot's time for every decode item), which hide one
+// another in part (the `power` mean of the two); then the merge, by its partials' bytes
+// and the splits of a row. A tile's key takes `key` alone and `key_full` with every slot
+// taken (for 16 positions 5 % above the fit, which timed full chips of them too short).
 struct SharedCost {
-  double fixed, item, key, key_full, decode_item, decode_key, row, row_key, tbs, tbs_many, mb, split;
+  double fixed, item, key, key_full, decode_item, decode_key, row, row_key, tbs, tbs_many, decode_slot, power, mb, split;
 };
-constexpr SharedCost kShared16{8.8, 0.08, 0.0168, 0.0251, 0.46, 0.0083, 1.23, 0.0429, 6.13, 4.55, 0.543, 0.082};
-constexpr SharedCost kShared32{4.1, 6.29, 0.0233, 0.0252, 7.76, 0.0080, 10.1, 0.0401, 4.29, 4.29, 0.384, 0.064};
+constexpr SharedCost kShared16{7.05, 5.0, 0.0168, 0.0258, 4.9, 0.0088, 9.5, 0.0374, 21.4, 7.27, 4.1, 1.33, 0.295, 0.095};
+constexpr SharedCost kShared32{7.74, 6.7, 0.0233, 0.0244, 5.4, 0.0100, 14.2, 0.0376, 9.35, 6.49, 5.0, 2.61, 0.297, 0.066};
+double together(double slots_us, double memory_us, double power) {
+  const double most = std::max(slots_us, memory_us), least = std::min(slots_us, memory_us);
+  return most <= 0 ? 0 : most * std::pow(1 + std::pow(least / most, power), 1 / power);
+}
 
 // Items of one length: their keys, and how many (per KV head).
 struct Lot {
@@ -303,7 +309,7 @@ SharedCut choose_shared(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_c
     const Tiles* t;
     const Decode* d;
     bool pack;
-    double bound, rest;   // rest: what does not depend on the slots
+    double bound, rest, memory;   // rest: what depends on neither the slots nor memory
   };
   std::vector<Option> options;
   auto waves = [](const Tiles& t) { return t.tile == kTilePosSmall ? 4.0 : 8.0; };
@@ -321,10 +327,12 @@ SharedCut choose_shared(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_c
         for (const Lot& l : d.rows)
           work += pack ? l.count / waves(t) * (c.row + c.row_key * l.keys) : l.count * (c.decode_item + c.decode_key * l.keys);
         n += pack ? d.n_rows / waves(t) : d.n_rows;
-        const double bytes = hkv * d.keys * 4.0 * kHeadDim / ((n * hkv <= num_cus ? c.tbs : c.tbs_many) * 1e6);
+        const double memory = hkv * d.keys * 4.0 * kHeadDim / ((n * hkv <= num_cus ? c.tbs : c.tbs_many) * 1e6) +
+                              hkv * (d.n_items + (pack ? 0 : d.n_rows)) * c.decode_slot / slots_of(t);
         const double rest = c.fixed + c.mb * hkv * (t.slots + d.slots) * (kHeadDim + 2) * 4e-6 + c.split * (t.splits + d.splits);
         const double one = t.items.empty() ? 0 : c.item + per_key(t, c) * t.items[0].keys;
-        options.push_back(Option{&t, &d, pack, rest + std::max(std::max(work * hkv / slots_of(t), bytes), one), rest});
+        options.push_back(Option{&t, &d, pack, rest + together(std::max(work * hkv / slots_of(t), one), memory, c.power),
+                                 rest, memory});
       }
   }
   std::sort(options.begin(), options.end(), [](const Option& x, const Option& y) { return x.bound < y.bound; });
@@ -342,7 +350,7 @@ SharedCut choose_shared(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_c
     std::sort(lots.begin(), lots.end(), longest_first);
     if (o.pack)
       for (const Lot& l : o.d->rows) lots.push_back(Lot{c.row + c.row_key * l.keys, l.count * hkv / waves(*o.t)});
-    const double us = std::max(o.bound, o.rest + last_end(lots, slots_of(*o.t)));
+    const double us = o.rest + together(last_end(lots, slots_of(*o.t)), o.memory, c.power);
     if (best.tile == 0 || us < best_us) {
       best_us = us;
       best.tile = o.t->tile;
