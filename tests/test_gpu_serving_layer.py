@@ -1,0 +1,168 @@
+"""The operators together, as a server runs them: two decoder layers over three iterations of requests that share a system
+prompt, with 8-bit projections and positions scaled beyond the learned length.
+
+An iteration makes one plan for both layers. Each layer quantises its hidden states by token, projects Q, K and V in one
+8-bit product, turns and appends them from that product's rows, attends with the shared prefix, projects the output,
+and runs the MLP, all 8-bit. Every stage is checked on the inputs that it was given (the previous stage's own outputs),
+by the bounds of its operator's own tests; the cache is then read back at the end against every key and value that was
+ever appended.
+"""
+import numpy as np
+import pytest
+
+import oracle.attention as OA
+import oracle.int8 as Q
+import oracle.kv_cache as OK
+import oracle.rope as R
+import oracle.rope_forms as F
+from paper_2608_15171_amd import inputs as I
+
+pytestmark = pytest.mark.gpu
+
+HIDDEN, INTER, HQ, HKV, D = 256, 384, 16, 2, 128
+FORM = dict(layout="interleaved", rotary_dim=96, theta=1e6)
+SCALED = dict(scaling="bands", factor=8.0, original_len=512, low=1.0, high=4.0)
+W_REL = 2.0 ** -8 + 6e-4
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2608_15171_amd import ppas, step
+    return ppas, step, torch
+
+
+class Layer:
+    def __init__(self, lib, seed, pages):
+        ppas, step, torch = lib
+        g = torch.Generator(device="cuda").manual_seed(seed)
+
+        def weight(n, k):
+            w = (torch.randn(n, k, device="cuda", generator=g) * 0.05).bfloat16()
+            q, s = torch.empty(n, k, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+            ppas.quant_i8(w, q, s)                     # by output channel, once
+            return q, s
+        self.qkv, self.o = weight((HQ + 2 * HKV) * D, HIDDEN), weight(HIDDEN, HQ * D)
+        self.gate_up, self.down = weight(2 * INTER, HIDDEN), weight(HIDDEN, INTER)
+        self.kp = torch.full((pages, HKV, D // 8, 16, 8), -1, dtype=torch.int16, device="cuda").view(torch.bfloat16)
+        self.vp = torch.full((pages, HKV, D, 16), -1, dtype=torch.int16, device="cuda").view(torch.bfloat16)
+        self.hist = {}                                  # request -> appended keys and values, as bf16 bits
+
+
+def quantised(lib, x, check=True):
+    ppas, step, torch = lib
+    x = x.view(x.shape[0], -1)
+    q, s = torch.empty(x.shape, dtype=torch.int8, device="cuda"), torch.empty(x.shape[0], device="cuda")
+    ppas.quant_i8(x, q, s)
+    if check:
+        qr, sr = Q.quantise(step.bits_of(x))
+        assert np.array_equal(q.cpu().numpy(), qr)
+        assert (np.abs(s.double().cpu().numpy() - sr) <= 2.0 ** -24 * sr).all()
+    return q, s
+
+
+def product(lib, x, w, n, act=False):
+    ppas, step, torch = lib
+    (q, s), (wq, ws) = quantised(lib, x), w
+    y = torch.empty(x.shape[0], n, dtype=torch.bfloat16, device="cuda")
+    size = ppas.gateup_act_i8_workspace_bytes if act else ppas.gateup_i8_workspace_bytes
+    work = torch.empty(max(256, size(x.shape[0], wq.shape[1], n)), dtype=torch.uint8, device="cuda")
+    (ppas.gateup_act_i8 if act else ppas.gateup_proj_i8)(q, s, wq, ws, y, work)
+    c = Q.product(q.cpu().numpy(), s.cpu().numpy(), wq.cpu().numpy(), ws.cpu().numpy())
+    got = y.double().cpu().numpy()
+    if act:
+        g, u = c[:, :n], c[:, n:]
+        z = g / (1 + np.exp(-g)) * u
+        bound = (2.0 ** -8 * np.abs(z) + 3 * 2.0 ** -24 * (1.1 * np.abs(g * u) + np.abs(z)) + 2.0 ** -24 * (np.abs(g) + 4) * np.abs(z)) / (1 - 2.0 ** -8)
+    else:
+        z, bound = c, (2.0 ** -8 + 2.0 ** -22) * np.abs(c)
+    assert (np.abs(got - z) <= bound + 1e-30).all()
+    return y
+
+
+def run_layer(lib, L, x, plan, shape, desc, bt, bt_host, ids):
+    ppas, step, torch = lib
+    T = x.shape[0]
+    rows = product(lib, x, L.qkv, (HQ + 2 * HKV) * D).view(T, HQ + 2 * HKV, D)
+    q = torch.empty(T, HQ, D, dtype=torch.bfloat16, device="cuda")
+    rope = ppas.rope(**FORM, **SCALED)
+    plan.rope_qkv_append(rope, q, L.kp, L.vp, rows[:, :HQ], rows[:, HQ:-HKV], rows[:, -HKV:], bt)
+    bits = step.bits_of(rows)
+    pos = R.row_positions(desc)
+    kp, vp = step.bits_of(L.kp), step.bits_of(L.vp)
+    turned = {}
+    for name, got, src in (("q", step.bits_of(q), bits[:, :HQ]), ("k", None, bits[:, HQ:-HKV])):
+        if got is None:
+            got = np.empty((T, HKV, D), np.uint16)
+            for s, (at, n, c) in enumerate(desc.tolist()):
+                got[at:at + n] = OK.gather(kp, vp, bt_host[s], c + n, 16)[0][c:]
+        xs = R.bf16_bits_to_f64(src)
+        ref = F.turn(xs, pos, FORM["layout"], FORM["rotary_dim"], FORM["theta"], **SCALED)
+        a, b = F.pairs_of(FORM["layout"], FORM["rotary_dim"])
+        tol = 2.0 ** -8 * np.abs(ref)
+        for one in (a, b):
+            tol[..., one] += 1e-6 * (np.abs(xs[..., a]) + np.abs(xs[..., b]))
+        assert (np.abs(R.bf16_bits_to_f64(got) - ref) <= tol).all(), name
+        turned[name] = got
+    # what the requests' histories hold now: the new keys as they are in the pages, the values as projected
+    for s, (at, n, c) in enumerate(desc.tolist()):
+        k, v = L.hist.get(ids[s], (np.zeros((0, HKV, D), np.uint16),) * 2)
+        assert len(k) == c
+        L.hist[ids[s]] = np.concatenate([k, turned["k"][at:at + n]]), np.concatenate([v, bits[at:at + n, -HKV:]])
+    out = torch.empty_like(q)
+    work = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+    plan.attn_step(out, q, L.kp, L.vp, bt, work)
+    O, A = OA.mixed_step_attention(turned["q"], desc, [L.hist[i][0] for i in ids], [L.hist[i][1] for i in ids],
+                                   shape.scale, HKV, with_abs=True)
+    g = out.double().cpu().numpy()
+    assert (np.abs(g - O) <= 2.0 ** -8 * np.abs(g) + W_REL * (A + np.abs(O)) + 1e-6).all()
+    h = product(lib, out.view(T, -1), L.o, HIDDEN) + x
+    return h + product(lib, product(lib, h, L.gate_up, INTER, act=True), L.down, HIDDEN)
+
+
+def test_iterations_of_two_layers(lib):
+    ppas, step, torch = lib
+    prompt, users, pages = 1040, 6, 400
+    layers = [Layer(lib, s, pages) for s in (1, 2)]
+    shape = ppas.make_shape(HQ, HKV, pages)
+    order = I.rng(1, 5).permutation(pages).astype(np.int32)
+    table = np.full((1 + users, 80), -1, np.int32)
+    table[0, :65] = order[:65]                                   # the system prompt's pages, prefilled as request 0
+    for u in range(users):
+        table[1 + u, :65] = order[:65]
+        table[1 + u, 65:80] = order[65 + 15 * u:80 + 15 * u]
+    table[0, 65:] = order[300:315]
+    g = torch.Generator(device="cuda").manual_seed(3)
+    length = {}
+    # iteration 0 prefills the system prompt; 1 prefills the users' own prompts behind it; 2 and 3 decode
+    for it in range(4):
+        if it == 0:
+            ids, new = [0], [prompt]
+        elif it == 1:
+            for L in layers:
+                for u in range(users):
+                    L.hist[1 + u] = tuple(t[:prompt] for t in L.hist[0])
+            length.update({1 + u: prompt for u in range(users)})
+            ids, new = list(range(1, 1 + users)), [3, 17, 1, 40, 64, 29]
+        else:
+            ids, new = list(range(1, 1 + users)), [1] * users
+        desc, at = np.zeros((len(ids), 3), np.int32), 0
+        for i, (r, n) in enumerate(zip(ids, new)):
+            desc[i] = (at, n, length.get(r, 0))
+            at += n
+            length[r] = length.get(r, 0) + n
+        bt_host = np.ascontiguousarray(table[ids])
+        bt = torch.from_numpy(bt_host).cuda()
+        prefixes = [] if it == 0 else [(0, users, prompt)]
+        x = torch.randn(at, HIDDEN, device="cuda", generator=g).bfloat16()
+        print(f"iteration {it}: rows={at} desc={desc.tolist()}", flush=True)
+        with ppas.StepPlan(shape, desc, bt_host, opts=ppas.plan_opts(256, 0, 0), prefixes=prefixes) as plan:
+            for L in layers:
+                x = run_layer(lib, L, x, plan, shape, desc, bt, bt_host, ids)
+                assert bool(torch.isfinite(x).all())
+    for L in layers:
+        kp, vp = step.bits_of(L.kp), step.bits_of(L.vp)
+        for u in range(users):
+            k, v = OK.gather(kp, vp, table[1 + u], length[1 + u], 16)
+            assert np.array_equal(k, L.hist[1 + u][0]) and np.array_equal(v, L.hist[1 + u][1])
