@@ -253,7 +253,7 @@ SharedCut choose_shared(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_c
   for (int64_t ds : kDecode) {
     if (opts.decode_split > 0 && !decode.empty()) break;
     Decode d;
-    d.most = opts.decode_split > 0 ? std::min<int64_t>(up(opts.decode_split, kDecodeBlock), kDecodeMaxKeys) : ds;
+    d.most = opts.decode_split > 0 ? std::min<int64_t>(up(opts.decode_split, kDecodeBlock), kDecodeMaxKeys - kDecodeBlock) : ds;
     for (int32_t s = 0; s < n_seqs; ++s) {
       if (seqs[s].n_query != 1) continue;
       const int64_t keys = int64_t(seqs[s].cached_len) + 1 - own[size_t(s)], n = ceil_div(keys, d.most);
@@ -491,7 +491,7 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
   auto piece_bounds = [&](int64_t lo, int64_t hi, int64_t pos0, int kind) -> const std::vector<int64_t>& {
     b.assign(1, lo);
     const int64_t kend = hi - lo;
-    if (cut.tile) {   // even pieces
+    if (cut.tile) {   // even pieces (the last one may have up to a block more than the others)
       const int64_t n = ceil_div(kend, kind == kKindDecode ? ksd : ksp);
       const int64_t unit = kind == kKindDecode ? kDecodeBlock : kPrefillBlock;
       const int64_t top = kind == kKindDecode ? hi : pos0 / kPrefillBlock * kPrefillBlock;

@@ -177,6 +177,21 @@ int main() {
     make_plan(sh, st.seqs.data(), n, cus[(t / 3) % 4], o, plan, st.prefixes.data(), np);
     check(st, plan, hkv);
   }
+  // own ranges around multiples of the longest decode item, cut as long as can be
+  for (int keys : {16384, 16385, 32767, 32768, 32769, 49151, 65535}) {
+    Step st;
+    st.seqs = {ppas_seq{0, 1, 1024 + keys - 1}, ppas_seq{1, 1, 1024 + keys - 1}, ppas_seq{2, 1, 1024}};
+    st.len = {1024, 1024, 1024};
+    st.prefixes = {ppas_prefix{0, 3, 1024}};
+    ppas_shape sh{8, 1, 128, 16, 1 << 20, 0.1f};
+    CHECK(validate(&sh, st.seqs.data(), 3, nullptr, INT32_MAX, false) == PPAS_OK);
+    PlanOpts o;
+    o.prefill_split = 1024;
+    o.decode_split = 1 << 20;
+    Plan plan;
+    make_plan(sh, st.seqs.data(), 3, 256, o, plan, st.prefixes.data(), 1);
+    check(st, plan, 1);
+  }
   if (g_failures) return 1;
   std::printf("ok\n");
   return 0;
