@@ -264,7 +264,8 @@ typedef struct ppas_qkv {
  * keys and the values go to the pages; the rows themselves are not modified. q_out may
  * be rows->q where q_stride is n_q_heads * 128 (in place); otherwise it must not overlap
  * the rows (PPAS_EINVAL, as for strides below a row's features or pools off 16 bytes).
- * Validation, ownership, streams and errors otherwise as ppas_rope_kv_append.
+ * Validation, ownership, streams and errors otherwise as ppas_rope_kv_append
+ * (PPAS_ERANGE from 2^24 touched pages on).
  */
 ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope, const ppas_qkv* rows, void* q_out,
                                  void* k_pages, void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
@@ -531,7 +532,8 @@ ppas_status ppas_quant_i8(const void* x, int64_t x_stride, void* xq, float* scal
  * nearest-even. The sums are exact int32, so that results depend neither on the number
  * of tokens beside a token, nor on the workspace or kernel; the product of the scales,
  * the sum and their product are each rounded to fp32. hidden is 1..131071 (the sums
- * then fit; above: PPAS_ERANGE); multiples of 128 with x and w on 16 bytes are fast, and
+ * then fit; above: PPAS_ERANGE); multiples of 128 from 256 on, with x and w on 16 bytes,
+ * are fast, and
  * may be split over workgroups with int32 partial sums in the workspace (optional, as in
  * ppas_gateup_proj; any size, 16-byte aligned). x_scale and w_scale may be any fp32
  * values. n_tokens == 0 is a no-op. Other arguments, events, streams and errors as for

@@ -337,8 +337,8 @@ bool off(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p)
 
 // T: the step's token rows.
 ppas_status check_qkv(const ppas_shape& s, const ppas_rope* rope, const ppas_qkv* r, const void* q_out,
-                      const void* k_pages, const void* v_pages, const int32_t* bt_dev, int64_t T) {
-  const ppas_status st = rope_table(rope, s.head_dim, nullptr);
+                      const void* k_pages, const void* v_pages, const int32_t* bt_dev, int64_t T, RopeTable& table) {
+  const ppas_status st = rope_table(rope, s.head_dim, table);
   if (st != PPAS_OK) return st;
   if (!r || !r->q || !r->k || !r->v || !q_out || !k_pages || !v_pages || !bt_dev) return PPAS_EINVAL;
   const int64_t q_row = int64_t(s.n_q_heads) * s.head_dim, kv_row = int64_t(s.n_kv_heads) * s.head_dim;
@@ -358,14 +358,12 @@ ppas_status check_qkv(const ppas_shape& s, const ppas_rope* rope, const ppas_qkv
   return PPAS_OK;
 }
 
-ppas_status run_qkv_append(const ppas_step_plan& p, const ppas_rope& rope, const ppas_qkv& rows, void* q_out,
+ppas_status run_qkv_append(const ppas_step_plan& p, const RopeTable& table, const ppas_qkv& rows, void* q_out,
                            void* k_pages, void* v_pages, const int32_t* bt_dev, const ppas_events* ev,
                            void* hip_stream) {
   if (!p.buf || p.n_append == 0) return PPAS_EINVAL;   // a plan made without the page-write list
+  if (p.n_append > kAppendMaxItems) return PPAS_ERANGE;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const RopeTable* table = nullptr;
-  const ppas_status st = rope_table(&rope, p.shape.head_dim, &table);
-  if (st != PPAS_OK) return st;
   RopeAppend r;
   r.q = static_cast<const uint16_t*>(rows.q);
   r.k = static_cast<const uint16_t*>(rows.k);
@@ -384,7 +382,7 @@ ppas_status run_qkv_append(const ppas_step_plan& p, const ppas_rope& rope, const
   r.bt_stride = p.bt_stride;
   r.hq = p.shape.n_q_heads;
   r.hkv = p.shape.n_kv_heads;
-  const hipError_t e = launch_rope_qkv_append(r, *table, stream, ev_of(ev, 0), ev_of(ev, 1));
+  const hipError_t e = launch_rope_qkv_append(r, table, stream, ev_of(ev, 0), ev_of(ev, 1));
   const bool noted = note_use(p.buf, stream);
   return (e == hipSuccess && noted) ? PPAS_OK : PPAS_EHIP;
 }
@@ -566,10 +564,11 @@ ppas_status ppas_rope_qkv_append_planned(const ppas_step_plan* plan, const ppas_
   ppas_status st = check_events(events);
   if (st != PPAS_OK) return st;
   try {
-    if (plan->n_seqs == 0) return rope_table(rope, kHeadDim, nullptr);
-    st = check_qkv(plan->shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, plan->n_rows);
+    RopeTable table;
+    if (plan->n_seqs == 0) return rope_table(rope, kHeadDim, table);
+    st = check_qkv(plan->shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, plan->n_rows, table);
     if (st != PPAS_OK) return st;
-    return run_qkv_append(*plan, *rope, *rows, q_out, k_pages, v_pages, block_table_dev, events, hip_stream);
+    return run_qkv_append(*plan, table, *rows, q_out, k_pages, v_pages, block_table_dev, events, hip_stream);
   } catch (...) {
     return PPAS_EINVAL;
   }
@@ -851,10 +850,11 @@ ppas_status ppas_rope_kv_append(const ppas_shape* shape, float rope_theta, void*
 }
 
 ppas_status ppas_rope_frequencies(const ppas_rope* rope, int32_t head_dim, double* out) {
-  const ppas_status st = rope_table(rope, head_dim, nullptr);
+  double w[kRopeMaxPairs];
+  const ppas_status st = rope_frequencies(rope, head_dim, w);
   if (st != PPAS_OK) return st;
   if (!out) return PPAS_EINVAL;
-  for (int32_t j = 0; j < rope->rotary_dim / 2; ++j) out[j] = rope_frequency(*rope, j);
+  std::copy(w, w + rope->rotary_dim / 2, out);
   return PPAS_OK;
 }
 
@@ -864,8 +864,8 @@ ppas_status ppas_rope_rows(const ppas_rope* rope, const void* x, int64_t x_strid
   try {
     if (n_rows < 0 || n_heads < 1 || n_heads > 65536 || head_dim < 2 || head_dim % 2 != 0) return PPAS_EINVAL;
     if (head_dim > 2 * kRopeMaxPairs) return PPAS_EUNSUPPORTED;
-    const RopeTable* table = nullptr;
-    ppas_status st = rope_table(rope, head_dim, &table);
+    RopeTable table;
+    ppas_status st = rope_table(rope, head_dim, table);
     if (st != PPAS_OK) return st;
     st = check_events(events);
     if (st != PPAS_OK) return st;
@@ -880,7 +880,7 @@ ppas_status ppas_rope_rows(const ppas_rope* rope, const void* x, int64_t x_strid
     if (!current_device().gfx950) return PPAS_EUNSUPPORTED;
     const RopeRows r{static_cast<const uint16_t*>(x), static_cast<uint16_t*>(y), x_stride, y_stride, positions_dev,
                      n_rows, n_heads, head_dim, transposed != 0};
-    const hipError_t e = launch_rope_rows(r, *table, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
+    const hipError_t e = launch_rope_rows(r, table, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
                                           ev_of(events, 1));
     return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
   } catch (...) {
@@ -896,14 +896,15 @@ ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope,
   try {
     ppas_status st = validate(shape, seqs, n_seqs, block_table_host, bt_stride, true);
     if (st != PPAS_OK) return st;
-    if (n_seqs == 0) return rope_table(rope, kHeadDim, nullptr);
+    RopeTable table;
+    if (n_seqs == 0) return rope_table(rope, kHeadDim, table);
     const int64_t T = int64_t(seqs[n_seqs - 1].query_start) + seqs[n_seqs - 1].n_query;
-    st = check_qkv(*shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, T);
+    st = check_qkv(*shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, T, table);
     if (st != PPAS_OK) return st;
     // validated above; build only the page-write list
     st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantAppend, false);
     if (st == PPAS_OK)
-      st = run_qkv_append(p, *rope, *rows, q_out, k_pages, v_pages, block_table_dev, nullptr, hip_stream);
+      st = run_qkv_append(p, table, *rows, q_out, k_pages, v_pages, block_table_dev, nullptr, hip_stream);
     release(p.buf);
     return st;
   } catch (...) {

@@ -9,6 +9,7 @@
 
 #include "device.h"
 #include "gateup_device.h"
+#include "grid.h"
 
 namespace ppas {
 namespace {
@@ -76,8 +77,8 @@ template <int kRow, int kC>
 __global__ __launch_bounds__(256) void quant_i8_kernel(QuantArgs a) {
   static_assert(kRow == 64 || kRow == 256, "a wave or a workgroup per row");
   const int t = threadIdx.x % kRow;
-  const int64_t row = int64_t(blockIdx.x) * (256 / kRow) + threadIdx.x / kRow;
-  if (row >= a.T) return;   // whole waves; with a workgroup per row, none
+  const int64_t row = block_of() * (256 / kRow) + threadIdx.x / kRow;
+  if (row >= a.T) return;   // whole waves, or the workgroup
   const int chunks = a.H / 8;
   const uint16_t* x = a.x + row * a.x_stride;
   u32x4 v[kC];
@@ -114,15 +115,17 @@ __global__ __launch_bounds__(256) void quant_i8_kernel(QuantArgs a) {
 
 // Any length and alignment: a workgroup reads its row twice, element by element.
 __global__ __launch_bounds__(256) void quant_i8_any_kernel(QuantArgs a) {
-  const int64_t row = blockIdx.x;
+  const int64_t row = block_of();
+  if (row >= a.T) return;
   const uint16_t* x = a.x + row * a.x_stride;
+  const uint32_t H = a.H;
   uint32_t m = 0;
-  for (int i = threadIdx.x; i < a.H; i += 256) m = max(m, uint32_t(x[i]) & 0x7fffu);
+  for (uint32_t i = threadIdx.x; i < H; i += 256) m = max(m, uint32_t(x[i]) & 0x7fffu);
   m = row_max<256>(m);
   const float r = ratio_of(m);
   const bool ok = usable(m);
   int8_t* out = a.xq + row * a.H;
-  for (int i = threadIdx.x; i < a.H; i += 256) out[i] = ok ? int8_t(quantise(lo_f(x[i]), r)) : int8_t(0);
+  for (uint32_t i = threadIdx.x; i < H; i += 256) out[i] = ok ? int8_t(quantise(lo_f(x[i]), r)) : int8_t(0);
   if (threadIdx.x == 0) a.scale[row] = scale_of(m);
 }
 
@@ -142,7 +145,9 @@ __global__ __launch_bounds__(256) void gateup_i8_any_kernel(Int8Product a) {
   const int ncols = kAct ? I : a.N2;
   constexpr int kCols = kAct ? kAny / 2 : kAny;
   const int tiles_n = (ncols + kCols - 1) / kCols;
-  const int m0 = int(blockIdx.x / tiles_n) * kAny, n0 = int(blockIdx.x % tiles_n) * kCols;
+  const uint32_t tile = uint32_t(block_of());   // at most 2^31 tiles
+  if (tile >= uint32_t(tiles_n) * ((uint32_t(a.T) + kAny - 1) / kAny)) return;
+  const int m0 = int(tile / tiles_n) * kAny, n0 = int(tile % tiles_n) * kCols;
   // thread t brings 16 bytes of row t / 4
   const int lr = tid / 4, lc = 16 * (tid % 4);
   const int xrow = m0 + lr;
@@ -201,7 +206,7 @@ hipError_t launch_quant_i8(const uint16_t* x, int64_t x_stride, int8_t* xq, floa
   const QuantArgs a{x, x_stride, xq, scale, T, H};
   const bool vec = H % 8 == 0 && x_stride % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0 &&
                    reinterpret_cast<uintptr_t>(xq) % 8 == 0;
-  const dim3 block(256), rows{unsigned(T)}, waves{unsigned((int64_t(T) + 3) / 4)};
+  const dim3 block(256), rows = grid_of(T), waves = grid_of((int64_t(T) + 3) / 4);
   const int chunks = H / 8;
   if (!vec || chunks > 8 * 256)
     hipExtLaunchKernelGGL(quant_i8_any_kernel, rows, block, 0, stream, ev_start, ev_stop, 0, a);
@@ -226,7 +231,7 @@ hipError_t launch_gateup_i8_any(const Int8Product& p, bool act, hipStream_t stre
                                 hipEvent_t ev_stop) {
   const int64_t tiles = gateup_i8_any_tiles(p.T, p.N2, act);
   if (tiles > INT32_MAX) return hipErrorInvalidValue;
-  const dim3 grid{unsigned(tiles)};
+  const dim3 grid = grid_of(tiles);
   if (act)
     hipExtLaunchKernelGGL(gateup_i8_any_kernel<true>, grid, dim3(256), 0, stream, ev_start, ev_stop, 0, p);
   else

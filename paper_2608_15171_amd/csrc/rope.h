@@ -17,15 +17,15 @@ struct RopeTable {
   int32_t layout = 0;
   int32_t pairs = 0;
   float magnitude = 1.f;
-  double turns[kRopeMaxPairs] = {};
+  double turns[kRopeMaxPairs];   // `pairs` of them
 };
 
-// Radians per position of pair j, in 64 bits (host only).
-double rope_frequency(const ppas_rope& rope, int32_t j);
-// The table of a ppas_rope, or PPAS_EINVAL for a field out of range (host only). The
-// table of the thread's last values is kept: a layer's calls come with the same ones,
-// and its powers take 3 us. Valid until the thread's next call.
-ppas_status rope_table(const ppas_rope* rope, int32_t head_dim, const RopeTable** table);
+constexpr int32_t kAppendMaxItems = (1 << 24) - 1;   // pages of a step's append
+
+// Radians per position of every pair (kRopeMaxPairs doubles), and the table made of them;
+// PPAS_EINVAL for a field out of range (host only).
+ppas_status rope_frequencies(const ppas_rope* rope, int32_t head_dim, double* w);
+ppas_status rope_table(const ppas_rope* rope, int32_t head_dim, RopeTable& table);
 
 // Rows of heads turned by their positions; x == y is allowed.
 struct RopeRows {

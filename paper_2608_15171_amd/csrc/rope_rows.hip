@@ -27,6 +27,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "grid.h"
 #include "rope.h"
 
 namespace ppas {
@@ -210,12 +211,14 @@ struct RowsArgs {
 template <int kMode>
 __global__ __launch_bounds__(kThreads) void rope_rows_kernel(RowsArgs a) {
   __shared__ float2 cs[kMaxRows * kRopeMaxPairs];
-  const int row0 = blockIdx.x * a.per, n = min(a.per, a.r.rows - row0);
+  const int64_t row0 = block_of() * a.per;
+  if (row0 >= a.r.rows) return;
+  const int n = int(min(int64_t(a.per), a.r.rows - row0));
   const Head h{a.r.head_dim, a.t.pairs, a.t.layout == PPAS_ROPE_HALF};
   turn_rows<kMode>(
       n, a.r.heads, h, a.r.x != a.r.y, cs,
-      [&](int row, int head) { return a.r.x + int64_t(row0 + row) * a.r.x_stride + int64_t(head) * a.r.head_dim; },
-      [&](int row, int head) { return a.r.y + int64_t(row0 + row) * a.r.y_stride + int64_t(head) * a.r.head_dim; },
+      [&](int row, int head) { return a.r.x + (row0 + row) * a.r.x_stride + int64_t(head) * a.r.head_dim; },
+      [&](int row, int head) { return a.r.y + (row0 + row) * a.r.y_stride + int64_t(head) * a.r.head_dim; },
       [&]() {
         for (int e = threadIdx.x; e < n * h.pairs; e += kThreads) {
           const int row = e / h.pairs, j = e % h.pairs;
@@ -237,6 +240,7 @@ __global__ __launch_bounds__(kThreads) void rope_rows_kernel(RowsArgs a) {
 // ---------------------------------------------------------------------------
 constexpr int kSlots = 4;                     // query slots of a workgroup
 constexpr int kParts = kPage / kSlots + 1;    // workgroups of a page
+static_assert(int64_t(kAppendMaxItems) * kThreads < int64_t(1) << 32, "one grid dimension");
 static_assert(kThreads == 2 * kHeadDim && kThreads == 16 * kPage, "one value task and one 16-byte run per thread");
 
 struct AppendArgs {
@@ -362,7 +366,7 @@ hipError_t launch_rope_rows(const RopeRows& r, const RopeTable& t, hipStream_t s
   // one batch of loads per thread, but at least about four workgroups per compute unit
   const int64_t units = int64_t(r.heads) * std::max(1, t.layout == PPAS_ROPE_HALF ? t.pairs / 8 : r.head_dim / 8);
   a.per = int32_t(std::max<int64_t>(1, std::min<int64_t>({kMaxRows, r.rows / 1024, kThreads * kAhead / units})));
-  const dim3 grid(unsigned((int64_t(r.rows) + a.per - 1) / a.per));
+  const dim3 grid = grid_of((int64_t(r.rows) + a.per - 1) / a.per);
   const bool aligned = on16(r.x) && on16(r.y) && r.x_stride % 8 == 0 && r.y_stride % 8 == 0;
   switch (mode_of(t, r.head_dim, aligned)) {
     case kHalf: hipExtLaunchKernelGGL(rope_rows_kernel<kHalf>, grid, dim3(kThreads), 0, stream, ev_start, ev_stop, 0, a); break;
@@ -377,7 +381,7 @@ hipError_t launch_rope_rows(const RopeRows& r, const RopeTable& t, hipStream_t s
 hipError_t launch_rope_qkv_append(const RopeAppend& r, const RopeTable& t, hipStream_t stream, hipEvent_t ev_start,
                                   hipEvent_t ev_stop) {
   if (r.n_items <= 0) return hipSuccess;
-  if (t.pairs > kHeadDim / 2 || r.n_desc > kAppendInline) return hipErrorInvalidValue;
+  if (t.pairs > kHeadDim / 2 || r.n_desc > kAppendInline || r.n_items > kAppendMaxItems) return hipErrorInvalidValue;
   AppendArgs a;
   a.r = r;
   a.layout = t.layout;

@@ -308,3 +308,31 @@ def test_binding_refusals(lib):
     for bad in ((b.float(), x, sx), (b, x[:, :32], sx), (b, x, sx[:3]), (b.t(), x.t(), sx), (b.cpu(), x, sx), (b, b, sx)):
         with pytest.raises(ValueError):
             ppas.quant_i8(*bad)
+
+
+@pytest.mark.parametrize("hidden", [3, 8])
+def test_quantiser_of_more_workgroups_than_a_grid_dimension(lib, hidden):
+    """Every row is the one of its number modulo 1,009."""
+    ppas, step, torch = lib
+    n = (4 if hidden % 8 == 0 else 1) * (1 << 22) + 77
+    bits = I.normal_bf16(I.rng(3, hidden), (1009, hidden))
+    qr, sr = Q.quantise(bits)
+    at = torch.arange(n, device="cuda") % 1009
+    x = torch.from_numpy(bits.view(np.int16)).cuda()[at].view(torch.bfloat16)
+    q, s = torch.full((n, hidden), 99, dtype=torch.int8, device="cuda"), torch.full((n,), -1.0, device="cuda")
+    ppas.quant_i8(x, q, s)
+    assert torch.equal(q, torch.from_numpy(qr.astype(np.int8)).cuda()[at])
+    ref = torch.from_numpy(sr).cuda()[at]
+    assert bool(((s.double() - ref).abs() <= 2.0 ** -24 * ref).all())
+
+
+def test_product_of_more_workgroups_than_a_grid_dimension(lib):
+    """One feature, one channel, 2^28 + 70 tokens."""
+    ppas, step, torch = lib
+    n = (1 << 28) + 70
+    x = torch.randint(-128, 128, (n, 1), dtype=torch.int8, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    sx = torch.full((n,), 0.5, device="cuda")
+    w, sw = torch.full((1, 1), -3, dtype=torch.int8, device="cuda"), torch.ones(1, device="cuda")
+    y = torch.full((n, 1), 7.0, dtype=torch.bfloat16, device="cuda")
+    ppas.gateup_proj_i8(x, sx, w, sw, y, torch.empty(256, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(y, (x.float() * -1.5).bfloat16())

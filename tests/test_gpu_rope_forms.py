@@ -272,3 +272,20 @@ def test_binding_refusals(lib):
             ppas.rope_rows(ppas.rope(), *args)
     with pytest.raises(ppas.PPASError):
         ppas.rope_rows(ppas.rope(), x[:2], p[:2], x[1:3])       # overlapping rows
+
+
+def test_more_workgroups_than_a_grid_dimension(lib):
+    """67 million rows of one pair: every row is the one of its number modulo 1,009."""
+    ppas, step, torch = lib
+    n = 16 * (1 << 22) + 777
+    g = torch.Generator(device="cuda").manual_seed(5)
+    some = torch.randn(1009, 1, 2, device="cuda", generator=g).bfloat16()
+    pos = torch.randint(0, 1 << 20, (1009,), device="cuda", dtype=torch.int32, generator=g)
+    want = torch.empty_like(some)
+    r = ppas.rope("interleaved", 2)
+    ppas.rope_rows(r, some, pos, want)
+    at = torch.arange(n, device="cuda") % 1009
+    x, p = some[at], pos[at]
+    y = torch.full_like(x, -1)
+    ppas.rope_rows(r, x, p, y)
+    assert torch.equal(y, want[at])
