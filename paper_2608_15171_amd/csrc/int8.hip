@@ -28,6 +28,9 @@ namespace {
 // Rows whose maximum is below 2^-110 (the scale and r would leave fp32's normal range)
 // count as zero: scale 0. A row with an infinity or NaN gets a NaN scale and zeros, so
 // that it cannot pass for a number in any product.
+//
+// Bound by memory: 16,384 rows of 2,048 take 19 us, 5.3 TB/s (a large copy 5.2); 24 rows
+// take 2 us, mostly the launch.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kTiny = (127 - 110) << 7;   // bf16 bits of 2^-110
 constexpr uint32_t kInf = 0x7f80;
