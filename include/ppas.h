@@ -265,7 +265,9 @@ typedef struct ppas_qkv {
  * be rows->q where q_stride is n_q_heads * 128 (in place); otherwise it must not overlap
  * the rows (PPAS_EINVAL, as for strides below a row's features or pools off 16 bytes).
  * Validation, ownership, streams and errors otherwise as ppas_rope_kv_append
- * (PPAS_ERANGE from 2^24 touched pages on).
+ * (PPAS_ERANGE from 2^24 touched pages on). The page-write list is staged per call or
+ * plan, so a call on a stream that captures a HIP graph is PPAS_EUNSUPPORTED, planned or
+ * not.
  */
 ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope, const ppas_qkv* rows, void* q_out,
                                  void* k_pages, void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
@@ -370,7 +372,8 @@ ppas_status ppas_step_plan_create_shared(const ppas_shape* shape, const ppas_seq
 
 /* As ppas_attn_step and ppas_attn_workspace_bytes, for a step with shared prefixes:
  * equivalent to ppas_step_plan_create_shared with default options,
- * ppas_attn_step_planned, and destroying the plan. */
+ * ppas_attn_step_planned, and destroying the plan. With prefixes, a call on a stream
+ * that captures a HIP graph is PPAS_EUNSUPPORTED. */
 ppas_status ppas_attn_step_shared(const ppas_shape* shape, void* out, const void* q,
                                   const void* k_pages, const void* v_pages,
                                   const ppas_seq* seqs, int32_t n_seqs,

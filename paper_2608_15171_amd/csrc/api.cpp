@@ -325,6 +325,17 @@ ppas_status run_append(const ppas_step_plan& p, bool rope, float theta, void* q,
   return (e == hipSuccess && noted) ? PPAS_OK : PPAS_EHIP;
 }
 
+// Lists in host memory are staged per call or plan and reused once its launches have
+// ended, which a graph's replays would read again.
+bool capturing(hipStream_t stream) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(stream, &st) != hipSuccess) {
+    (void)hipGetLastError();
+    return false;
+  }
+  return st != hipStreamCaptureStatusNone;
+}
+
 // Bytes that T rows of `row` elements, `stride` apart, span.
 uint64_t span_bytes(int64_t T, int64_t stride, int64_t row) { return 2 * (uint64_t(T - 1) * uint64_t(stride) + uint64_t(row)); }
 
@@ -364,6 +375,7 @@ ppas_status run_qkv_append(const ppas_step_plan& p, const RopeTable& table, cons
   if (!p.buf || p.n_append == 0) return PPAS_EINVAL;   // a plan made without the page-write list
   if (p.n_append > kAppendMaxItems) return PPAS_ERANGE;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (capturing(stream)) return PPAS_EUNSUPPORTED;
   RopeAppend r;
   r.q = static_cast<const uint16_t*>(rows.q);
   r.k = static_cast<const uint16_t*>(rows.k);
@@ -948,6 +960,7 @@ ppas_status ppas_attn_step_shared(const ppas_shape* shape, void* out, const void
     if (st != PPAS_OK) return st;
     if (n_seqs == 0) return PPAS_OK;
     if (!out || !q || !k_pages || !v_pages || !block_table_dev || !workspace) return PPAS_EINVAL;
+    if (n_prefixes > 0 && capturing(static_cast<hipStream_t>(hip_stream))) return PPAS_EUNSUPPORTED;
     // validated above
     st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantAttn, false, prefixes, n_prefixes);
     if (st == PPAS_OK)

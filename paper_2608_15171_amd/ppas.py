@@ -259,6 +259,14 @@ def _stream(stream):
     return getattr(stream, "cuda_stream", stream)
 
 
+def _here(*tensors):
+    """Device tensors of a call live on the current device, whose stream it takes."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"tensors of device {t.get_device()}, but the current device is {here}")
+
+
 def _check(st: int, what: str):
     if st != PPAS_OK:
         raise PPASError(st, what)
@@ -335,7 +343,9 @@ def rope_rows(rope: Rope, x, positions, y, transposed: bool = False, events: Eve
     if positions.element_size() != 4 or positions.is_floating_point():
         raise ValueError("positions must be int32")
     n, h, d = x.shape
-    st = _lib.ppas_rope_rows(ctypes.byref(rope), xp, xs, yp, ys, _dev(positions, "positions"), n, h, d,
+    pp = _dev(positions, "positions")
+    _here(x, y, positions)
+    st = _lib.ppas_rope_rows(ctypes.byref(rope), xp, xs, yp, ys, pp, n, h, d,
                              int(bool(transposed)), None if events is None else ctypes.byref(events), _stream(stream))
     _check(st, "ppas_rope_rows")
 
@@ -375,9 +385,10 @@ def rope_qkv_append(shape: Shape, rope: Rope, q, k_pages, v_pages, q_new, k_new,
     rows = _rows(d)
     _check_buffers(shape, d, q=q, k_pages=k_pages, v_pages=v_pages, bt_dev=bt_dev, rows=rows)
     x = _qkv(q_new, k_new, v_new, rows, shape.n_q_heads, shape.n_kv_heads, shape.head_dim)
-    st = _lib.ppas_rope_qkv_append(ctypes.byref(shape), ctypes.byref(rope), ctypes.byref(x), _dev(q, "q"),
-                                   _dev(k_pages, "k_pages"), _dev(v_pages, "v_pages"), _host_ptr(d), len(d),
-                                   _dev(bt_dev, "block_table"), bt_dev.shape[1], _host_ptr(bt), _stream(stream))
+    ptrs = [_dev(t, n) for t, n in ((q, "q"), (k_pages, "k_pages"), (v_pages, "v_pages"), (bt_dev, "block_table"))]
+    _here(q, k_pages, v_pages, q_new, k_new, v_new, bt_dev)
+    st = _lib.ppas_rope_qkv_append(ctypes.byref(shape), ctypes.byref(rope), ctypes.byref(x), *ptrs[:3], _host_ptr(d),
+                                   len(d), ptrs[3], bt_dev.shape[1], _host_ptr(bt), _stream(stream))
     _check(st, "ppas_rope_qkv_append")
 
 
@@ -385,8 +396,9 @@ def _prefixes(prefixes):
     """Shared prefixes as int32 [P, 3] rows of (first request, requests, positions), or None."""
     if prefixes is None or len(prefixes) == 0:
         return None
-    p = np.ascontiguousarray(prefixes, dtype=np.int32)
-    if p.ndim != 2 or p.shape[1] != 3:
+    given = np.asarray(prefixes)
+    p = np.ascontiguousarray(given, dtype=np.int32)
+    if p.ndim != 2 or p.shape[1] != 3 or (given.dtype != np.int32 and not np.array_equal(p, given)):
         raise ValueError("prefixes must be int32 [P, 3] (first_seq, n_seqs, len)")
     return p
 
@@ -408,11 +420,11 @@ def attn_step_shared(shape: Shape, out, q, k_pages, v_pages, desc, prefixes, bt_
     else:
         rows = _rows(d) * shape.n_q_heads * shape.head_dim * 2
         pool = int(shape.num_pages) * shape.n_kv_heads * shape.page_size * shape.head_dim * 2
-    st = _lib.ppas_attn_step_shared(ctypes.byref(shape), _buffer(out, "out", rows), _buffer(q, "q", rows),
-                                    _buffer(k_pages, "k_pages", pool), _buffer(v_pages, "v_pages", pool),
-                                    _host_ptr(d), len(d), _host_ptr(p),
-                                    0 if p is None else len(p), _dev(bt_dev, "block_table"), bt_dev.shape[1],
-                                    _host_ptr(bt), _dev(workspace, "workspace"),
+    ptrs = (_buffer(out, "out", rows), _buffer(q, "q", rows), _buffer(k_pages, "k_pages", pool),
+            _buffer(v_pages, "v_pages", pool), _dev(bt_dev, "block_table"), _dev(workspace, "workspace"))
+    _here(out, q, k_pages, v_pages, bt_dev, workspace)
+    st = _lib.ppas_attn_step_shared(ctypes.byref(shape), *ptrs[:4], _host_ptr(d), len(d), _host_ptr(p),
+                                    0 if p is None else len(p), ptrs[4], bt_dev.shape[1], _host_ptr(bt), ptrs[5],
                                     workspace.numel() * workspace.element_size(), _stream(stream))
     _check(st, "ppas_attn_step_shared")
 
@@ -514,9 +526,10 @@ def quant_i8(x, xq, scale, events: Events | None = None, stream=None) -> None:
         raise ValueError(f"xq must be int8 {(R, H)} and scale fp32 {(R,)}, got {tuple(xq.shape)} {tuple(scale.shape)}")
     if not x.is_cuda:
         raise ValueError("x must be a device tensor")
-    st = _lib.ppas_quant_i8(x.data_ptr(), x.stride(0) if R > 1 else max(x.stride(0), H), _dev(xq, "xq"),
-                            _dev(scale, "scale"), R, H, None if events is None else ctypes.byref(events),
-                            _stream(stream))
+    qp, sp = _dev(xq, "xq"), _dev(scale, "scale")
+    _here(x, xq, scale)
+    st = _lib.ppas_quant_i8(x.data_ptr(), x.stride(0) if R > 1 else max(x.stride(0), H), qp, sp, R, H,
+                            None if events is None else ctypes.byref(events), _stream(stream))
     _check(st, "ppas_quant_i8")
 
 
@@ -539,8 +552,10 @@ def _gateup_i8(fn, what, x, x_scale, w, w_scale, y, per, workspace, events, stre
             and x_scale.is_floating_point() and w_scale.is_floating_point()):
         raise ValueError(f"x_scale must hold {T} fp32 values and w_scale {N}")
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    st = fn(_dev(x, "x"), _dev(x_scale, "x_scale"), _dev(w, "w"), _dev(w_scale, "w_scale"), _dev(y, "y"), T, H, N // per,
-            _dev(workspace, "workspace"), ws_bytes, None if events is None else ctypes.byref(events), _stream(stream))
+    xp, sp, wp, vp, yp = (_dev(x, "x"), _dev(x_scale, "x_scale"), _dev(w, "w"), _dev(w_scale, "w_scale"), _dev(y, "y"))
+    ws = _dev(workspace, "workspace")
+    _here(x, x_scale, w, w_scale, y, workspace)
+    st = fn(xp, sp, wp, vp, yp, T, H, N // per, ws, ws_bytes, None if events is None else ctypes.byref(events), _stream(stream))
     _check(st, what)
 
 
@@ -664,10 +679,10 @@ class StepPlan:
         if bt.element_size() != 4 or bt.shape[0] < len(self.desc):
             _check_buffers(self.shape, self.desc, bt_dev=bt)
         x = _qkv(q_new, k_new, v_new, self._n_rows, *self._heads)
-        st = _lib.ppas_rope_qkv_append_planned(self._h, ctypes.byref(rope), ctypes.byref(x),
-                                               _buffer(q, "q", self._q_bytes),
-                                               _buffer(k_pages, "k_pages", self._pool_bytes),
-                                               _buffer(v_pages, "v_pages", self._pool_bytes), _dev(bt, "block_table"),
+        ptrs = (_buffer(q, "q", self._q_bytes), _buffer(k_pages, "k_pages", self._pool_bytes),
+                _buffer(v_pages, "v_pages", self._pool_bytes), _dev(bt, "block_table"))
+        _here(q, k_pages, v_pages, q_new, k_new, v_new, bt)
+        st = _lib.ppas_rope_qkv_append_planned(self._h, ctypes.byref(rope), ctypes.byref(x), *ptrs,
                                                None if events is None else ctypes.byref(events), _stream(stream))
         _check(st, "ppas_rope_qkv_append_planned")
 

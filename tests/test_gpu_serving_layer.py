@@ -166,3 +166,67 @@ def test_iterations_of_two_layers(lib):
         for u in range(users):
             k, v = OK.gather(kp, vp, table[1 + u], length[1 + u], 16)
             assert np.array_equal(k, L.hist[1 + u][0]) and np.array_equal(v, L.hist[1 + u][1])
+
+
+def calls(lib):
+    """One valid call of every entry point, by name."""
+    ppas, step, torch = lib
+    spec = I.StepSpec("pair", [I.Seq(1, 64, 0), I.Seq(1, 64, 1)])
+    data = I.make_step_data(spec, 1)
+    bt, pages = I.make_block_table(spec, 1)
+    bt[1, :4] = bt[0, :4]
+    ds = step.DeviceStep(data, bt, pages)
+    prefixes = [(0, 2, 64)]
+    plan = ppas.StepPlan(ds.shape, ds.desc, ds.bt_host, prefixes=prefixes)
+    work = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    x, q8 = torch.randn(2, 256, device="cuda").bfloat16(), torch.zeros(2, 256, dtype=torch.int8, device="cuda")
+    one, pos = torch.ones(2, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    w, sw = torch.zeros(4, 256, dtype=torch.int8, device="cuda"), torch.ones(4, device="cuda")
+    y, z = torch.empty(2, 4, device="cuda").bfloat16(), torch.empty(2, 2, device="cuda").bfloat16()
+    rows, r = ds.q.clone(), ppas.rope()
+    return plan, {
+        "rows": lambda: ppas.rope_rows(r, ds.q, pos, rows),
+        "append": lambda: ppas.rope_qkv_append(ds.shape, r, rows, ds.k_pages, ds.v_pages, ds.q, ds.k_new, ds.v_new, ds.desc,
+                                               ds.bt, ds.bt_host),
+        "append planned": lambda: plan.rope_qkv_append(r, rows, ds.k_pages, ds.v_pages, ds.q, ds.k_new, ds.v_new, ds.bt),
+        "attention": lambda: ppas.attn_step_shared(ds.shape, ds.out, ds.q, ds.k_pages, ds.v_pages, ds.desc, prefixes, ds.bt,
+                                                   work, ds.bt_host),
+        "quantiser": lambda: ppas.quant_i8(x, q8, one),
+        "product": lambda: ppas.gateup_proj_i8(q8, one, w, sw, y, work),
+        "activation": lambda: ppas.gateup_act_i8(q8, one, w, sw, z, work)}
+
+
+def test_another_current_device_is_refused(lib, monkeypatch):
+    ppas, step, torch = lib
+    plan, each = calls(lib)
+    for f in each.values():
+        f()
+    torch.cuda.synchronize()
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: 1)
+        for name, f in each.items():
+            with pytest.raises(ValueError, match="current device is 1"):
+                f()
+    plan.close()
+
+
+def test_calls_that_stage_lists_refuse_capture(lib):
+    ppas, step, torch = lib
+    plan, each = calls(lib)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        each["rows"]()
+        for name in ("append", "append planned", "attention"):
+            with pytest.raises(ppas.PPASError) as e:
+                each[name]()
+            assert e.value.status == ppas.PPAS_EUNSUPPORTED, name
+        each["quantiser"]()
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        for f in each.values():
+            f()
+        torch.cuda.synchronize()
+    plan.close()

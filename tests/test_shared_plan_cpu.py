@@ -84,3 +84,10 @@ def test_workspace_covers_the_plan_and_no_prefix_is_the_plain_step():
     assert ppas.attn_shared_workspace_bytes(sh, desc, []) == ppas.attn_workspace_bytes(sh, desc)
     assert ppas.attn_shared_workspace_bytes(sh, desc, [(0, 40, 0)]) == ppas.attn_workspace_bytes(sh, desc)
     assert ppas.attn_shared_workspace_bytes(sh, desc, [(0, 40, 4096)]) > 40 * 16 * 2 * 520
+
+
+@pytest.mark.parametrize("bad", [np.array([[0, 2, 2 ** 32 + 32]]), np.array([[0, 2, 32.5]]), np.zeros((2, 2), np.int32),
+                                 [(0, 2)], [0, 2, 32]])
+def test_prefixes_that_are_no_int32_rows(bad):
+    with pytest.raises(ValueError):
+        ppas.attn_shared_workspace_bytes(ppas.make_shape(16, 2, 100), DESC, bad)
