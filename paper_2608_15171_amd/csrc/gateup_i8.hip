@@ -10,15 +10,51 @@
 #include <cstdint>
 
 #include "device.h"
+#include "gateup_i8_mid.h"
 #include "gateup_kernels.h"
 
 namespace ppas {
 
 namespace {
 
+// How token rows go: the projection's choice, or the tiles of 128 x 128.
+struct Way {
+  GateupChoice c;
+  bool mid = false;
+  double cost = 0;
+};
+
+// Microseconds of the 128 x 128 tiles where they fit one round, else none; by the share of
+// the compute units that they fill. Fitted to calls of 64 to 4,096 tokens and seven
+// projections (7 %), weights from memory. They win from a few hundred tokens to about
+// 2,000: 700 x 2,048 x 2,048 11.3 us against 13.2, 1,024 x 5,504 x 2,048 22.1 against 25.2,
+// 512 x 4,096 x 4,096 19.1 against 24.0, 2,048 x 11,008 x 2,048 53.6 against 67.1; not on
+// a full chip with a short reduction (1,500 x 2,048 x 2,560 17.3 against 16.1), nor where
+// the others can split a long one (1,024 x 11,008 x 2,048 51.1 against 39.5).
+bool mid_cost(int32_t T, int32_t H, int32_t N2, int cus, double* us) {
+  const int64_t tiles = (int64_t(T) + 127) / 128 * ((int64_t(N2) + 127) / 128);
+  if (tiles > cus) return false;
+  const double full = double(tiles) / cus;
+  *us = 5.5 + 4.0 * full * full + H / 128 * (0.33 + 0.17 * full);
+  return true;
+}
+
+Way choose_way(int32_t T, const Int8Product& p, bool act, int max_splits, int cus) {
+  Way r;
+  r.c = gateup_choose(T, p.H / 2, p.N2, act, true, max_splits, cus, true);
+  r.cost = r.c.cost;
+  double us = 0;
+  if (!act && r.c.kernel == GateupChoice::kTiles && mid_cost(T, p.H, p.N2, cus, &us) && us < r.cost) {
+    r.mid = true;
+    r.cost = us;
+  }
+  return r;
+}
+
 // One launch (two with splits) of token rows first .. first + T - 1.
-hipError_t launch_rows_of(const Int8Product& p, int32_t first, int32_t T, const GateupChoice& c, bool act, void* part,
+hipError_t launch_rows_of(const Int8Product& p, int32_t first, int32_t T, const Way& way, bool act, void* part,
                           hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop) {
+  const GateupChoice& c = way.c;
   GemmArgs a{};
   a.x = reinterpret_cast<const uint16_t*>(p.x + size_t(first) * p.H);
   a.w = reinterpret_cast<const uint16_t*>(p.w);
@@ -29,6 +65,7 @@ hipError_t launch_rows_of(const Int8Product& p, int32_t first, int32_t T, const 
   a.T = T;
   a.H = p.H / 2;
   a.N2 = p.N2;
+  if (way.mid) return launch_gateup_i8_mid(a, stream, ev_start, ev_stop);
   const hipError_t e = launch_choice<Int8>(a, c, act, stream, ev_start, ev_stop);
   return e != hipSuccess || c.splits == 1 ? e : launch_reduce<Int8>(a, act, c.splits, stream, ev_stop);
 }
@@ -44,22 +81,21 @@ hipError_t launch_gateup_i8(const Int8Product& p, bool act, int max_splits, void
   const bool aligned = p.H % (2 * kBK) == 0 && p.H > 2 * kBK && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 &&
                        reinterpret_cast<uintptr_t>(p.w) % 16 == 0;
   if (!aligned) return launch_gateup_i8_any(p, act, stream, ev_start, ev_stop);
-  auto choose = [&](int32_t T, int splits) { return gateup_choose(T, p.H / 2, p.N2, act, true, splits, cus, true); };
-  const GateupChoice c = choose(p.T, max_splits);
-  if (c.kernel == GateupChoice::kGeneral) return launch_gateup_i8_any(p, act, stream, ev_start, ev_stop);
+  const Way all = choose_way(p.T, p, act, max_splits, cus);
+  if (all.c.kernel == GateupChoice::kGeneral) return launch_gateup_i8_any(p, act, stream, ev_start, ev_stop);
   // The rows past the last whole 64 in a launch of their own, where they would make a
   // round of tiles for themselves (the sums are the same): 2,056 tokens x 11,008 x 2,048,
   // a chunk with eight decode rows, with the quantiser 73 us instead of 78.
   const int32_t tail = p.T % kTailBM, main = p.T - tail;
-  if (c.kernel == GateupChoice::kTiles && tail > 0 && main > 0) {
+  if (all.c.kernel == GateupChoice::kTiles && tail > 0 && main > 0) {
     // both parts' partial sums fit where the whole call's do
-    const GateupChoice m = choose(main, max_splits), t = choose(tail, 1);
-    if (m.kernel != GateupChoice::kGeneral && t.kernel != GateupChoice::kGeneral && m.cost + t.cost < 0.97 * c.cost) {
+    const Way m = choose_way(main, p, act, max_splits, cus), t = choose_way(tail, p, act, 1, cus);
+    if (m.c.kernel != GateupChoice::kGeneral && t.c.kernel != GateupChoice::kGeneral && m.cost + t.cost < 0.97 * all.cost) {
       const hipError_t e = launch_rows_of(p, 0, main, m, act, part, stream, ev_start, nullptr);
       return e != hipSuccess ? e : launch_rows_of(p, main, tail, t, act, part, stream, nullptr, ev_stop);
     }
   }
-  return launch_rows_of(p, 0, p.T, c, act, part, stream, ev_start, ev_stop);
+  return launch_rows_of(p, 0, p.T, all, act, part, stream, ev_start, ev_stop);
 }
 
 }  // namespace ppas

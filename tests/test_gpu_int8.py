@@ -336,3 +336,12 @@ def test_product_of_more_workgroups_than_a_grid_dimension(lib):
     y = torch.full((n, 1), 7.0, dtype=torch.bfloat16, device="cuda")
     ppas.gateup_proj_i8(x, sx, w, sw, y, torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert torch.equal(y, (x.float() * -1.5).bfloat16())
+
+
+@pytest.mark.parametrize("T,H,N", [(700, 2048, 2048), (513, 1152, 2700), (300, 1280, 4097), (1024, 5504, 2048), (520, 4096, 4096),
+                                   (1000, 2176, 2559), (2056, 11008, 2048), (2111, 5632, 1930)])
+def test_tiles_of_128_rows_and_columns(lib, T, H, N):
+    """Sizes that fill most of a round of 128 x 128 tiles, ragged ones and odd numbers of stages among them."""
+    print(f"i8 T={T} H={H} N={N}", flush=True)
+    a = make(lib, T, H, N, 31)
+    check(lib, *a, call(lib, *a, False), False, f"T{T} H{H} N{N}")
