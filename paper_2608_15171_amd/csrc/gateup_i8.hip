@@ -1,4 +1,4 @@
-// The projection of 8-bit integers, whose kernels are the bf16 projection's with 16x16x64
+// The projection of 8-bit integers, whose kernels (but for the tiles of 128 x 128) are the bf16 projection's with 16x16x64
 // integer MFMAs: rows of 128 features are 128 bytes as 64 bf16 features are, so stages,
 // transfers, swizzles and schedule are the same, and one instruction takes as long. The
 // int32 sums are exact, so no sum needs two levels and any split gives the same result;
@@ -85,7 +85,8 @@ hipError_t launch_gateup_i8(const Int8Product& p, bool act, int max_splits, void
   if (all.c.kernel == GateupChoice::kGeneral) return launch_gateup_i8_any(p, act, stream, ev_start, ev_stop);
   // The rows past the last whole 64 in a launch of their own, where they would make a
   // round of tiles for themselves (the sums are the same): 2,056 tokens x 11,008 x 2,048,
-  // a chunk with eight decode rows, with the quantiser 73 us instead of 78.
+  // a chunk with eight decode rows, with the quantiser 73 us instead of 78 (65 with the
+  // tiles of 128 x 128).
   const int32_t tail = p.T % kTailBM, main = p.T - tail;
   if (all.c.kernel == GateupChoice::kTiles && tail > 0 && main > 0) {
     // both parts' partial sums fit where the whole call's do
