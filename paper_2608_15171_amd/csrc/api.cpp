@@ -251,9 +251,11 @@ struct ppas_step_plan {
 
 namespace {
 
-enum : int { kWantAttn = 1, kWantAppend = 2 };
+// kWantInline: the page-write list, but only by request where that is enough
+enum : int { kWantAttn = 1, kWantAppend = 2, kWantInline = 4 };
 
-// Validate, plan and stage. On success p.buf holds the lists (nullptr for an empty step).
+// Validate, plan and stage. On success p.buf holds the lists (nullptr for an empty step,
+// and where a page-write list by request is all that is wanted).
 ppas_status build_plan(ppas_step_plan& p, const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,
                        const int32_t* bt_host, int32_t bt_stride, const ppas_plan_opts* opts, int want,
                        bool check_overlap, const ppas_prefix* prefixes = nullptr, int32_t n_prefixes = 0) {
@@ -274,18 +276,21 @@ ppas_status build_plan(ppas_step_plan& p, const ppas_shape* shape, const ppas_se
   if (want & kWantAttn)
     make_plan(*shape, seqs, n_seqs, (opts && opts->num_cus > 0) ? opts->num_cus : dev.cus, to_opts(opts), p.plan,
               prefixes, n_prefixes);
-  if (want & kWantAppend) make_append_items(seqs, n_seqs, app);
-  if (!plan_fits(p.plan, app.size())) return PPAS_ERANGE;
-  p.n_append = int32_t(app.size());
-  if ((want & kWantAppend) && n_seqs <= kAppendInline) {
-    int32_t item = 0;
+  const bool by_request = (want & (kWantAppend | kWantInline)) && n_seqs <= kAppendInline;
+  if (by_request) {
+    int32_t item = 0;   // at most a page per token row
     for (int32_t s = 0; s < n_seqs; ++s) {
       const ppas_seq& q = seqs[s];
       p.desc[s] = AppendDesc{item, q.query_start, q.n_query, q.cached_len};
       item += (q.cached_len + q.n_query - 1) / kPage - q.cached_len / kPage + 1;
     }
     p.n_desc = n_seqs;
+    p.n_append = item;
+    if (want == kWantInline) return PPAS_OK;
   }
+  if (want & (kWantAppend | kWantInline)) make_append_items(seqs, n_seqs, app);
+  if (!plan_fits(p.plan, app.size())) return PPAS_ERANGE;
+  p.n_append = int32_t(app.size());
   const size_t list = (want & kWantAttn) ? p.plan.list_bytes : 0;
   p.off_append = (list + 255) / 256 * 256;
   const size_t bytes = p.off_append + app.size() * sizeof(AppendItem);
@@ -372,7 +377,7 @@ ppas_status check_qkv(const ppas_shape& s, const ppas_rope* rope, const ppas_qkv
 ppas_status run_qkv_append(const ppas_step_plan& p, const RopeTable& table, const ppas_qkv& rows, void* q_out,
                            void* k_pages, void* v_pages, const int32_t* bt_dev, const ppas_events* ev,
                            void* hip_stream) {
-  if (!p.buf || p.n_append == 0) return PPAS_EINVAL;   // a plan made without the page-write list
+  if (p.n_append == 0 || (p.n_desc == 0 && !p.buf)) return PPAS_EINVAL;   // a plan made without the page-write list
   if (p.n_append > kAppendMaxItems) return PPAS_ERANGE;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (capturing(stream)) return PPAS_EUNSUPPORTED;
@@ -386,7 +391,7 @@ ppas_status run_qkv_append(const ppas_step_plan& p, const RopeTable& table, cons
   r.q_out = static_cast<uint16_t*>(q_out);
   r.k_pages = static_cast<uint16_t*>(k_pages);
   r.v_pages = static_cast<uint16_t*>(v_pages);
-  r.items = reinterpret_cast<const AppendItem*>(p.buf->dev + p.off_append);
+  if (p.n_desc == 0) r.items = reinterpret_cast<const AppendItem*>(p.buf->dev + p.off_append);
   r.bt = bt_dev;
   r.desc = p.desc;
   r.n_desc = p.n_desc;
@@ -395,7 +400,8 @@ ppas_status run_qkv_append(const ppas_step_plan& p, const RopeTable& table, cons
   r.hq = p.shape.n_q_heads;
   r.hkv = p.shape.n_kv_heads;
   const hipError_t e = launch_rope_qkv_append(r, table, stream, ev_of(ev, 0), ev_of(ev, 1));
-  const bool noted = note_use(p.buf, stream);
+  // a list by request travels in the kernel's arguments: no buffer is read
+  const bool noted = p.n_desc > 0 || note_use(p.buf, stream);
   return (e == hipSuccess && noted) ? PPAS_OK : PPAS_EHIP;
 }
 
@@ -914,7 +920,7 @@ ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope,
     st = check_qkv(*shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, T, table);
     if (st != PPAS_OK) return st;
     // validated above; build only the page-write list
-    st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantAppend, false);
+    st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantInline, false);
     if (st == PPAS_OK)
       st = run_qkv_append(p, table, *rows, q_out, k_pages, v_pages, block_table_dev, nullptr, hip_stream);
     release(p.buf);

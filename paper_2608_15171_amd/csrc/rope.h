@@ -48,7 +48,7 @@ struct RopeAppend {
   uint16_t* q_out;
   uint16_t* k_pages;
   uint16_t* v_pages;
-  const AppendItem* items;
+  const AppendItem* items = nullptr;
   const AppendDesc* desc;       // n_desc of them (host memory) in place of the items, or none
   const int32_t* bt;
   int32_t n_items, n_desc, bt_stride, hq, hkv;

@@ -259,12 +259,15 @@ def _stream(stream):
     return getattr(stream, "cuda_stream", stream)
 
 
-def _here(*tensors):
-    """Device tensors of a call live on the current device, whose stream it takes."""
+def _here(stream, *tensors):
+    """The stream of a call, whose tensors have to live on the current device."""
     here = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensors of device {t.get_device()}, but the current device is {here}")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(here)
+    return _stream(stream)
 
 
 def _check(st: int, what: str):
@@ -344,9 +347,9 @@ def rope_rows(rope: Rope, x, positions, y, transposed: bool = False, events: Eve
         raise ValueError("positions must be int32")
     n, h, d = x.shape
     pp = _dev(positions, "positions")
-    _here(x, y, positions)
+    hs = _here(stream, x, y, positions)
     st = _lib.ppas_rope_rows(ctypes.byref(rope), xp, xs, yp, ys, pp, n, h, d,
-                             int(bool(transposed)), None if events is None else ctypes.byref(events), _stream(stream))
+                             int(bool(transposed)), None if events is None else ctypes.byref(events), hs)
     _check(st, "ppas_rope_rows")
 
 
@@ -386,9 +389,9 @@ def rope_qkv_append(shape: Shape, rope: Rope, q, k_pages, v_pages, q_new, k_new,
     _check_buffers(shape, d, q=q, k_pages=k_pages, v_pages=v_pages, bt_dev=bt_dev, rows=rows)
     x = _qkv(q_new, k_new, v_new, rows, shape.n_q_heads, shape.n_kv_heads, shape.head_dim)
     ptrs = [_dev(t, n) for t, n in ((q, "q"), (k_pages, "k_pages"), (v_pages, "v_pages"), (bt_dev, "block_table"))]
-    _here(q, k_pages, v_pages, q_new, k_new, v_new, bt_dev)
+    hs = _here(stream, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev)
     st = _lib.ppas_rope_qkv_append(ctypes.byref(shape), ctypes.byref(rope), ctypes.byref(x), *ptrs[:3], _host_ptr(d),
-                                   len(d), ptrs[3], bt_dev.shape[1], _host_ptr(bt), _stream(stream))
+                                   len(d), ptrs[3], bt_dev.shape[1], _host_ptr(bt), hs)
     _check(st, "ppas_rope_qkv_append")
 
 
@@ -422,10 +425,10 @@ def attn_step_shared(shape: Shape, out, q, k_pages, v_pages, desc, prefixes, bt_
         pool = int(shape.num_pages) * shape.n_kv_heads * shape.page_size * shape.head_dim * 2
     ptrs = (_buffer(out, "out", rows), _buffer(q, "q", rows), _buffer(k_pages, "k_pages", pool),
             _buffer(v_pages, "v_pages", pool), _dev(bt_dev, "block_table"), _dev(workspace, "workspace"))
-    _here(out, q, k_pages, v_pages, bt_dev, workspace)
+    hs = _here(stream, out, q, k_pages, v_pages, bt_dev, workspace)
     st = _lib.ppas_attn_step_shared(ctypes.byref(shape), *ptrs[:4], _host_ptr(d), len(d), _host_ptr(p),
                                     0 if p is None else len(p), ptrs[4], bt_dev.shape[1], _host_ptr(bt), ptrs[5],
-                                    workspace.numel() * workspace.element_size(), _stream(stream))
+                                    workspace.numel() * workspace.element_size(), hs)
     _check(st, "ppas_attn_step_shared")
 
 
@@ -527,9 +530,9 @@ def quant_i8(x, xq, scale, events: Events | None = None, stream=None) -> None:
     if not x.is_cuda:
         raise ValueError("x must be a device tensor")
     qp, sp = _dev(xq, "xq"), _dev(scale, "scale")
-    _here(x, xq, scale)
+    hs = _here(stream, x, xq, scale)
     st = _lib.ppas_quant_i8(x.data_ptr(), x.stride(0) if R > 1 else max(x.stride(0), H), qp, sp, R, H,
-                            None if events is None else ctypes.byref(events), _stream(stream))
+                            None if events is None else ctypes.byref(events), hs)
     _check(st, "ppas_quant_i8")
 
 
@@ -554,8 +557,8 @@ def _gateup_i8(fn, what, x, x_scale, w, w_scale, y, per, workspace, events, stre
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     xp, sp, wp, vp, yp = (_dev(x, "x"), _dev(x_scale, "x_scale"), _dev(w, "w"), _dev(w_scale, "w_scale"), _dev(y, "y"))
     ws = _dev(workspace, "workspace")
-    _here(x, x_scale, w, w_scale, y, workspace)
-    st = fn(xp, sp, wp, vp, yp, T, H, N // per, ws, ws_bytes, None if events is None else ctypes.byref(events), _stream(stream))
+    hs = _here(stream, x, x_scale, w, w_scale, y, workspace)
+    st = fn(xp, sp, wp, vp, yp, T, H, N // per, ws, ws_bytes, None if events is None else ctypes.byref(events), hs)
     _check(st, what)
 
 
@@ -681,9 +684,9 @@ class StepPlan:
         x = _qkv(q_new, k_new, v_new, self._n_rows, *self._heads)
         ptrs = (_buffer(q, "q", self._q_bytes), _buffer(k_pages, "k_pages", self._pool_bytes),
                 _buffer(v_pages, "v_pages", self._pool_bytes), _dev(bt, "block_table"))
-        _here(q, k_pages, v_pages, q_new, k_new, v_new, bt)
+        hs = _here(stream, q, k_pages, v_pages, q_new, k_new, v_new, bt)
         st = _lib.ppas_rope_qkv_append_planned(self._h, ctypes.byref(rope), ctypes.byref(x), *ptrs,
-                                               None if events is None else ctypes.byref(events), _stream(stream))
+                                               None if events is None else ctypes.byref(events), hs)
         _check(st, "ppas_rope_qkv_append_planned")
 
     def attn_step(self, out, q, k_pages, v_pages, bt_dev, workspace, events: Events | None = None,

@@ -289,3 +289,12 @@ def test_more_workgroups_than_a_grid_dimension(lib):
     y = torch.full_like(x, -1)
     ppas.rope_rows(r, x, p, y)
     assert torch.equal(y, want[at])
+
+
+@pytest.mark.parametrize("n", [63, 64, 65, 150])
+@pytest.mark.parametrize("planned", [True, False])
+def test_append_of_many_requests(lib, n, planned):
+    """Up to 64 requests travel in the kernel's arguments, more as a list in host memory."""
+    g = I.rng(17, n)
+    spec = I.StepSpec("many", [I.Seq(int(g.integers(1, 4)) if g.random() < 0.2 else 1, int(g.integers(0, 70)), i) for i in range(n)])
+    append_case(lib, spec, n, "half", 64, planned=planned, **BANDS)
