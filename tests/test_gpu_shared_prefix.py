@@ -206,3 +206,30 @@ def test_without_prefixes_is_the_plain_step(lib):
     for p in ([], None, [(0, len(spec.seqs), 0)]):
         assert bool((attend(lib, ds, p) == plain).all())
         assert bool((attend(lib, ds, p, direct=True) == plain).all())
+
+
+def test_pages_past_32_bit_offsets(lib, monkeypatch):
+    """Pools of 4.9 GB each, in whose last pages the step's keys and values lie."""
+    make = I.make_block_table
+
+    def shifted(spec, seed, spare_pages=0):
+        bt, pages = make(spec, seed, spare_pages=spare_pages)
+        return np.where(bt >= 0, bt + (600000 - pages), bt).astype(np.int32), 600000
+
+    monkeypatch.setattr(I, "make_block_table", shifted)
+    seqs = [I.Seq(1, 2048 + 50 * i, i) for i in range(20)] + [I.Seq(20, 2048, 20)]
+    spec, prefixes = I.StepSpec("far", seqs), [(0, 21, 2048)]
+    data, ds = make_step(lib, spec, prefixes, 9)
+    ref = OA.step_attention_from_data(data, ds.shape.scale, with_abs=True)
+    for tile in (16, 32):
+        compare(attend(lib, ds, prefixes, lib[0].plan_opts(512, 0, tile)), ref, f"far tile={tile}")
+
+
+@pytest.mark.parametrize("own", [16385, 32767])
+def test_own_ranges_in_the_longest_pieces(lib, own):
+    seqs = [I.Seq(1, 1024 + own - 1, i) for i in range(2)] + [I.Seq(1, 1030, 2)]
+    spec, prefixes = I.StepSpec("pieces", seqs), [(0, 3, 1024)]
+    data, ds = make_step(lib, spec, prefixes, 10)
+    ref = OA.step_attention_from_data(data, ds.shape.scale, with_abs=True)
+    for tile in (16, 32):
+        compare(attend(lib, ds, prefixes, lib[0].plan_opts(1024, 1 << 20, tile)), ref, f"own={own} tile={tile}")
