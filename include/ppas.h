@@ -359,8 +359,7 @@ ppas_status ppas_step_plan_create(const ppas_shape* shape, const ppas_seq* seqs,
  * sums. Used are whole blocks of 64 keys of a prefix; requests of more than 64 new
  * tokens fill tiles of their own and read it for themselves, and a step that would
  * save little is planned without sharing (opts->prefill_split > 0 shares whatever it
- * saves). The pages of a prefix are
- * taken from its first member's table row. PPAS_EINVAL for a prefix out of range, out of
+ * saves). The pages of a prefix are taken from its first member's table row. PPAS_EINVAL for a prefix out of range, out of
  * order, of a length that is no multiple of 16 or longer than a member's cached_len, or,
  * when block_table_host is not NULL, whose members' entries differ. n_prefixes == 0
  * (prefixes may be NULL) is ppas_step_plan_create. Used and destroyed like any plan.
@@ -536,9 +535,8 @@ ppas_status ppas_quant_i8(const void* x, int64_t x_stride, void* xq, float* scal
  * of tokens beside a token, nor on the workspace or kernel; the product of the scales,
  * the sum and their product are each rounded to fp32. hidden is 1..131071 (the sums
  * then fit; above: PPAS_ERANGE); multiples of 128 from 256 on, with x and w on 16 bytes,
- * are fast, and
- * may be split over workgroups with int32 partial sums in the workspace (optional, as in
- * ppas_gateup_proj; any size, 16-byte aligned). x_scale and w_scale may be any fp32
+ * are fast, and may be split over workgroups with int32 partial sums in the workspace
+ * (optional, as in ppas_gateup_proj; any size, 16-byte aligned). x_scale and w_scale may be any fp32
  * values. n_tokens == 0 is a no-op. Other arguments, events, streams and errors as for
  * ppas_gateup_proj. No call allocates or keeps anything; each may be captured into a
  * HIP graph, and graphs that share a workspace must not run at once.

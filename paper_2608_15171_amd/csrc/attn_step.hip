@@ -1139,8 +1139,8 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const CombineI
 hipError_t launch_attn_step(const uint16_t* q, uint16_t* out, const uint16_t* kp, const uint16_t* vp,
                             const int32_t* bt, int32_t bt_stride, int32_t hq, int32_t hkv, float scale,
                             const WorkItem* items, int n_items, const WorkItem* rows, int n_rows,
-                            const CombineItem* comb, int n_comb, int comb_pos, float2* part_ml, float* part_acc, int tile_pos, hipStream_t stream,
-                            hipEvent_t ev_start, hipEvent_t ev_stop, hipEvent_t ev_merge_start,
+                            const CombineItem* comb, int n_comb, int comb_pos, float2* part_ml, float* part_acc,
+                            int tile_pos, hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop, hipEvent_t ev_merge_start,
                             hipEvent_t ev_merge_stop) {
   if (tile_pos != kTilePosSmall && tile_pos != kTilePosLarge) return hipErrorInvalidValue;
   const int per_wg = tile_pos == kTilePosLarge ? 8 : 4;

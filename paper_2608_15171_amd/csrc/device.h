@@ -20,13 +20,13 @@ struct DeviceInfo {
 // Without a usable device: 256 CUs, not gfx950.
 DeviceInfo current_device();
 
-// The packed attention launch (of n_items items, then n_rows short decode rows) and, when n_comb > 0, the split-merge launch (of items of
-// at most comb_pos positions).
+// The packed attention launch (of n_items items, then n_rows short decode rows) and,
+// when n_comb > 0, the split-merge launch (of items of at most comb_pos positions).
 hipError_t launch_attn_step(const uint16_t* q, uint16_t* out, const uint16_t* kp, const uint16_t* vp,
                             const int32_t* bt, int32_t bt_stride, int32_t hq, int32_t hkv, float scale,
                             const WorkItem* items, int n_items, const WorkItem* rows, int n_rows,
-                            const CombineItem* comb, int n_comb, int comb_pos, float2* part_ml, float* part_acc, int tile_pos, hipStream_t stream,
-                            hipEvent_t ev_start, hipEvent_t ev_stop, hipEvent_t ev_merge_start,
+                            const CombineItem* comb, int n_comb, int comb_pos, float2* part_ml, float* part_acc,
+                            int tile_pos, hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop, hipEvent_t ev_merge_start,
                             hipEvent_t ev_merge_stop);
 
 // The gate-up projection: y = x w^T (hidden a multiple of 64), or with `act` the
