@@ -450,22 +450,27 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int m_f
   // its last phase every wave has waited for fewer transfers to be in flight than it has
   // issued since (loads into registers would have to drain the stream: 8 % of a tile).
   int sc_half = 0;
+  // As values: a choice between kernel arguments becomes one between their addresses, which
+  // keeps them in scratch memory, and every load from there drains the stream.
+  const float *sx = a.sx, *sw = a.sw;
+  int rows_total = a.T, cols_total = a.N2;
+  if constexpr (E::kInt) asm volatile("" : "+s"(sx), "+s"(sw), "+s"(rows_total), "+s"(cols_total));
   auto issue_scales = [&](const Item& it) {
     const int part = w & 3;
     int first, total;
     const float* src;
     if (w >= kWaves / 2) {
-      src = a.sx;
+      src = sx;
       first = it.m0 + 64 * part;
-      total = 64 * part < BM ? a.T : 0;
+      total = 64 * part < BM ? rows_total : 0;
     } else if (kAct) {
-      src = a.sw + (part >= 2 ? a.I : 0);
+      src = sw + (part >= 2 ? a.I : 0);
       first = it.n0 / 2 + 64 * (part & 1);
       total = a.I;
     } else {
-      src = a.sw;
+      src = sw;
       first = it.n0 + 64 * part;
-      total = a.N2;
+      total = cols_total;
     }
     const int valid = max(0, min(64, total - first));
     const uint64_t b = reinterpret_cast<uint64_t>(src + (valid > 0 ? first : 0));
