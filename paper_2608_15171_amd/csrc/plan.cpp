@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <limits>
 #include <numeric>
 
 namespace ppas {
@@ -135,10 +136,10 @@ struct SharedCut {
   int64_t prefill = 0, decode = 0, row_keys = 0;   // rows of at most row_keys own keys go to single waves
 };
 
-// Sharing pays where it saves a step about 100,000 keys (times KV heads) or more: below,
-// the requests find the prefix in the caches, and the tiles' longer items and the join
-// cost as much as they save. Measured, attention with its merge, 2 KV heads: 8 requests
-// of 2,048 shared keys (29,000 saved) 12.3 us against 11.6 apart; 16 of 4,096 (123,000)
+// Sharing pays where it can save a step about 100,000 keys (times KV heads) or more, those of
+// every row of a group but one: below, the requests find the prefix in the caches, and the
+// tiles' longer items and the join cost as much as they save. Measured, attention with its
+// merge, decode rows, 2 KV heads: 8 requests of 2,048 shared keys (29,000 saved) 12.3 us against 11.6 apart; 16 of 4,096 (123,000)
 // 16.8 against 15.3 to 17.0 against 18.6 with what else they hold; 32 of 4,096
 // (254,000) 17.2 against 23.7; 64 of 8,192 with up to 4,000 of their own 38 against 92.
 constexpr int64_t kShareMinSaved = 100000;
@@ -219,9 +220,245 @@ Place place_of(const Job& j, size_t job) {
                uint64_t(j.piece) << 32 | uint64_t(job)};
 }
 
-}  // namespace
+// What a step's items are cut from, by length. `own` is the first own key of every request.
+struct Load {          // tiles' keys, runs' and chunks'
+  double len = 0, rows = 0, tiles[2] = {0, 0};   // of kTilePosSmall and kTilePosLarge
+};
+struct Own {           // decode rows' keys, by whole blocks, which is all that a piece's length depends on
+  int64_t blocks;
+  double count = 0, behind = 0;   // rows, and those behind a shared prefix
+};
+struct StepLoads {
+  std::vector<Load> tiles;
+  std::vector<Own> decode;
+  int64_t longest_run = 0, decode_keys = 0;
+};
 
-namespace {
+// Tiles come in at most kLoads steps of length (a mean each), so that an option of the choice
+// costs the same for any number of requests (2,048 of 33 rows took 14 ms in lots of their own).
+// Requests of several tiles count their middle one.
+StepLoads loads_of(const ppas_seq* seqs, int32_t n_seqs, const std::vector<SharedRun>& runs,
+                   const std::vector<int32_t>& own) {
+  constexpr int64_t kLoads = 64;
+  StepLoads r;
+  std::vector<int64_t> each;   // twice a decode row's blocks, and one where there is a prefix
+  auto chunk_len = [&](int32_t s) { return int64_t(seqs[s].cached_len) + (seqs[s].n_query + 1) / 2 - own[size_t(s)]; };
+  for (const SharedRun& run : runs) r.longest_run = std::max(r.longest_run, run.len);
+  int64_t longest = r.longest_run;
+  for (int32_t s = 0; s < n_seqs; ++s) {
+    if (seqs[s].n_query > 1) {
+      longest = std::max(longest, chunk_len(s));
+      continue;
+    }
+    const int64_t keys = int64_t(seqs[s].cached_len) + 1 - own[size_t(s)];
+    r.decode_keys += keys;
+    each.push_back(2 * ceil_div(keys, kDecodeBlock) + (own[size_t(s)] ? 1 : 0));
+  }
+  const int64_t step = std::max<int64_t>(kPrefillBlock, longest / kLoads + 1);
+  std::vector<Load> by_len(size_t(longest / step) + 1);
+  auto put = [&](int64_t rows, int64_t len) {
+    Load& l = by_len[size_t(len / step)];
+    l.len += double(len) * double(rows);
+    l.rows += double(rows);
+    l.tiles[0] += double(ceil_div(rows, kTilePosSmall));
+    l.tiles[1] += double(ceil_div(rows, kTilePosLarge));
+  };
+  for (const SharedRun& run : runs) put(run.rows, run.len);
+  for (int32_t s = 0; s < n_seqs; ++s)
+    if (seqs[s].n_query > 1) put(seqs[s].n_query, chunk_len(s));
+  for (Load& l : by_len)
+    if (l.rows > 0) {
+      l.len /= l.rows;
+      r.tiles.push_back(l);
+    }
+  std::sort(each.begin(), each.end());
+  for (const int64_t e : each) {
+    if (r.decode.empty() || r.decode.back().blocks != e / 2) r.decode.push_back(Own{e / 2});
+    r.decode.back().count += 1;
+    r.decode.back().behind += double(e & 1);
+  }
+  return r;
+}
+
+void add_lot(std::vector<Lot>& lots, double keys, double count) {
+  for (Lot& l : lots)
+    if (std::fabs(l.keys - keys) < 1) {
+      l.count += count;
+      return;
+    }
+  lots.push_back(Lot{keys, count});
+}
+bool longer(const Lot& x, const Lot& y) { return x.keys > y.keys; }
+
+// The decode rows in pieces of at most `most` keys, by length in steps of 128: those that a
+// wave can take apart.
+struct DecodePieces {
+  int64_t most = 0;
+  std::vector<Lot> items, rows;
+  double n_items = 0, n_rows = 0, keys = 0, slots = 0, splits = 1;
+};
+DecodePieces decode_pieces(const StepLoads& loads, int64_t most) {
+  DecodePieces d;
+  d.most = most;
+  d.keys = double(loads.decode_keys);
+  for (const Own& o : loads.decode) {
+    const int64_t keys = o.blocks * kDecodeBlock, n = ceil_div(keys, most);
+    const double len = keys <= 64 * n ? 32 : 128.0 * double(ceil_div(keys, 128 * n)) - 64;
+    if (n == 1 && keys <= kRowKeys) {
+      add_lot(d.rows, len, o.count);
+      d.n_rows += o.count;
+    } else {
+      add_lot(d.items, len, o.count * double(n));
+      d.n_items += o.count * double(n);
+    }
+    d.slots += (n > 1 ? o.count : o.behind) * double(n) * kGroup;
+    d.splits = std::max(d.splits, double(n));
+  }
+  std::sort(d.items.begin(), d.items.end(), longer);
+  std::sort(d.rows.begin(), d.rows.end(), longer);
+  return d;
+}
+
+// The tiles in pieces of at most `most` keys, or, in a plan apart, of about as many, where
+// rows in one piece are written whole.
+struct TilePieces {
+  int32_t tile;
+  int64_t most;
+  std::vector<Lot> items;
+  double n = 0, keys = 0, slots = 0, splits = 0;
+};
+TilePieces tile_pieces(const StepLoads& loads, int32_t tile, int64_t most, bool apart) {
+  TilePieces t{tile, most, {}};
+  for (const Load& l : loads.tiles) {
+    const double n = std::max(1.0, apart ? std::floor(l.len / double(most) + 0.5) : std::ceil(l.len / double(most)));
+    const double items = l.tiles[tile == kTilePosLarge] * n;
+    add_lot(t.items, l.len / n, items);
+    t.n += items;
+    t.keys += items * l.len / n;
+    if (!apart || n > 1) t.slots += l.rows * n * kGroup;
+    if (apart) t.splits = std::max(t.splits, n);
+  }
+  if (!apart) t.splits = double(ceil_div(loads.longest_run, most));
+  std::sort(t.items.begin(), t.items.end(), longer);
+  return t;
+}
+
+// A way to cut a step, and its time by the model: `bound` with no slot idle, and time_of.
+struct Option {
+  const TilePieces* t;
+  const DecodePieces* d;
+  bool pack;                    // the decode rows of few keys go to single waves
+  double bound, rest, memory;   // rest: what depends on neither the slots nor memory
+};
+const SharedCost& cost_of(const TilePieces& t) { return t.tile == kTilePosSmall ? kShared16 : kShared32; }
+double waves_of(const TilePieces& t) { return t.tile == kTilePosSmall ? 4.0 : 8.0; }
+double slots_of(const TilePieces& t, int num_cus) { return double(num_cus) * (t.tile == kTilePosSmall ? 2 : 1); }
+double per_key(const TilePieces& t, int hkv, int num_cus) {
+  const SharedCost& c = cost_of(t);
+  return c.key + (c.key_full - c.key) * std::min(1.0, t.n * hkv / slots_of(t, num_cus));
+}
+Option option_of(const TilePieces& t, const DecodePieces& d, bool pack, int hkv, int num_cus) {
+  const SharedCost& c = cost_of(t);
+  const double key = per_key(t, hkv, num_cus), slots = slots_of(t, num_cus);
+  double work = t.n * c.item + t.keys * key, n = t.n + d.n_items;
+  for (const Lot& l : d.items) work += l.count * (c.decode_item + c.decode_key * l.keys);
+  for (const Lot& l : d.rows)
+    work += pack ? l.count / waves_of(t) * (c.row + c.row_key * l.keys) : l.count * (c.decode_item + c.decode_key * l.keys);
+  n += pack ? d.n_rows / waves_of(t) : d.n_rows;
+  const double memory = hkv * d.keys * 4.0 * kHeadDim / ((n * hkv <= num_cus ? c.tbs : c.tbs_many) * 1e6) +
+                        hkv * (d.n_items + (pack ? 0 : d.n_rows)) * c.decode_slot / slots;
+  const double rest = c.fixed + c.mb * hkv * (t.slots + d.slots) * (kHeadDim + 2) * 4e-6 + c.split * (t.splits + d.splits);
+  const double one = t.items.empty() ? 0 : c.item + key * t.items[0].keys;
+  return Option{&t, &d, pack, rest + together(std::max(work * hkv / slots, one), memory, c.power), rest, memory};
+}
+double time_of(const Option& o, int hkv, int num_cus) {
+  const SharedCost& c = cost_of(*o.t);
+  const double key = per_key(*o.t, hkv, num_cus);
+  // lots in launch order, as their times: tiles and decode items, longest first, then the rows
+  std::vector<Lot> lots;
+  for (const Lot& l : o.t->items) lots.push_back(Lot{c.item + key * l.keys, l.count * hkv});
+  for (const Lot& l : o.d->items) lots.push_back(Lot{c.decode_item + c.decode_key * l.keys, l.count * hkv});
+  if (!o.pack)
+    for (const Lot& l : o.d->rows) lots.push_back(Lot{c.decode_item + c.decode_key * l.keys, l.count * hkv});
+  std::sort(lots.begin(), lots.end(), longer);
+  if (o.pack)
+    for (const Lot& l : o.d->rows) lots.push_back(Lot{c.row + c.row_key * l.keys, l.count * hkv / waves_of(*o.t)});
+  return o.rest + together(last_end(lots, slots_of(*o.t, num_cus)), o.memory, c.power);
+}
+
+// How a step is cut without shared prefixes: the tile's positions, and the most keys of a
+// piece (about as many, of a tile).
+struct PlainCut {
+  int32_t tile = 0;
+  int64_t prefill = 0, decode = 0, prefill_keys = 0, decode_keys = 0;
+};
+PlainCut plain_cut(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_cus, const PlanOpts& opts) {
+  PlainCut cut;
+  // Total work, to size the key splits so that the launch has several
+  // workgroups per compute unit: keys summed over prefill tiles (of either
+  // size) and over decode rows.
+  auto prefill_keys_for = [&](int32_t tile) {
+    int64_t keys = 0;
+    for (int32_t s = 0; s < n_seqs; ++s) {
+      const ppas_seq& q = seqs[s];
+      if (q.n_query == 1) continue;
+      for (int32_t t0 = 0; t0 < q.n_query; t0 += tile)
+        keys += int64_t(q.cached_len) + std::min(q.n_query, t0 + tile);
+    }
+    return keys * hkv;
+  };
+  int64_t large_tiles = 0;
+  for (int32_t s = 0; s < n_seqs; ++s) {
+    const ppas_seq& q = seqs[s];
+    if (q.n_query == 1)
+      cut.decode_keys += int64_t(q.cached_len + 1) * hkv;
+    else
+      large_tiles += ceil_div(q.n_query, kTilePosLarge) * hkv;
+  }
+
+  // Tile shape. The eight-wave kernel stages each K/V block once for 256 rows
+  // instead of 128, which pays when the step's prefill alone fills the chip with
+  // 32-position tiles (two per CU before any key split) and decode rows are a
+  // small share of the work (a workgroup then holds a whole CU, so a prefill
+  // tile no longer shares its CU with a decode item).
+  cut.tile = opts.tile_pos;
+  if (cut.tile != kTilePosSmall && cut.tile != kTilePosLarge) {
+    const int64_t small_keys = prefill_keys_for(kTilePosSmall);
+    const bool big = large_tiles >= int64_t(2) * num_cus;
+    const bool few_decodes = double(cut.decode_keys) * 2.0 < kLargeTileDecodeShare * double(small_keys);
+    cut.tile = (big && few_decodes) ? kTilePosLarge : kTilePosSmall;
+  }
+  cut.prefill_keys = prefill_keys_for(cut.tile);
+
+  cut.prefill = opts.prefill_split;
+  if (cut.prefill <= 0) {
+    const int64_t target = int64_t(PPAS_PREFILL_ITEMS_PER_CU) * num_cus;
+    cut.prefill = std::max<int64_t>(256, ceil_div(cut.prefill_keys, target));
+  }
+  cut.prefill = std::max<int64_t>(kPrefillBlock, ceil_div(cut.prefill, kPrefillBlock) * kPrefillBlock);
+  cut.decode = opts.decode_split;
+  if (cut.decode <= 0) {
+    const int64_t target = int64_t(2) * num_cus;
+    cut.decode = std::min<int64_t>(8192, std::max<int64_t>(512, ceil_div(cut.decode_keys, target)));
+  }
+  cut.decode = std::max<int64_t>(kDecodeBlock, ceil_div(cut.decode, kDecodeBlock) * kDecodeBlock);
+  cut.decode = std::min<int64_t>(cut.decode, kDecodeMaxKeys);
+  return cut;
+}
+
+// Whether requests first..end-1 need fewer tiles together than apart (or decode rows' streams,
+// all but one of them): the rows of a chunk share its tiles' keys already, so that requests of 16,
+// 32, 48 or 64 rows save nothing, and their partials are all that sharing them adds (64 of 64 rows
+// behind 1,024 keys 79 us, apart 50; 128 behind 4,096 303, apart 247; two or eight of them as long
+// either way).
+bool saves_tiles(const ppas_seq* seqs, int32_t first, int32_t end) {
+  int64_t apart = 0, chunk_rows = 0;
+  for (int32_t s = first; s < end; ++s) {
+    apart += ceil_div(seqs[s].n_query, kTilePosSmall);
+    if (seqs[s].n_query > 1) chunk_rows += seqs[s].n_query;
+  }
+  return apart > std::max<int64_t>(1, ceil_div(chunk_rows, kTilePosSmall));
+}
 
 // `own` is the first own key of every request; opts' fields that are set stand.
 SharedCut choose_shared(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_cus, const PlanOpts& opts,
@@ -233,176 +470,50 @@ SharedCut choose_shared(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_c
   static constexpr int64_t kPrefill[] = {128, 256, 512, 768, 1024, 1280, 1536, 2048, 2816, 4224, 5632, 8448};
   static constexpr int64_t kDecode[] = {256, 512, 768, 1024, 1536, 2048, 2560, 4096};
   auto up = [](int64_t keys, int64_t block) { return std::max(block, ceil_div(keys, block) * block); };
-  auto add = [](std::vector<Lot>& lots, double keys, double count) {
-    for (Lot& l : lots)
-      if (std::fabs(l.keys - keys) < 1) {
-        l.count += count;
-        return;
-      }
-    lots.push_back(Lot{keys, count});
-  };
-  auto longest_first = [](const Lot& x, const Lot& y) { return x.keys > y.keys; };
+  const StepLoads loads = loads_of(seqs, n_seqs, runs, own);
 
-  // The decode rows' pieces by length, in steps of 128 keys: those that a wave can take apart.
-  struct Decode {
-    int64_t most = 0;
-    std::vector<Lot> items, rows;
-    double n_items = 0, n_rows = 0, keys = 0, slots = 0, splits = 1;
-  };
-  // Their keys by whole blocks, which is all that a piece's length depends on.
-  struct Own {
-    int64_t blocks;
-    double count = 0, behind = 0;   // rows, and those behind a shared prefix
-  };
-  std::vector<Own> owns;
-  int64_t decode_keys = 0;
-  {
-    std::vector<int64_t> each;   // twice the blocks, and one where there is a prefix
-    for (int32_t s = 0; s < n_seqs; ++s) {
-      if (seqs[s].n_query != 1) continue;
-      const int64_t keys = int64_t(seqs[s].cached_len) + 1 - own[size_t(s)];
-      decode_keys += keys;
-      each.push_back(2 * ceil_div(keys, kDecodeBlock) + (own[size_t(s)] ? 1 : 0));
+  std::vector<DecodePieces> decode;
+  if (opts.decode_split > 0)
+    decode.push_back(decode_pieces(loads, std::min<int64_t>(up(opts.decode_split, kDecodeBlock), kDecodeMaxKeys - kDecodeBlock)));
+  else
+    for (int64_t most : kDecode) {
+      decode.push_back(decode_pieces(loads, most));
+      if (decode.back().splits == 1) break;   // longer pieces are the same ones
     }
-    std::sort(each.begin(), each.end());
-    for (const int64_t e : each) {
-      if (owns.empty() || owns.back().blocks != e / 2) owns.push_back(Own{e / 2});
-      owns.back().count += 1;
-      owns.back().behind += double(e & 1);
-    }
-  }
-  std::vector<Decode> decode;
-  for (int64_t ds : kDecode) {
-    if (opts.decode_split > 0 && !decode.empty()) break;
-    Decode d;
-    d.most = opts.decode_split > 0 ? std::min<int64_t>(up(opts.decode_split, kDecodeBlock), kDecodeMaxKeys - kDecodeBlock) : ds;
-    d.keys = double(decode_keys);
-    for (const Own& o : owns) {
-      const int64_t keys = o.blocks * kDecodeBlock, n = ceil_div(keys, d.most);
-      const double len = keys <= 64 * n ? 32 : 128.0 * double(ceil_div(keys, 128 * n)) - 64;
-      if (n == 1 && keys <= kRowKeys) {
-        add(d.rows, len, o.count);
-        d.n_rows += o.count;
-      } else {
-        add(d.items, len, o.count * double(n));
-        d.n_items += o.count * double(n);
-      }
-      d.slots += (n > 1 ? o.count : o.behind) * double(n) * kGroup;
-      d.splits = std::max(d.splits, double(n));
-    }
-    std::sort(d.items.begin(), d.items.end(), longest_first);
-    std::sort(d.rows.begin(), d.rows.end(), longest_first);
-    const bool whole = d.splits == 1;
-    decode.push_back(std::move(d));
-    if (whole) break;   // longer pieces are the same ones
-  }
-  // The tiles' keys, runs' and chunks', by length in at most kLoads steps (a mean length each), so
-  // that an option costs the same for any number of requests (2,048 of 33 rows took 14 ms in lots of
-  // their own). Requests of several tiles count their middle one.
-  struct Load {
-    double len = 0, rows = 0, tiles[2] = {0, 0};   // of kTilePosSmall and kTilePosLarge
-  };
-  constexpr int64_t kLoads = 64;
-  auto chunk_len = [&](int32_t s) { return int64_t(seqs[s].cached_len) + (seqs[s].n_query + 1) / 2 - own[size_t(s)]; };
-  int64_t longest = 0, longest_run = 0;
-  for (const SharedRun& r : runs) longest_run = std::max(longest_run, r.len);
-  longest = longest_run;
-  for (int32_t s = 0; s < n_seqs; ++s)
-    if (seqs[s].n_query > 1) longest = std::max(longest, chunk_len(s));
-  std::vector<Load> loads;
-  {
-    const int64_t step = std::max<int64_t>(kPrefillBlock, longest / kLoads + 1);
-    std::vector<Load> by_len(size_t(longest / step) + 1);
-    auto put = [&](int64_t rows, int64_t len) {
-      Load& l = by_len[size_t(len / step)];
-      l.len += double(len) * double(rows);
-      l.rows += double(rows);
-      l.tiles[0] += double(ceil_div(rows, kTilePosSmall));
-      l.tiles[1] += double(ceil_div(rows, kTilePosLarge));
-    };
-    for (const SharedRun& r : runs) put(r.rows, r.len);
-    for (int32_t s = 0; s < n_seqs; ++s)
-      if (seqs[s].n_query > 1) put(seqs[s].n_query, chunk_len(s));
-    for (Load& l : by_len)
-      if (l.rows > 0) {
-        l.len /= l.rows;
-        loads.push_back(l);
-      }
-  }
-  // Their pieces.
-  struct Tiles {
-    int32_t tile;
-    int64_t most;
-    std::vector<Lot> items;
-    double n = 0, keys = 0, slots = 0, splits = 0;
-  };
-  std::vector<Tiles> tiles;
+  std::vector<TilePieces> tiles;
   for (int32_t tile : {kTilePosSmall, kTilePosLarge}) {
     if (opts.tile_pos != 0 && opts.tile_pos != tile) continue;
-    for (int64_t p : kPrefill) {
-      if (opts.prefill_split > 0 && p != kPrefill[0]) break;
-      Tiles t{tile, opts.prefill_split > 0 ? up(opts.prefill_split, kPrefillBlock) : p, {}};
-      for (const Load& l : loads) {
-        const double n = std::max(1.0, std::ceil(l.len / double(t.most))), items = l.tiles[tile == kTilePosLarge] * n;
-        add(t.items, l.len / n, items);
-        t.n += items;
-        t.keys += items * l.len / n;
-        t.slots += l.rows * n * kGroup;
-      }
-      t.splits = double(ceil_div(longest_run, t.most));
-      std::sort(t.items.begin(), t.items.end(), longest_first);
-      tiles.push_back(std::move(t));
-    }
+    if (opts.prefill_split > 0)
+      tiles.push_back(tile_pieces(loads, tile, up(opts.prefill_split, kPrefillBlock), false));
+    else
+      for (int64_t most : kPrefill) tiles.push_back(tile_pieces(loads, tile, most, false));
   }
 
-  // Every combination's lower bound (no slot idle); then, from the lowest on, the time with
-  // idle slots, until no bound is below the best time.
-  struct Option {
-    const Tiles* t;
-    const Decode* d;
-    bool pack;
-    double bound, rest, memory;   // rest: what depends on neither the slots nor memory
-  };
-  std::vector<Option> options;
-  auto waves = [](const Tiles& t) { return t.tile == kTilePosSmall ? 4.0 : 8.0; };
-  auto slots_of = [&](const Tiles& t) { return double(num_cus) * (t.tile == kTilePosSmall ? 2 : 1); };
-  auto per_key = [&](const Tiles& t, const SharedCost& c) {
-    return c.key + (c.key_full - c.key) * std::min(1.0, t.n * hkv / slots_of(t));
-  };
-  for (const Tiles& t : tiles) {
-    const SharedCost& c = t.tile == kTilePosSmall ? kShared16 : kShared32;
-    for (const Decode& d : decode)
-      for (const bool pack : {false, true}) {
-        if (pack && d.n_rows == 0) continue;
-        double work = t.n * c.item + t.keys * per_key(t, c), n = t.n + d.n_items;
-        for (const Lot& l : d.items) work += l.count * (c.decode_item + c.decode_key * l.keys);
-        for (const Lot& l : d.rows)
-          work += pack ? l.count / waves(t) * (c.row + c.row_key * l.keys) : l.count * (c.decode_item + c.decode_key * l.keys);
-        n += pack ? d.n_rows / waves(t) : d.n_rows;
-        const double memory = hkv * d.keys * 4.0 * kHeadDim / ((n * hkv <= num_cus ? c.tbs : c.tbs_many) * 1e6) +
-                              hkv * (d.n_items + (pack ? 0 : d.n_rows)) * c.decode_slot / slots_of(t);
-        const double rest = c.fixed + c.mb * hkv * (t.slots + d.slots) * (kHeadDim + 2) * 4e-6 + c.split * (t.splits + d.splits);
-        const double one = t.items.empty() ? 0 : c.item + per_key(t, c) * t.items[0].keys;
-        options.push_back(Option{&t, &d, pack, rest + together(std::max(work * hkv / slots_of(t), one), memory, c.power),
-                                 rest, memory});
-      }
+  // With chunks in the groups, the plan apart by the same model: a few tiles saved may not be
+  // worth the partials of every row (128 requests of 17 rows behind 512 keys 46 us, apart 32).
+  double apart_us = std::numeric_limits<double>::infinity();
+  const bool chunks = std::any_of(runs.begin(), runs.end(), [](const SharedRun& r) { return r.rows > r.end_seq - r.first_seq; });
+  if (chunks && opts.prefill_split <= 0) {
+    const PlainCut cut = plain_cut(seqs, n_seqs, hkv, num_cus, opts);
+    const StepLoads all = loads_of(seqs, n_seqs, {}, std::vector<int32_t>(size_t(n_seqs), 0));
+    const TilePieces t = tile_pieces(all, cut.tile, cut.prefill, true);
+    const DecodePieces d = decode_pieces(all, cut.decode);
+    apart_us = time_of(option_of(t, d, false, hkv, num_cus), hkv, num_cus);
   }
+
+  // Every combination's lower bound; then, from the lowest on, the time with idle slots,
+  // until no bound is below the best time.
+  std::vector<Option> options;
+  for (const TilePieces& t : tiles)
+    for (const DecodePieces& d : decode)
+      for (const bool pack : {false, true})
+        if (!pack || d.n_rows > 0) options.push_back(option_of(t, d, pack, hkv, num_cus));
   std::sort(options.begin(), options.end(), [](const Option& x, const Option& y) { return x.bound < y.bound; });
   double best_us = 0;
   for (const Option& o : options) {
     if (best.tile != 0 && o.bound >= best_us) break;
-    const SharedCost& c = o.t->tile == kTilePosSmall ? kShared16 : kShared32;
-    const double key = per_key(*o.t, c);
-    // lots in launch order, as their times: tiles and decode items, longest first, then the rows
-    std::vector<Lot> lots;
-    for (const Lot& l : o.t->items) lots.push_back(Lot{c.item + key * l.keys, l.count * hkv});
-    for (const Lot& l : o.d->items) lots.push_back(Lot{c.decode_item + c.decode_key * l.keys, l.count * hkv});
-    if (!o.pack)
-      for (const Lot& l : o.d->rows) lots.push_back(Lot{c.decode_item + c.decode_key * l.keys, l.count * hkv});
-    std::sort(lots.begin(), lots.end(), longest_first);
-    if (o.pack)
-      for (const Lot& l : o.d->rows) lots.push_back(Lot{c.row + c.row_key * l.keys, l.count * hkv / waves(*o.t)});
-    const double us = o.rest + together(last_end(lots, slots_of(*o.t)), o.memory, c.power);
+    if (o.bound >= apart_us) break;
+    const double us = time_of(o, hkv, num_cus);
     if (best.tile == 0 || us < best_us) {
       best_us = us;
       best.tile = o.t->tile;
@@ -411,6 +522,7 @@ SharedCut choose_shared(const ppas_seq* seqs, int32_t n_seqs, int hkv, int num_c
       best.row_keys = o.pack ? kRowKeys : 0;
     }
   }
+  if (best_us >= apart_us) best.tile = 0;
   return best;
 }
 
@@ -440,7 +552,7 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
     for (int32_t s = p.first_seq; s < end;) {
       int32_t e = s;
       while (e < end && seqs[e].n_query <= kShareMaxRows) ++e;
-      if (e - s > 1) {
+      if (e - s > 1 && (opts.prefill_split > 0 || saves_tiles(seqs, s, e))) {
         const int32_t row0 = seqs[s].query_start;
         runs.push_back(SharedRun{p.first_seq, s, e, row0, seqs[e - 1].query_start + seqs[e - 1].n_query - row0, len, {}});
         for (int32_t i = s; i < e; ++i) own[size_t(i)] = len;
@@ -458,57 +570,12 @@ void make_plan(const ppas_shape& shape, const ppas_seq* seqs, int32_t n_seqs, in
     }
   }
 
-  // Total work, to size the key splits so that the launch has several
-  // workgroups per compute unit: keys summed over prefill tiles (of either
-  // size) and over decode rows.
-  auto prefill_keys_for = [&](int32_t tile) {
-    int64_t keys = 0;
-    for (int32_t s = 0; s < n_seqs; ++s) {
-      const ppas_seq& q = seqs[s];
-      if (q.n_query == 1) continue;
-      for (int32_t t0 = 0; t0 < q.n_query; t0 += tile)
-        keys += int64_t(q.cached_len) + std::min(q.n_query, t0 + tile) - own[size_t(s)];
-    }
-    for (const SharedRun& r : runs) keys += ceil_div(r.rows, tile) * r.len;
-    return keys * hkv;
-  };
-  int64_t decode_keys = 0, large_tiles = 0;
-  for (int32_t s = 0; s < n_seqs; ++s) {
-    const ppas_seq& q = seqs[s];
-    if (q.n_query == 1)
-      decode_keys += int64_t(q.cached_len + 1 - own[size_t(s)]) * hkv;
-    else
-      large_tiles += ceil_div(q.n_query, kTilePosLarge) * hkv;
-  }
-
-  // Tile shape. The eight-wave kernel stages each K/V block once for 256 rows
-  // instead of 128, which pays when the step's prefill alone fills the chip with
-  // 32-position tiles (two per CU before any key split) and decode rows are a
-  // small share of the work (a workgroup then holds a whole CU, so a prefill
-  // tile no longer shares its CU with a decode item).
-  int32_t tile = cut.tile ? cut.tile : opts.tile_pos;
-  if (tile != kTilePosSmall && tile != kTilePosLarge) {
-    const int64_t small_keys = prefill_keys_for(kTilePosSmall);
-    const bool big = large_tiles >= int64_t(2) * num_cus;
-    const bool few_decodes = double(decode_keys) * 2.0 < kLargeTileDecodeShare * double(small_keys);
-    tile = (big && few_decodes) ? kTilePosLarge : kTilePosSmall;
-  }
+  PlainCut plain;
+  if (!cut.tile) plain = plain_cut(seqs, n_seqs, hkv, num_cus, opts);
+  const int32_t tile = cut.tile ? cut.tile : plain.tile;
+  const int64_t ksp = cut.tile ? cut.prefill : plain.prefill, ksd = cut.tile ? cut.decode : plain.decode;
+  const int64_t prefill_keys = plain.prefill_keys, decode_keys = plain.decode_keys;
   plan.tile_pos = tile;
-  const int64_t prefill_keys = prefill_keys_for(tile);
-
-  int64_t ksp = cut.tile ? cut.prefill : opts.prefill_split;
-  if (ksp <= 0) {
-    const int64_t target = int64_t(PPAS_PREFILL_ITEMS_PER_CU) * num_cus;
-    ksp = std::max<int64_t>(256, ceil_div(prefill_keys, target));
-  }
-  ksp = std::max<int64_t>(kPrefillBlock, ceil_div(ksp, kPrefillBlock) * kPrefillBlock);
-  int64_t ksd = cut.tile ? cut.decode : opts.decode_split;
-  if (ksd <= 0) {
-    const int64_t target = int64_t(2) * num_cus;
-    ksd = std::min<int64_t>(8192, std::max<int64_t>(512, ceil_div(decode_keys, target)));
-  }
-  ksd = std::max<int64_t>(kDecodeBlock, ceil_div(ksd, kDecodeBlock) * kDecodeBlock);
-  ksd = std::min<int64_t>(ksd, kDecodeMaxKeys);
 
   // Prefill tiles load the matrix cores and decode items the memory system. When
   // the decode work is comparable to the prefill work, the two kinds are

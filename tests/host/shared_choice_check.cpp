@@ -1,5 +1,5 @@
 // Host-side check of the choice that a step with shared prefixes is planned by, built by
-// tests/test_shared_choice_cpu.py with optimisation: what it costs. Prints "ok" and returns 0.
+// tests/test_shared_choice_cpu.py with optimisation: what it costs, and where it shares. Prints "ok" and returns 0.
 #include <algorithm>
 #include <chrono>
 #include <cstdint>
@@ -60,9 +60,45 @@ void check_time(int requests, int rows) {
   }
 }
 
+Step group(int requests, int rows, int prefix, int own) {
+  Step s;
+  for (int i = 0; i < requests; ++i) s.add(rows, prefix + own * (i % 3));
+  s.prefixes = {ppas_prefix{0, requests, prefix}};
+  return s;
+}
+
+bool same_plan(const Step& s) {
+  const Plan a = plan_of(s, false), b = plan_of(s, true);
+  return a.items.size() == b.items.size() && a.part_slots == b.part_slots && a.combine.size() == b.combine.size() &&
+         a.tile_pos == b.tile_pos && b.rows.empty();
+}
+
+void check_shares(int requests, int rows, int prefix, bool want) {
+  for (int own : {0, 50}) {
+    if (same_plan(group(requests, rows, prefix, own)) != want) continue;
+    std::fprintf(stderr, "%d requests of %d rows behind %d: %s\n", requests, rows, prefix, want ? "apart" : "shared");
+    ++g_failures;
+  }
+}
+
 }  // namespace
 
 int main() {
+  // whole tiles of rows share their keys already: together they are as many tiles
+  for (int requests : {2, 4, 8, 16, 64, 128})
+    for (int rows : {16, 32, 48, 64})
+      for (int prefix : {512, 1024, 2048, 4096, 8192}) check_shares(requests, rows, prefix, false);
+  // a few tiles saved, and the partials of every row for it
+  check_shares(128, 17, 512, false);
+  check_shares(128, 33, 512, false);
+  check_shares(128, 17, 1024, false);
+  check_shares(64, 33, 1024, false);
+  // many saved
+  check_shares(64, 1, 8192, true);
+  check_shares(256, 1, 24576, true);
+  check_shares(64, 2, 8192, true);
+  check_shares(128, 8, 8192, true);
+  check_shares(64, 33, 16384, true);
   check_time(256, 2);
   check_time(1024, 2);
   check_time(2048, 33);
