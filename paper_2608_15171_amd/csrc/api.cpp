@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "device.h"
+#include "list_pool.h"
 #include "plan.h"
 #include "ppas.h"
 #include "rope.h"
@@ -104,32 +105,24 @@ hipEvent_t ev_of(const ppas_events* ev, int which) {
 // handed out again only after every launch that read it has completed (an event
 // is recorded behind those launches, one per stream).
 // ---------------------------------------------------------------------------
-struct Pinned {
+struct Pinned : ListBuffer<hipStream_t, hipEvent_t> {
   void* host = nullptr;
   char* dev = nullptr;      // the same memory as the device addresses it
-  size_t cap = 0;
-  bool in_use = false;
-  bool settled = true;      // every recorded use is known to have completed
-  std::vector<std::pair<hipStream_t, hipEvent_t>> uses;
 };
 
 constexpr size_t kPoolMax = 64;   // buffers kept; beyond that a call reuses a released one
 std::mutex g_pool_mu;
 std::vector<Pinned*> g_pool;
 
-bool idle(Pinned& b) {
-  if (b.settled) return true;
-  for (const auto& u : b.uses) {
-    const hipError_t e = hipEventQuery(u.second);
-    if (e == hipErrorNotReady) return false;
-    if (e != hipSuccess) (void)hipGetLastError();
-  }
-  b.settled = true;
+bool completed(hipEvent_t ev) {
+  const hipError_t e = hipEventQuery(ev);
+  if (e == hipErrorNotReady) return false;
+  if (e != hipSuccess) (void)hipGetLastError();
   return true;
 }
 
 void drop_events(Pinned& b) {
-  for (auto& u : b.uses) (void)hipEventDestroy(u.second);
+  for (auto& u : b.uses) (void)hipEventDestroy(u.event);
   b.uses.clear();
 }
 
@@ -159,31 +152,20 @@ ppas_status grow(Pinned& b, size_t bytes) {
 // A buffer of at least `bytes`, marked in use.
 ppas_status acquire(size_t bytes, Pinned*& out) {
   std::lock_guard<std::mutex> lk(g_pool_mu);
-  Pinned* pick = nullptr;
-  // The smallest idle buffer that fits. The pool is in the order of release, and an event's
-  // query takes about 0.3 us: where the oldest buffers' launches are still running, the
-  // others' are too, and the search ends.
-  int busy = 0;
-  for (Pinned* b : g_pool) {
-    if (b->in_use || b->cap < bytes || (pick && b->cap >= pick->cap)) continue;
-    if (idle(*b)) pick = b;
-    else if (++busy == 4) break;
-  }
+  Pinned* pick = idle_buffer(g_pool, bytes, completed);
   if (!pick && g_pool.size() < kPoolMax) {
     pick = new (std::nothrow) Pinned;
     if (!pick) return PPAS_EHIP;
     g_pool.push_back(pick);
   }
-  if (!pick)   // the pool is full: an idle buffer that is too small, grown
-    for (Pinned* b : g_pool)
-      if (!b->in_use && idle(*b)) pick = b;
+  if (!pick) pick = any_idle_buffer(g_pool, bytes, completed);   // the pool is full: a small one is grown
   if (!pick) {  // else wait for a released buffer whose launches are still running
-    for (Pinned* b : g_pool)
-      if (!b->in_use) pick = b;
+    pick = oldest_buffer(g_pool);
     if (pick) {
-      for (auto& u : pick->uses)
-        if (hipEventSynchronize(u.second) != hipSuccess) return PPAS_EHIP;
-      pick->settled = true;
+      for (auto& u : pick->uses) {
+        if (u.pending && hipEventSynchronize(u.event) != hipSuccess) return PPAS_EHIP;
+        u.pending = false;
+      }
     }
   }
   if (!pick) {  // every buffer belongs to a live plan: the pool grows past its cap
@@ -203,21 +185,20 @@ ppas_status acquire(size_t bytes, Pinned*& out) {
 // Without the event the stream is drained, so the buffer is never reused early.
 bool note_use(Pinned* b, hipStream_t stream) {
   std::lock_guard<std::mutex> lk(g_pool_mu);
-  hipEvent_t ev = nullptr;
-  for (auto& u : b->uses)
-    if (u.first == stream) ev = u.second;
-  if (!ev) {
+  auto use = std::find_if(b->uses.begin(), b->uses.end(), [&](const auto& u) { return u.stream == stream; });
+  if (use == b->uses.end()) {
+    hipEvent_t ev = nullptr;
     if (hipEventCreateWithFlags(&ev, hipEventDisableTiming) != hipSuccess) {
       (void)hipStreamSynchronize(stream);
       return false;
     }
-    b->uses.emplace_back(stream, ev);
+    use = b->uses.insert(b->uses.end(), {stream, ev, false});
   }
-  if (hipEventRecord(ev, stream) != hipSuccess) {
+  if (hipEventRecord(use->event, stream) != hipSuccess) {
     (void)hipStreamSynchronize(stream);
     return false;
   }
-  b->settled = false;
+  use->pending = true;
   return true;
 }
 
