@@ -207,6 +207,14 @@ def _dev(t, name):
     return t.data_ptr()
 
 
+# bf16 rows: as such, or as their bit patterns
+_BF16 = (torch.bfloat16, torch.int16, torch.uint16) if torch is not None else ()
+
+
+def _is_table(t) -> bool:
+    return t.dim() == 2 and t.element_size() == 4 and not t.is_floating_point()
+
+
 def _rows(d) -> int:
     # plain integers up to where numpy's fixed cost of four small operations is made up:
     # 1 us against 7 at one request, even at about 100
@@ -241,7 +249,7 @@ def _check_buffers(shape: Shape, d, q=None, out=None, k_new=None, v_new=None, k_
     _need(k_pages, "k_pages", pool)
     _need(v_pages, "v_pages", pool)
     if bt_dev is not None:
-        if bt_dev.element_size() != 4 or bt_dev.dim() != 2:
+        if not _is_table(bt_dev):
             raise ValueError("block_table must be an int32 [n_seqs, stride] device tensor")
         if bt_dev.shape[0] < len(d):
             raise ValueError(f"block_table has {bt_dev.shape[0]} rows for {len(d)} requests")
@@ -322,13 +330,13 @@ def rope_frequencies(rope: Rope, head_dim: int = 128) -> np.ndarray:
     return out[:int(rope.rotary_dim) // 2]
 
 
-def _heads(t, name, elem: int = 2):
+def _heads(t, name):
     """A device tensor [rows, heads, features] of packed heads (any row stride):
     its data pointer and row stride."""
+    if t.dim() != 3 or t.dtype not in _BF16:
+        raise ValueError(f"{name} must be [rows, heads, features] of bf16, got {tuple(t.shape)} {t.dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.dim() != 3 or t.element_size() != elem:
-        raise ValueError(f"{name} must be [rows, heads, features] of {elem}-byte elements, got {tuple(t.shape)} {t.dtype}")
     n, h, d = t.shape
     row, head, one = t.stride()
     if (one != 1 and d > 1) or (head != d and h > 1):
@@ -343,7 +351,7 @@ def rope_rows(rope: Rope, x, positions, y, transposed: bool = False, events: Eve
     yp, ys = (xp, xs) if y is x else _heads(y, "y")
     if x.shape != y.shape or positions.dim() != 1 or positions.shape[0] != x.shape[0]:
         raise ValueError(f"shapes x {tuple(x.shape)}, y {tuple(y.shape)}, positions {tuple(positions.shape)} do not match")
-    if positions.element_size() != 4 or positions.is_floating_point():
+    if positions.dtype != torch.int32:
         raise ValueError("positions must be int32")
     n, h, d = x.shape
     pp = _dev(positions, "positions")
@@ -371,9 +379,10 @@ def _qkv(q, k, v, rows: int, hq: int, hkv: int, dim: int) -> Qkv:
 
 
 def _buffer(t, name, nbytes: int):
-    """_need and _dev in one: the pointer of a contiguous device buffer of 2-byte elements."""
-    size = t.element_size()
-    if size != 2 or t.numel() * size < nbytes or not t.is_cuda or not t.is_contiguous():
+    """_need and _dev in one: the pointer of a contiguous device buffer of bf16."""
+    if t.dtype not in _BF16:
+        raise ValueError(f"{name} must be bf16, got {t.dtype}")
+    if t.numel() * 2 < nbytes or not t.is_cuda or not t.is_contiguous():
         _need(t, name, nbytes)
         _dev(t, name)
     return t.data_ptr()
@@ -386,9 +395,11 @@ def rope_qkv_append(shape: Shape, rope: Rope, q, k_pages, v_pages, q_new, k_new,
     d = _desc(desc)
     bt = _bt_host(bt_host, bt_dev)
     rows = _rows(d)
-    _check_buffers(shape, d, q=q, k_pages=k_pages, v_pages=v_pages, bt_dev=bt_dev, rows=rows)
+    _check_buffers(shape, d, bt_dev=bt_dev)
     x = _qkv(q_new, k_new, v_new, rows, shape.n_q_heads, shape.n_kv_heads, shape.head_dim)
-    ptrs = [_dev(t, n) for t, n in ((q, "q"), (k_pages, "k_pages"), (v_pages, "v_pages"), (bt_dev, "block_table"))]
+    pool = int(shape.num_pages) * shape.n_kv_heads * shape.page_size * shape.head_dim * 2 if len(d) else 0
+    ptrs = (_buffer(q, "q", rows * shape.n_q_heads * shape.head_dim * 2), _buffer(k_pages, "k_pages", pool),
+            _buffer(v_pages, "v_pages", pool), _dev(bt_dev, "block_table"))
     hs = _here(stream, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev)
     st = _lib.ppas_rope_qkv_append(ctypes.byref(shape), ctypes.byref(rope), ctypes.byref(x), *ptrs[:3], _host_ptr(d),
                                    len(d), ptrs[3], bt_dev.shape[1], _host_ptr(bt), hs)
@@ -417,7 +428,7 @@ def attn_step_shared(shape: Shape, out, q, k_pages, v_pages, desc, prefixes, bt_
     """attn_step for a step whose requests share prefixes: rows (first request, requests, shared positions)."""
     d, p = _desc(desc), _prefixes(prefixes)
     bt = _bt_host(bt_host, bt_dev)
-    if len(d) == 0 or bt_dev.element_size() != 4 or bt_dev.dim() != 2 or bt_dev.shape[0] < len(d):
+    if len(d) == 0 or not _is_table(bt_dev) or bt_dev.shape[0] < len(d):
         _check_buffers(shape, d, bt_dev=bt_dev)
         rows, pool = 0, 0
     else:
@@ -522,11 +533,12 @@ def gateup_act(x, w, y, workspace=None, events: Events | None = None, stream=Non
 def quant_i8(x, xq, scale, events: Events | None = None, stream=None) -> None:
     """The rows of x [R, H] (bf16, any row stride) as 8-bit integers xq [R, H] (int8) and a scale each (fp32 [R]):
     token rows of activations, or output channels of weights."""
-    if x.dim() != 2 or x.element_size() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
-        raise ValueError("x must be a 2-D bf16 tensor of packed rows")
+    if x.dim() != 2 or x.dtype not in _BF16 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"x must be a 2-D bf16 tensor of packed rows, got {tuple(x.shape)} {x.dtype}")
     R, H = x.shape
-    if tuple(xq.shape) != (R, H) or xq.element_size() != 1 or tuple(scale.shape) != (R,) or scale.element_size() != 4:
-        raise ValueError(f"xq must be int8 {(R, H)} and scale fp32 {(R,)}, got {tuple(xq.shape)} {tuple(scale.shape)}")
+    if tuple(xq.shape) != (R, H) or xq.dtype != torch.int8 or tuple(scale.shape) != (R,) or scale.dtype != torch.float32:
+        raise ValueError(f"xq must be int8 {(R, H)} and scale fp32 {(R,)}, got {tuple(xq.shape)} {xq.dtype} and "
+                         f"{tuple(scale.shape)} {scale.dtype}")
     if not x.is_cuda:
         raise ValueError("x must be a device tensor")
     qp, sp = _dev(xq, "xq"), _dev(scale, "scale")
@@ -545,14 +557,13 @@ def gateup_act_i8_workspace_bytes(n_tokens: int, hidden: int, n_inter: int) -> i
 
 
 def _gateup_i8(fn, what, x, x_scale, w, w_scale, y, per, workspace, events, stream):
-    if not (x.dim() == w.dim() == y.dim() == 2 and x.element_size() == w.element_size() == 1 and y.element_size() == 2):
+    if not (x.dim() == w.dim() == y.dim() == 2 and x.dtype == w.dtype == torch.int8 and y.dtype in _BF16):
         raise ValueError(f"x and w must be 2-D int8 tensors and y a 2-D bf16 tensor, got {x.dtype}, {w.dtype}, {y.dtype}")
     T, H = x.shape
     N = w.shape[0]
     if N % per or w.shape[1] != H or tuple(y.shape) != (T, N // per):
         raise ValueError(f"shapes x {tuple(x.shape)}, w {tuple(w.shape)}, y {tuple(y.shape)} do not match")
-    if not (x_scale.numel() == T and w_scale.numel() == N and x_scale.element_size() == w_scale.element_size() == 4
-            and x_scale.is_floating_point() and w_scale.is_floating_point()):
+    if not (x_scale.numel() == T and w_scale.numel() == N and x_scale.dtype == w_scale.dtype == torch.float32):
         raise ValueError(f"x_scale must hold {T} fp32 values and w_scale {N}")
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     xp, sp, wp, vp, yp = (_dev(x, "x"), _dev(x_scale, "x_scale"), _dev(w, "w"), _dev(w_scale, "w_scale"), _dev(y, "y"))
@@ -679,7 +690,7 @@ class StepPlan:
     def rope_qkv_append(self, rope: Rope, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev,
                         events: Events | None = None, stream=None) -> None:
         bt = self._bt(bt_dev)
-        if bt.element_size() != 4 or bt.shape[0] < len(self.desc):
+        if not _is_table(bt) or bt.shape[0] < len(self.desc):
             _check_buffers(self.shape, self.desc, bt_dev=bt)
         x = _qkv(q_new, k_new, v_new, self._n_rows, *self._heads)
         ptrs = (_buffer(q, "q", self._q_bytes), _buffer(k_pages, "k_pages", self._pool_bytes),
