@@ -25,6 +25,10 @@
  *   - All device work is enqueued on `hip_stream` (a hipStream_t, NULL = the
  *     null stream) and the call returns without synchronising the host. Calls
  *     on the same stream execute in order; append before attending.
+ *   - The appends and attention calls, planned or not, read a step's lists, which
+ *     return to that pool: on a stream that captures a HIP graph they are
+ *     PPAS_EUNSUPPORTED and leave the capture as it was. The other calls, and
+ *     ppas_attn_step_noalloc, can be captured.
  *   - Every argument is validated on the host before anything is enqueued; a
  *     failed validation enqueues nothing. No C++ exception crosses the ABI.
  *   - Compiled shapes: head_dim 128, page_size 16, n_q_heads / n_kv_heads == 8
@@ -66,7 +70,8 @@ typedef enum ppas_status {
   PPAS_ENOSPACE = -3,      /* workspace smaller than ppas_attn_workspace_bytes(), or a step too large
                                for the fixed array of ppas_attn_step_noalloc */
   PPAS_EHIP = -4,          /* a HIP runtime call or kernel launch failed */
-  PPAS_EUNSUPPORTED = -5   /* shape outside the compiled set, or no gfx950 device */
+  PPAS_EUNSUPPORTED = -5   /* shape outside the compiled set, no gfx950 device, or a capturing stream
+                               where the call reads a step's lists */
 } ppas_status;
 
 typedef struct ppas_shape {
@@ -265,9 +270,7 @@ typedef struct ppas_qkv {
  * be rows->q where q_stride is n_q_heads * 128 (in place); otherwise it must not overlap
  * the rows (PPAS_EINVAL, as for strides below a row's features or pools off 16 bytes).
  * Validation, ownership, streams and errors otherwise as ppas_rope_kv_append
- * (PPAS_ERANGE from 2^24 touched pages on). The page-write list is staged per call or
- * plan, so a call on a stream that captures a HIP graph is PPAS_EUNSUPPORTED, planned or
- * not.
+ * (PPAS_ERANGE from 2^24 touched pages on).
  */
 ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope, const ppas_qkv* rows, void* q_out,
                                  void* k_pages, void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
@@ -311,9 +314,9 @@ size_t ppas_attn_workspace_bytes(const ppas_shape* shape, const ppas_seq* seqs, 
  * by the caller, not read before being written; it must not be used by another
  * call still in flight. The work list travels in pinned host memory from a pool
  * the library owns, read by the kernels directly; a buffer of the pool is
- * reused only after the launches that read it have completed. Because the work
- * list is staged per call, a call cannot be captured into a HIP graph and
- * replayed. Calls from several threads or on several streams are safe (each
+ * reused only after the launches that read it have completed; a replay would
+ * read it later, so a call on a stream that captures a HIP graph is
+ * PPAS_EUNSUPPORTED (ppas_attn_step_noalloc can be captured). Calls from several threads or on several streams are safe (each
  * with its own workspace). Equivalent to creating a step plan with default
  * options, ppas_attn_step_planned, and destroying the plan.
  * Returns PPAS_OK, a validation status, PPAS_ENOSPACE or PPAS_EHIP.
@@ -371,8 +374,7 @@ ppas_status ppas_step_plan_create_shared(const ppas_shape* shape, const ppas_seq
 
 /* As ppas_attn_step and ppas_attn_workspace_bytes, for a step with shared prefixes:
  * equivalent to ppas_step_plan_create_shared with default options,
- * ppas_attn_step_planned, and destroying the plan. With prefixes, a call on a stream
- * that captures a HIP graph is PPAS_EUNSUPPORTED. */
+ * ppas_attn_step_planned, and destroying the plan. */
 ppas_status ppas_attn_step_shared(const ppas_shape* shape, void* out, const void* q,
                                   const void* k_pages, const void* v_pages,
                                   const ppas_seq* seqs, int32_t n_seqs,

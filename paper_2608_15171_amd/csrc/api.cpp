@@ -287,6 +287,19 @@ ppas_status build_plan(ppas_step_plan& p, const ppas_shape* shape, const ppas_se
   return PPAS_OK;
 }
 
+// Lists in host memory are staged per call or plan and reused once its launches have
+// ended, which a graph's replays would read again: every call that reads one refuses a
+// capturing stream, and does so before it asks the pool for a buffer (an allocation would
+// end the capture). The appends refuse it also where few requests' list is in the arguments.
+bool capturing(void* hip_stream) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(static_cast<hipStream_t>(hip_stream), &st) != hipSuccess) {
+    (void)hipGetLastError();
+    return false;
+  }
+  return st != hipStreamCaptureStatusNone;
+}
+
 ppas_status run_append(const ppas_step_plan& p, bool rope, float theta, void* q, void* k_pages, void* v_pages,
                        const void* k_new, const void* v_new, const int32_t* bt_dev, const ppas_events* ev,
                        void* hip_stream) {
@@ -309,17 +322,6 @@ ppas_status run_append(const ppas_step_plan& p, bool rope, float theta, void* q,
   // after a failed launch: a kernel that did start may still read it)
   const bool noted = note_use(p.buf, stream);
   return (e == hipSuccess && noted) ? PPAS_OK : PPAS_EHIP;
-}
-
-// Lists in host memory are staged per call or plan and reused once its launches have
-// ended, which a graph's replays would read again.
-bool capturing(hipStream_t stream) {
-  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(stream, &st) != hipSuccess) {
-    (void)hipGetLastError();
-    return false;
-  }
-  return st != hipStreamCaptureStatusNone;
 }
 
 // Bytes that T rows of `row` elements, `stride` apart, span.
@@ -361,7 +363,6 @@ ppas_status run_qkv_append(const ppas_step_plan& p, const RopeTable& table, cons
   if (p.n_append == 0 || (p.n_desc == 0 && !p.buf)) return PPAS_EINVAL;   // a plan made without the page-write list
   if (p.n_append > kAppendMaxItems) return PPAS_ERANGE;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  if (capturing(stream)) return PPAS_EUNSUPPORTED;
   RopeAppend r;
   r.q = static_cast<const uint16_t*>(rows.q);
   r.k = static_cast<const uint16_t*>(rows.k);
@@ -533,6 +534,7 @@ ppas_status ppas_kv_append_planned(const ppas_step_plan* plan, void* k_pages, vo
   const ppas_status st = check_events(events);
   if (st != PPAS_OK) return st;
   try {
+    if (plan->n_seqs > 0 && capturing(hip_stream)) return PPAS_EUNSUPPORTED;
     return run_append(*plan, false, 0.f, nullptr, k_pages, v_pages, k_new, v_new, block_table_dev, events,
                       hip_stream);
   } catch (...) {
@@ -549,6 +551,7 @@ ppas_status ppas_rope_kv_append_planned(const ppas_step_plan* plan, float rope_t
   const ppas_status st = check_events(events);
   if (st != PPAS_OK) return st;
   try {
+    if (plan->n_seqs > 0 && capturing(hip_stream)) return PPAS_EUNSUPPORTED;
     return run_append(*plan, true, rope_theta, q, k_pages, v_pages, k_new, v_new, block_table_dev, events,
                       hip_stream);
   } catch (...) {
@@ -567,6 +570,7 @@ ppas_status ppas_rope_qkv_append_planned(const ppas_step_plan* plan, const ppas_
     if (plan->n_seqs == 0) return rope_table(rope, kHeadDim, table);
     st = check_qkv(plan->shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, plan->n_rows, table);
     if (st != PPAS_OK) return st;
+    if (capturing(hip_stream)) return PPAS_EUNSUPPORTED;
     return run_qkv_append(*plan, table, *rows, q_out, k_pages, v_pages, block_table_dev, events, hip_stream);
   } catch (...) {
     return PPAS_EINVAL;
@@ -580,6 +584,7 @@ ppas_status ppas_attn_step_planned(const ppas_step_plan* plan, void* out, const 
   const ppas_status st = check_events(events);
   if (st != PPAS_OK) return st;
   try {
+    if (plan->n_seqs > 0 && capturing(hip_stream)) return PPAS_EUNSUPPORTED;
     return run_attn(*plan, out, q, k_pages, v_pages, block_table_dev, workspace, workspace_bytes, events,
                     hip_stream);
   } catch (...) {
@@ -814,6 +819,7 @@ ppas_status ppas_kv_append(const ppas_shape* shape, void* k_pages, void* v_pages
     if (st != PPAS_OK) return st;
     if (n_seqs == 0) return PPAS_OK;
     if (!k_pages || !v_pages || !k_new || !v_new || !block_table_dev) return PPAS_EINVAL;
+    if (capturing(hip_stream)) return PPAS_EUNSUPPORTED;
     // validated above; build only the page-write list
     st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantAppend, false);
     if (st == PPAS_OK) st = run_append(p, false, 0.f, nullptr, k_pages, v_pages, k_new, v_new, block_table_dev,
@@ -837,6 +843,7 @@ ppas_status ppas_rope_kv_append(const ppas_shape* shape, float rope_theta, void*
     if (st != PPAS_OK) return st;
     if (n_seqs == 0) return PPAS_OK;
     if (!q || !k_pages || !v_pages || !k_new || !v_new || !block_table_dev) return PPAS_EINVAL;
+    if (capturing(hip_stream)) return PPAS_EUNSUPPORTED;
     st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantAppend, false);
     if (st == PPAS_OK) st = run_append(p, true, rope_theta, q, k_pages, v_pages, k_new, v_new, block_table_dev,
                                        nullptr, hip_stream);
@@ -900,6 +907,7 @@ ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope,
     const int64_t T = int64_t(seqs[n_seqs - 1].query_start) + seqs[n_seqs - 1].n_query;
     st = check_qkv(*shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, T, table);
     if (st != PPAS_OK) return st;
+    if (capturing(hip_stream)) return PPAS_EUNSUPPORTED;
     // validated above; build only the page-write list
     st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantInline, false);
     if (st == PPAS_OK)
@@ -947,7 +955,7 @@ ppas_status ppas_attn_step_shared(const ppas_shape* shape, void* out, const void
     if (st != PPAS_OK) return st;
     if (n_seqs == 0) return PPAS_OK;
     if (!out || !q || !k_pages || !v_pages || !block_table_dev || !workspace) return PPAS_EINVAL;
-    if (n_prefixes > 0 && capturing(static_cast<hipStream_t>(hip_stream))) return PPAS_EUNSUPPORTED;
+    if (capturing(hip_stream)) return PPAS_EUNSUPPORTED;
     // validated above
     st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantAttn, false, prefixes, n_prefixes);
     if (st == PPAS_OK)
