@@ -602,7 +602,9 @@ ppas_status ppas_stream_read(const void* buf, size_t bytes, void* sink, const pp
  * the same stream. Every call on one device shares that device's array, which
  * keeps the last call's contents (nothing in it needs to start at zero): calls
  * ordered on one stream are safe, but calls that overlap in time on one device
- * (other streams, other threads) race and give undefined results.
+ * (other streams, other threads) race and give undefined results. A call may be
+ * captured into a HIP graph, whose replays copy the list again: it stays in host
+ * memory until the process ends.
  *
  * A step whose work list and partials do not fit the array returns
  * PPAS_ENOSPACE and enqueues nothing (steps of up to ~40 MB of partials fit,

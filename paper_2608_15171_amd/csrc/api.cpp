@@ -57,6 +57,15 @@ DeviceInfo current_device() {
   return d;
 }
 
+bool capturing(void* hip_stream) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(static_cast<hipStream_t>(hip_stream), &st) != hipSuccess) {
+    (void)hipGetLastError();
+    return false;
+  }
+  return st != hipStreamCaptureStatusNone;
+}
+
 namespace {
 
 // Work-item counts and partial-slot offsets travel as int32 (and the item count
@@ -291,15 +300,6 @@ ppas_status build_plan(ppas_step_plan& p, const ppas_shape* shape, const ppas_se
 // ended, which a graph's replays would read again: every call that reads one refuses a
 // capturing stream, and does so before it asks the pool for a buffer (an allocation would
 // end the capture). The appends refuse it also where few requests' list is in the arguments.
-bool capturing(void* hip_stream) {
-  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(static_cast<hipStream_t>(hip_stream), &st) != hipSuccess) {
-    (void)hipGetLastError();
-    return false;
-  }
-  return st != hipStreamCaptureStatusNone;
-}
-
 ppas_status run_append(const ppas_step_plan& p, bool rope, float theta, void* q, void* k_pages, void* v_pages,
                        const void* k_new, const void* v_new, const int32_t* bt_dev, const ppas_events* ev,
                        void* hip_stream) {

@@ -20,6 +20,9 @@ struct DeviceInfo {
 // Without a usable device: 256 CUs, not gfx950.
 DeviceInfo current_device();
 
+// Whether the stream is being captured into a HIP graph.
+bool capturing(void* hip_stream);
+
 // The packed attention launch (of n_items items, then n_rows short decode rows) and,
 // when n_comb > 0, the split-merge launch (of items of at most comb_pos positions).
 hipError_t launch_attn_step(const uint16_t* q, uint16_t* out, const uint16_t* kp, const uint16_t* vp,

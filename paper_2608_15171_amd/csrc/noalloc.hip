@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <cstring>
 #include <mutex>
+#include <utility>
 #include <vector>
 
 #include "device.h"
@@ -46,6 +47,14 @@ ppas_status scratch_of_current_device(char** out) {
   return PPAS_OK;
 }
 
+// Host memory that stays until the process ends.
+const char* keep(std::vector<char>&& list) {
+  static std::vector<std::vector<char>>* const kept = new std::vector<std::vector<char>>;
+  std::lock_guard<std::mutex> lk(g_scratch_mu);
+  kept->push_back(std::move(list));   // a vector's elements stay where they are when it moves
+  return kept->back().data();
+}
+
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 ppas_status run(const ppas_shape* shape, void* out, const void* q, const void* k_pages, const void* v_pages,
@@ -74,8 +83,10 @@ ppas_status run(const ppas_shape* shape, void* out, const void* q, const void* k
   if (!plan.combine.empty())
     std::memcpy(list.data() + plan.off_combine, plan.combine.data(), plan.combine.size() * sizeof(CombineItem));
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  // From pageable host memory: the source has been consumed when the call returns.
-  if (hipMemcpyAsync(base, list.data(), list.size(), hipMemcpyHostToDevice, stream) != hipSuccess) {
+  // From pageable host memory: the source has been consumed when the call returns. A graph's
+  // replays copy from it again, so that a captured call's list is kept.
+  const char* src = capturing(stream) ? keep(std::move(list)) : list.data();
+  if (hipMemcpyAsync(base, src, plan.list_bytes, hipMemcpyHostToDevice, stream) != hipSuccess) {
     (void)hipGetLastError();
     return PPAS_EHIP;
   }

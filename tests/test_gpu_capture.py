@@ -1,5 +1,5 @@
 """Capture into a HIP graph: every call that reads a step's lists from the pool of pinned buffers refuses it and leaves the
-capture as it was."""
+capture as it was; the call that allocates nothing can be captured and replayed."""
 import numpy as np
 import pytest
 
@@ -76,3 +76,29 @@ def test_calls_that_read_lists_refuse_capture(lib, n):
         torch.cuda.synchronize()
     plain.close()
     shared.close()
+
+
+def test_the_call_that_allocates_nothing_is_replayed(lib):
+    """Between the replays another step's list takes the device array, and host memory as large as the list is written."""
+    ppas, step, torch = lib
+    a, b = make(lib, 7, 3000, seed=3), make(lib, 30, 500, seed=4)
+
+    def call(ds):
+        ppas.attn_step_noalloc(ds.shape, ds.out, ds.q, ds.k_pages, ds.v_pages, ds.desc, ds.bt, ds.bt_host)
+    call(a)
+    torch.cuda.synchronize()
+    want = a.out.clone()
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        call(a)
+    for k in range(4):
+        call(b)
+        torch.cuda.synchronize()
+        junk = [np.full(n, 7, np.uint8) for n in (1 << 10, 1 << 12, 1 << 14, 1 << 16) for _ in range(20)]
+        a.out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a.out.view(torch.int16), want.view(torch.int16)), k
+        del junk
