@@ -447,6 +447,15 @@ int32_t ppas_plan_items(const ppas_shape* shape, const ppas_seq* seqs, int32_t n
                         const ppas_plan_opts* opts, int32_t* items_out, int32_t capacity);
 
 /*
+ * The same of a step with shared prefixes: items whose rows belong to several requests
+ * come with their prefix's first request as seq and the prefix's used length as pos0, and
+ * behind the launch's items, with kind 2, those decode rows that one wave takes.
+ */
+int32_t ppas_plan_shared_items(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,
+                               const ppas_prefix* prefixes, int32_t n_prefixes,
+                               const ppas_plan_opts* opts, int32_t* items_out, int32_t capacity);
+
+/*
  * The fused gate-up projection of a decoder block's MLP, the other prefill
  * operation the paper profiles next to attention (Section 6.1: cumulative time
  * of eight 2k chunks against one 16k chunk, Fig. 4b; SM throughput, L2 hit rate

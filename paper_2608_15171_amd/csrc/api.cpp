@@ -436,30 +436,32 @@ ppas_status ppas_validate_step(const ppas_shape* shape, const ppas_seq* seqs, in
 
 int32_t ppas_plan_items(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs, const ppas_plan_opts* opts,
                         int32_t* items_out, int32_t capacity) {
+  return ppas_plan_shared_items(shape, seqs, n_seqs, nullptr, 0, opts, items_out, capacity);
+}
+
+int32_t ppas_plan_shared_items(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,
+                               const ppas_prefix* prefixes, int32_t n_prefixes, const ppas_plan_opts* opts,
+                               int32_t* items_out, int32_t capacity) {
   try {
     ppas_status st = check_opts(opts);
     if (st != PPAS_OK) return st;
     st = validate(shape, seqs, n_seqs, nullptr, INT32_MAX, false);
     if (st != PPAS_OK) return st;
+    st = validate_prefixes(seqs, n_seqs, nullptr, INT32_MAX, prefixes, n_prefixes);
+    if (st != PPAS_OK) return st;
     Plan plan;
-    make_plan(*shape, seqs, n_seqs, (opts && opts->num_cus > 0) ? opts->num_cus : 256, to_opts(opts), plan);
+    make_plan(*shape, seqs, n_seqs, (opts && opts->num_cus > 0) ? opts->num_cus : 256, to_opts(opts), plan, prefixes,
+              n_prefixes);
     if (!plan_fits(plan, 0)) return PPAS_ERANGE;
-    const int32_t n = int32_t(plan.items.size());
-    if (items_out) {
-      for (int32_t i = 0; i < n && i < capacity; ++i) {
-        const WorkItem& w = plan.items[size_t(i)];
-        int32_t* o = items_out + 8 * size_t(i);
-        o[0] = w.npos_kind >> 16;
-        o[1] = w.seq;
-        o[2] = w.kvh;
-        o[3] = w.row0;
-        o[4] = w.pos0;
-        o[5] = w.npos_kind & 0xffff;
-        o[6] = w.key_lo;
-        o[7] = w.key_hi;
-      }
+    const size_t n = plan.items.size() + plan.rows.size();
+    for (size_t i = 0; items_out && i < n && int64_t(i) < capacity; ++i) {
+      const bool row = i >= plan.items.size();
+      const WorkItem& w = row ? plan.rows[i - plan.items.size()] : plan.items[i];
+      const int32_t v[8] = {row ? 2 : w.npos_kind >> 16, w.seq,  w.kvh, w.row0, w.pos0, w.npos_kind & 0xffff,
+                            w.key_lo,                    w.key_hi};
+      std::copy(v, v + 8, items_out + 8 * i);
     }
-    return n;
+    return int32_t(n);
   } catch (...) {
     return PPAS_EINVAL;
   }

@@ -122,6 +122,8 @@ _lib.ppas_stream_read.restype = ctypes.c_int
 _lib.ppas_stream_read.argtypes = [_vp, _sz, _vp, _E, _vp]
 _lib.ppas_plan_items.restype = _i32
 _lib.ppas_plan_items.argtypes = [_P, _vp, _i32, _O, _vp, _i32]
+_lib.ppas_plan_shared_items.restype = _i32
+_lib.ppas_plan_shared_items.argtypes = [_P, _vp, _i32, _vp, _i32, _O, _vp, _i32]
 _lib.ppas_step_plan_create.restype = ctypes.c_int
 _lib.ppas_step_plan_create.argtypes = [_P, _vp, _i32, _vp, _i32, _O, ctypes.POINTER(ctypes.c_void_p)]
 _lib.ppas_step_plan_info.restype = ctypes.c_int
@@ -609,18 +611,20 @@ def _opts_ptr(opts):
     return None if opts is None else ctypes.byref(opts)
 
 
-def plan_items(shape: Shape, desc, num_cus: int = 256, opts: PlanOpts | None = None) -> np.ndarray:
-    """The planned work list as int32 [n, 8]: kind, seq, kv_head, row0, pos0, npos, key_lo, key_hi."""
-    d = _desc(desc)
+def plan_items(shape: Shape, desc, num_cus: int = 256, opts: PlanOpts | None = None, prefixes=None) -> np.ndarray:
+    """The planned work list as int32 [n, 8]: kind, seq, kv_head, row0, pos0, npos, key_lo, key_hi (with prefixes: see
+    ppas_plan_shared_items)."""
+    d, p = _desc(desc), _prefixes(prefixes)
     o = PlanOpts() if opts is None else PlanOpts(opts.prefill_split, opts.decode_split, opts.tile_positions,
                                                  opts.num_cus)
     if o.num_cus == 0:
         o.num_cus = int(num_cus)
-    n = _lib.ppas_plan_items(ctypes.byref(shape), _host_ptr(d), len(d), ctypes.byref(o), None, 0)
+    args = ctypes.byref(shape), _host_ptr(d), len(d), _host_ptr(p), 0 if p is None else len(p), ctypes.byref(o)
+    n = _lib.ppas_plan_shared_items(*args, None, 0)
     if n < 0:
-        raise PPASError(n, "ppas_plan_items")
+        raise PPASError(n, "ppas_plan_shared_items")
     out = np.zeros((max(n, 1), 8), dtype=np.int32)
-    _lib.ppas_plan_items(ctypes.byref(shape), _host_ptr(d), len(d), ctypes.byref(o), out.ctypes.data, n)
+    _lib.ppas_plan_shared_items(*args, out.ctypes.data, n)
     return out[:n]
 
 
