@@ -580,6 +580,15 @@ ppas_status ppas_gateup_choice(int32_t n_tokens, int32_t hidden, int32_t n_out, 
                                int32_t aligned, size_t workspace_bytes, int32_t num_cus, int32_t* choice);
 
 /*
+ * The same of an 8-bit product: 16 int32, eight for each of its launches (a reducing one
+ * apart): token rows (0: no second launch, else the call's last rows), kernel (0 tiles, 1
+ * few rows, 2 general, 3 tiles of 128 x 128), then as above from the rows of a main tile to
+ * the reduction splits.
+ */
+ppas_status ppas_gateup_i8_choice(int32_t n_tokens, int32_t hidden, int32_t n_out, int32_t activation,
+                                  int32_t aligned, size_t workspace_bytes, int32_t num_cus, int32_t* choice);
+
+/*
  * A plain streaming read of `bytes` bytes of device memory at `buf`: the
  * device's attainable HBM read rate, the measured ceiling beside the spec peak
  * for the memory-bound kernels above (the library's own measurement aid, not a

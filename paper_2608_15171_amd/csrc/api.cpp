@@ -709,6 +709,13 @@ int splits_i8(int32_t n_tokens, int32_t hidden, int32_t n_out, int cus) {
   return hidden % 128 ? 1 : gateup_splits(n_tokens, hidden / 2, n_out, cus);
 }
 
+// The most splits that the workspace holds.
+int allowed_splits_i8(int32_t n_tokens, int32_t hidden, int32_t n_out, size_t workspace_bytes, int cus) {
+  int splits = splits_i8(n_tokens, hidden, n_out, cus);
+  while (splits > 1 && gateup_workspace_bytes(n_tokens, n_out, splits) > workspace_bytes) --splits;
+  return gateup_tiles(n_tokens, n_out) * splits > INT32_MAX ? 1 : splits;
+}
+
 ppas_status gateup_i8_call(const void* x, const float* sx, const void* w, const float* sw, void* y, int32_t n_tokens,
                            int32_t hidden, int32_t n_out, bool act, void* workspace, size_t workspace_bytes,
                            const ppas_events* events, void* hip_stream) {
@@ -721,9 +728,7 @@ ppas_status gateup_i8_call(const void* x, const float* sx, const void* w, const 
   if (off(sx, 4) || off(sw, 4) || off(y, 2) || off(workspace, 16)) return PPAS_EINVAL;
   const DeviceInfo dev = current_device();
   if (!dev.gfx950) return PPAS_EUNSUPPORTED;
-  int splits = splits_i8(n_tokens, hidden, n_out, dev.cus);
-  while (splits > 1 && gateup_workspace_bytes(n_tokens, n_out, splits) > workspace_bytes) --splits;
-  if (gateup_tiles(n_tokens, n_out) * splits > INT32_MAX) splits = 1;
+  const int splits = allowed_splits_i8(n_tokens, hidden, n_out, workspace_bytes, dev.cus);
   const Int8Product p{static_cast<const int8_t*>(x), sx, static_cast<const int8_t*>(w), sw,
                       static_cast<uint16_t*>(y), n_tokens, hidden, n_out};
   const hipError_t e = launch_gateup_i8(p, act, splits, workspace, dev.cus, static_cast<hipStream_t>(hip_stream),
@@ -789,6 +794,17 @@ size_t ppas_gateup_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t 
 size_t ppas_gateup_act_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t n_inter) {
   const int32_t n_out = act_rows(n_inter);
   return n_out < 0 ? 0 : ppas_gateup_i8_workspace_bytes(n_tokens, hidden, n_out);
+}
+
+ppas_status ppas_gateup_i8_choice(int32_t n_tokens, int32_t hidden, int32_t n_out, int32_t activation, int32_t aligned,
+                                  size_t workspace_bytes, int32_t num_cus, int32_t* choice) {
+  const ppas_status st = check_gateup_i8(n_tokens, hidden, n_out, activation != 0);
+  if (st != PPAS_OK) return st;
+  if (!choice || n_tokens == 0 || num_cus < 0 || (activation && n_out % 2 != 0)) return PPAS_EINVAL;
+  const int cus = num_cus > 0 ? num_cus : 256;
+  gateup_i8_choice(n_tokens, hidden, n_out, activation != 0, aligned != 0,
+                   allowed_splits_i8(n_tokens, hidden, n_out, workspace_bytes, cus), cus, choice);
+  return PPAS_OK;
 }
 
 ppas_status ppas_stream_read(const void* buf, size_t bytes, void* sink, const ppas_events* events,

@@ -76,6 +76,8 @@ hipError_t launch_gateup_i8(const Int8Product& p, bool act, int max_splits, void
 hipError_t launch_gateup_i8_any(const Int8Product& p, bool act, hipStream_t stream, hipEvent_t ev_start,
                                 hipEvent_t ev_stop);
 int64_t gateup_i8_any_tiles(int32_t T, int32_t N2, bool act);
+// The launches that launch_gateup_i8 makes (host only), as ppas_gateup_i8_choice has them.
+void gateup_i8_choice(int32_t T, int32_t H, int32_t N2, bool act, bool aligned, int max_splits, int cus, int32_t* choice);
 // Rows of bf16 to 8-bit integers and a scale each (x_stride elements between rows).
 hipError_t launch_quant_i8(const uint16_t* x, int64_t x_stride, int8_t* xq, float* scale, int32_t T, int32_t H,
                            hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop);

@@ -70,33 +70,69 @@ hipError_t launch_rows_of(const Int8Product& p, int32_t first, int32_t T, const 
   return e != hipSuccess || c.splits == 1 ? e : launch_reduce<Int8>(a, act, c.splits, stream, ev_stop);
 }
 
+// A call's launches: its token rows in one, or the last ones in another one.
+struct Ways {
+  Way first, last;
+  int32_t last_rows = 0;
+  bool general = false;
+};
+
+// The rows past the last whole 64 in a launch of their own, where they would make a
+// round of tiles for themselves (the sums are the same): 2,056 tokens x 11,008 x 2,048,
+// a chunk with eight decode rows, with the quantiser 73 us instead of 78 (65 with the
+// tiles of 128 x 128).
+Ways choose_ways(const Int8Product& p, bool act, bool aligned, int max_splits, int cus) {
+  Ways r;
+  // whole 128-byte stages of 16-byte aligned rows, and at least two of them (the scales'
+  // transfer); anything else in the general kernel
+  r.general = !aligned || p.H % (2 * kBK) != 0 || p.H <= 2 * kBK;
+  if (r.general) return r;
+  r.first = choose_way(p.T, p, act, max_splits, cus);
+  r.general = r.first.c.kernel == GateupChoice::kGeneral;
+  const int32_t tail = p.T % kTailBM, main = p.T - tail;
+  if (r.first.c.kernel != GateupChoice::kTiles || tail == 0 || main == 0) return r;
+  // both parts' partial sums fit where the whole call's do
+  const Way m = choose_way(main, p, act, max_splits, cus), t = choose_way(tail, p, act, 1, cus);
+  if (m.c.kernel != GateupChoice::kGeneral && t.c.kernel != GateupChoice::kGeneral && m.cost + t.cost < 0.97 * r.first.cost) {
+    r.first = m;
+    r.last = t;
+    r.last_rows = tail;
+  }
+  return r;
+}
+
 }  // namespace
 
 hipError_t launch_gateup_i8(const Int8Product& p, bool act, int max_splits, void* part, int cus, hipStream_t stream,
                             hipEvent_t ev_start, hipEvent_t ev_stop) {
   if (p.T <= 0) return hipSuccess;
   if (max_splits < 1 || (max_splits > 1 && !part) || (act && p.N2 % 2 != 0)) return hipErrorInvalidValue;
-  // whole 128-byte stages of 16-byte aligned rows, and at least two of them (the scales'
-  // transfer); anything else in the general kernel
-  const bool aligned = p.H % (2 * kBK) == 0 && p.H > 2 * kBK && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 &&
-                       reinterpret_cast<uintptr_t>(p.w) % 16 == 0;
-  if (!aligned) return launch_gateup_i8_any(p, act, stream, ev_start, ev_stop);
-  const Way all = choose_way(p.T, p, act, max_splits, cus);
-  if (all.c.kernel == GateupChoice::kGeneral) return launch_gateup_i8_any(p, act, stream, ev_start, ev_stop);
-  // The rows past the last whole 64 in a launch of their own, where they would make a
-  // round of tiles for themselves (the sums are the same): 2,056 tokens x 11,008 x 2,048,
-  // a chunk with eight decode rows, with the quantiser 73 us instead of 78 (65 with the
-  // tiles of 128 x 128).
-  const int32_t tail = p.T % kTailBM, main = p.T - tail;
-  if (all.c.kernel == GateupChoice::kTiles && tail > 0 && main > 0) {
-    // both parts' partial sums fit where the whole call's do
-    const Way m = choose_way(main, p, act, max_splits, cus), t = choose_way(tail, p, act, 1, cus);
-    if (m.c.kernel != GateupChoice::kGeneral && t.c.kernel != GateupChoice::kGeneral && m.cost + t.cost < 0.97 * all.cost) {
-      const hipError_t e = launch_rows_of(p, 0, main, m, act, part, stream, ev_start, nullptr);
-      return e != hipSuccess ? e : launch_rows_of(p, main, tail, t, act, part, stream, nullptr, ev_stop);
-    }
+  const bool aligned = reinterpret_cast<uintptr_t>(p.x) % 16 == 0 && reinterpret_cast<uintptr_t>(p.w) % 16 == 0;
+  const Ways r = choose_ways(p, act, aligned, max_splits, cus);
+  if (r.general) return launch_gateup_i8_any(p, act, stream, ev_start, ev_stop);
+  if (r.last_rows == 0) return launch_rows_of(p, 0, p.T, r.first, act, part, stream, ev_start, ev_stop);
+  const int32_t main = p.T - r.last_rows;
+  const hipError_t e = launch_rows_of(p, 0, main, r.first, act, part, stream, ev_start, nullptr);
+  return e != hipSuccess ? e : launch_rows_of(p, main, r.last_rows, r.last, act, part, stream, nullptr, ev_stop);
+}
+
+void gateup_i8_choice(int32_t T, int32_t H, int32_t N2, bool act, bool aligned, int max_splits, int cus, int32_t* choice) {
+  const Ways r = choose_ways(Int8Product{nullptr, nullptr, nullptr, nullptr, nullptr, T, H, N2}, act, aligned, max_splits, cus);
+  std::fill(choice, choice + 16, 0);
+  auto put = [&](int32_t* to, const Way& w, int32_t rows) {
+    const GateupChoice& c = w.c;
+    const int32_t v[8] = {rows, w.mid ? 3 : int32_t(c.kernel), w.mid ? 128 : c.rows, w.mid ? 0 : c.main_m, w.mid ? 0 : c.tail_m,
+                          w.mid ? 0 : c.g, w.mid ? 0 : c.wr, w.mid ? 1 : c.splits};
+    std::copy(v, v + 8, to);
+  };
+  if (r.general) {
+    choice[0] = T;
+    choice[1] = GateupChoice::kGeneral;
+    choice[7] = 1;
+    return;
   }
-  return launch_rows_of(p, 0, p.T, all, act, part, stream, ev_start, ev_stop);
+  put(choice, r.first, T - r.last_rows);
+  if (r.last_rows > 0) put(choice + 8, r.last, r.last_rows);
 }
 
 }  // namespace ppas

@@ -118,6 +118,8 @@ _lib.ppas_gateup_act_workspace_bytes.restype = _sz
 _lib.ppas_gateup_act_workspace_bytes.argtypes = [_i32, _i32, _i32]
 _lib.ppas_gateup_choice.restype = ctypes.c_int
 _lib.ppas_gateup_choice.argtypes = [_i32, _i32, _i32, _i32, _i32, _sz, _i32, _vp]
+_lib.ppas_gateup_i8_choice.restype = ctypes.c_int
+_lib.ppas_gateup_i8_choice.argtypes = [_i32, _i32, _i32, _i32, _i32, _sz, _i32, _vp]
 _lib.ppas_stream_read.restype = ctypes.c_int
 _lib.ppas_stream_read.argtypes = [_vp, _sz, _vp, _E, _vp]
 _lib.ppas_plan_items.restype = _i32
@@ -556,6 +558,20 @@ def gateup_i8_workspace_bytes(n_tokens: int, hidden: int, n_out: int) -> int:
 
 def gateup_act_i8_workspace_bytes(n_tokens: int, hidden: int, n_inter: int) -> int:
     return int(_lib.ppas_gateup_act_i8_workspace_bytes(int(n_tokens), int(hidden), int(n_inter)))
+
+
+def gateup_i8_choice(n_tokens: int, hidden: int, n_out: int, activation: bool = False, aligned: bool = True,
+                     workspace_bytes: int | None = None, num_cus: int = 0) -> list:
+    """The launches of an 8-bit product (host only, for tests), one or two; n_out: its weight rows."""
+    out = np.zeros(16, dtype=np.int32)
+    nbytes = (1 << 62) if workspace_bytes is None else int(workspace_bytes)
+    _check(_lib.ppas_gateup_i8_choice(int(n_tokens), int(hidden), int(n_out), int(activation), int(aligned), nbytes,
+                                      int(num_cus), _host_ptr(out)), "ppas_gateup_i8_choice")
+    names = ("tokens", "kernel", "rows", "main_tiles", "small_tiles", "weight_tiles", "weight_rows", "splits")
+    launches = [dict(zip(names, out[i:i + 8].tolist())) for i in (0, 8) if out[i] > 0]
+    for c in launches:
+        c["kernel"] = ("tiles", "rows", "general", "mid")[c["kernel"]]
+    return launches
 
 
 def _gateup_i8(fn, what, x, x_scale, w, w_scale, y, per, workspace, events, stream):
