@@ -214,7 +214,9 @@ ppas_status ppas_rope_kv_append(const ppas_shape* shape, float rope_theta, void*
  *           w_j = u_j (1 - t + t / factor), t = (j - first) / (last - first) kept within
  *           0..1 (t = 0 up to `first` where last <= first, 1 behind it)
  * Frequencies and angles are computed in fp64 (whole turns removed), cos and sin in
- * fp32, the turn in fp32, and results rounded to bf16 nearest-even.
+ * fp32, the turn in fp32, and results rounded to bf16 nearest-even. A pair of more than
+ * 4,096 turns per position, or of none, is PPAS_EINVAL: fp64 would not hold its angle at
+ * far positions.
  */
 enum { PPAS_ROPE_HALF = 0, PPAS_ROPE_INTERLEAVED = 1 };
 enum { PPAS_ROPE_PLAIN = 0, PPAS_ROPE_LINEAR = 1, PPAS_ROPE_BASE = 2, PPAS_ROPE_BANDS = 3, PPAS_ROPE_RAMP = 4 };

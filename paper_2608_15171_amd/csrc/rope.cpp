@@ -74,9 +74,11 @@ ppas_status rope_frequencies(const ppas_rope* rope, int32_t head_dim, double* w)
   const ppas_status st = check_rope(*rope);
   if (st != PPAS_OK) return st;
   frequencies(*rope, w);
-  // every pair has to turn (a base or factor at the ends of fp64's range can leave it)
+  // Every pair has to turn (a base or factor at the ends of fp64's range can leave it), and at most
+  // 2^12 times per position: an angle at position 2^31 is then known to 2^-10 of a turn. Far beyond
+  // it would be a whole number of turns, whatever the position, and then infinite.
   for (int32_t j = 0; j < rope->rotary_dim / 2; ++j)
-    if (!positive(w[j])) return PPAS_EINVAL;
+    if (!positive(w[j]) || w[j] > 4096 * 2.0 * M_PI) return PPAS_EINVAL;
   return PPAS_OK;
 }
 
