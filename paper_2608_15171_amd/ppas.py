@@ -675,6 +675,7 @@ class StepPlan:
                                                    _opts_ptr(opts), ctypes.byref(h))
             _check(st, "ppas_step_plan_create_shared")
         self._h = h.value
+        self._shared = p is not None
         self.info = PlanInfo()
         _check(_lib.ppas_step_plan_info(self._h, ctypes.byref(self.info)), "ppas_step_plan_info")
 
@@ -724,10 +725,11 @@ class StepPlan:
                   stream=None) -> None:
         _check_buffers(self.shape, self.desc, q=q, out=out, k_pages=k_pages, v_pages=v_pages,
                        bt_dev=self._bt(bt_dev), rows=self._n_rows)
+        hs = _here(stream, out, q, k_pages, v_pages, bt_dev, workspace) if self._shared else _stream(stream)
         st = _lib.ppas_attn_step_planned(self._h, _dev(out, "out"), _dev(q, "q"), _dev(k_pages, "k_pages"),
                                          _dev(v_pages, "v_pages"), _dev(bt_dev, "block_table"),
                                          _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(),
-                                         None if events is None else ctypes.byref(events), _stream(stream))
+                                         None if events is None else ctypes.byref(events), hs)
         _check(st, "ppas_attn_step_planned")
 
     def close(self) -> None:
