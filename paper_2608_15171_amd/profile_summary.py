@@ -34,7 +34,8 @@ SOURCES = {
     "attn_step_kernel": ["paper_2608_15171_amd/csrc/attn_step.hip", "paper_2608_15171_amd/csrc/plan.cpp",
                          "paper_2608_15171_amd/csrc/plan.h"],
     "rope_append_kernel": ["paper_2608_15171_amd/csrc/rope_append.hip"],
-    "gateup_kernel": ["paper_2608_15171_amd/csrc/gateup.hip", "paper_2608_15171_amd/csrc/gateup_device.h"],
+    "gateup_kernel": ["paper_2608_15171_amd/csrc/gateup.hip", "paper_2608_15171_amd/csrc/gateup_kernels.h",
+                      "paper_2608_15171_amd/csrc/gateup_device.h"],
 }
 DESCRIPTION = {
     "attn_step_kernel": "One packed attention launch of the mixed step on one MI355X (gfx950); bf16 inputs, fp32 "
