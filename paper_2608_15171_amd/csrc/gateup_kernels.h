@@ -451,7 +451,9 @@ __device__ __forceinline__ void run_tiles(const GemmArgs& a, char* smem, int m_f
   // issued since (loads into registers would have to drain the stream: 8 % of a tile).
   int sc_half = 0;
   // As values: a choice between kernel arguments becomes one between their addresses, which
-  // keeps them in scratch memory, and every load from there drains the stream.
+  // keeps them in scratch memory, and every load from there waits for the whole stream, a few
+  // times per tile (16,384 tokens x 2,048 x 11,008, 11 tiles a workgroup, 343 -> 338 us; x
+  // 2,048 x 2,048, two tiles, 67.5 -> 68.6).
   const float *sx = a.sx, *sw = a.sw;
   int rows_total = a.T, cols_total = a.N2;
   if constexpr (E::kInt) asm volatile("" : "+s"(sx), "+s"(sw), "+s"(rows_total), "+s"(cols_total));

@@ -153,12 +153,13 @@ static_assert(kRowKeys <= kRowMaxKeys, "a wave takes the row");
 
 // Microseconds of a step with pieces of at most so many keys, fitted to 32,000 plans of 105
 // steps, each timed over a hundred passes in a row (5 to 6 % rms; the choice made with it
-// is 3 % slower than the best of them on average): a fixed part; the time that the items
-// take on the workgroup slots in launch order, and the one that the decode rows' keys take
-// from memory (with a share of a slot's time for every decode item), which hide one
-// another in part (the `power` mean of the two); then the merge, by its partials' bytes
-// and the splits of a row. A tile's key takes `key` alone and `key_full` with every slot
-// taken (for 16 positions 5 % above the fit, which timed full chips of them too short).
+// takes 4 % longer than the best of them on average, 1.3 times at worst): a fixed part; the
+// time that the items take on the workgroup slots in launch order, and the one that the
+// decode rows' keys take from memory (with a share of a slot's time for every decode item),
+// which hide one another in part (the `power` mean of the two); then the merge, by its
+// partials' bytes and the splits of a row. A tile's key takes `key` alone and `key_full` with
+// every slot taken (for 16 positions 5 % above the fit, which timed full chips of them too
+// short).
 struct SharedCost {
   double fixed, item, key, key_full, decode_item, decode_key, row, row_key, tbs, tbs_many, decode_slot, power, mb, split;
 };
