@@ -280,6 +280,43 @@ ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope,
                                  const int32_t* block_table_host, void* hip_stream);
 
 /*
+ * Norms of query and key heads before their turn, in the same pass (the library's own
+ * offer to models that normalise them; the paper does not describe it). A head x of D
+ * features becomes
+ *   z_i = (x_i - mu) / sqrt(var + eps) * (offset + w_i),  var = mean_i (x_i - mu)^2
+ * with mu its mean where `center` is not 0, and 0 otherwise (the root-mean-square form);
+ * then z turns as the calls without a norm turn x. Statistics, norm and turn are fp32 and
+ * rounded once to bf16 nearest-even; the magnitude of a ppas_rope is on the turned
+ * features only. Every finite head has its finite norm (a head of zeros gives zeros); one
+ * that holds an infinity or a NaN gives what the formula gives in IEEE arithmetic.
+ */
+typedef struct ppas_head_norm {
+  const void* weight;   /* device bf16: head_dim weights, or a row of them per head; NULL: no weights
+                           (z without its last factor) */
+  int64_t head_stride;  /* elements between the heads' rows, at least head_dim; 0: one row for all heads */
+  float eps;            /* finite, at least 2^-100 */
+  float offset;         /* added to every weight (1 where a model holds differences from one), finite */
+  int32_t center;
+} ppas_head_norm;
+
+/*
+ * As ppas_rope_rows (without `transposed`) and ppas_rope_qkv_append, of normalised
+ * heads: the rows' heads, or a step's queries and keys, each with their norm. Values are
+ * copied as they are. PPAS_EINVAL also for a norm that is NULL or out of range; the
+ * outputs must not overlap the weights. Weights on 16 bytes with a head_stride that is a
+ * multiple of 8 are faster.
+ */
+ppas_status ppas_norm_rope_rows(const ppas_head_norm* norm, const ppas_rope* rope, const void* x, int64_t x_stride,
+                                void* y, int64_t y_stride, const int32_t* positions_dev, int32_t n_rows,
+                                int32_t n_heads, int32_t head_dim, const ppas_events* events, void* hip_stream);
+
+ppas_status ppas_norm_rope_qkv_append(const ppas_shape* shape, const ppas_head_norm* q_norm,
+                                      const ppas_head_norm* k_norm, const ppas_rope* rope, const ppas_qkv* rows,
+                                      void* q_out, void* k_pages, void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
+                                      const int32_t* block_table_dev, int32_t bt_stride,
+                                      const int32_t* block_table_host, void* hip_stream);
+
+/*
  * Requests first_seq .. first_seq + n_seqs - 1 of a step hold the same first `len`
  * positions in the same pages (a system prompt, a document, sampled continuations):
  * their block-table rows start with the same len / 16 entries. len is a multiple of 16
@@ -423,6 +460,13 @@ ppas_status ppas_rope_qkv_append_planned(const ppas_step_plan* plan, const ppas_
                                          void* q_out, void* k_pages, void* v_pages,
                                          const int32_t* block_table_dev, const ppas_events* events,
                                          void* hip_stream);
+
+/* As ppas_norm_rope_qkv_append, with the plan's descriptors and validation; events may be NULL. */
+ppas_status ppas_norm_rope_qkv_append_planned(const ppas_step_plan* plan, const ppas_head_norm* q_norm,
+                                              const ppas_head_norm* k_norm, const ppas_rope* rope,
+                                              const ppas_qkv* rows, void* q_out, void* k_pages, void* v_pages,
+                                              const int32_t* block_table_dev, const ppas_events* events,
+                                              void* hip_stream);
 
 /*
  * As ppas_attn_step, with the plan's descriptors, validation and work list

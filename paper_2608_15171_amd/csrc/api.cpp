@@ -357,8 +357,24 @@ ppas_status check_qkv(const ppas_shape& s, const ppas_rope* rope, const ppas_qkv
   return PPAS_OK;
 }
 
-ppas_status run_qkv_append(const ppas_step_plan& p, const RopeTable& table, const ppas_qkv& rows, void* q_out,
-                           void* k_pages, void* v_pages, const int32_t* bt_dev, const ppas_events* ev,
+// The norms of a call's heads, where it has any.
+struct Norms {
+  const ppas_head_norm *q, *k;
+};
+
+ppas_status check_norm(const ppas_head_norm* n, int64_t heads, int32_t head_dim) {
+  if (!n || !std::isfinite(n->eps) || !(n->eps >= 0x1p-100f) || !std::isfinite(n->offset)) return PPAS_EINVAL;
+  if (!n->weight) return PPAS_OK;
+  if (off(n->weight, 2) || (n->head_stride != 0 && n->head_stride < head_dim)) return PPAS_EINVAL;
+  return n->head_stride > (int64_t(1) << 61) / heads ? PPAS_ERANGE : PPAS_OK;
+}
+
+HeadNorm norm_of(const ppas_head_norm& n) {
+  return HeadNorm{static_cast<const uint16_t*>(n.weight), n.head_stride, n.eps, n.offset, n.center != 0};
+}
+
+ppas_status run_qkv_append(const ppas_step_plan& p, const RopeTable& table, const Norms* norms, const ppas_qkv& rows,
+                           void* q_out, void* k_pages, void* v_pages, const int32_t* bt_dev, const ppas_events* ev,
                            void* hip_stream) {
   if (p.n_append == 0 || (p.n_desc == 0 && !p.buf)) return PPAS_EINVAL;   // a plan made without the page-write list
   if (p.n_append > kAppendMaxItems) return PPAS_ERANGE;
@@ -381,7 +397,9 @@ ppas_status run_qkv_append(const ppas_step_plan& p, const RopeTable& table, cons
   r.bt_stride = p.bt_stride;
   r.hq = p.shape.n_q_heads;
   r.hkv = p.shape.n_kv_heads;
-  const hipError_t e = launch_rope_qkv_append(r, table, stream, ev_of(ev, 0), ev_of(ev, 1));
+  const hipError_t e =
+      norms ? launch_norm_rope_qkv_append(r, norm_of(*norms->q), norm_of(*norms->k), table, stream, ev_of(ev, 0), ev_of(ev, 1))
+            : launch_rope_qkv_append(r, table, stream, ev_of(ev, 0), ev_of(ev, 1));
   // a list by request travels in the kernel's arguments: no buffer is read
   const bool noted = p.n_desc > 0 || note_use(p.buf, stream);
   return (e == hipSuccess && noted) ? PPAS_OK : PPAS_EHIP;
@@ -561,22 +579,49 @@ ppas_status ppas_rope_kv_append_planned(const ppas_step_plan* plan, float rope_t
   }
 }
 
-ppas_status ppas_rope_qkv_append_planned(const ppas_step_plan* plan, const ppas_rope* rope, const ppas_qkv* rows,
-                                         void* q_out, void* k_pages, void* v_pages, const int32_t* block_table_dev,
-                                         const ppas_events* events, void* hip_stream) {
+namespace {
+
+ppas_status check_norms(const Norms* norms, const ppas_shape& s) {
+  if (!norms) return PPAS_OK;
+  const ppas_status st = check_norm(norms->q, s.n_q_heads, kHeadDim);
+  return st != PPAS_OK ? st : check_norm(norms->k, s.n_kv_heads, kHeadDim);
+}
+
+ppas_status qkv_append_planned(const ppas_step_plan* plan, const Norms* norms, const ppas_rope* rope,
+                               const ppas_qkv* rows, void* q_out, void* k_pages, void* v_pages,
+                               const int32_t* block_table_dev, const ppas_events* events, void* hip_stream) {
   if (!plan) return PPAS_EINVAL;
   ppas_status st = check_events(events);
   if (st != PPAS_OK) return st;
   try {
+    st = check_norms(norms, plan->shape);
+    if (st != PPAS_OK) return st;
     RopeTable table;
     if (plan->n_seqs == 0) return rope_table(rope, kHeadDim, table);
     st = check_qkv(plan->shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, plan->n_rows, table);
     if (st != PPAS_OK) return st;
     if (capturing(hip_stream)) return PPAS_EUNSUPPORTED;
-    return run_qkv_append(*plan, table, *rows, q_out, k_pages, v_pages, block_table_dev, events, hip_stream);
+    return run_qkv_append(*plan, table, norms, *rows, q_out, k_pages, v_pages, block_table_dev, events, hip_stream);
   } catch (...) {
     return PPAS_EINVAL;
   }
+}
+
+}  // namespace
+
+ppas_status ppas_rope_qkv_append_planned(const ppas_step_plan* plan, const ppas_rope* rope, const ppas_qkv* rows,
+                                         void* q_out, void* k_pages, void* v_pages, const int32_t* block_table_dev,
+                                         const ppas_events* events, void* hip_stream) {
+  return qkv_append_planned(plan, nullptr, rope, rows, q_out, k_pages, v_pages, block_table_dev, events, hip_stream);
+}
+
+ppas_status ppas_norm_rope_qkv_append_planned(const ppas_step_plan* plan, const ppas_head_norm* q_norm,
+                                              const ppas_head_norm* k_norm, const ppas_rope* rope,
+                                              const ppas_qkv* rows, void* q_out, void* k_pages, void* v_pages,
+                                              const int32_t* block_table_dev, const ppas_events* events,
+                                              void* hip_stream) {
+  const Norms norms{q_norm, k_norm};
+  return qkv_append_planned(plan, &norms, rope, rows, q_out, k_pages, v_pages, block_table_dev, events, hip_stream);
 }
 
 ppas_status ppas_attn_step_planned(const ppas_step_plan* plan, void* out, const void* q, const void* k_pages,
@@ -882,9 +927,11 @@ ppas_status ppas_rope_frequencies(const ppas_rope* rope, int32_t head_dim, doubl
   return PPAS_OK;
 }
 
-ppas_status ppas_rope_rows(const ppas_rope* rope, const void* x, int64_t x_stride, void* y, int64_t y_stride,
-                           const int32_t* positions_dev, int32_t n_rows, int32_t n_heads, int32_t head_dim,
-                           int32_t transposed, const ppas_events* events, void* hip_stream) {
+namespace {
+
+ppas_status rope_rows_call(const ppas_head_norm* norm, const ppas_rope* rope, const void* x, int64_t x_stride, void* y,
+                           int64_t y_stride, const int32_t* positions_dev, int32_t n_rows, int32_t n_heads,
+                           int32_t head_dim, bool transposed, const ppas_events* events, void* hip_stream) {
   try {
     if (n_rows < 0 || n_heads < 1 || n_heads > 65536 || head_dim < 2 || head_dim % 2 != 0) return PPAS_EINVAL;
     if (head_dim > 2 * kRopeMaxPairs) return PPAS_EUNSUPPORTED;
@@ -893,7 +940,8 @@ ppas_status ppas_rope_rows(const ppas_rope* rope, const void* x, int64_t x_strid
     if (st != PPAS_OK) return st;
     st = check_events(events);
     if (st != PPAS_OK) return st;
-    if (n_rows == 0) return PPAS_OK;
+    if (norm) st = check_norm(norm, n_heads, head_dim);
+    if (st != PPAS_OK || n_rows == 0) return st;
     const int64_t row = int64_t(n_heads) * head_dim, most = (int64_t(1) << 61) / n_rows;
     if (!x || !y || !positions_dev || x_stride < row || y_stride < row) return PPAS_EINVAL;
     if (x_stride > most || y_stride > most) return PPAS_ERANGE;
@@ -903,22 +951,45 @@ ppas_status ppas_rope_rows(const ppas_rope* rope, const void* x, int64_t x_strid
       return PPAS_EINVAL;
     if (!current_device().gfx950) return PPAS_EUNSUPPORTED;
     const RopeRows r{static_cast<const uint16_t*>(x), static_cast<uint16_t*>(y), x_stride, y_stride, positions_dev,
-                     n_rows, n_heads, head_dim, transposed != 0};
-    const hipError_t e = launch_rope_rows(r, table, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
-                                          ev_of(events, 1));
+                     n_rows, n_heads, head_dim, transposed};
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e =
+        norm ? launch_norm_rope_rows(r, norm_of(*norm), table, stream, ev_of(events, 0), ev_of(events, 1))
+             : launch_rope_rows(r, table, stream, ev_of(events, 0), ev_of(events, 1));
     return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
   } catch (...) {
     return PPAS_EINVAL;
   }
 }
 
-ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope, const ppas_qkv* rows, void* q_out,
-                                 void* k_pages, void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
-                                 const int32_t* block_table_dev, int32_t bt_stride,
-                                 const int32_t* block_table_host, void* hip_stream) {
+}  // namespace
+
+ppas_status ppas_rope_rows(const ppas_rope* rope, const void* x, int64_t x_stride, void* y, int64_t y_stride,
+                           const int32_t* positions_dev, int32_t n_rows, int32_t n_heads, int32_t head_dim,
+                           int32_t transposed, const ppas_events* events, void* hip_stream) {
+  return rope_rows_call(nullptr, rope, x, x_stride, y, y_stride, positions_dev, n_rows, n_heads, head_dim,
+                        transposed != 0, events, hip_stream);
+}
+
+ppas_status ppas_norm_rope_rows(const ppas_head_norm* norm, const ppas_rope* rope, const void* x, int64_t x_stride,
+                                void* y, int64_t y_stride, const int32_t* positions_dev, int32_t n_rows,
+                                int32_t n_heads, int32_t head_dim, const ppas_events* events, void* hip_stream) {
+  if (!norm) return PPAS_EINVAL;
+  return rope_rows_call(norm, rope, x, x_stride, y, y_stride, positions_dev, n_rows, n_heads, head_dim, false, events,
+                        hip_stream);
+}
+
+namespace {
+
+ppas_status qkv_append(const ppas_shape* shape, const Norms* norms, const ppas_rope* rope, const ppas_qkv* rows,
+                       void* q_out, void* k_pages, void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
+                       const int32_t* block_table_dev, int32_t bt_stride, const int32_t* block_table_host,
+                       void* hip_stream) {
   ppas_step_plan p;
   try {
     ppas_status st = validate(shape, seqs, n_seqs, block_table_host, bt_stride, true);
+    if (st != PPAS_OK) return st;
+    st = check_norms(norms, *shape);
     if (st != PPAS_OK) return st;
     RopeTable table;
     if (n_seqs == 0) return rope_table(rope, kHeadDim, table);
@@ -929,13 +1000,33 @@ ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope,
     // validated above; build only the page-write list
     st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantInline, false);
     if (st == PPAS_OK)
-      st = run_qkv_append(p, table, *rows, q_out, k_pages, v_pages, block_table_dev, nullptr, hip_stream);
+      st = run_qkv_append(p, table, norms, *rows, q_out, k_pages, v_pages, block_table_dev, nullptr, hip_stream);
     release(p.buf);
     return st;
   } catch (...) {
     release(p.buf);
     return PPAS_EINVAL;
   }
+}
+
+}  // namespace
+
+ppas_status ppas_rope_qkv_append(const ppas_shape* shape, const ppas_rope* rope, const ppas_qkv* rows, void* q_out,
+                                 void* k_pages, void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
+                                 const int32_t* block_table_dev, int32_t bt_stride,
+                                 const int32_t* block_table_host, void* hip_stream) {
+  return qkv_append(shape, nullptr, rope, rows, q_out, k_pages, v_pages, seqs, n_seqs, block_table_dev, bt_stride,
+                    block_table_host, hip_stream);
+}
+
+ppas_status ppas_norm_rope_qkv_append(const ppas_shape* shape, const ppas_head_norm* q_norm,
+                                      const ppas_head_norm* k_norm, const ppas_rope* rope, const ppas_qkv* rows,
+                                      void* q_out, void* k_pages, void* v_pages, const ppas_seq* seqs, int32_t n_seqs,
+                                      const int32_t* block_table_dev, int32_t bt_stride,
+                                      const int32_t* block_table_host, void* hip_stream) {
+  const Norms norms{q_norm, k_norm};
+  return qkv_append(shape, &norms, rope, rows, q_out, k_pages, v_pages, seqs, n_seqs, block_table_dev, bt_stride,
+                    block_table_host, hip_stream);
 }
 
 size_t ppas_attn_shared_workspace_bytes(const ppas_shape* shape, const ppas_seq* seqs, int32_t n_seqs,

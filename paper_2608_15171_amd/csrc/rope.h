@@ -56,4 +56,18 @@ struct RopeAppend {
 hipError_t launch_rope_qkv_append(const RopeAppend& r, const RopeTable& t, hipStream_t stream, hipEvent_t ev_start,
                                   hipEvent_t ev_stop);
 
+// The norm of a head before its turn: (x - mu) / sqrt(var + eps) * (offset + weight).
+struct HeadNorm {
+  const uint16_t* weight;   // bf16, nullptr: none
+  int64_t head_stride;      // elements between the heads' weights (0: one set for all)
+  float eps, offset;
+  bool center;              // mu is the mean (otherwise 0)
+};
+// As the two above, of normalised heads (RopeRows::transposed is not read).
+hipError_t launch_norm_rope_rows(const RopeRows& r, const HeadNorm& norm, const RopeTable& t, hipStream_t stream,
+                                 hipEvent_t ev_start, hipEvent_t ev_stop);
+hipError_t launch_norm_rope_qkv_append(const RopeAppend& r, const HeadNorm& q_norm, const HeadNorm& k_norm,
+                                       const RopeTable& t, hipStream_t stream, hipEvent_t ev_start,
+                                       hipEvent_t ev_stop);
+
 }  // namespace ppas

@@ -86,6 +86,13 @@ class Qkv(ctypes.Structure):
                 ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
+class HeadNorm(ctypes.Structure):
+    """The norm of a head before its turn: see ppas_head_norm, and head_norm() below."""
+    _fields_ = [("weight", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("eps", ctypes.c_float),
+                ("offset", ctypes.c_float), ("center", ctypes.c_int32)]
+    tensor = None   # the weights, which head_norm keeps
+
+
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 
@@ -148,6 +155,14 @@ _lib.ppas_rope_qkv_append.restype = ctypes.c_int
 _lib.ppas_rope_qkv_append.argtypes = [_P, _R, ctypes.POINTER(Qkv), _vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp]
 _lib.ppas_rope_qkv_append_planned.restype = ctypes.c_int
 _lib.ppas_rope_qkv_append_planned.argtypes = [_vp, _R, ctypes.POINTER(Qkv), _vp, _vp, _vp, _vp, _E, _vp]
+_N = ctypes.POINTER(HeadNorm)
+_lib.ppas_norm_rope_rows.restype = ctypes.c_int
+_lib.ppas_norm_rope_rows.argtypes = [_N, _R, _vp, _i64, _vp, _i64, _vp, _i32, _i32, _i32, _E, _vp]
+_lib.ppas_norm_rope_qkv_append.restype = ctypes.c_int
+_lib.ppas_norm_rope_qkv_append.argtypes = [_P, _N, _N, _R, ctypes.POINTER(Qkv), _vp, _vp, _vp, _vp, _i32, _vp, _i32,
+                                           _vp, _vp]
+_lib.ppas_norm_rope_qkv_append_planned.restype = ctypes.c_int
+_lib.ppas_norm_rope_qkv_append_planned.argtypes = [_vp, _N, _N, _R, ctypes.POINTER(Qkv), _vp, _vp, _vp, _vp, _E, _vp]
 _lib.ppas_step_plan_create_shared.restype = ctypes.c_int
 _lib.ppas_step_plan_create_shared.argtypes = [_P, _vp, _i32, _vp, _i32, _vp, _i32, _O, ctypes.POINTER(ctypes.c_void_p)]
 _lib.ppas_attn_step_shared.restype = ctypes.c_int
@@ -348,21 +363,59 @@ def _heads(t, name):
     return t.data_ptr(), row if n > 1 else max(row, h * d)
 
 
-def rope_rows(rope: Rope, x, positions, y, transposed: bool = False, events: Events | None = None, stream=None) -> None:
-    """y[r] = the heads of x[r] turned by positions[r] (x, y [rows, heads, features] bf16 with any row stride,
-    positions int32). y may be x. `transposed` turns the other way: the gradient, and without a magnitude the inverse."""
+def _rope_rows_args(x, positions, y):
+    """The pointers and strides of rows to turn, their positions and sizes."""
     xp, xs = _heads(x, "x")
     yp, ys = (xp, xs) if y is x else _heads(y, "y")
     if x.shape != y.shape or positions.dim() != 1 or positions.shape[0] != x.shape[0]:
         raise ValueError(f"shapes x {tuple(x.shape)}, y {tuple(y.shape)}, positions {tuple(positions.shape)} do not match")
     if positions.dtype != torch.int32:
         raise ValueError("positions must be int32")
-    n, h, d = x.shape
-    pp = _dev(positions, "positions")
+    return xp, xs, yp, ys, _dev(positions, "positions"), *x.shape
+
+
+def rope_rows(rope: Rope, x, positions, y, transposed: bool = False, events: Events | None = None, stream=None) -> None:
+    """y[r] = the heads of x[r] turned by positions[r] (x, y [rows, heads, features] bf16 with any row stride,
+    positions int32). y may be x. `transposed` turns the other way: the gradient, and without a magnitude the inverse."""
+    args = _rope_rows_args(x, positions, y)
     hs = _here(stream, x, y, positions)
-    st = _lib.ppas_rope_rows(ctypes.byref(rope), xp, xs, yp, ys, pp, n, h, d,
-                             int(bool(transposed)), None if events is None else ctypes.byref(events), hs)
+    st = _lib.ppas_rope_rows(ctypes.byref(rope), *args, int(bool(transposed)),
+                             None if events is None else ctypes.byref(events), hs)
     _check(st, "ppas_rope_rows")
+
+
+def head_norm(weight=None, eps: float = 1e-6, offset: float = 0.0, center: bool = False) -> HeadNorm:
+    """The norm of heads, (x - mu) / sqrt(var + eps) * (offset + weight): `weight` a bf16 device tensor [features] for
+    all heads or [heads, features], or None; `center` takes mu as the head's mean (otherwise 0). Keeps the tensor."""
+    if weight is not None and not (weight.dtype in _BF16 and 1 <= weight.dim() <= 2 and
+                                   (weight.stride(-1) == 1 or weight.shape[-1] == 1)):
+        raise ValueError(f"weight must be [features] or [heads, features] of bf16, got {tuple(weight.shape)} {weight.dtype}")
+    if weight is not None and not weight.is_cuda:
+        raise ValueError("weight must be a device tensor")
+    stride = 0
+    if weight is not None and weight.dim() == 2:
+        stride = weight.stride(0) if weight.shape[0] > 1 else max(weight.stride(0), weight.shape[1])
+    n = HeadNorm(None if weight is None else weight.data_ptr(), stride, float(eps), float(offset), int(bool(center)))
+    n.tensor = weight
+    return n
+
+
+def _norm(norm: HeadNorm, name, heads: int, dim: int):
+    """Refuses a norm whose weights are not of such heads; its weights' tensor (or None)."""
+    w = norm.tensor
+    if w is not None and (w.shape[-1] != dim or (w.dim() == 2 and w.shape[0] != heads)):
+        raise ValueError(f"{name}'s weight must be [{dim}] or [{heads}, {dim}], got {tuple(w.shape)}")
+    return w
+
+
+def norm_rope_rows(norm: HeadNorm, rope: Rope, x, positions, y, events: Events | None = None, stream=None) -> None:
+    """rope_rows of normalised heads."""
+    args = _rope_rows_args(x, positions, y)
+    w = _norm(norm, "norm", x.shape[1], x.shape[2])
+    hs = _here(stream, x, y, positions, w)
+    st = _lib.ppas_norm_rope_rows(ctypes.byref(norm), ctypes.byref(rope), *args,
+                                  None if events is None else ctypes.byref(events), hs)
+    _check(st, "ppas_norm_rope_rows")
 
 
 def _step_rows(t, name, rows: int, heads: int, dim: int):
@@ -392,10 +445,7 @@ def _buffer(t, name, nbytes: int):
     return t.data_ptr()
 
 
-def rope_qkv_append(shape: Shape, rope: Rope, q, k_pages, v_pages, q_new, k_new, v_new, desc, bt_dev, bt_host=None,
-                    stream=None) -> None:
-    """Rotate the rows q_new into q and k_new into the pages at their positions, and copy v_new into the pages. The
-    rows are [T, heads, 128] at any row stride, as a fused QKV projection leaves them."""
+def _qkv_append(fn, what, shape, norms, rope, q, k_pages, v_pages, q_new, k_new, v_new, desc, bt_dev, bt_host, stream):
     d = _desc(desc)
     bt = _bt_host(bt_host, bt_dev)
     rows = _rows(d)
@@ -404,10 +454,27 @@ def rope_qkv_append(shape: Shape, rope: Rope, q, k_pages, v_pages, q_new, k_new,
     pool = int(shape.num_pages) * shape.n_kv_heads * shape.page_size * shape.head_dim * 2 if len(d) else 0
     ptrs = (_buffer(q, "q", rows * shape.n_q_heads * shape.head_dim * 2), _buffer(k_pages, "k_pages", pool),
             _buffer(v_pages, "v_pages", pool), _dev(bt_dev, "block_table"))
-    hs = _here(stream, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev)
-    st = _lib.ppas_rope_qkv_append(ctypes.byref(shape), ctypes.byref(rope), ctypes.byref(x), *ptrs[:3], _host_ptr(d),
-                                   len(d), ptrs[3], bt_dev.shape[1], _host_ptr(bt), hs)
-    _check(st, "ppas_rope_qkv_append")
+    weights = [_norm(n, name, h, shape.head_dim)
+               for n, name, h in zip(norms, ("q_norm", "k_norm"), (shape.n_q_heads, shape.n_kv_heads))]
+    hs = _here(stream, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev, *weights)
+    st = fn(ctypes.byref(shape), *map(ctypes.byref, norms), ctypes.byref(rope), ctypes.byref(x), *ptrs[:3], _host_ptr(d),
+            len(d), ptrs[3], bt_dev.shape[1], _host_ptr(bt), hs)
+    _check(st, what)
+
+
+def rope_qkv_append(shape: Shape, rope: Rope, q, k_pages, v_pages, q_new, k_new, v_new, desc, bt_dev, bt_host=None,
+                    stream=None) -> None:
+    """Rotate the rows q_new into q and k_new into the pages at their positions, and copy v_new into the pages. The
+    rows are [T, heads, 128] at any row stride, as a fused QKV projection leaves them."""
+    _qkv_append(_lib.ppas_rope_qkv_append, "ppas_rope_qkv_append", shape, (), rope, q, k_pages, v_pages, q_new, k_new,
+                v_new, desc, bt_dev, bt_host, stream)
+
+
+def norm_rope_qkv_append(shape: Shape, q_norm: HeadNorm, k_norm: HeadNorm, rope: Rope, q, k_pages, v_pages, q_new, k_new,
+                         v_new, desc, bt_dev, bt_host=None, stream=None) -> None:
+    """rope_qkv_append of normalised query and key heads."""
+    _qkv_append(_lib.ppas_norm_rope_qkv_append, "ppas_norm_rope_qkv_append", shape, (q_norm, k_norm), rope, q, k_pages,
+                v_pages, q_new, k_new, v_new, desc, bt_dev, bt_host, stream)
 
 
 def _prefixes(prefixes):
@@ -708,18 +775,29 @@ class StepPlan:
                                               None if events is None else ctypes.byref(events), _stream(stream))
         _check(st, "ppas_rope_kv_append_planned")
 
-    def rope_qkv_append(self, rope: Rope, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev,
-                        events: Events | None = None, stream=None) -> None:
+    def _qkv_append(self, fn, what, norms, rope, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev, events, stream) -> None:
         bt = self._bt(bt_dev)
         if not _is_table(bt) or bt.shape[0] < len(self.desc):
             _check_buffers(self.shape, self.desc, bt_dev=bt)
         x = _qkv(q_new, k_new, v_new, self._n_rows, *self._heads)
         ptrs = (_buffer(q, "q", self._q_bytes), _buffer(k_pages, "k_pages", self._pool_bytes),
                 _buffer(v_pages, "v_pages", self._pool_bytes), _dev(bt, "block_table"))
-        hs = _here(stream, q, k_pages, v_pages, q_new, k_new, v_new, bt)
-        st = _lib.ppas_rope_qkv_append_planned(self._h, ctypes.byref(rope), ctypes.byref(x), *ptrs,
-                                               None if events is None else ctypes.byref(events), hs)
-        _check(st, "ppas_rope_qkv_append_planned")
+        hq, hkv, dim = self._heads
+        weights = [_norm(n, name, h, dim) for n, name, h in zip(norms, ("q_norm", "k_norm"), (hq, hkv))]
+        hs = _here(stream, q, k_pages, v_pages, q_new, k_new, v_new, bt, *weights)
+        st = fn(self._h, *map(ctypes.byref, norms), ctypes.byref(rope), ctypes.byref(x), *ptrs,
+                None if events is None else ctypes.byref(events), hs)
+        _check(st, what)
+
+    def rope_qkv_append(self, rope: Rope, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev,
+                        events: Events | None = None, stream=None) -> None:
+        self._qkv_append(_lib.ppas_rope_qkv_append_planned, "ppas_rope_qkv_append_planned", (), rope, q, k_pages,
+                         v_pages, q_new, k_new, v_new, bt_dev, events, stream)
+
+    def norm_rope_qkv_append(self, q_norm: HeadNorm, k_norm: HeadNorm, rope: Rope, q, k_pages, v_pages, q_new, k_new,
+                             v_new, bt_dev, events: Events | None = None, stream=None) -> None:
+        self._qkv_append(_lib.ppas_norm_rope_qkv_append_planned, "ppas_norm_rope_qkv_append_planned", (q_norm, k_norm),
+                         rope, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev, events, stream)
 
     def attn_step(self, out, q, k_pages, v_pages, bt_dev, workspace, events: Events | None = None,
                   stream=None) -> None:
