@@ -618,6 +618,49 @@ size_t ppas_gateup_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t 
 size_t ppas_gateup_act_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t n_inter);
 
 /*
+ * Log probabilities of logit rows, as a request is answered with them: of a given token per
+ * row (a sampled one, or a prompt's next), its rank, the row's entropy and the top
+ * alternatives (the library's own; the paper's requests are measured, not read). Row r <
+ * n_rows holds `vocab` logits x_i (type PPAS_BF16 or PPAS_F32, row_stride elements apart,
+ * any alignment of their type); with l_i = scale x_i (scale: 1 / temperature) and
+ * lse = ln sum_i e^(l_i):
+ *   logprob[r] = l_t - lse, t = tokens_dev[r]
+ *   rank[r]    = the number of tokens before t: of a larger x, or an equal one and a lower
+ *                number; -1 if e^(l_t) is 0 because x_t is -infinity
+ *   entropy[r] = lse - sum_i p_i l_i, p_i = e^(l_i - lse)
+ *   top_ids[r][j], top_logprobs[r][j], j < top_k: the tokens in that order and their
+ *                l - lse; -1 and -infinity behind the last token that is not masked
+ * A logit of -infinity has probability 0 and adds nothing. A row with a NaN, a +infinity or
+ * nothing but -infinity has no distribution: its results are NaN, its ids and ranks -1. A
+ * token out of range (-1: none given) has logprob NaN and rank -1. Sums are fp32: up to 2^18
+ * tokens, a log probability is within 1e-5 plus 2^-21 of the spread of the row's l_i. The order is that of the logits themselves, before any rounding.
+ * Outputs may each be NULL; logprob and rank need tokens_dev. top_k is 0..64
+ * (PPAS_EUNSUPPORTED above); scale is 2^-100..2^100; vocab at most 2^30 (PPAS_ERANGE).
+ * Few rows are split over workgroups that meet in the workspace
+ * (ppas_logprobs_workspace_bytes, 16-byte aligned; a smaller one, NULL with 0 bytes
+ * included, gives fewer splits), by which the sums' rounding, but no id or rank, may
+ * differ. Nothing is allocated or kept; a call may be captured into a HIP graph, and calls
+ * that share a workspace must not run at once. n_rows == 0 is a no-op.
+ */
+enum { PPAS_BF16 = 0, PPAS_F32 = 1 };
+
+typedef struct ppas_logprob_out {
+  float* logprob;        /* [n_rows] */
+  int32_t* rank;         /* [n_rows] */
+  float* entropy;        /* [n_rows] */
+  int32_t* top_ids;      /* [n_rows][top_k] */
+  float* top_logprobs;   /* [n_rows][top_k] */
+} ppas_logprob_out;
+
+ppas_status ppas_logprobs(const void* logits, int32_t type, int64_t row_stride, int32_t n_rows, int32_t vocab,
+                          float scale, const int32_t* tokens_dev, int32_t top_k, const ppas_logprob_out* out,
+                          void* workspace, size_t workspace_bytes, const ppas_events* events, void* hip_stream);
+
+/* The most workspace that such a call can use on the current device (0 where rows are not
+ * split, or for an invalid shape). */
+size_t ppas_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t top_k);
+
+/*
  * Kernel choice of a projection call, for tests (host only, no HIP call): the
  * kernel that ppas_gateup_proj, or with `activation` ppas_gateup_act (n_out = 2
  * n_inter), takes for this shape and workspace size on a device of num_cus compute

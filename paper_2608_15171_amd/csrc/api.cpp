@@ -12,6 +12,7 @@
 
 #include "device.h"
 #include "list_pool.h"
+#include "logprobs.h"
 #include "plan.h"
 #include "ppas.h"
 #include "rope.h"
@@ -850,6 +851,60 @@ ppas_status ppas_gateup_i8_choice(int32_t n_tokens, int32_t hidden, int32_t n_ou
   gateup_i8_choice(n_tokens, hidden, n_out, activation != 0, aligned != 0,
                    allowed_splits_i8(n_tokens, hidden, n_out, workspace_bytes, cus), cus, choice);
   return PPAS_OK;
+}
+
+namespace {
+
+// what bounds a call's logit rows: token numbers and vectors stay far inside int32
+constexpr int32_t kMaxVocab = 1 << 30;
+
+ppas_status check_logprobs(int32_t n_rows, int32_t vocab, int32_t top_k) {
+  if (n_rows < 0 || vocab <= 0 || top_k < 0) return PPAS_EINVAL;
+  if (top_k > kLogprobsMaxTop) return PPAS_EUNSUPPORTED;
+  return vocab > kMaxVocab ? PPAS_ERANGE : PPAS_OK;
+}
+
+}  // namespace
+
+size_t ppas_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t top_k) {
+  if (check_logprobs(n_rows, vocab, top_k) != PPAS_OK || n_rows == 0) return 0;
+  try {
+    return logprob_workspace_bytes(n_rows, top_k, logprob_splits(n_rows, vocab, current_device().cus));
+  } catch (...) {
+    return 0;
+  }
+}
+
+ppas_status ppas_logprobs(const void* logits, int32_t type, int64_t row_stride, int32_t n_rows, int32_t vocab,
+                          float scale, const int32_t* tokens_dev, int32_t top_k, const ppas_logprob_out* out,
+                          void* workspace, size_t workspace_bytes, const ppas_events* events, void* hip_stream) {
+  try {
+    ppas_status st = check_logprobs(n_rows, vocab, top_k);
+    if (st != PPAS_OK) return st;
+    if (type != PPAS_BF16 && type != PPAS_F32) return PPAS_EINVAL;
+    if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) return PPAS_EINVAL;
+    st = check_events(events);
+    if (st != PPAS_OK || n_rows == 0) return st;
+    if (!logits || !out || row_stride < vocab || (workspace_bytes > 0 && !workspace)) return PPAS_EINVAL;
+    if (row_stride > (int64_t(1) << 60) / n_rows) return PPAS_ERANGE;
+    const LogprobRows r{logits,          row_stride,   tokens_dev,    out->logprob,      out->rank,
+                        out->entropy,    top_k ? out->top_ids : nullptr, top_k ? out->top_logprobs : nullptr,
+                        scale,           n_rows,       vocab,         out->top_ids || out->top_logprobs ? top_k : 0, type == PPAS_F32};
+    if ((r.logprob || r.rank) && !r.tokens) return PPAS_EINVAL;
+    if (off(logits, type == PPAS_F32 ? 4 : 2) || off(r.tokens, 4) || off(r.logprob, 4) || off(r.rank, 4) ||
+        off(r.entropy, 4) || off(r.top_ids, 4) || off(r.top_logprobs, 4) || off(workspace, 16))
+      return PPAS_EINVAL;
+    if (!r.logprob && !r.rank && !r.entropy && !r.top) return PPAS_OK;
+    const DeviceInfo dev = current_device();
+    if (!dev.gfx950) return PPAS_EUNSUPPORTED;
+    int splits = logprob_splits(n_rows, vocab, dev.cus);
+    while (splits > 1 && logprob_workspace_bytes(n_rows, r.top, splits) > workspace_bytes) --splits;
+    const hipError_t e = launch_logprobs(r, splits, workspace, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
+                                         ev_of(events, 1));
+    return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
+  } catch (...) {
+    return PPAS_EINVAL;
+  }
 }
 
 ppas_status ppas_stream_read(const void* buf, size_t bytes, void* sink, const ppas_events* events,

@@ -93,6 +93,11 @@ class HeadNorm(ctypes.Structure):
     tensor = None   # the weights, which head_norm keeps
 
 
+class LogprobOut(ctypes.Structure):
+    _fields_ = [("logprob", ctypes.c_void_p), ("rank", ctypes.c_void_p), ("entropy", ctypes.c_void_p),
+                ("top_ids", ctypes.c_void_p), ("top_logprobs", ctypes.c_void_p)]
+
+
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 
@@ -177,6 +182,11 @@ for _f in (_lib.ppas_gateup_proj_i8, _lib.ppas_gateup_act_i8):
 for _f in (_lib.ppas_gateup_i8_workspace_bytes, _lib.ppas_gateup_act_i8_workspace_bytes):
     _f.restype = _sz
     _f.argtypes = [_i32, _i32, _i32]
+_lib.ppas_logprobs.restype = ctypes.c_int
+_lib.ppas_logprobs.argtypes = [_vp, _i32, _i64, _i32, _i32, ctypes.c_float, _vp, _i32, ctypes.POINTER(LogprobOut), _vp, _sz,
+                               _E, _vp]
+_lib.ppas_logprobs_workspace_bytes.restype = _sz
+_lib.ppas_logprobs_workspace_bytes.argtypes = [_i32, _i32, _i32]
 
 
 def status_string(status: int) -> str:
@@ -668,6 +678,44 @@ def gateup_act_i8(x, x_scale, w, w_scale, y, workspace=None, events: Events | No
     """The gated activation of such products, as gateup_act (w [2I, H], y [T, I]).
     workspace: see gateup_act_i8_workspace_bytes, or None."""
     _gateup_i8(_lib.ppas_gateup_act_i8, "ppas_gateup_act_i8", x, x_scale, w, w_scale, y, 2, workspace, events, stream)
+
+
+def logprobs_workspace_bytes(n_rows: int, vocab: int, top_k: int = 0) -> int:
+    return int(_lib.ppas_logprobs_workspace_bytes(int(n_rows), int(vocab), int(top_k)))
+
+
+def _result(t, name, dtype, *shape):
+    """The pointer of an optional result of that type and shape."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    return _dev(t, name)
+
+
+def logprobs(logits, tokens=None, logprob=None, rank=None, entropy=None, top_ids=None, top_logprobs=None, scale: float = 1.0,
+             workspace=None, events: Events | None = None, stream=None) -> None:
+    """Log probabilities from logits [R, V] (bf16 or fp32, any row stride), times `scale`: into logprob (fp32 [R]) and rank
+    (int32 [R]) those of tokens (int32 [R]), into entropy (fp32 [R]) the rows', into top_ids (int32 [R, k]) and top_logprobs
+    (fp32 [R, k]) the top k tokens. Results that are None are left out. workspace: see logprobs_workspace_bytes, or None."""
+    if logits.dim() != 2 or (logits.dtype not in _BF16 and logits.dtype != torch.float32) or \
+            (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits must be 2-D bf16 or fp32 rows, got {tuple(logits.shape)} {logits.dtype}")
+    R, V = logits.shape
+    k = next((t.shape[-1] for t in (top_ids, top_logprobs) if t is not None and t.dim() > 0), 0)
+    f32, i32 = torch.float32, torch.int32
+    tp = _result(tokens, "tokens", i32, R)
+    out = LogprobOut(_result(logprob, "logprob", f32, R), _result(rank, "rank", i32, R), _result(entropy, "entropy", f32, R),
+                     _result(top_ids, "top_ids", i32, R, k), _result(top_logprobs, "top_logprobs", f32, R, k))
+    if not logits.is_cuda:
+        raise ValueError("logits must be a device tensor")
+    ws = _dev(workspace, "workspace")
+    hs = _here(stream, logits, tokens, logprob, rank, entropy, top_ids, top_logprobs, workspace)
+    st = _lib.ppas_logprobs(logits.data_ptr(), int(logits.dtype == f32), logits.stride(0) if R > 1 else max(logits.stride(0), V),
+                            R, V, float(scale), tp, k, ctypes.byref(out), ws,
+                            0 if workspace is None else workspace.numel() * workspace.element_size(),
+                            None if events is None else ctypes.byref(events), hs)
+    _check(st, "ppas_logprobs")
 
 
 def stream_read(buf, sink, events: Events | None = None, stream=None) -> None:
