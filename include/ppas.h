@@ -618,6 +618,70 @@ size_t ppas_gateup_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t 
 size_t ppas_gateup_act_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t n_inter);
 
 /*
+ * Low-rank adapters of many requests beside a shared projection (the library's own; the
+ * paper's requests run the plain model). A set holds n_adapters adapters of one projection
+ * from `hidden` to n_out features: A [n_adapters][rank][hidden] and B [n_adapters][n_out]
+ * [rank] bf16, contiguous, and a scale each; ranks below the set's are padded with zeros. A
+ * row t with adapter a gets
+ *   out[t] = y[t] + scale[a] (x[t] A_a^T) B_a^T
+ * on top of the projection's output y (any projection of this library or another, bf16),
+ * and a row of no adapter out[t] = y[t]. The product with A is summed in fp32, taken on with
+ * 16 bits, summed in fp32 with y and rounded once to bf16 nearest-even. Weights have to be
+ * finite.
+ *
+ * Rows of one adapter may lie anywhere in a step: ppas_adapter_rows brings the row numbers
+ * into the order of their adapters once per step, for every layer and projection that uses
+ * as many adapters. row_adapter_dev [n_tokens] holds the rows' adapters; -1, like every
+ * number outside 0..n_adapters - 1, is a row without one. `rows` is device memory of
+ * ppas_adapter_rows_bytes(n_tokens, n_adapters) on 16 bytes; the calls that read it have to
+ * be given the n_tokens and adapters it was made for (others' results are undefined, but
+ * stay inside the call's rows) and must come behind it on their stream.
+ */
+typedef struct ppas_adapters {
+  const void* a;
+  const void* b;
+  const float* scale;    /* device fp32 [n_adapters]; NULL: 1 */
+  int32_t n_adapters;    /* 1..1024 (PPAS_EUNSUPPORTED above) */
+  int32_t rank;          /* 1..128 (PPAS_EUNSUPPORTED above) */
+  int32_t hidden, n_out;
+} ppas_adapters;
+
+size_t ppas_adapter_rows_bytes(int32_t n_tokens, int32_t n_adapters);
+
+ppas_status ppas_adapter_rows(const int32_t* row_adapter_dev, int32_t n_tokens, int32_t n_adapters, void* rows,
+                              size_t rows_bytes, const ppas_events* events, void* hip_stream);
+
+/*
+ * The adapters' share added to y [n_tokens][n_out], x being the projection's input
+ * [n_tokens][hidden]; strides are elements between rows, so that parts of fused rows may be
+ * given. out may be y with the same stride: rows without an adapter are then not touched;
+ * otherwise it must not overlap y, nor ever x (PPAS_EINVAL, as for strides below a row's
+ * features). `workspace` is device memory of ppas_adapter_workspace_bytes() on 16 bytes (a
+ * smaller one is PPAS_ENOSPACE). Bases and strides on 16 bytes with hidden, rank and n_out
+ * that are multiples of 8 are faster. Two launches (events: start on the first, stop on the
+ * last); nothing is allocated or kept, and calls may be captured into a HIP graph; calls
+ * that share a workspace must not run at once. A row's result may differ in the rounding
+ * of its sums with n_tokens and n_adapters, on which the split of hidden depends.
+ * n_tokens == 0 is a no-op, above 2^24 PPAS_ERANGE.
+ */
+ppas_status ppas_adapter_add(const ppas_adapters* set, const void* x, int64_t x_stride, const void* y, int64_t y_stride,
+                             void* out, int64_t out_stride, int32_t n_tokens, const void* rows, size_t rows_bytes,
+                             void* workspace, size_t workspace_bytes, const ppas_events* events, void* hip_stream);
+
+/*
+ * The same before the MLP's gated activation: y holds the gate and up halves [n_tokens]
+ * [n_out] as ppas_gateup_proj (or ppas_gateup_proj_i8) writes them, B the rows of both, and
+ *   out[t][f] = silu(g) u,  f < n_out / 2
+ * with g and u the two halves of y[t] with the adapters' share, not rounded before; out
+ * [n_tokens][n_out / 2] must not overlap y or x. n_out is even.
+ */
+ppas_status ppas_adapter_act(const ppas_adapters* set, const void* x, int64_t x_stride, const void* y, int64_t y_stride,
+                             void* out, int64_t out_stride, int32_t n_tokens, const void* rows, size_t rows_bytes,
+                             void* workspace, size_t workspace_bytes, const ppas_events* events, void* hip_stream);
+
+size_t ppas_adapter_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t rank, int32_t n_adapters);
+
+/*
  * Log probabilities of logit rows, as a request is answered with them: of a given token per
  * row (a sampled one, or a prompt's next), its rank, the row's entropy and the top
  * alternatives (the library's own; the paper's requests are measured, not read). Row r <

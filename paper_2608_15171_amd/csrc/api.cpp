@@ -10,6 +10,7 @@
 #include <utility>
 #include <vector>
 
+#include "adapters.h"
 #include "device.h"
 #include "list_pool.h"
 #include "logprobs.h"
@@ -851,6 +852,117 @@ ppas_status ppas_gateup_i8_choice(int32_t n_tokens, int32_t hidden, int32_t n_ou
   gateup_i8_choice(n_tokens, hidden, n_out, activation != 0, aligned != 0,
                    allowed_splits_i8(n_tokens, hidden, n_out, workspace_bytes, cus), cus, choice);
   return PPAS_OK;
+}
+
+namespace {
+
+constexpr int32_t kMaxAdapterRows = 1 << 24;   // token rows of an adapters' call
+
+ppas_status check_adapter_rows(int32_t n_tokens, int32_t n_adapters) {
+  if (n_tokens < 0 || n_adapters <= 0) return PPAS_EINVAL;
+  if (n_adapters > kAdaptersMax) return PPAS_EUNSUPPORTED;
+  return n_tokens > kMaxAdapterRows ? PPAS_ERANGE : PPAS_OK;
+}
+
+ppas_status check_adapter_sizes(int32_t n_tokens, int32_t hidden, int32_t rank, int32_t n_adapters) {
+  const ppas_status st = check_adapter_rows(n_tokens, n_adapters);
+  if (st != PPAS_OK) return st;
+  if (hidden <= 0 || rank <= 0) return PPAS_EINVAL;
+  if (rank > kAdapterMaxRank) return PPAS_EUNSUPPORTED;
+  return hidden > INT32_MAX - 512 ? PPAS_ERANGE : PPAS_OK;
+}
+
+ppas_status adapter_call(const ppas_adapters* set, const void* x, int64_t x_stride, const void* y, int64_t y_stride,
+                         void* out, int64_t out_stride, int32_t n_tokens, const void* rows, size_t rows_bytes, bool act,
+                         void* workspace, size_t workspace_bytes, const ppas_events* events, void* hip_stream) {
+  if (!set) return PPAS_EINVAL;
+  ppas_status st = check_adapter_sizes(n_tokens, set->hidden, set->rank, set->n_adapters);
+  if (st != PPAS_OK) return st;
+  if (set->n_out <= 0 || (act && set->n_out % 2 != 0)) return PPAS_EINVAL;
+  if (set->n_out > INT32_MAX - 512) return PPAS_ERANGE;
+  st = check_events(events);
+  if (st != PPAS_OK || n_tokens == 0) return st;
+  const int64_t cols = act ? set->n_out / 2 : set->n_out, most = (int64_t(1) << 61) / n_tokens;
+  if (!set->a || !set->b || !x || !y || !out || !rows || !workspace) return PPAS_EINVAL;
+  if (x_stride < set->hidden || y_stride < set->n_out || out_stride < cols) return PPAS_EINVAL;
+  if (x_stride > most || y_stride > most || out_stride > most) return PPAS_ERANGE;
+  if (off(set->a, 2) || off(set->b, 2) || off(set->scale, 4) || off(x, 2) || off(y, 2) || off(out, 2) || off(rows, 16) ||
+      off(workspace, 16))
+    return PPAS_EINVAL;
+  const uint64_t out_bytes = span_bytes(n_tokens, out_stride, cols);
+  const bool in_place = !act && out == y && out_stride == y_stride;
+  if ((!in_place && overlap(out, out_bytes, y, span_bytes(n_tokens, y_stride, set->n_out))) ||
+      overlap(out, out_bytes, x, span_bytes(n_tokens, x_stride, set->hidden)))
+    return PPAS_EINVAL;
+  if (rows_bytes < AdapterOrder{n_tokens, set->n_adapters}.bytes()) return PPAS_ENOSPACE;
+  const DeviceInfo dev = current_device();
+  if (!dev.gfx950) return PPAS_EUNSUPPORTED;
+  if (workspace_bytes < adapter_workspace_bytes(n_tokens, set->hidden, set->rank, set->n_adapters, dev.cus))
+    return PPAS_ENOSPACE;
+  const AdapterCall c{static_cast<const uint16_t*>(set->a), static_cast<const uint16_t*>(set->b), set->scale,
+                      static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(y), static_cast<uint16_t*>(out),
+                      x_stride, y_stride, out_stride, n_tokens, set->hidden, set->n_out, set->rank, set->n_adapters,
+                      rows, static_cast<float*>(workspace)};
+  const hipError_t e = launch_adapters(c, act, dev.cus, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
+                                       ev_of(events, 1));
+  return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
+}
+
+}  // namespace
+
+size_t ppas_adapter_rows_bytes(int32_t n_tokens, int32_t n_adapters) {
+  if (check_adapter_rows(n_tokens, n_adapters) != PPAS_OK || n_tokens == 0) return 0;
+  return AdapterOrder{n_tokens, n_adapters}.bytes();
+}
+
+ppas_status ppas_adapter_rows(const int32_t* row_adapter_dev, int32_t n_tokens, int32_t n_adapters, void* rows,
+                              size_t rows_bytes, const ppas_events* events, void* hip_stream) {
+  try {
+    ppas_status st = check_adapter_rows(n_tokens, n_adapters);
+    if (st != PPAS_OK) return st;
+    st = check_events(events);
+    if (st != PPAS_OK || n_tokens == 0) return st;
+    if (!row_adapter_dev || !rows || off(row_adapter_dev, 4) || off(rows, 16)) return PPAS_EINVAL;
+    const AdapterOrder o{n_tokens, n_adapters};
+    if (rows_bytes < o.bytes()) return PPAS_ENOSPACE;
+    if (!current_device().gfx950) return PPAS_EUNSUPPORTED;
+    const hipError_t e = launch_adapter_rows(row_adapter_dev, o, rows, static_cast<hipStream_t>(hip_stream),
+                                             ev_of(events, 0), ev_of(events, 1));
+    return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
+  } catch (...) {
+    return PPAS_EINVAL;
+  }
+}
+
+size_t ppas_adapter_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t rank, int32_t n_adapters) {
+  if (check_adapter_sizes(n_tokens, hidden, rank, n_adapters) != PPAS_OK || n_tokens == 0) return 0;
+  try {
+    return adapter_workspace_bytes(n_tokens, hidden, rank, n_adapters, current_device().cus);
+  } catch (...) {
+    return 0;
+  }
+}
+
+ppas_status ppas_adapter_add(const ppas_adapters* set, const void* x, int64_t x_stride, const void* y, int64_t y_stride,
+                             void* out, int64_t out_stride, int32_t n_tokens, const void* rows, size_t rows_bytes,
+                             void* workspace, size_t workspace_bytes, const ppas_events* events, void* hip_stream) {
+  try {
+    return adapter_call(set, x, x_stride, y, y_stride, out, out_stride, n_tokens, rows, rows_bytes, false, workspace,
+                        workspace_bytes, events, hip_stream);
+  } catch (...) {
+    return PPAS_EINVAL;
+  }
+}
+
+ppas_status ppas_adapter_act(const ppas_adapters* set, const void* x, int64_t x_stride, const void* y, int64_t y_stride,
+                             void* out, int64_t out_stride, int32_t n_tokens, const void* rows, size_t rows_bytes,
+                             void* workspace, size_t workspace_bytes, const ppas_events* events, void* hip_stream) {
+  try {
+    return adapter_call(set, x, x_stride, y, y_stride, out, out_stride, n_tokens, rows, rows_bytes, true, workspace,
+                        workspace_bytes, events, hip_stream);
+  } catch (...) {
+    return PPAS_EINVAL;
+  }
 }
 
 namespace {

@@ -93,6 +93,13 @@ class HeadNorm(ctypes.Structure):
     tensor = None   # the weights, which head_norm keeps
 
 
+class Adapters(ctypes.Structure):
+    """Low-rank adapters of one projection: see ppas_adapters, and adapters() below."""
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("n_adapters", ctypes.c_int32),
+                ("rank", ctypes.c_int32), ("hidden", ctypes.c_int32), ("n_out", ctypes.c_int32)]
+    tensors = ()   # the weights, which adapters() keeps
+
+
 class LogprobOut(ctypes.Structure):
     _fields_ = [("logprob", ctypes.c_void_p), ("rank", ctypes.c_void_p), ("entropy", ctypes.c_void_p),
                 ("top_ids", ctypes.c_void_p), ("top_logprobs", ctypes.c_void_p)]
@@ -182,6 +189,15 @@ for _f in (_lib.ppas_gateup_proj_i8, _lib.ppas_gateup_act_i8):
 for _f in (_lib.ppas_gateup_i8_workspace_bytes, _lib.ppas_gateup_act_i8_workspace_bytes):
     _f.restype = _sz
     _f.argtypes = [_i32, _i32, _i32]
+_lib.ppas_adapter_rows_bytes.restype = _sz
+_lib.ppas_adapter_rows_bytes.argtypes = [_i32, _i32]
+_lib.ppas_adapter_rows.restype = ctypes.c_int
+_lib.ppas_adapter_rows.argtypes = [_vp, _i32, _i32, _vp, _sz, _E, _vp]
+_lib.ppas_adapter_workspace_bytes.restype = _sz
+_lib.ppas_adapter_workspace_bytes.argtypes = [_i32, _i32, _i32, _i32]
+for _f in (_lib.ppas_adapter_add, _lib.ppas_adapter_act):
+    _f.restype = ctypes.c_int
+    _f.argtypes = [ctypes.POINTER(Adapters), _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _sz, _vp, _sz, _E, _vp]
 _lib.ppas_logprobs.restype = ctypes.c_int
 _lib.ppas_logprobs.argtypes = [_vp, _i32, _i64, _i32, _i32, ctypes.c_float, _vp, _i32, ctypes.POINTER(LogprobOut), _vp, _sz,
                                _E, _vp]
@@ -678,6 +694,89 @@ def gateup_act_i8(x, x_scale, w, w_scale, y, workspace=None, events: Events | No
     """The gated activation of such products, as gateup_act (w [2I, H], y [T, I]).
     workspace: see gateup_act_i8_workspace_bytes, or None."""
     _gateup_i8(_lib.ppas_gateup_act_i8, "ppas_gateup_act_i8", x, x_scale, w, w_scale, y, 2, workspace, events, stream)
+
+
+class AdapterRows:
+    """A step's rows in the order of their adapters (ppas_adapter_rows), in device memory of its own: sorted once per step,
+    used by every adapter_add and adapter_act of the step."""
+
+    def __init__(self, n_tokens: int, n_adapters: int, device="cuda"):
+        self.n_tokens, self.n_adapters, self.sorted = int(n_tokens), int(n_adapters), False
+        size = int(_lib.ppas_adapter_rows_bytes(self.n_tokens, self.n_adapters))
+        if size == 0 and self.n_tokens != 0:
+            raise ValueError(f"no rows of {self.n_tokens} tokens and {self.n_adapters} adapters")
+        self.buf = torch.empty(max(size, 16), dtype=torch.uint8, device=device)
+
+    def sort(self, row_adapter, events: Events | None = None, stream=None) -> None:
+        """row_adapter: int32 [n_tokens], the rows' adapters (-1: none)."""
+        if row_adapter.dtype != torch.int32 or tuple(row_adapter.shape) != (self.n_tokens,):
+            raise ValueError(f"row_adapter must be int32 [{self.n_tokens}], got {row_adapter.dtype} {tuple(row_adapter.shape)}")
+        p, q = _dev(row_adapter, "row_adapter"), _dev(self.buf, "rows")
+        hs = _here(stream, row_adapter, self.buf)
+        st = _lib.ppas_adapter_rows(p, self.n_tokens, self.n_adapters, q, self.buf.numel(),
+                                    None if events is None else ctypes.byref(events), hs)
+        _check(st, "ppas_adapter_rows")
+        self.sorted = True
+
+
+def adapters(a, b, scale=None) -> Adapters:
+    """Low-rank adapters of one projection: a [n, rank, hidden] and b [n, out, rank] bf16, scale fp32 [n] or None (1).
+    Keeps the tensors."""
+    if not (a.dim() == b.dim() == 3 and a.dtype in _BF16 and b.dtype in _BF16 and a.shape[0] == b.shape[0] and
+            a.shape[1] == b.shape[2]):
+        raise ValueError(f"a must be [n, rank, hidden] and b [n, out, rank] of bf16, got {tuple(a.shape)} {a.dtype} and "
+                         f"{tuple(b.shape)} {b.dtype}")
+    n, r, h = a.shape
+    if scale is not None and (scale.dtype != torch.float32 or tuple(scale.shape) != (n,)):
+        raise ValueError(f"scale must be fp32 [{n}], got {scale.dtype} {tuple(scale.shape)}")
+    s = Adapters(_dev(a, "a"), _dev(b, "b"), _dev(scale, "scale"), n, r, h, b.shape[1])
+    s.tensors = (a, b) if scale is None else (a, b, scale)
+    return s
+
+
+def adapter_workspace_bytes(n_tokens: int, hidden: int, rank: int, n_adapters: int) -> int:
+    return int(_lib.ppas_adapter_workspace_bytes(int(n_tokens), int(hidden), int(rank), int(n_adapters)))
+
+
+def _packed_rows(t, name, rows: int, cols: int):
+    """The pointer and row stride of a device tensor [rows, cols] of bf16 with packed rows at any stride."""
+    if t.dim() != 2 or t.dtype not in _BF16 or tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name} must be bf16 [{rows}, {cols}], got {tuple(t.shape)} {t.dtype}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"the rows of {name} must be packed")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), cols)
+
+
+def _adapt(fn, what, adapters, x, y, out, rows, per, workspace, events, stream):
+    if x.dim() != 2:
+        raise ValueError(f"x must be 2-D, got {tuple(x.shape)}")
+    T, N = x.shape[0], adapters.n_out
+    if rows.n_tokens != T or rows.n_adapters != adapters.n_adapters:
+        raise ValueError(f"rows are of {rows.n_tokens} tokens and {rows.n_adapters} adapters, the call of {T} and "
+                         f"{adapters.n_adapters}")
+    if not rows.sorted:
+        raise ValueError("rows have not been sorted")
+    if N % per:
+        raise ValueError(f"{N} outputs are not a gate and an up half")
+    ptrs = (*_packed_rows(x, "x", T, adapters.hidden), *_packed_rows(y, "y", T, N), *_packed_rows(out, "out", T, N // per))
+    ws = _dev(workspace, "workspace")
+    hs = _here(stream, x, y, out, workspace, rows.buf, *adapters.tensors)
+    st = fn(ctypes.byref(adapters), *ptrs, T, rows.buf.data_ptr(), rows.buf.numel(), ws,
+            workspace.numel() * workspace.element_size(), None if events is None else ctypes.byref(events), hs)
+    _check(st, what)
+
+
+def adapter_add(adapters: Adapters, x, y, out, rows: AdapterRows, workspace, events: Events | None = None, stream=None) -> None:
+    """out = y with the adapters' share of its rows: x [T, hidden] the projection's input, y and out [T, n_out] (bf16 rows at
+    any stride; out may be y). workspace: a device buffer of adapter_workspace_bytes."""
+    _adapt(_lib.ppas_adapter_add, "ppas_adapter_add", adapters, x, y, out, rows, 1, workspace, events, stream)
+
+
+def adapter_act(adapters: Adapters, x, y, out, rows: AdapterRows, workspace, events: Events | None = None, stream=None) -> None:
+    """out [T, n_out / 2] = silu(g) * u of the halves g and u of y with the adapters' share; otherwise as adapter_add."""
+    _adapt(_lib.ppas_adapter_act, "ppas_adapter_act", adapters, x, y, out, rows, 2, workspace, events, stream)
 
 
 def logprobs_workspace_bytes(n_rows: int, vocab: int, top_k: int = 0) -> int:
