@@ -11,9 +11,10 @@ namespace ppas {
 constexpr int kAdaptersMax = 1024, kAdapterMaxRank = 128;
 
 // Rows of one adapter (-1: of none): places first .. first + count - 1 of the order, at
-// most 16 or 64 of them.
+// most 16 or 64 of them. `row` is the first one where they follow each other, -1 otherwise:
+// a decode row's number then comes with its tile, and a chunk's.
 struct AdapterTile {
-  int32_t adapter, first, count, pad;
+  int32_t adapter, first, count, row;
 };
 static_assert(sizeof(AdapterTile) == 16, "read as one vector");
 

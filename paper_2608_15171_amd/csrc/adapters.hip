@@ -68,12 +68,24 @@ __global__ __launch_bounds__(kSortThreads) void adapter_rows_kernel(const int32_
   __syncthreads();
   const int32_t per = (o.T + kSortThreads - 1) / kSortThreads * 64;   // rows of a wave, whole steps
   const int64_t lo = int64_t(wave) * per, hi = min(lo + per, int64_t(o.T));
+  // a step's groups and their lanes; a wave's first step keeps them for its rows' places
+  struct Step {
+    int g;
+    uint64_t same;
+    bool valid;
+  };
+  auto look = [&](int64_t t) {
+    Step s;
+    s.valid = t + lane < hi;
+    s.g = s.valid ? group_of(row_adapter[t + lane], o.n) : 0;
+    s.same = same_group(s.g, s.valid);
+    return s;
+  };
+  const Step kept = look(lo);
   for (int64_t t = lo; t < hi; t += 64) {
-    const bool valid = t + lane < hi;
-    const int g = valid ? group_of(row_adapter[t + lane], o.n) : 0;
-    const uint64_t same = same_group(g, valid);
+    const Step s = t == lo ? kept : look(t);
     // the group's first lane counts for all
-    if (valid && lane == int(__ffsll((unsigned long long)same)) - 1) count[wave][g] += int(__popcll(same));
+    if (s.valid && lane == int(__ffsll((unsigned long long)s.same)) - 1) count[wave][s.g] += int(__popcll(s.same));
   }
   __syncthreads();
   for (int g = tid; g < groups; g += kSortThreads) {
@@ -108,30 +120,30 @@ __global__ __launch_bounds__(kSortThreads) void adapter_rows_kernel(const int32_
     }
   }
   __syncthreads();
+  for (int64_t t = lo; t < hi; t += 64) {
+    const Step s = t == lo ? kept : look(t);
+    if (!s.valid) continue;
+    const int before = int(__popcll(s.same & ((uint64_t(1) << lane) - 1)));
+    const int base = count[wave][s.g];
+    order[first[s.g] + base + before] = int32_t(t + lane);
+    // behind every lane's read: a wave's accesses to LDS are in order
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (before == 0) count[wave][s.g] = base + int(__popcll(s.same));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  __syncthreads();   // the order is read below
   auto list = [&](AdapterTile* tiles, const int32_t* starts, int height) {
     for (int i = tid; i < starts[groups]; i += kSortThreads) {
       int g = 0;   // the last group that starts at or before tile i
       for (int d = 1024; d >= 1; d >>= 1)
         if (g + d < groups && starts[g + d] <= i) g += d;
-      const int at = first[g] + (i - starts[g]) * height;
-      tiles[i] = AdapterTile{g < o.n ? g : -1, at, min(height, first[g + 1] - at), 0};
+      const int at = first[g] + (i - starts[g]) * height, n = min(height, first[g + 1] - at);
+      const int32_t row = order[at], last = order[at + n - 1];
+      tiles[i] = AdapterTile{g < o.n ? g : -1, at, n, last - row == n - 1 ? row : -1};
     }
   };
   list(tiles16, first16, 16);
   list(tiles64, first64, 64);
-  for (int64_t t = lo; t < hi; t += 64) {
-    const bool valid = t + lane < hi;
-    const int g = valid ? group_of(row_adapter[t + lane], o.n) : 0;
-    const uint64_t same = same_group(g, valid);
-    if (!valid) continue;
-    const int before = int(__popcll(same & ((uint64_t(1) << lane) - 1)));
-    const int base = count[wave][g];
-    order[first[g] + base + before] = int32_t(t + lane);
-    // behind every lane's read: a wave's accesses to LDS are in order
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (before == 0) count[wave][g] = base + int(__popcll(same));
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  }
 }
 
 // ---------------------------------------------------------------------------
@@ -144,6 +156,7 @@ struct AdapterArgs {
   const int32_t* order;
   int64_t slots;              // of the tile list
   int32_t splits, per;        // of hidden: per features each, a multiple of 256
+  int32_t parts;              // of a tile that are workgroups of their own in the first product
   int32_t blocks, block;      // of the outputs: `block` columns each
   bool rows_vec;              // y and out by 16 bytes
   bool in_place;
@@ -152,15 +165,14 @@ struct AdapterArgs {
 // The tile of a workgroup. What it says is checked against the call: an order that was
 // made for another one reads and writes nothing past the call's rows.
 __device__ __forceinline__ bool tile_of(const AdapterArgs& a, int64_t i, int height, AdapterTile& t) {
-  const int64_t n = height == 16 ? a.head->tiles16 : a.head->tiles64;
-  if (i >= min(n, a.slots)) return false;
-  t = a.tiles[i];
-  return t.adapter >= -1 && t.adapter < a.c.adapters && t.count >= 1 && t.count <= height && t.first >= 0 &&
+  const int64_t n = height == 16 ? a.head->tiles16 : a.head->tiles64;   // both asked for at once
+  t = a.tiles[min(i, a.slots - 1)];
+  return i < min(n, a.slots) && t.adapter >= -1 && t.adapter < a.c.adapters && t.count >= 1 && t.count <= height && t.first >= 0 &&
          t.first <= a.c.T - t.count;
 }
 __device__ __forceinline__ int32_t row_of(const AdapterArgs& a, const AdapterTile& t, int local) {
-  const int32_t r = a.order[t.first + min(local, t.count - 1)];   // rows past the tile's are its last one again
-  return min(max(r, 0), a.c.T - 1);
+  const int at = min(local, t.count - 1);   // rows past the tile's are its last one again
+  return min(max(t.row >= 0 ? t.row + at : a.order[t.first + at], 0), a.c.T - 1);
 }
 
 // Eight elements of a row of n, from element k on: zeros past its end.
@@ -177,56 +189,98 @@ __device__ __forceinline__ u32x4 eight(const uint16_t* row, int64_t k, int64_t n
   return v;
 }
 
-// v = x A^T. A workgroup takes a tile of 16 MF rows, 16 RF ranks and a split of hidden; its
-// waves take 64 features of every 256 and add up through LDS.
+// LDS that the lanes of one wave exchange: in order as it is, but not for the compiler.
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+// Both products bring their operands as 16-byte pieces of whole 128-byte lines, eight lanes
+// to a row, and turn them into operand order in LDS, as they turn the share into the order
+// of y's memory. Straight in the order of the matrix instructions, 64 bytes of a row at a
+// time, 16,384 rows of rank 64 onto 22,016 columns took 754 us where this takes 312 (a copy
+// of as many bytes 288).
+
+// v = x A^T. A workgroup takes a tile of 16 MF rows (half of one of 64), 16 RF ranks and a
+// split of hidden; its waves take 64 features of every 256 and add up through LDS. Each wave
+// for itself, without a barrier on the way; whole tiles of 64 rows leave a compute unit one
+// workgroup (16,384 rows of rank 64: 21 us either way, 700 rows of 11,008: 9.4 against 8.2).
+constexpr int kDownPitch = 72;   // elements of a row of 64 in LDS: 16 rows' reads spread over the banks
+
 template <int MF, int RF, bool kVec>
 __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs a) {
-  constexpr int F = MF * RF, kBatch = F < 8 ? F : 8;
-  __shared__ f32x4 sums[4][kBatch][64];
+  constexpr int F = MF * RF, kBatch = F < 8 ? F : 8, kRows = 16 * (MF + RF), kLoads = kRows / 8;
+  constexpr int kStage = 4 * kRows * kDownPitch * 2, kSums = 4 * kBatch * 64 * 16;
+  __shared__ __attribute__((aligned(16))) char smem[kStage > kSums ? kStage : kSums];
   const int64_t block = block_of();
   AdapterTile t;
-  if (!tile_of(a, block / a.splits, 16 * MF, t) || t.adapter < 0) return;
+  // a tile of the list is `parts` of the workgroup's rows
+  const int64_t which = block / a.splits;
+  if (!tile_of(a, which / a.parts, 16 * MF * a.parts, t) || t.adapter < 0) return;
+  const int skip = int(which % a.parts) * 16 * MF;
+  if (skip >= t.count) return;
+  t.first += skip;
+  t.count = min(t.count - skip, 16 * MF);
+  if (t.row >= 0) t.row += skip;
   const int split = int(block % a.splits);
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, col = lane & 15, g = lane >> 4;
   const int64_t H = a.c.hidden;
-  const uint16_t *x[MF], *w[RF];
+  uint16_t* stage = reinterpret_cast<uint16_t*>(smem) + wave * kRows * kDownPitch;
+  // the lane's rows: the tile's of x, then the adapter's of A; those past either's end are zeros
+  const int piece = 8 * (lane % 8);
+  const uint16_t* src[kLoads];
 #pragma unroll
-  for (int m = 0; m < MF; ++m) x[m] = a.c.x + row_of(a, t, 16 * m + col) * a.c.x_stride;
-#pragma unroll
-  for (int r = 0; r < RF; ++r)
-    w[r] = a.c.a + (int64_t(t.adapter) * a.c.rank + min(16 * r + col, a.c.rank - 1)) * H;
+  for (int j = 0; j < kLoads; ++j) {
+    const int row = 8 * j + lane / 8, rank = row - 16 * MF;
+    if (j < 2 * MF) src[j] = row < t.count ? a.c.x + row_of(a, t, row) * a.c.x_stride + piece : nullptr;
+    else src[j] = rank < a.c.rank ? a.c.a + (int64_t(t.adapter) * a.c.rank + rank) * H + piece : nullptr;
+  }
   f32x4 acc[MF][RF];
 #pragma unroll
   for (int m = 0; m < MF; ++m)
 #pragma unroll
     for (int r = 0; r < RF; ++r) acc[m][r] = Bf16::zero();
   const int64_t k1 = min(H, (int64_t(split) + 1) * a.per);
-  for (int64_t k = int64_t(split) * a.per + 64 * wave; k < k1; k += 256) {
+  u32x4 raw[kLoads];
+  auto bring = [&](int64_t k) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      raw[j] = u32x4{0, 0, 0, 0};
+      if (src[j]) raw[j] = eight<kVec>(src[j], k, H - piece);
+    }
+  };
+  int64_t k = int64_t(split) * a.per + 64 * wave;
+  if (k < k1) bring(k);
+  for (; k < k1; k += 256) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      *reinterpret_cast<u32x4*>(stage + (8 * j + lane / 8) * kDownPitch + piece) = raw[j];
+    wave_fence();
+    if (k + 256 < k1) bring(k + 256);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t at = k + 32 * h + 8 * g;
       u32x4 fx[MF], fw[RF];
+      const uint16_t* at = stage + col * kDownPitch + 32 * h + 8 * g;
 #pragma unroll
-      for (int m = 0; m < MF; ++m) fx[m] = eight<kVec>(x[m], at, H);
+      for (int m = 0; m < MF; ++m) fx[m] = *reinterpret_cast<const u32x4*>(at + 16 * m * kDownPitch);
 #pragma unroll
-      for (int r = 0; r < RF; ++r) fw[r] = eight<kVec>(w[r], at, H);
+      for (int r = 0; r < RF; ++r) fw[r] = *reinterpret_cast<const u32x4*>(at + 16 * (MF + r) * kDownPitch);
 #pragma unroll
       for (int m = 0; m < MF; ++m)
 #pragma unroll
         for (int r = 0; r < RF; ++r) acc[m][r] = Bf16::mma(fw[r], fx[m], acc[m][r]);
     }
+    wave_fence();
   }
+  f32x4* sums = reinterpret_cast<f32x4*>(smem);   // [4][kBatch][64]
   float* part = a.c.part + (int64_t(split) * a.c.T + t.first) * (16 * RF);
 #pragma unroll
   for (int f0 = 0; f0 < F; f0 += kBatch) {
-    if (f0) __syncthreads();
+    __syncthreads();
 #pragma unroll
-    for (int f = 0; f < kBatch; ++f) sums[wave][f][lane] = acc[(f0 + f) / RF][(f0 + f) % RF];
+    for (int f = 0; f < kBatch; ++f) sums[(wave * kBatch + f) * 64 + lane] = acc[(f0 + f) / RF][(f0 + f) % RF];
     __syncthreads();
     for (int f = wave; f < kBatch; f += 4) {
-      f32x4 s = sums[0][f][lane];
+      f32x4 s = sums[f * 64 + lane];
 #pragma unroll
-      for (int i = 1; i < 4; ++i) s += sums[i][f][lane];
+      for (int i = 1; i < 4; ++i) s += sums[(i * kBatch + f) * 64 + lane];
       const int row = 16 * ((f0 + f) / RF) + col;
       if (row < t.count)
         *reinterpret_cast<f32x4*>(part + int64_t(row) * (16 * RF) + 16 * ((f0 + f) % RF) + 4 * g) = s;
@@ -269,124 +323,174 @@ __device__ __forceinline__ void row_store(uint16_t* row, int n, int lim, bool ve
   }
 }
 
-// out = y + (s v) B^T. A workgroup takes a tile of 16 MF rows and a block of columns; a wave
-// 32 kPairs columns at a time (kAct: half of them gate, half up of the same features). The
-// rows of B go to the matrix instructions in an order that leaves a lane with eight columns
-// of one row, 16 bytes of y. Up to rank 16 (RS = 0) one instruction takes both numbers of
-// s v against the same B; else RS of 32 ranks each take B once for two.
-template <int MF, int RS, bool kVec, bool kAct>
+// out = y + (s v) B^T. A workgroup takes a tile and a block of columns; a wave 16 rows and 64
+// columns at a time: of a tile of 64 rows each wave its own rows and all the same columns,
+// whose rows of B they share in LDS, two steps in turn with one barrier each (kWide); of a
+// tile of 16 each wave its own columns and B. The share goes through LDS into the order of
+// memory, 128 bytes of a row to eight lanes. With the activation a step is 64 gate columns
+// and the up columns of the same features. Up to rank 16 (RS = 0) one instruction takes both
+// numbers of s v against the same B; else RS of 32 ranks each take B once for two.
+// Loads come back in the order in which they were asked for: a step's y and then its B are
+// asked for behind the results of the step before.
+constexpr int kSharePitch = 68;   // floats of a row of 64 in LDS
+
+// A barrier that waits for this wave's LDS accesses, but not for its loads and stores.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+  bare_barrier();
+}
+
+template <bool kWide, int RS, bool kVec, bool kAct>
 __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a) {
-  constexpr int S = RS ? RS : 1, kParts = RS ? 2 : 1;
-  constexpr int kPairs = MF * S >= 16 && !kAct ? 1 : 2;
-  constexpr int kStep = kAct ? 16 * kPairs : 32 * kPairs;   // columns of out
+  constexpr int S = RS ? RS : 1, kParts = RS ? 2 : 1, kHalves = kAct ? 2 : 1;
+  constexpr int kChunks = RS ? 4 * RS : 2;      // of eight ranks, in a row of B
+  constexpr int kPitch = 8 * kChunks + 8;       // elements of such a row in LDS
+  constexpr int kBufs = kWide ? 2 : 4, kStep = kWide ? 64 : 256;
+  constexpr int kThreads = kWide ? 256 : 64, kItems = kHalves * 64 * kChunks, kLoads = (kItems + kThreads - 1) / kThreads;
+  // a wave's own B is in registers before its share takes its place
+  constexpr bool kOver = !kWide && !kAct;
+  constexpr int kB = kHalves * 64 * kPitch, kShare = 16 * kSharePitch * 2;
+  constexpr int kBPitch = kOver && kB < kShare ? kShare : kB;   // of a buffer of B
+  __shared__ __attribute__((aligned(16))) uint16_t b_stage[kBufs][kBPitch];
+  __shared__ __attribute__((aligned(16))) float share_stage[kOver ? 1 : 4][kOver ? 4 : 16 * kSharePitch];
   const int64_t block = block_of();
   AdapterTile t;
-  if (!tile_of(a, block / a.blocks, 16 * MF, t)) return;
+  if (!tile_of(a, block / a.blocks, kWide ? 64 : 16, t)) return;
   if (t.adapter < 0 && a.in_place) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, col = lane & 15, g = lane >> 4;
   const int R = a.c.rank, half = a.c.n_out / 2, lim = kAct ? half : a.c.n_out;
-  const int n0 = int(block % a.blocks) * a.block, n1 = min(n0 + a.block, lim);
-  const uint16_t* y[MF];
-  uint16_t* out[MF];
+  const int first = int(block % a.blocks) * a.block, n1 = min(first + a.block, lim);
+  const int n0 = kWide ? first : first + 64 * wave;
+  const int wave_row = kWide ? 16 * wave : 0, count = t.count - wave_row;   // of this wave, maybe none
+  float* ss = kOver ? reinterpret_cast<float*>(b_stage[wave]) : share_stage[kOver ? 0 : wave];
+  // the lane's two rows and eight columns
+  const int sub = lane / 8, at = 8 * (lane % 8);
+  int32_t rows[2];
 #pragma unroll
-  for (int m = 0; m < MF; ++m) {
-    const int64_t row = row_of(a, t, 16 * m + col);
-    y[m] = a.c.y + row * a.c.y_stride;
-    out[m] = a.c.out + row * a.c.out_stride;
-  }
-  u32x4 v[MF][S][kParts];
-  const uint16_t* b = nullptr;
-  if (t.adapter >= 0) {
-    b = a.c.b + int64_t(t.adapter) * a.c.n_out * R;
+  for (int i = 0; i < 2; ++i) rows[i] = row_of(a, t, wave_row + 8 * i + sub);
+  const uint16_t* b = t.adapter < 0 ? nullptr : a.c.b + int64_t(t.adapter) * a.c.n_out * R;
+  const int item0 = kWide ? int(threadIdx.x) : lane;
+  u32x4 raw[kLoads];
+  auto bring = [&](int n) {   // B of the step's columns
+    if (!b) return;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int i = item0 + j * kThreads, c = n + i / kChunks % 64, up = kAct && i >= kItems / 2 ? half : 0;
+      raw[j] = u32x4{0, 0, 0, 0};
+      if (i < kItems && c < lim) raw[j] = eight<kVec>(b + int64_t(c + up) * R, 8 * (i % kChunks), R);
+    }
+  };
+  auto stage = [&](int buf) {
+    if (!b) return;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int i = item0 + j * kThreads;
+      if (i < kItems) *reinterpret_cast<u32x4*>(&b_stage[buf][i / kChunks * kPitch + 8 * (i % kChunks)]) = raw[j];
+    }
+  };
+  if (n0 < n1) bring(n0);
+  u32x4 v[S][kParts];
+  if (b) {
     const float scale = a.c.scale ? a.c.scale[t.adapter] : 1.f;
-    constexpr int kPitch = RS ? 32 * RS : 16;
+    constexpr int kPart = RS ? 32 * RS : 16;
 #pragma unroll
-    for (int m = 0; m < MF; ++m)
+    for (int s = 0; s < S; ++s) {
+      const int r0 = RS ? 32 * s + 8 * g : 8 * (g & 1);
+      const float* p = a.c.part + (int64_t(t.first) + min(wave_row + col, t.count - 1)) * kPart + r0;
+      f32x4 sum[2] = {};
+      for (int i = 0; i < a.splits; ++i) {
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
-        const int r0 = RS ? 32 * s + 8 * g : 8 * (g & 1);
-        const float* p = a.c.part + (int64_t(t.first) + min(16 * m + col, t.count - 1)) * kPitch + r0;
-        f32x4 sum[2] = {};
-        for (int i = 0; i < a.splits; ++i) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) sum[h] += *reinterpret_cast<const f32x4*>(p + int64_t(i) * a.c.T * kPitch + 4 * h);
-        }
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = r0 + e < R ? scale * sum[e / 4][e % 4] : 0.f;
-        u32x4 hi, lo;
-        halves(f, hi, lo);
-        if (RS) {
-          v[m][s][0] = hi;
-          v[m][s][kParts - 1] = lo;
-        } else {
-          v[m][s][0] = g < 2 ? hi : lo;
-        }
+        for (int h = 0; h < 2; ++h) sum[h] += *reinterpret_cast<const f32x4*>(p + int64_t(i) * a.c.T * kPart + 4 * h);
       }
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = r0 + e < R ? scale * sum[e / 4][e % 4] : 0.f;
+      u32x4 hi, lo;
+      halves(f, hi, lo);
+      v[s][0] = RS || g < 2 ? hi : lo;
+      if (RS) v[s][kParts - 1] = lo;
+    }
   }
-  // the column of frag q of a pair that this lane brings: lane group c / 4 gets eight of them
-  const int brings = 8 * (col >> 2) + (col & 3);
-  for (int n = n0 + wave * kStep; n < n1; n += 4 * kStep) {
-    u32x4 old[MF][kPairs];
+  u32x4 old[2][kHalves];
+  auto fetch = [&](int i, int n) {
+    if (8 * i + sub >= count || n + at >= lim) return;
+    const uint16_t* y = a.c.y + rows[i] * a.c.y_stride;
+    old[i][0] = row_load(y, n + at, lim, a.rows_vec);
+    if (kAct) old[i][kHalves - 1] = row_load(y + half, n + at, lim, a.rows_vec);
+  };
 #pragma unroll
-    for (int m = 0; m < MF; ++m)
+  for (int i = 0; i < 2; ++i) fetch(i, n0);
+  int buf = kWide ? 0 : wave;
+  if (kWide) {
+    stage(0);
+    if (n0 + kStep < n1) bring(n0 + kStep);
+    lds_barrier();
+  }
+  for (int n = n0; n < n1; n += kStep) {
+    if (!kWide) {
+      stage(buf);
+      wave_fence();
+      if (n + kStep < n1) bring(n + kStep);
+    }
+    if (count > 0) {
+      float f[kHalves][2][8];
 #pragma unroll
-      for (int p = 0; p < kPairs; ++p) {
-        // with the activation a pair is the gate columns, the next the up columns of the same features
-        const int at = n + (kAct ? 32 * (p / 2) : 32 * p) + 8 * g;
-        const uint16_t* row = kAct && p % 2 ? y[m] + half : y[m];
-        old[m][p] = row_load(row, at, lim, a.rows_vec);
-      }
-    f32x4 acc[MF][kPairs][2];
+      for (int h = 0; h < kHalves; ++h) {
+        if (b) {
+          f32x4 acc[4];
 #pragma unroll
-    for (int m = 0; m < MF; ++m)
+          for (int q = 0; q < 4; ++q) acc[q] = Bf16::zero();
 #pragma unroll
-      for (int p = 0; p < kPairs; ++p) acc[m][p][0] = acc[m][p][1] = Bf16::zero();
-    if (t.adapter >= 0) {
+          for (int s = 0; s < S; ++s)
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
-        const int r0 = RS ? 32 * s + 8 * g : 8 * (g & 1);
-        u32x4 fb[kPairs][2];
+            for (int q = 0; q < 4; ++q) {
+              const u32x4 fb = *reinterpret_cast<const u32x4*>(
+                  &b_stage[buf][(64 * h + 16 * q + col) * kPitch + (RS ? 32 * s + 8 * g : 8 * (g & 1))]);
 #pragma unroll
-        for (int p = 0; p < kPairs; ++p)
+              for (int i = 0; i < kParts; ++i) acc[q] = Bf16::mma(fb, v[s][i], acc[q]);
+            }
+          wave_fence();
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const int c = min(n + (kAct ? 32 * (p / 2) : 32 * p) + brings + 4 * q, lim - 1);
-            fb[p][q] = eight<kVec>(b + int64_t(kAct && p % 2 ? c + half : c) * R, r0, R);
+          for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4*>(ss + col * kSharePitch + 16 * q + 4 * g) = acc[q];
+          wave_fence();
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; e += 4) {
+            f32x4 d = {};
+            if (b) d = *reinterpret_cast<const f32x4*>(ss + (8 * i + sub) * kSharePitch + at + e);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t w = old[i][h][(e + j) / 2];
+              f[h][i][e + j] = (j % 2 ? hi_f(w) : lo_f(w)) + d[j];
+            }
           }
+        wave_fence();
+      }
 #pragma unroll
-        for (int m = 0; m < MF; ++m)
+      for (int i = 0; i < 2; ++i) {
+        u32x4 done = old[i][0];   // a row of no adapter is copied bit for bit
+        if (kAct || b) {
 #pragma unroll
-          for (int p = 0; p < kPairs; ++p)
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-              for (int i = 0; i < kParts; ++i) acc[m][p][q] = Bf16::mma(fb[p][q], v[m][s][i], acc[m][p][q]);
+          for (int w = 0; w < 4; ++w) {
+            float x0 = f[0][i][2 * w], x1 = f[0][i][2 * w + 1];
+            if (kAct) {
+              x0 = silu_f32(x0) * f[kHalves - 1][i][2 * w];
+              x1 = silu_f32(x1) * f[kHalves - 1][i][2 * w + 1];
+            }
+            done[w] = pack_bf16x2(x0, x1);
+          }
+        }
+        if (8 * i + sub < count) row_store(a.c.out + rows[i] * a.c.out_stride, n + at, n1, a.rows_vec, done);
+        if (n + kStep < n1) fetch(i, n + kStep);
       }
     }
-#pragma unroll
-    for (int m = 0; m < MF; ++m) {
-      if (16 * m + col >= t.count) continue;
-#pragma unroll
-      for (int p = 0; p < kPairs; p += kAct ? 2 : 1) {
-        const int at = n + (kAct ? 32 * (p / 2) : 32 * p) + 8 * g;
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t w = old[m][p][e / 2];
-          f[e] = (e % 2 ? hi_f(w) : lo_f(w)) + acc[m][p][e / 4][e % 4];
-          if (kAct) {
-            const uint32_t u = old[m][p + 1 < kPairs ? p + 1 : p][e / 2];
-            f[e] = silu_f32(f[e]) * ((e % 2 ? hi_f(u) : lo_f(u)) + acc[m][p + 1 < kPairs ? p + 1 : p][e / 4][e % 4]);
-          }
-        }
-        u32x4 v8 = old[m][p];   // a row of no adapter is copied bit for bit
-        if (kAct || t.adapter >= 0) {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) v8[w] = pack_bf16x2(f[2 * w], f[2 * w + 1]);
-        }
-        row_store(out[m], at, n1, a.rows_vec, v8);
-      }
+    if (kWide && b) {
+      buf ^= 1;
+      if (n + kStep < n1) stage(buf);
+      if (n + 2 * kStep < n1) bring(n + 2 * kStep);
+      lds_barrier();
     }
   }
 }
@@ -407,18 +511,20 @@ void launch_down(const AdapterArgs& a, bool vec, dim3 grid, hipStream_t stream, 
     hipExtLaunchKernelGGL((adapter_down_kernel<MF, RF, false>), grid, dim3(256), 0, stream, ev_start, nullptr, 0, a);
 }
 
-template <int MF, int RS, bool kAct>
+template <bool kWide, int RS, bool kAct>
 void launch_up(const AdapterArgs& a, bool vec, dim3 grid, hipStream_t stream, hipEvent_t ev_stop) {
   if (vec)
-    hipExtLaunchKernelGGL((adapter_up_kernel<MF, RS, true, kAct>), grid, dim3(256), 0, stream, nullptr, ev_stop, 0, a);
+    hipExtLaunchKernelGGL((adapter_up_kernel<kWide, RS, true, kAct>), grid, dim3(256), 0, stream, nullptr, ev_stop, 0, a);
   else
-    hipExtLaunchKernelGGL((adapter_up_kernel<MF, RS, false, kAct>), grid, dim3(256), 0, stream, nullptr, ev_stop, 0, a);
+    hipExtLaunchKernelGGL((adapter_up_kernel<kWide, RS, false, kAct>), grid, dim3(256), 0, stream, nullptr, ev_stop, 0, a);
 }
 
-template <int MF>
+template <bool kWide>
 void launch_both(AdapterArgs& a, bool act, bool down_vec, bool up_vec, hipStream_t stream, hipEvent_t ev_start,
                  hipEvent_t ev_stop) {
-  const dim3 down = grid_of(a.slots * a.splits), up = grid_of(a.slots * a.blocks);
+  constexpr int MF = kWide ? 2 : 1;   // rows of the first product's workgroups, in 16: tiles of 64 as two of them
+  a.parts = kWide ? 4 / MF : 1;
+  const dim3 down = grid_of(a.slots * a.parts * a.splits), up = grid_of(a.slots * a.blocks);
   switch (rank_frags(a.c.rank)) {
     case 1: launch_down<MF, 1>(a, down_vec, down, stream, ev_start); break;
     case 2: launch_down<MF, 2>(a, down_vec, down, stream, ev_start); break;
@@ -426,14 +532,14 @@ void launch_both(AdapterArgs& a, bool act, bool down_vec, bool up_vec, hipStream
     default: launch_down<MF, 8>(a, down_vec, down, stream, ev_start);
   }
   switch (rank_frags(a.c.rank) + (act ? 16 : 0)) {
-    case 1: launch_up<MF, 0, false>(a, up_vec, up, stream, ev_stop); break;
-    case 2: launch_up<MF, 1, false>(a, up_vec, up, stream, ev_stop); break;
-    case 4: launch_up<MF, 2, false>(a, up_vec, up, stream, ev_stop); break;
-    case 8: launch_up<MF, 4, false>(a, up_vec, up, stream, ev_stop); break;
-    case 17: launch_up<MF, 0, true>(a, up_vec, up, stream, ev_stop); break;
-    case 18: launch_up<MF, 1, true>(a, up_vec, up, stream, ev_stop); break;
-    case 20: launch_up<MF, 2, true>(a, up_vec, up, stream, ev_stop); break;
-    default: launch_up<MF, 4, true>(a, up_vec, up, stream, ev_stop);
+    case 1: launch_up<kWide, 0, false>(a, up_vec, up, stream, ev_stop); break;
+    case 2: launch_up<kWide, 1, false>(a, up_vec, up, stream, ev_stop); break;
+    case 4: launch_up<kWide, 2, false>(a, up_vec, up, stream, ev_stop); break;
+    case 8: launch_up<kWide, 4, false>(a, up_vec, up, stream, ev_stop); break;
+    case 17: launch_up<kWide, 0, true>(a, up_vec, up, stream, ev_stop); break;
+    case 18: launch_up<kWide, 1, true>(a, up_vec, up, stream, ev_stop); break;
+    case 20: launch_up<kWide, 2, true>(a, up_vec, up, stream, ev_stop); break;
+    default: launch_up<kWide, 4, true>(a, up_vec, up, stream, ev_stop);
   }
 }
 
@@ -454,7 +560,7 @@ hipError_t launch_adapter_rows(const int32_t* row_adapter, AdapterOrder o, void*
 // About two workgroups per compute unit, each of 256 features at least.
 int adapter_splits(int32_t T, int32_t hidden, int32_t adapters, int cus) {
   const int64_t tiles = AdapterOrder{T, adapters}.slots(tile_height(T, adapters));
-  const int64_t most = std::min<int64_t>(16, (int64_t(hidden) + 255) / 256);
+  const int64_t most = std::min<int64_t>(8, (int64_t(hidden) + 255) / 256);
   return int(std::max<int64_t>(1, std::min<int64_t>(most, 2 * int64_t(cus) / tiles)));
 }
 
@@ -478,17 +584,20 @@ hipError_t launch_adapters(const AdapterCall& c, bool act, int cus, hipStream_t 
   a.slots = o.slots(height);
   a.splits = adapter_splits(c.T, c.hidden, c.adapters, cus);
   a.per = int32_t(((int64_t(c.hidden) + a.splits - 1) / a.splits + 255) / 256 * 256);
-  // blocks of columns: about eight workgroups per compute unit, 256 columns at least
-  const int32_t cols = act ? c.n_out / 2 : c.n_out;
-  const int64_t want = std::max<int64_t>(1, 8 * int64_t(cus) / a.slots);
-  a.block = int32_t(std::max<int64_t>(256, ((int64_t(cols) + want - 1) / want + 255) / 256 * 256));
+  // blocks of columns: whole steps, about four workgroups per compute unit where that leaves
+  // as many, up to 512 columns (256 of a small rank, whose B and share cost a start less):
+  // 2,056 rows with the activation take 71 us a step of 64 at a time, 53 at 512, 76 at 1,024;
+  // 16,384 of rank 64 439, 315 and 336; 56 decode rows 17.4 at 256, 13.7 at 512
+  const int32_t cols = act ? c.n_out / 2 : c.n_out, step = height == 16 ? 256 : 64;
+  const int64_t each = int64_t(cols) * a.slots / (4 * int64_t(cus)) / step * step;
+  a.block = int32_t(std::min<int64_t>(std::max<int64_t>(step, each), height == 64 && c.rank <= 16 ? 256 : 512));
   a.blocks = int32_t((int64_t(cols) + a.block - 1) / a.block);
   a.rows_vec = on16(c.y) && on16(c.out) && c.y_stride % 8 == 0 && c.out_stride % 8 == 0 && (!act || cols % 8 == 0);
   a.in_place = !act && c.y == c.out && c.y_stride == c.out_stride;
   const bool down_vec = on16(c.x) && on16(c.a) && c.x_stride % 8 == 0 && c.hidden % 8 == 0;
   const bool up_vec = on16(c.b) && c.rank % 8 == 0;
-  if (height == 16) launch_both<1>(a, act, down_vec, up_vec, stream, ev_start, ev_stop);
-  else launch_both<4>(a, act, down_vec, up_vec, stream, ev_start, ev_stop);
+  if (height == 16) launch_both<false>(a, act, down_vec, up_vec, stream, ev_start, ev_stop);
+  else launch_both<true>(a, act, down_vec, up_vec, stream, ev_start, ev_stop);
   return hipGetLastError();
 }
 

@@ -198,7 +198,9 @@ def test_order(lib, T, n, pattern):
         tiles = words[4 + 4 * (slots[0] if i else 0):][:4 * words[i]].reshape(-1, 4)
         want, at = [], 0
         for a, rows in enumerate(groups):
-            want += [(a if a < n else -1, at + c, min(h, len(rows) - c), 0) for c in range(0, len(rows), h)]
+            for c in range(0, len(rows), h):
+                part = rows[c:c + h]       # and the first row, where they follow each other
+                want.append((a if a < n else -1, at + c, len(part), part[0] if part[-1] - part[0] == len(part) - 1 else -1))
             at += len(rows)
         assert words[i] <= slots[i] and tiles.tolist() == [list(w) for w in want]
 
