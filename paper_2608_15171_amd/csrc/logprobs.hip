@@ -11,12 +11,14 @@
 // count as probability 0 (2^-150 is below fp32's least), so that masked tokens, whether
 // -inf or the type's lowest value, add nothing.
 //
-// The top k (largest first, equal logits by lower token) are found in the same pass: each
-// wave keeps a list in LDS of the logits above a bound that at least k of its logits
-// reach. The bound starts as the k-th largest of the first 64 vectors' maxima; when the
-// list fills, each lane takes the largest of its share of it, and the k-th largest of those
-// becomes the bound. A vector whose maximum does not pass the bound costs one comparison.
-// Lists of the waves, then of the workgroups of a row, are merged at the end.
+// The top k (largest first, equal logits by lower token) come from the same pass and a few
+// vectors read again. In the pass every lane notes the largest logit of each quarter of its
+// vectors, and the vector that has it first. Then the k-th best of each wave's lanes is a
+// bound that k logits reach, the best such bound of the waves holds for the row, and only
+// the quarters whose note reaches it, k of them and some more, can hold logits that do: they
+// are read once more, by all lanes, and what reaches the bound is ordered by counting. Notes
+// are ordered as the logits are (value, then vector), so that rows of equal logits end in as
+// few candidates as others.
 //
 // What bounds it: reading the logits, and for bf16 as much the vector unit: an unpacking,
 // an fma, an exponential (four slots), a sum, an fma, two maxima and a comparison per
@@ -80,20 +82,33 @@ __device__ __forceinline__ float value_of(uint64_t key) {
 __device__ __forceinline__ int32_t id_of(uint64_t key) { return int32_t(~uint32_t(key)); }
 
 __device__ __forceinline__ uint64_t lanes_below() { return (uint64_t(1) << (threadIdx.x & 63)) - 1; }
+template <int kCtrl, int kRows = 0xf>
+__device__ __forceinline__ float from_lane(float x, float other) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(other), __float_as_int(x), kCtrl, kRows, 0xf, false));
+}
+__device__ __forceinline__ float last_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+// Over a wave, by lane exchanges: within quads, their pairs, rows of 16 (mirrored), and
+// from a row's last lane to the next rows. The same in every lane.
+template <typename Op>
+__device__ __forceinline__ float over_wave(float v, float none, Op op) {
+  v = op(v, from_lane<0xb1>(v, none));
+  v = op(v, from_lane<0x4e>(v, none));
+  v = op(v, from_lane<0x141>(v, none));
+  v = op(v, from_lane<0x140>(v, none));
+  v = op(v, from_lane<0x142, 0xa>(v, none));
+  v = op(v, from_lane<0x143, 0xc>(v, none));
+  return last_lane(v);
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  return over_wave(v, -__builtin_inff(), [](float x, float y) { return fmaxf(x, y); });
 }
 __device__ __forceinline__ float wave_min(float v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = fminf(v, __shfl_xor(v, d));
-  return v;
+  return over_wave(v, __builtin_inff(), [](float x, float y) { return fminf(x, y); });
 }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  return over_wave(v, 0.f, [](float x, float y) { return x + y; });
 }
 
 // ---------------------------------------------------------------------------
@@ -132,40 +147,53 @@ __device__ __forceinline__ float tree(const float (&v)[W]) {
   return s[0];
 }
 
-// A batch of N vectors; top and low are the largest and the smallest of its logits.
+// A batch of N vectors; top is the largest of its logits. Where a t is -infinity (masked
+// logits, or differences past fp32) its term comes out NaN, and the batch is taken again
+// with such terms as 0; `masked` says that the last one was, and the next goes there at once.
 template <int N, int W>
-__device__ __forceinline__ void add(Sums& a, const float (&x)[N][W], float top, float low, float c) {
-  const float t_top = fmaf(top, c, -a.r), t_low = fmaf(low, c, -a.r);
-  // NaNs among numbers pass here and reach the sums; infinities and lone NaNs do not
-  if (!__any(!(t_top <= 2.f) || !(t_low >= -150.f))) {
+__device__ __forceinline__ void add(Sums& a, bool& masked, const float (&x)[N][W], float top, float c) {
+  float s = 0.f, u = 0.f;
+  const bool moves = __any(!(fmaf(top, c, -a.r) <= 2.f));
+  if (!moves && !masked) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      float e[W], u = 0.f;
+      float e[W], v = 0.f;
 #pragma unroll
       for (int i = 0; i < W; ++i) {
         const float t = fmaf(x[j][i], c, -a.r);
         e[i] = __builtin_amdgcn_exp2f(t);
-        u = fmaf(e[i], t, u);
+        v = fmaf(e[i], t, v);
       }
-      a.S += tree<W>(e);
-      a.U += u;
+      s += tree<W>(e);
+      u += v;
     }
-  } else {
-    if ((top - a.ref) * c > 2.f) a.move(top, c, false);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      float e[W], u = 0.f;
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float t = fmaf(x[j][i] - a.ref, c, a.off);
-        const bool none = t < -150.f;
-        e[i] = none ? 0.f : __builtin_amdgcn_exp2f(t);
-        u = none ? u : fmaf(e[i], t, u);
-      }
-      a.S += tree<W>(e);
+    masked = __any(!(fabsf(u) < __builtin_inff()));
+    if (!masked) {
+      a.S += s;
       a.U += u;
+      return;
     }
+    s = u = 0.f;
   }
+  if ((top - a.ref) * c > 2.f) a.move(top, c, false);
+  bool some = false;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    float e[W], v = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float t = fmaf(x[j][i] - a.ref, c, a.off);
+      const bool none = t < -150.f;   // as good as 0
+      some = some || none;
+      e[i] = none ? 0.f : __builtin_amdgcn_exp2f(t);
+      v = none ? v : fmaf(e[i], t, v);
+    }
+    s += tree<W>(e);
+    u += v;
+  }
+  masked = __any(some);
+  a.S += s;
+  a.U += u;
 }
 
 // ---------------------------------------------------------------------------
@@ -177,18 +205,62 @@ static_assert(kCap >= kLogprobsMaxTop + 64 * 8, "the kept ones and a whole vecto
 // LDS that the lanes of one wave exchange: in order as it is, but not for the compiler.
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// The k-th largest of the lanes' values (k <= 64; equal ones counted each).
+// The k-th largest of the lanes' values (k <= 64; equal ones counted each): a few by taking
+// the largest away, more by counting for each lane (12 instructions for each of the k
+// against 200).
 __device__ __forceinline__ float kth_value(float v, int k) {
+  if (k <= 16) {
+    float m = wave_max(v);
+    for (int i = 1; i < k; ++i) {
+      const uint64_t b = __ballot(v == m);
+      if (!b) return -__builtin_inff();   // NaNs only
+      if (int(threadIdx.x & 63) == int(__ffsll((unsigned long long)b)) - 1) v = -__builtin_inff();
+      m = wave_max(v);
+    }
+    return m;
+  }
   int above = 0;
 #pragma unroll 16
   for (int j = 0; j < 64; ++j) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), j)) > v;
   return wave_min(above < k ? v : __builtin_inff());
 }
 
+// A lane's largest logit and the first vector that has it (-infinity: none).
+struct Note {
+  float x = -__builtin_inff();
+  int32_t v = 0;
+};
+__device__ __forceinline__ uint64_t key_of(const Note& n) { return n.x > -__builtin_inff() ? key_of(n.x, n.v) : 0; }
+
+// The key of the k-th best note of the lanes, 0 where fewer have one.
+__device__ __forceinline__ uint64_t kth_note(const Note& n, int k) {
+  const float x = kth_value(n.x, k);
+  if (!(x > -__builtin_inff())) return 0;
+  uint64_t equal = __ballot(n.x == x);
+  // of equal ones as many as are left, from the first vector on
+  int left = k - int(__popcll(__ballot(n.x > x)));
+  if (int(__popcll(equal)) > left) {
+    int32_t v = -1;
+    bool in = n.x == x;
+    for (; left > 0; --left) {
+      v = in ? n.v : INT32_MAX;
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) v = min(v, __shfl_xor(v, d));
+      in = in && n.v != v;
+    }
+    return key_of(x, v);
+  }
+  int32_t v = 0;
+  for (; equal; equal &= equal - 1)
+    v = max(v, int32_t(__builtin_amdgcn_readlane(n.v, int(__ffsll((unsigned long long)equal)) - 1)));
+  return key_of(x, v);
+}
+
+// The candidates that a wave finds, in LDS.
 struct List {
-  uint64_t* buf;   // LDS, kCap keys
+  uint64_t* buf;   // kCap keys
   int count, k;
-  float bound;     // logits that do not pass it are not among the first k
+  float bound;     // logits below it are not among the first k
 
   // All but the k largest are dropped, one by one from the top.
   __device__ __forceinline__ void exact() {
@@ -214,66 +286,19 @@ struct List {
     wave_fence();
   }
 
-  // Keeps the keys whose logits are at or above v.
-  __device__ __forceinline__ void keep(float v) {
-    const int lane = threadIdx.x & 63;
-    uint64_t mine[kShare];
-#pragma unroll
-    for (int j = 0; j < kShare; ++j) mine[j] = lane + 64 * j < count ? buf[lane + 64 * j] : 0;
-    int n = 0;
-#pragma unroll
-    for (int j = 0; j < kShare; ++j) {
-      const bool kept = mine[j] != 0 && value_of(mine[j]) >= v;
-      const uint64_t b = __ballot(kept);
-      if (kept) buf[n + int(__popcll(b & lanes_below()))] = mine[j];
-      n += int(__popcll(b));
-    }
-    count = n;
-    wave_fence();
-  }
-
-  // Keeps what reaches a bound that at least k keys of the list reach.
-  __device__ __forceinline__ void tighten() {
-    const int lane = threadIdx.x & 63;
-    uint64_t best = 0;
-#pragma unroll
-    for (int j = 0; j < kShare; ++j) {
-      const uint64_t key = lane + 64 * j < count ? buf[lane + 64 * j] : 0;
-      best = key > best ? key : best;
-    }
-    bound = fmaxf(bound, kth_value(best ? value_of(best) : -__builtin_inff(), k));
-    keep(bound);
-  }
-
-  template <int W>
-  __device__ __forceinline__ void room() {
-    if (count > kCap - 64 * W) {
-      tighten();
-      if (count > kCap - 64 * W) exact();
-    }
-  }
-
   // The logits of the lanes' vectors for which hit(e) holds.
   template <int W, typename Hit>
   __device__ __forceinline__ void push(const float (&x)[W], int32_t id0, Hit hit) {
-    room<W>();
+    if (count > kCap - 64 * W) exact();
 #pragma unroll
     for (int e = 0; e < W; ++e) {
       const bool h = hit(e);
       const uint64_t b = __ballot(h);
+      if (!b) continue;
       if (h) buf[count + int(__popcll(b & lanes_below()))] = key_of(x[e], id0 + e);
       count += int(__popcll(b));
     }
     wave_fence();
-  }
-
-  // The first vectors of the wave: the k-th largest of the lanes' maxima is a bound, equal
-  // ones counted from the first lane (their tokens ascend). Whether the lane's is among them.
-  __device__ __forceinline__ bool begin(float top) {
-    bound = kth_value(top, k);
-    const bool equal = top == bound;
-    const int want = k - int(__popcll(__ballot(top > bound)));
-    return top > bound || (equal && int(__popcll(__ballot(equal) & lanes_below())) < want);
   }
 };
 
@@ -340,13 +365,17 @@ __device__ __forceinline__ Given given_token(const Args& a, int64_t row) {
   return g;
 }
 
+constexpr int kQuarters = 4;
+
 template <typename T, bool kTop>
 __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
-  constexpr int W = Type<T>::kW;
+  constexpr int W = Type<T>::kW, kBatch = kAhead * kThreads;
   __shared__ uint64_t lists[kTop ? kWaves * kCap : 1];
+  __shared__ uint64_t notes[kTop ? kQuarters * kThreads : 1];
+  __shared__ uint16_t pairs[kTop ? kQuarters * kThreads : 1];
   __shared__ RowStats parts[kWaves];
-  __shared__ float bounds[kWaves];
-  __shared__ int counts[kWaves];
+  __shared__ uint64_t bounds[kWaves];
+  __shared__ int counts[kWaves], n_pairs;
   const int64_t block = block_of();
   const int64_t row = block / a.splits;
   if (row >= a.r.rows) return;
@@ -361,42 +390,43 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   const int32_t whole = max(v1 - v0, 0);
   const int32_t per = (whole + a.splits - 1) / a.splits;
   const int32_t lo = v0 + min(split * per, whole), hi = v0 + min((split + 1) * per, whole);
-  auto load = [&](int32_t v) {
-    u32x4 r;
-    r[0] = r[1] = r[2] = r[3] = Type<T>::kMasked;
-    if (v < hi) r = *reinterpret_cast<const u32x4*>(base + int64_t(v) * W);
-    return r;
-  };
+  // batches of kAhead vectors for each lane; the last one is broken
+  const int32_t batches = (hi - lo) / kBatch, quarter = batches / kQuarters + 1;
+  auto load = [&](int32_t v) { return *reinterpret_cast<const u32x4*>(base + int64_t(v) * W); };
   u32x4 next[kAhead];
+  if (batches > 0) {
 #pragma unroll
-  for (int j = 0; j < kAhead; ++j) next[j] = load(lo + j * kThreads + int(threadIdx.x));
+    for (int j = 0; j < kAhead; ++j) next[j] = load(lo + j * kThreads + int(threadIdx.x));
+  }
 
   const Given g = given_token<T>(a, row);
   const int32_t given_at = g.id >= 0 ? (g.id + shift) / W : -1;
   const float not_below = below(g.x);
+  if (kTop && threadIdx.x == 0) n_pairs = 0;
   Sums sums;
-  List list;
-  list.buf = lists + (kTop ? wave * kCap : 0);
-  list.count = 0;
-  list.k = a.r.top;
-  list.bound = -__builtin_inff();
+  bool masked = false;
   int above = 0;
+  Note best, note;   // of the lane, and of its quarter
 
-  // N vectors of the lane, v and each kThreads behind the other
+  // N vectors of the lane, v and each kThreads behind the other; their largest logit
   auto stats = [&](const auto& raw, int32_t v, auto size) {
     constexpr int N = decltype(size)::value;
-    float x[N][W], top = -__builtin_inff(), low = __builtin_inff();
+    float x[N][W], top = -__builtin_inff();
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       Type<T>::unpack(raw[j], x[j]);
+      float t = fmaxf(x[j][0], x[j][1]);
 #pragma unroll
-      for (int e = 0; e < W; ++e) {
-        top = fmaxf(top, x[j][e]);
-        low = fminf(low, x[j][e]);
+      for (int e = 2; e < W; e += 2) t = fmaxf(fmaxf(t, x[j][e]), x[j][e + 1]);
+      top = fmaxf(top, t);
+      if (kTop && N > 1) {
+        const bool more = t > note.x;
+        note.x = more ? t : note.x;
+        note.v = more ? v + j * kThreads : note.v;
       }
     }
-    add<N, W>(sums, x, top, low, a.c);
-    if (a.r.rank) {
+    add<N, W>(sums, masked, x, top, a.c);
+    if (a.r.rank && __any(top > not_below)) {
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const int32_t at = v + j * kThreads;
@@ -412,68 +442,63 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
     }
     return top;
   };
+  auto end_quarter = [&](int q) {
+    if (!kTop) return;
+    notes[q * kThreads + threadIdx.x] = key_of(note);
+    if (note.x > best.x) best = note;
+    note = Note{};
+  };
 
-  bool first = true;
-  for (int32_t v = lo + int(threadIdx.x); v - lane < hi; v += kAhead * kThreads) {   // whole waves
+  int q = 0;
+  int32_t left = quarter;   // batches of the quarter
+  for (int32_t i = 0; i < batches; ++i) {
+    const int32_t v = lo + i * kBatch + int(threadIdx.x);
     u32x4 raw[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) raw[j] = next[j];
+    // behind the last batch it is asked for again: loads under a condition would all be waited for
+    const int32_t ahead = i + 1 < batches ? v + kBatch : v;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) next[j] = load(v + (kAhead + j) * kThreads);
-    const float top = stats(raw, v, Size<kAhead>{});
-    if (kTop && __any(first || top > list.bound)) {
-#pragma unroll 1
-      for (int j = 0; j < kAhead; ++j) {
-        u32x4 r = raw[0];
-#pragma unroll
-        for (int i = 1; i < kAhead; ++i) r = j == i ? raw[i] : r;
-        float x[W];
-        Type<T>::unpack(r, x);
-        float best = x[0];
-#pragma unroll
-        for (int e = 1; e < W; ++e) best = fmaxf(best, x[e]);
-        const int32_t id0 = (v + j * kThreads) * W - shift;
-        bool taken = best > list.bound;
-        bool equal = false;
-        if (first) {
-          taken = list.begin(best);
-          equal = true;
-          first = false;
-        }
-        if (__any(taken))
-          list.push<W>(x, id0, [&](int e) {
-            return taken && x[e] > -__builtin_inff() && (equal ? x[e] >= list.bound : x[e] > list.bound);
-          });
-      }
+    for (int j = 0; j < kAhead; ++j) next[j] = load(ahead + j * kThreads);
+    stats(raw, v, Size<kAhead>{});
+    if (kTop && --left == 0) {
+      end_quarter(q++);
+      left = quarter;
     }
   }
-  // the row's broken vectors, before and behind the whole ones, by lanes 0 and 1 of a wave.
-  // Tokens before those seen already may come: logits equal to the bound count
+  if (int32_t v = lo + batches * kBatch + int(threadIdx.x); v - lane < hi) {   // whole waves
+    u32x4 raw[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      raw[j][0] = raw[j][1] = raw[j][2] = raw[j][3] = Type<T>::kMasked;
+      if (v + j * kThreads < hi) raw[j] = load(v + j * kThreads);
+    }
+    stats(raw, v, Size<kAhead>{});
+  }
+  if (kTop)
+    for (; q < kQuarters; ++q) end_quarter(q);
+  // the row's broken vectors, before and behind the whole ones, by lanes 0 and 1 of a wave
   const bool head = split == 0 && shift != 0, tail = split == a.splits - 1 && (shift == 0 || v1 > 0);
+  u32x4 edge[1];
+  edge[0][0] = edge[0][1] = edge[0][2] = edge[0][3] = Type<T>::kMasked;
+  const int32_t edge_v = lane == 0 ? 0 : v1;
+  float edge_top = -__builtin_inff();
   if (wave == 0 && (head || tail)) {
-    u32x4 r[1];
-    r[0][0] = r[0][1] = r[0][2] = r[0][3] = Type<T>::kMasked;
-    const int32_t v = lane == 0 ? 0 : v1;
     if (lane == 0 ? head : lane == 1 && tail) {
 #pragma unroll
       for (int e = 0; e < W; ++e) {
-        const int32_t id = v * W - shift + e;
+        const int32_t id = edge_v * W - shift + e;
         if (id >= 0 && id < a.r.vocab) {
           if constexpr (sizeof(T) == 2) {
             const uint32_t b = x0[id];
-            r[0][e / 2] = e % 2 ? (r[0][e / 2] & 0xffffu) | (b << 16) : (r[0][e / 2] & 0xffff0000u) | b;
+            edge[0][e / 2] = e % 2 ? (edge[0][e / 2] & 0xffffu) | (b << 16) : (edge[0][e / 2] & 0xffff0000u) | b;
           } else {
-            r[0][e] = __float_as_uint(x0[id]);
+            edge[0][e] = __float_as_uint(x0[id]);
           }
         }
       }
     }
-    const float top = stats(r, v, Size<1>{});
-    if (kTop && __any(top >= list.bound && top > -__builtin_inff())) {
-      float x[W];
-      Type<T>::unpack(r[0], x);
-      list.push<W>(x, v * W - shift, [&](int e) { return x[e] >= list.bound && x[e] > -__builtin_inff(); });
-    }
+    edge_top = stats(edge, edge_v, Size<1>{});
   }
 
   // the wave's sums, then the workgroup's
@@ -481,8 +506,8 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   sums.move(ref, a.c, true);
   RowStats s{ref, wave_sum(sums.S), wave_sum(sums.U), above};
   if (kTop) {
-    if (list.count > list.k) list.tighten();
-    if (lane == 0) bounds[wave] = list.bound;
+    const uint64_t bound = kth_note(best, a.r.top);
+    if (lane == 0) bounds[wave] = bound;
   }
   if (lane == 0) parts[wave] = s;
   __syncthreads();
@@ -503,11 +528,61 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
     else write_row(a, row, s, g);
   }
   if (!kTop) return;
-  // any wave's bound holds for the row; what reaches it is ordered by counting
-  float bound = bounds[0];
+  // any wave's bound holds for the row: the quarters that reach it
+  uint64_t bound = bounds[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) bound = fmaxf(bound, bounds[w]);
-  list.keep(bound);
+  for (int w = 1; w < kWaves; ++w) bound = max(bound, bounds[w]);
+  for (int i = 0; i < kQuarters; ++i) {
+    const uint64_t key = notes[i * kThreads + threadIdx.x];
+    const bool in = key != 0 && key >= bound;
+    const uint64_t b = __ballot(in);
+    if (!b) continue;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&n_pairs, int(__popcll(b)));
+    at = __builtin_amdgcn_readfirstlane(at);
+    if (in) pairs[at + int(__popcll(b & lanes_below()))] = uint16_t(i * kThreads + threadIdx.x);
+  }
+  __syncthreads();
+  // their vectors: logits that the bound's vector has come in it or before it
+  const float bound_x = bound ? value_of(bound) : -__builtin_inff();
+  const int32_t bound_v = bound ? id_of(bound) : INT32_MAX;
+  List list{lists + wave * kCap, 0, a.r.top, bound_x};
+  const int32_t each = quarter * kAhead;   // vectors of a quarter
+  auto find = [&](const u32x4& raw, int32_t v, bool in) {
+    float x[W];
+    Type<T>::unpack(raw, x);
+    bool some = false;
+#pragma unroll
+    for (int e = 0; e < W; ++e) some = some || x[e] >= list.bound;
+    if (__any(in && some))
+      list.push<W>(x, v * W - shift, [&](int e) {
+        return in && x[e] >= list.bound && x[e] > -__builtin_inff() && (x[e] > bound_x || v <= bound_v);
+      });
+  };
+  const int64_t items = int64_t(n_pairs) * each;
+  for (int64_t i = 64 * wave; i < items; i += 2 * kThreads) {
+    u32x4 raw[2];
+    int32_t at[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int64_t item = min(i + j * kThreads + lane, items - 1);   // past the end the last one, not taken
+      const int32_t p = int32_t(item / each), n = int32_t(item - int64_t(p) * each);
+      const int32_t pair = pairs[p], batch = pair / kThreads * quarter + n / kAhead;
+      at[j] = lo + (batch * kAhead + n % kAhead) * kThreads + pair % kThreads;
+      // a quarter's last vectors may lie past the split
+      if (at[j] >= hi || i + j * kThreads + lane >= items) at[j] = -1;
+      raw[j] = load(at[j] < 0 ? lo : at[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (i + j * kThreads < items) find(raw[j], at[j], at[j] >= 0);
+  }
+  if (wave == 0 && __any(edge_top >= bound_x && edge_top > -__builtin_inff())) {
+    // before or behind all others, so that the bound's vector does not count
+    float x[W];
+    Type<T>::unpack(edge[0], x);
+    list.push<W>(x, edge_v * W - shift, [&](int e) { return x[e] >= bound_x && x[e] > -__builtin_inff(); });
+  }
   if (lane == 0) counts[wave] = list.count;
   __syncthreads();
   uint64_t* out = a.splits > 1 ? a.keys + block * a.r.top : nullptr;
@@ -518,6 +593,26 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   int n = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) n += counts[w];
+  if (n <= 64) {   // a wave, a key for each lane
+    if (wave != 0) return;
+    uint64_t key = 0;
+    int from = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (lane >= from && lane < from + counts[w]) key = lists[w * kCap + lane - from];
+      from += counts[w];
+    }
+    const int hi32 = int(key >> 32), lo32 = int(key);
+    int before = 0;
+    for (int j = 0; j < n; ++j) {
+      const uint64_t other = (uint64_t(uint32_t(__builtin_amdgcn_readlane(hi32, j))) << 32) |
+                             uint32_t(__builtin_amdgcn_readlane(lo32, j));
+      before += other > key;
+    }
+    if (lane < n && before < a.r.top) put(before, key);
+    if (lane >= n && lane < a.r.top) put(lane, 0);
+    return;
+  }
   for (int i = lane; i < list.count; i += 64) {
     const uint64_t key = list.buf[i];
     int before = 0;
@@ -525,19 +620,22 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
       for (int j = 0; j < counts[w]; ++j) before += lists[w * kCap + j] > key;
     if (before < a.r.top) put(before, key);
   }
-  for (int i = n + int(threadIdx.x); i < a.r.top; i += kThreads) put(i, 0);
 }
 
-// The splits of a row: a wave, each lane with a split and its ordered keys (tokens ascend
-// with the splits, so that the first of equal lanes is next).
+// The splits of a row: a wave, each lane with a split and its ordered keys, in LDS (tokens
+// ascend with the splits, so that the first of equal lanes is next).
 template <typename T>
 __global__ __launch_bounds__(64) void logprob_merge_kernel(Args a) {
+  __shared__ uint64_t keys[kLogprobsMaxSplits * (kLogprobsMaxTop + 1)];
   const int64_t row = block_of();
   if (row >= a.r.rows) return;
-  const int lane = threadIdx.x;
+  const int lane = threadIdx.x, top = a.r.top;
   RowStats s{kNone, 0.f, 0.f, 0};
-  const int64_t at = row * a.splits + lane;
-  if (lane < a.splits) s = a.stats[at];
+  if (lane < a.splits) s = a.stats[row * a.splits + lane];
+  const uint64_t* from = a.keys + row * a.splits * top;
+  for (int i = lane; i < a.splits * top; i += 64) keys[i / top * (top + 1) + i % top] = from[i];
+  if (lane < a.splits) keys[lane * (top + 1) + top] = 0;
+  const Given g = given_token<T>(a, row);
   Sums sums{s.ref, s.S, s.U};
   const float ref = wave_max(s.ref);
   sums.move(ref, a.c, true);
@@ -545,23 +643,21 @@ __global__ __launch_bounds__(64) void logprob_merge_kernel(Args a) {
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) above += __shfl_xor(above, d);
   s = RowStats{ref, wave_sum(sums.S), wave_sum(sums.U), above};
-  const Given g = given_token<T>(a, row);
   if (lane == 0) write_row(a, row, s, g);
-  const uint64_t* keys = a.keys + at * a.r.top;
-  int next = 0;
-  uint64_t key = lane < a.splits && a.r.top > 0 ? keys[0] : 0;
-  uint64_t mine = 0;
-  for (int i = 0; i < a.r.top; ++i) {
-    const float v = key ? value_of(key) : -__builtin_inff();
-    const float m = wave_max(v);
+  __syncthreads();
+  int next = lane * (top + 1);
+  uint64_t key = lane < a.splits ? keys[next] : 0, mine = 0;
+  for (int i = 0; i < top; ++i) {
+    const float v = key ? value_of(key) : -__builtin_inff(), m = wave_max(v);
     const uint64_t b = __ballot(key != 0 && v == m);
     if (!b) break;
-    const int from = int(__ffsll((unsigned long long)b)) - 1;
-    const uint64_t won = __shfl((unsigned long long)key, from);
+    const int winner = int(__ffsll((unsigned long long)b)) - 1;
+    const uint64_t won = (uint64_t(uint32_t(__builtin_amdgcn_readlane(int(key >> 32), winner))) << 32) |
+                         uint32_t(__builtin_amdgcn_readlane(int(key), winner));
     if (lane == i) mine = won;
-    if (lane == from) key = ++next < a.r.top ? keys[next] : 0;
+    if (lane == winner) key = keys[++next];   // behind the last one 0
   }
-  if (lane < a.r.top) write_top(a, row, s, lane, mine);
+  if (lane < top) write_top(a, row, s, lane, mine);
 }
 
 }  // namespace
