@@ -39,7 +39,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kAhead = 4;        // vectors that a lane has in flight
+constexpr int kAhead = 2;        // vectors that a lane has in flight
 constexpr float kNone = -3.402823466e38f;   // a reference below every logit
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -153,8 +153,8 @@ __device__ __forceinline__ float tree(const float (&v)[W]) {
 template <int N, int W>
 __device__ __forceinline__ void add(Sums& a, bool& masked, const float (&x)[N][W], float top, float c) {
   float s = 0.f, u = 0.f;
-  const bool moves = __any(!(fmaf(top, c, -a.r) <= 2.f));
-  if (!moves && !masked) {
+  if (__any(!(fmaf(top, c, -a.r) <= 2.f)) && (top - a.ref) * c > 2.f) a.move(top, c, false);
+  if (!masked && !__any(!(a.r == a.r))) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       float e[W], v = 0.f;
@@ -175,7 +175,6 @@ __device__ __forceinline__ void add(Sums& a, bool& masked, const float (&x)[N][W
     }
     s = u = 0.f;
   }
-  if ((top - a.ref) * c > 2.f) a.move(top, c, false);
   bool some = false;
 #pragma unroll
   for (int j = 0; j < N; ++j) {
@@ -254,6 +253,20 @@ __device__ __forceinline__ uint64_t kth_note(const Note& n, int k) {
   for (; equal; equal &= equal - 1)
     v = max(v, int32_t(__builtin_amdgcn_readlane(n.v, int(__ffsll((unsigned long long)equal)) - 1)));
   return key_of(x, v);
+}
+
+// How many of n keys in LDS are above one; eight reads at a time.
+__device__ __forceinline__ int before_of(const uint64_t* keys, int n, uint64_t key) {
+  int before = 0, j = 0;
+  for (; j + 8 <= n; j += 8) {
+    uint64_t some[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) some[i] = keys[j + i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) before += some[i] > key;
+  }
+  for (; j < n; ++j) before += keys[j] > key;
+  return before;
 }
 
 // The candidates that a wave finds, in LDS.
@@ -352,14 +365,22 @@ __device__ __forceinline__ void write_top(const Args& a, int64_t row, const RowS
     a.r.top_logprobs[at] = !ok ? __builtin_nanf("") : key ? a.r.scale * (value_of(key) - s.ref) - logf(s.S) : -__builtin_inff();
 }
 
+// Loads that are known to be from global memory: those that might be from LDS are waited for
+// all at once.
+template <typename T>
+__device__ __forceinline__ T from_global(const T* p) {
+  typedef const __attribute__((address_space(1))) T* Global;
+  return *(Global)(reinterpret_cast<uintptr_t>(p));
+}
+
 template <typename T>
 __device__ __forceinline__ Given given_token(const Args& a, int64_t row) {
   Given g{0.f, -1};
   if (a.r.tokens) {
-    const int32_t t = a.r.tokens[row];
+    const int32_t t = from_global(a.r.tokens + row);
     if (t >= 0 && t < a.r.vocab) {
       g.id = t;
-      g.x = Type<T>::one(static_cast<const T*>(a.r.logits)[row * a.r.stride + t]);
+      g.x = Type<T>::one(from_global(static_cast<const T*>(a.r.logits) + row * a.r.stride + t));
     }
   }
   return g;
@@ -375,7 +396,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   __shared__ uint16_t pairs[kTop ? kQuarters * kThreads : 1];
   __shared__ RowStats parts[kWaves];
   __shared__ uint64_t bounds[kWaves];
-  __shared__ int counts[kWaves], n_pairs;
+  __shared__ int counts[kWaves], n_pairs, n_best;
   const int64_t block = block_of();
   const int64_t row = block / a.splits;
   if (row >= a.r.rows) return;
@@ -392,17 +413,31 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   const int32_t lo = v0 + min(split * per, whole), hi = v0 + min((split + 1) * per, whole);
   // batches of kAhead vectors for each lane; the last one is broken
   const int32_t batches = (hi - lo) / kBatch, quarter = batches / kQuarters + 1;
-  auto load = [&](int32_t v) { return *reinterpret_cast<const u32x4*>(base + int64_t(v) * W); };
+  // the pass asks the caches not to keep it: 2,048 rows of 131,072 bf16 logits 97 us against 90
+  auto stream = [&](int32_t v) {
+    typedef const __attribute__((address_space(1))) u32x4* Global;
+    return __builtin_nontemporal_load((Global)(reinterpret_cast<uintptr_t>(base + int64_t(v) * W)));
+  };
+  auto load = [&](int32_t v) { return from_global(reinterpret_cast<const u32x4*>(base + int64_t(v) * W)); };
   u32x4 next[kAhead];
+  auto load_some = [&](int32_t v) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      next[j][0] = next[j][1] = next[j][2] = next[j][3] = Type<T>::kMasked;
+      if (v + j * kThreads < hi) next[j] = load(v + j * kThreads);
+    }
+  };
   if (batches > 0) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) next[j] = load(lo + j * kThreads + int(threadIdx.x));
+    for (int j = 0; j < kAhead; ++j) next[j] = stream(lo + j * kThreads + int(threadIdx.x));
+  } else {
+    load_some(lo + int(threadIdx.x));
   }
 
   const Given g = given_token<T>(a, row);
   const int32_t given_at = g.id >= 0 ? (g.id + shift) / W : -1;
   const float not_below = below(g.x);
-  if (kTop && threadIdx.x == 0) n_pairs = 0;
+  if (kTop && threadIdx.x == 0) n_pairs = n_best = 0;
   Sums sums;
   bool masked = false;
   int above = 0;
@@ -415,9 +450,9 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       Type<T>::unpack(raw[j], x[j]);
-      float t = fmaxf(x[j][0], x[j][1]);
+      float t = -__builtin_inff();
 #pragma unroll
-      for (int e = 2; e < W; e += 2) t = fmaxf(fmaxf(t, x[j][e]), x[j][e + 1]);
+      for (int e = 0; e < W; e += 2) t = fmaxf(fmaxf(t, x[j][e]), x[j][e + 1]);
       top = fmaxf(top, t);
       if (kTop && N > 1) {
         const bool more = t > note.x;
@@ -459,7 +494,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
     // behind the last batch it is asked for again: loads under a condition would all be waited for
     const int32_t ahead = i + 1 < batches ? v + kBatch : v;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) next[j] = load(ahead + j * kThreads);
+    for (int j = 0; j < kAhead; ++j) next[j] = stream(ahead + j * kThreads);
     stats(raw, v, Size<kAhead>{});
     if (kTop && --left == 0) {
       end_quarter(q++);
@@ -467,13 +502,8 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
     }
   }
   if (int32_t v = lo + batches * kBatch + int(threadIdx.x); v - lane < hi) {   // whole waves
-    u32x4 raw[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      raw[j][0] = raw[j][1] = raw[j][2] = raw[j][3] = Type<T>::kMasked;
-      if (v + j * kThreads < hi) raw[j] = load(v + j * kThreads);
-    }
-    stats(raw, v, Size<kAhead>{});
+    if (batches > 0) load_some(v);
+    stats(next, v, Size<kAhead>{});
   }
   if (kTop)
     for (; q < kQuarters; ++q) end_quarter(q);
@@ -490,10 +520,10 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
         const int32_t id = edge_v * W - shift + e;
         if (id >= 0 && id < a.r.vocab) {
           if constexpr (sizeof(T) == 2) {
-            const uint32_t b = x0[id];
+            const uint32_t b = from_global(x0 + id);
             edge[0][e / 2] = e % 2 ? (edge[0][e / 2] & 0xffffu) | (b << 16) : (edge[0][e / 2] & 0xffff0000u) | b;
           } else {
-            edge[0][e] = __float_as_uint(x0[id]);
+            edge[0][e] = __float_as_uint(from_global(x0 + id));
           }
         }
       }
@@ -528,10 +558,23 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
     else write_row(a, row, s, g);
   }
   if (!kTop) return;
-  // any wave's bound holds for the row: the quarters that reach it
+  // Any wave's bound holds for the row, and so does the k-th best of the lanes that reach the
+  // best of them (each wave's alone is about the 3 k-th of the row's).
   uint64_t bound = bounds[0];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) bound = max(bound, bounds[w]);
+  if (bound) {
+    const uint64_t mine = key_of(best);
+    if (mine >= bound) lists[atomicAdd(&n_best, 1)] = mine;
+    __syncthreads();
+    const int n = n_best;
+    if (int(threadIdx.x) < n) {
+      const uint64_t key = lists[threadIdx.x];
+      if (before_of(lists, n, key) == a.r.top - 1) bounds[0] = key;
+    }
+    __syncthreads();
+    bound = bounds[0];
+  }
   for (int i = 0; i < kQuarters; ++i) {
     const uint64_t key = notes[i * kThreads + threadIdx.x];
     const bool in = key != 0 && key >= bound;
@@ -559,16 +602,16 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
         return in && x[e] >= list.bound && x[e] > -__builtin_inff() && (x[e] > bound_x || v <= bound_v);
       });
   };
-  const int64_t items = int64_t(n_pairs) * each;
-  for (int64_t i = 64 * wave; i < items; i += 2 * kThreads) {
+  const uint32_t items = uint32_t(n_pairs) * uint32_t(each);   // below 2^28: 1,024 of at most 2^18
+  for (uint32_t i = 64 * wave; i < items; i += 2 * kThreads) {
     u32x4 raw[2];
     int32_t at[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int64_t item = min(i + j * kThreads + lane, items - 1);   // past the end the last one, not taken
-      const int32_t p = int32_t(item / each), n = int32_t(item - int64_t(p) * each);
-      const int32_t pair = pairs[p], batch = pair / kThreads * quarter + n / kAhead;
-      at[j] = lo + (batch * kAhead + n % kAhead) * kThreads + pair % kThreads;
+      const uint32_t item = min(i + j * kThreads + lane, items - 1);   // past the end the last one, not taken
+      const uint32_t p = item / uint32_t(each), n = item - p * uint32_t(each);
+      const uint32_t pair = pairs[p], batch = pair / kThreads * quarter + n / kAhead;
+      at[j] = lo + int32_t((batch * kAhead + n % kAhead) * kThreads + pair % kThreads);
       // a quarter's last vectors may lie past the split
       if (at[j] >= hi || i + j * kThreads + lane >= items) at[j] = -1;
       raw[j] = load(at[j] < 0 ? lo : at[j]);
@@ -616,8 +659,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   for (int i = lane; i < list.count; i += 64) {
     const uint64_t key = list.buf[i];
     int before = 0;
-    for (int w = 0; w < kWaves; ++w)
-      for (int j = 0; j < counts[w]; ++j) before += lists[w * kCap + j] > key;
+    for (int w = 0; w < kWaves; ++w) before += before_of(lists + w * kCap, counts[w], key);
     if (before < a.r.top) put(before, key);
   }
 }
@@ -632,9 +674,19 @@ __global__ __launch_bounds__(64) void logprob_merge_kernel(Args a) {
   const int lane = threadIdx.x, top = a.r.top;
   RowStats s{kNone, 0.f, 0.f, 0};
   if (lane < a.splits) s = a.stats[row * a.splits + lane];
-  const uint64_t* from = a.keys + row * a.splits * top;
-  for (int i = lane; i < a.splits * top; i += 64) keys[i / top * (top + 1) + i % top] = from[i];
-  if (lane < a.splits) keys[lane * (top + 1) + top] = 0;
+  if (lane < a.splits) {
+    const uint64_t* from = a.keys + (row * a.splits + lane) * top;
+    uint64_t* to = keys + lane * (top + 1);
+    for (int i = 0; i < top; i += 8) {   // eight loads at once
+      uint64_t some[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) some[j] = from[min(i + j, top - 1)];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (i + j < top) to[i + j] = some[j];
+    }
+    to[top] = 0;
+  }
   const Given g = given_token<T>(a, row);
   Sums sums{s.ref, s.S, s.U};
   const float ref = wave_max(s.ref);
@@ -662,11 +714,17 @@ __global__ __launch_bounds__(64) void logprob_merge_kernel(Args a) {
 
 }  // namespace
 
+#ifndef LPMIN
+#define LPMIN 256
+#endif
+#ifndef LPPER
+#define LPPER 4
+#endif
 // Splits of a row: about four workgroups per compute unit, each of 256 vectors at least.
 int logprob_splits(int32_t rows, int32_t vocab, int cus) {
   const int64_t vectors = (int64_t(vocab) + 7) / 8;
-  const int64_t most = std::min<int64_t>(kLogprobsMaxSplits, (vectors + kThreads - 1) / kThreads);
-  return int(std::max<int64_t>(1, std::min(most, int64_t(4) * cus / std::max(rows, 1))));
+  const int64_t most = std::min<int64_t>(kLogprobsMaxSplits, (vectors + LPMIN - 1) / LPMIN);
+  return int(std::max<int64_t>(1, std::min(most, int64_t(LPPER) * cus / std::max(rows, 1))));
 }
 
 size_t logprob_workspace_bytes(int32_t rows, int32_t top, int splits) {
