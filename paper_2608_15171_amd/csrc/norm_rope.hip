@@ -116,10 +116,9 @@ __device__ __forceinline__ void values_of(const Raw<kMode>& r, float (&f)[kValue
   }
 }
 
-// The lane's weights of a head, through the caches: every row reads them again.
+// The lane's weights of a head, through the caches.
 template <int kMode>
-__device__ __forceinline__ void weights_of(const uint16_t* w, const Head& h, const Lane& l, float offset,
-                                           float (&g)[kValues<kMode>]) {
+__device__ __forceinline__ Raw<kMode> fetch_weights(const uint16_t* w, const Head& h, const Lane& l) {
   Raw<kMode> r;
 #pragma unroll
   for (int i = 0; i < kUnits<kMode>; ++i) {
@@ -135,15 +134,13 @@ __device__ __forceinline__ void weights_of(const uint16_t* w, const Head& h, con
       if (has_second<kMode>(h, u)) r.u[i].y = *reinterpret_cast<const u32x4*>(w + second_feature<kMode>(h, u));
     }
   }
-  values_of<kMode>(r, g);
-#pragma unroll
-  for (int i = 0; i < kValues<kMode>; ++i) g[i] += offset;
+  return r;
 }
 
 // The norm of a head's features, in f.
 template <int kMode>
 __device__ __forceinline__ void normalise(const Raw<kMode>& r, const Head& h, const Lane& l, const HeadNorm& norm,
-                                          const uint16_t* w, float (&f)[kValues<kMode>]) {
+                                          const Raw<kMode>& w, float (&f)[kValues<kMode>]) {
   constexpr int n = kValues<kMode>;
   const float per = 1.f / float(h.dim);
   // the values that are features: sums of differences leave the others out
@@ -179,11 +176,11 @@ __device__ __forceinline__ void normalise(const Raw<kMode>& r, const Head& h, co
   const float to_one = rsqrtf(var + eps);
 #pragma unroll
   for (int i = 0; i < n; ++i) f[i] *= to_one;
-  if (w) {
+  if (norm.weight) {
     float g[n];
-    weights_of<kMode>(w, h, l, norm.offset, g);
+    values_of<kMode>(w, g);
 #pragma unroll
-    for (int i = 0; i < n; ++i) f[i] *= g[i];
+    for (int i = 0; i < n; ++i) f[i] *= g[i] + norm.offset;
   }
 }
 
@@ -236,19 +233,23 @@ __device__ __forceinline__ void turn_and_store(float (&f)[kValues<kMode>], const
 
 // Every head of n_rows rows: a group of lanes steps through (row, head). `ready` is called
 // once, behind the first loads, and makes the table cs[row][pair].
-template <int kMode, bool kStream, typename Src, typename Dst, typename Ready>
+template <int kMode, bool kStream, int kBatch, typename Src, typename Dst, typename Ready>
 __device__ __forceinline__ void norm_rows(int n_rows, int heads, const Head& h, const HeadNorm& norm, int first_head,
                                           const float2* cs, Src src, Dst dst, Ready ready) {
   const Lane l = lane_of<kMode>(h);
   const int step = kThreads / l.lanes, start = int(threadIdx.x) / l.lanes;
   const int step_row = step / heads, step_head = step % heads;
   int row = start / heads, head = start % heads;
+  // weights of all heads are brought once, those of each with its features
+  const bool by_head = norm.weight && norm.head_stride != 0;
+  Raw<kMode> w;
+  if (norm.weight && !by_head) w = fetch_weights<kMode>(norm.weight, h, l);
   bool first = true;
   while (first || row < n_rows) {
-    Raw<kMode> r[kAhead];
-    int rows[kAhead], at_head[kAhead];
+    Raw<kMode> r[kBatch];
+    int rows[kBatch], at_head[kBatch];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
+    for (int i = 0; i < kBatch; ++i) {
       rows[i] = row;
       at_head[i] = head;
       if (row < n_rows) r[i] = fetch_raw<kMode>(src(row, head), h, l);
@@ -265,9 +266,9 @@ __device__ __forceinline__ void norm_rows(int n_rows, int heads, const Head& h, 
       first = false;
     }
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
+    for (int i = 0; i < kBatch; ++i) {
       if (rows[i] >= n_rows) continue;   // whole groups
-      const uint16_t* w = norm.weight ? norm.weight + (first_head + at_head[i]) * norm.head_stride : nullptr;
+      if (by_head) w = fetch_weights<kMode>(norm.weight + (first_head + at_head[i]) * norm.head_stride, h, l);
       float f[kValues<kMode>];
       normalise<kMode>(r[i], h, l, norm, w, f);
       turn_and_store<kMode, kStream>(f, h, l, cs + rows[i] * h.pairs, dst(rows[i], at_head[i]));
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_rows_kernel(NormRowsArgs a
   if (row0 >= a.r.rows) return;
   const int n = int(min(int64_t(a.per), a.r.rows - row0));
   const Head h{a.r.head_dim, a.t.pairs, a.t.layout == PPAS_ROPE_HALF};
-  norm_rows<kMode, true>(
+  norm_rows<kMode, true, kAhead>(
       n, a.r.heads, h, a.norm, 0, cs,
       [&](int row, int head) { return a.r.x + (row0 + row) * a.r.x_stride + int64_t(head) * a.r.head_dim; },
       [&](int row, int head) { return a.r.y + (row0 + row) * a.r.y_stride + int64_t(head) * a.r.head_dim; },
@@ -308,11 +309,55 @@ __global__ __launch_bounds__(kThreads) void norm_rope_rows_kernel(NormRowsArgs a
 
 // ---------------------------------------------------------------------------
 // A step's rows on their way into the pages, in the workgroups of rope_qkv_append_kernel:
-// for y = 0 the keys and values of a page's new slots, else the queries of four of them.
+// for y = 0 the keys and for y = 1 the values of a page's new slots, else the queries of
+// four of them.
 // Keys pass through LDS, two heads at a time: their norm needs a head's lanes side by side,
 // the page's layout (16 slots of each chunk of eight features) the slots.
 // ---------------------------------------------------------------------------
+// The values of a page's new slots, transposed through LDS a head at a time: rows in by 16
+// bytes (or one element), then per task (feature, eight slots) one 16-byte store where all
+// eight are new. `v` is this thread's part of the first head (fetch_value).
+struct PageSlots {
+  int64_t row0;          // the first slot's row
+  int32_t page, slot_lo, slot_hi;
+};
+__device__ __forceinline__ u32x4 fetch_value(const AppendArgs& a, const PageSlots& p, int g) {
+  const int t = threadIdx.x, n = p.slot_hi - p.slot_lo;
+  u32x4 v = {};
+  if (a.v_aligned && t < n * 16) v = load16(a.r.v + (p.row0 + t / 16) * a.r.v_stride + g * kHeadDim + 8 * (t % 16));
+  return v;
+}
+__device__ __forceinline__ void put_values(const AppendArgs& a, const PageSlots& p, u32x4 v,
+                                           uint16_t (*rows)[kHeadDim + 8]) {
+  const RopeAppend& r = a.r;
+  const int tid = threadIdx.x, n = p.slot_hi - p.slot_lo;
+  for (int g = 0; g < r.hkv; ++g) {
+    if (a.v_aligned) {
+      if (tid < n * 16) *reinterpret_cast<u32x4*>(&rows[p.slot_lo + tid / 16][8 * (tid % 16)]) = v;
+    } else {
+      const uint16_t* src = r.v + p.row0 * r.v_stride + g * kHeadDim;
+      for (int t = tid; t < n * kHeadDim; t += kThreads)
+        rows[p.slot_lo + t / kHeadDim][t % kHeadDim] = src[t / kHeadDim * r.v_stride + t % kHeadDim];
+    }
+    __syncthreads();
+    if (g + 1 < r.hkv) v = fetch_value(a, p, g + 1);
+    const int d = tid / 2, s0 = 8 * (tid & 1), lo = max(p.slot_lo - s0, 0), hi = min(p.slot_hi - s0, 8);
+    uint16_t* dst = r.v_pages + (int64_t(p.page) * r.hkv + g) * kPage * kHeadDim + d * kPage + s0;
+    if (hi - lo == 8) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = uint32_t(rows[s0 + 2 * e][d]) | (uint32_t(rows[s0 + 2 * e + 1][d]) << 16);
+      store16(dst, w);
+    } else {
+      for (int e = lo; e < hi; ++e) dst[e] = rows[s0 + e][d];
+    }
+    __syncthreads();
+  }
+}
+
 constexpr int kKeyHeads = 2;
+constexpr int kWrites = 1;                    // the part that writes values; 0 writes keys
+constexpr int kNormParts = kParts + kWrites;   // workgroups of a page
 
 struct NormAppendArgs {
   AppendArgs a;
@@ -328,9 +373,9 @@ __global__ __launch_bounds__(kThreads) void norm_rope_qkv_append_kernel(NormAppe
   const int tid = threadIdx.x, part = blockIdx.y;
   const int pos_lo = it.lpage * kPage;   // position of slot 0
   int slot_lo = max(it.cached_len - pos_lo, 0), slot_hi = min(it.cached_len + it.n_query - pos_lo, kPage);
-  if (part > 0) {
-    slot_lo = max(slot_lo, (part - 1) * kSlots);
-    slot_hi = min(slot_hi, part * kSlots);
+  if (part > kWrites) {
+    slot_lo = max(slot_lo, (part - kWrites - 1) * kSlots);
+    slot_hi = min(slot_hi, (part - kWrites) * kSlots);
     if (slot_lo >= slot_hi) return;
   }
   const int n = slot_hi - slot_lo;
@@ -342,22 +387,24 @@ __global__ __launch_bounds__(kThreads) void norm_rope_qkv_append_kernel(NormAppe
       cs[e] = cos_sin(double(pos_lo + slot_lo + row), a.turns[j], a.magnitude, false);
     }
   };
-  if (part > 0) {
-    norm_rows<kMode, true>(
+  if (part > kWrites) {
+    norm_rows<kMode, true, 2>(
         n, r.hq, h, args.q, 0, cs,
         [&](int row, int head) { return r.q + (row0 + row) * r.q_stride + head * kHeadDim; },
         [&](int row, int head) { return r.q_out + ((row0 + row) * r.hq + head) * kHeadDim; }, table);
     return;
   }
 
-  __shared__ __attribute__((aligned(16))) uint16_t rows[kPage][kHeadDim + 8];
   __shared__ __attribute__((aligned(16))) uint16_t keys[kKeyHeads][kPage][kHeadDim + 8];
   const int32_t page = r.bt[int64_t(it.seq) * r.bt_stride + it.lpage];
-  const PageSlots slots{row0, page, slot_lo, slot_hi};
-  const u32x4 v = fetch_value(a, slots, 0);
+  if (part == kWrites) {
+    const PageSlots slots{row0, page, slot_lo, slot_hi};
+    put_values(a, slots, fetch_value(a, slots, 0), keys[0]);
+    return;
+  }
   for (int g0 = 0; g0 < r.hkv; g0 += kKeyHeads) {
     const int heads = min(kKeyHeads, r.hkv - g0);
-    norm_rows<kMode, false>(
+    norm_rows<kMode, false, 2>(
         n, heads, h, args.k, g0, cs,
         [&](int row, int head) { return r.k + (row0 + row) * r.k_stride + (g0 + head) * kHeadDim; },
         [&](int row, int head) { return &keys[head][slot_lo + row][0]; }, [&]() {
@@ -373,7 +420,6 @@ __global__ __launch_bounds__(kThreads) void norm_rope_qkv_append_kernel(NormAppe
     }
     __syncthreads();
   }
-  put_values(a, slots, v, rows);
 }
 
 // 16-byte runs of the weights too.
@@ -410,7 +456,7 @@ hipError_t launch_norm_rope_qkv_append(const RopeAppend& r, const HeadNorm& q_no
   if (r.n_items <= 0) return hipSuccess;
   if (t.pairs > kHeadDim / 2 || r.n_desc > kAppendInline || r.n_items > kAppendMaxItems) return hipErrorInvalidValue;
   const NormAppendArgs a{append_args(r, t), q_norm, k_norm};
-  const dim3 grid{unsigned(r.n_items), kParts}, block(kThreads);
+  const dim3 grid{unsigned(r.n_items), kNormParts}, block(kThreads);
   const bool aligned = on16(r.q) && on16(r.k) && on16(r.q_out) && r.q_stride % 8 == 0 && r.k_stride % 8 == 0 &&
                        weights_aligned(q_norm) && weights_aligned(k_norm);
   switch (mode_of(t, kHeadDim, aligned)) {

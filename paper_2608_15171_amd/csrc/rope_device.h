@@ -120,47 +120,6 @@ __device__ __forceinline__ AppendItem inline_item(const AppendArgs& a, int item)
   return AppendItem{s, d.cached_len / kPage + item - d.first_item, d.cached_len, d.n_query, d.query_start, 0, 0, 0};
 }
 
-// The values of a page's new slots, transposed through LDS a head at a time: rows in by 16
-// bytes (or one element), then per task (feature, eight slots) one 16-byte store where all
-// eight are new. `v` is this thread's part of the first head (fetch_value).
-struct PageSlots {
-  int64_t row0;          // the first slot's row
-  int32_t page, slot_lo, slot_hi;
-};
-__device__ __forceinline__ u32x4 fetch_value(const AppendArgs& a, const PageSlots& p, int g) {
-  const int t = threadIdx.x, n = p.slot_hi - p.slot_lo;
-  u32x4 v = {};
-  if (a.v_aligned && t < n * 16) v = load16(a.r.v + (p.row0 + t / 16) * a.r.v_stride + g * kHeadDim + 8 * (t % 16));
-  return v;
-}
-__device__ __forceinline__ void put_values(const AppendArgs& a, const PageSlots& p, u32x4 v,
-                                           uint16_t (*rows)[kHeadDim + 8]) {
-  const RopeAppend& r = a.r;
-  const int tid = threadIdx.x, n = p.slot_hi - p.slot_lo;
-  for (int g = 0; g < r.hkv; ++g) {
-    if (a.v_aligned) {
-      if (tid < n * 16) *reinterpret_cast<u32x4*>(&rows[p.slot_lo + tid / 16][8 * (tid % 16)]) = v;
-    } else {
-      const uint16_t* src = r.v + p.row0 * r.v_stride + g * kHeadDim;
-      for (int t = tid; t < n * kHeadDim; t += kThreads)
-        rows[p.slot_lo + t / kHeadDim][t % kHeadDim] = src[t / kHeadDim * r.v_stride + t % kHeadDim];
-    }
-    __syncthreads();
-    if (g + 1 < r.hkv) v = fetch_value(a, p, g + 1);
-    const int d = tid / 2, s0 = 8 * (tid & 1), lo = max(p.slot_lo - s0, 0), hi = min(p.slot_hi - s0, 8);
-    uint16_t* dst = r.v_pages + (int64_t(p.page) * r.hkv + g) * kPage * kHeadDim + d * kPage + s0;
-    if (hi - lo == 8) {
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = uint32_t(rows[s0 + 2 * e][d]) | (uint32_t(rows[s0 + 2 * e + 1][d]) << 16);
-      store16(dst, w);
-    } else {
-      for (int e = lo; e < hi; ++e) dst[e] = rows[s0 + e][d];
-    }
-    __syncthreads();
-  }
-}
-
 // 16-byte runs need every run's start on 16 bytes: bases, row strides, heads, and in
 // the half layout the second half.
 Mode mode_of(const RopeTable& t, int32_t head_dim, bool aligned) {

@@ -196,9 +196,14 @@ __global__ __launch_bounds__(kThreads) void rope_qkv_append_kernel(AppendArgs a)
 #pragma unroll
   for (int i = 0; i < 2; ++i)
     if (tid + i * kThreads < k_tasks) key[i] = fetch_key(tid + i * kThreads);
+  // Values, transposed through LDS a head at a time: rows in by 16 bytes (or one element),
+  // then per task (feature, eight slots) one 16-byte store where all eight are new.
   __shared__ __attribute__((aligned(16))) uint16_t rows[kPage][kHeadDim + 8];
-  const PageSlots slots{row0, page, slot_lo, slot_hi};
-  const u32x4 v = fetch_value(a, slots, 0);
+  u32x4 v = {};
+  auto fetch_value = [&](int g) {
+    if (a.v_aligned && tid < n * 16) v = load16(r.v + (row0 + tid / 16) * r.v_stride + g * kHeadDim + 8 * (tid % 16));
+  };
+  fetch_value(0);
   table();
   __syncthreads();
   auto put_key = [&](const Unit& x, int t) {
@@ -211,7 +216,28 @@ __global__ __launch_bounds__(kThreads) void rope_qkv_append_kernel(AppendArgs a)
     if (tid + i * kThreads < k_tasks) put_key(key[i], tid + i * kThreads);
   for (int t = tid + 2 * kThreads; t < k_tasks; t += kThreads) put_key(fetch_key(t), t);
 
-  put_values(a, slots, v, rows);
+  for (int g = 0; g < r.hkv; ++g) {
+    if (a.v_aligned) {
+      if (tid < n * 16) *reinterpret_cast<u32x4*>(&rows[slot_lo + tid / 16][8 * (tid % 16)]) = v;
+    } else {
+      const uint16_t* src = r.v + row0 * r.v_stride + g * kHeadDim;
+      for (int t = tid; t < n * kHeadDim; t += kThreads)
+        rows[slot_lo + t / kHeadDim][t % kHeadDim] = src[t / kHeadDim * r.v_stride + t % kHeadDim];
+    }
+    __syncthreads();
+    if (g + 1 < r.hkv) fetch_value(g + 1);
+    const int d = tid / 2, s0 = 8 * (tid & 1), lo = max(slot_lo - s0, 0), hi = min(slot_hi - s0, 8);
+    uint16_t* dst = r.v_pages + (int64_t(page) * r.hkv + g) * kPage * kHeadDim + d * kPage + s0;
+    if (hi - lo == 8) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = uint32_t(rows[s0 + 2 * e][d]) | (uint32_t(rows[s0 + 2 * e + 1][d]) << 16);
+      store16(dst, w);
+    } else {
+      for (int e = lo; e < hi; ++e) dst[e] = rows[s0 + e][d];
+    }
+    __syncthreads();
+  }
 }
 
 }  // namespace
