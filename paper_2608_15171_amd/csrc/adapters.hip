@@ -557,10 +557,12 @@ hipError_t launch_adapter_rows(const int32_t* row_adapter, AdapterOrder o, void*
   return hipGetLastError();
 }
 
-// About two workgroups per compute unit, each of 256 features at least.
+// About two workgroups per compute unit, each of 512 features at least, eight splits at most:
+// every workgroup of the second product adds them up (155 rows of 11,008, rank 64: 31 us with
+// 2, 23 with 4 or 8, 28 with 16, 44 with 32; 2,056 rows of 2,048, rank 32: 54 with 8, 50 with 4).
 int adapter_splits(int32_t T, int32_t hidden, int32_t adapters, int cus) {
   const int64_t tiles = AdapterOrder{T, adapters}.slots(tile_height(T, adapters));
-  const int64_t most = std::min<int64_t>(8, (int64_t(hidden) + 255) / 256);
+  const int64_t most = std::min<int64_t>(8, (int64_t(hidden) + 511) / 512);
   return int(std::max<int64_t>(1, std::min<int64_t>(most, 2 * int64_t(cus) / tiles)));
 }
 

@@ -257,15 +257,14 @@ __device__ __forceinline__ uint64_t kth_note(const Note& n, int k) {
 
 // How many of n keys in LDS are above one; eight reads at a time.
 __device__ __forceinline__ int before_of(const uint64_t* keys, int n, uint64_t key) {
-  int before = 0, j = 0;
-  for (; j + 8 <= n; j += 8) {
+  int before = 0;
+  for (int j = 0; j < n; j += 8) {
     uint64_t some[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) some[i] = keys[j + i];
+    for (int i = 0; i < 8; ++i) some[i] = keys[min(j + i, n - 1)];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) before += some[i] > key;
+    for (int i = 0; i < 8; ++i) before += j + i < n && some[i] > key;
   }
-  for (; j < n; ++j) before += keys[j] > key;
   return before;
 }
 
@@ -653,7 +652,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
       before += other > key;
     }
     if (lane < n && before < a.r.top) put(before, key);
-    if (lane >= n && lane < a.r.top) put(lane, 0);
+    if (lane >= n && lane < a.r.top) put(lane, 0);   // fewer than asked for
     return;
   }
   for (int i = lane; i < list.count; i += 64) {
@@ -664,67 +663,96 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   }
 }
 
-// The splits of a row: a wave, each lane with a split and its ordered keys, in LDS (tokens
-// ascend with the splits, so that the first of equal lanes is next).
+// The splits of a row. As in a split, a bound that enough keys reach, of the first (or, of
+// few splits, later) places of their lists, leaves few to be ordered by counting; where it
+// leaves many (ascending logits: all the best in one split), a wave takes them one by one,
+// each lane the next of a split's (tokens ascend with the splits, so that the first of equal
+// lanes is next).
+constexpr int kFew = 512;
+
 template <typename T>
-__global__ __launch_bounds__(64) void logprob_merge_kernel(Args a) {
-  __shared__ uint64_t keys[kLogprobsMaxSplits * (kLogprobsMaxTop + 1)];
+__global__ __launch_bounds__(kThreads) void logprob_merge_kernel(Args a) {
+  __shared__ uint64_t keys[kLogprobsMaxSplits * kLogprobsMaxTop];
+  __shared__ uint64_t heads[kLogprobsMaxSplits], few[kFew], bound;
+  __shared__ RowStats total;
+  __shared__ int n_few;
   const int64_t row = block_of();
   if (row >= a.r.rows) return;
-  const int lane = threadIdx.x, top = a.r.top;
-  RowStats s{kNone, 0.f, 0.f, 0};
-  if (lane < a.splits) s = a.stats[row * a.splits + lane];
-  if (lane < a.splits) {
-    const uint64_t* from = a.keys + (row * a.splits + lane) * top;
-    uint64_t* to = keys + lane * (top + 1);
-    for (int i = 0; i < top; i += 8) {   // eight loads at once
-      uint64_t some[8];
+  const int tid = threadIdx.x, top = a.r.top, n = a.splits * top;
+  const uint64_t* from = a.keys + row * n;
+  constexpr int kAtOnce = kLogprobsMaxSplits * kLogprobsMaxTop / kThreads;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) some[j] = from[min(i + j, top - 1)];
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (i + j < top) to[i + j] = some[j];
-    }
-    to[top] = 0;
+  for (int j = 0; j < kAtOnce; ++j)
+    if (tid + j * kThreads < n) keys[tid + j * kThreads] = from_global(from + tid + j * kThreads);
+  if (tid == 0) {
+    n_few = 0;
+    bound = 0;
   }
-  const Given g = given_token<T>(a, row);
-  Sums sums{s.ref, s.S, s.U};
-  const float ref = wave_max(s.ref);
-  sums.move(ref, a.c, true);
-  int above = s.above;
+  if (tid < 64) {
+    RowStats s{kNone, 0.f, 0.f, 0};
+    if (tid < a.splits) s = a.stats[row * a.splits + tid];
+    const Given g = given_token<T>(a, row);
+    Sums sums{s.ref, s.S, s.U};
+    const float ref = wave_max(s.ref);
+    sums.move(ref, a.c, true);
+    int above = s.above;
 #pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) above += __shfl_xor(above, d);
-  s = RowStats{ref, wave_sum(sums.S), wave_sum(sums.U), above};
-  if (lane == 0) write_row(a, row, s, g);
+    for (int d = 32; d >= 1; d >>= 1) above += __shfl_xor(above, d);
+    s = RowStats{ref, wave_sum(sums.S), wave_sum(sums.U), above};
+    if (tid == 0) {
+      total = s;
+      write_row(a, row, s, g);
+    }
+  }
+  if (top == 0) return;
   __syncthreads();
-  int next = lane * (top + 1);
-  uint64_t key = lane < a.splits ? keys[next] : 0, mine = 0;
+  // `lists` of the places 0 .. place hold top keys or more
+  const int place = (top - 1) / a.splits, lists = (top + place) / (place + 1);
+  if (tid < a.splits) heads[tid] = keys[tid * top + place];
+  __syncthreads();
+  if (tid < a.splits && heads[tid] != 0 && before_of(heads, a.splits, heads[tid]) == lists - 1) bound = heads[tid];
+  __syncthreads();
+  for (int i = tid; i < n; i += kThreads) {
+    const uint64_t key = keys[i];
+    if (key == 0 || key < bound) continue;
+    const int at = atomicAdd(&n_few, 1);
+    if (at < kFew) few[at] = key;
+  }
+  __syncthreads();
+  const int m = n_few;
+  if (m <= kFew) {
+    for (int i = tid; i < m; i += kThreads) {
+      const int before = before_of(few, m, few[i]);
+      if (before < top) write_top(a, row, total, before, few[i]);
+    }
+    for (int i = m + tid; i < top; i += kThreads) write_top(a, row, total, i, 0);
+    return;
+  }
+  if (tid >= 64) return;
+  int next = 0;
+  uint64_t key = tid < a.splits ? keys[tid * top] : 0, mine = 0;
   for (int i = 0; i < top; ++i) {
-    const float v = key ? value_of(key) : -__builtin_inff(), m = wave_max(v);
-    const uint64_t b = __ballot(key != 0 && v == m);
+    const float v = key ? value_of(key) : -__builtin_inff(), best = wave_max(v);
+    const uint64_t b = __ballot(key != 0 && v == best);
     if (!b) break;
     const int winner = int(__ffsll((unsigned long long)b)) - 1;
-    const uint64_t won = (uint64_t(uint32_t(__builtin_amdgcn_readlane(int(key >> 32), winner))) << 32) |
-                         uint32_t(__builtin_amdgcn_readlane(int(key), winner));
-    if (lane == i) mine = won;
-    if (lane == winner) key = keys[++next];   // behind the last one 0
+    const uint64_t won = __shfl((unsigned long long)key, winner);
+    if (tid == i) mine = won;
+    if (tid == winner) key = ++next < top ? keys[tid * top + next] : 0;
   }
-  if (lane < top) write_top(a, row, s, lane, mine);
+  if (tid < top) write_top(a, row, total, tid, mine);
 }
 
 }  // namespace
 
-#ifndef LPMIN
-#define LPMIN 256
-#endif
-#ifndef LPPER
-#define LPPER 4
-#endif
-// Splits of a row: about four workgroups per compute unit, each of 256 vectors at least.
+// Splits of a row: about three workgroups per compute unit (64 fp32 rows of 131,072 tokens with
+// 20 alternatives 21.4 us with two, 22.6 with three, 23.5 with four; 128 bf16 rows with 5 19.6,
+// 20.1, 19.1; 300 33.9, 29.3, 28.9), each of 8,192 tokens at least (8 rows 17.4 us, of 2,048
+// tokens 19.9).
 int logprob_splits(int32_t rows, int32_t vocab, int cus) {
   const int64_t vectors = (int64_t(vocab) + 7) / 8;
-  const int64_t most = std::min<int64_t>(kLogprobsMaxSplits, (vectors + LPMIN - 1) / LPMIN);
-  return int(std::max<int64_t>(1, std::min(most, int64_t(LPPER) * cus / std::max(rows, 1))));
+  const int64_t most = std::min<int64_t>(kLogprobsMaxSplits, (vectors + 1023) / 1024);
+  return int(std::max<int64_t>(1, std::min(most, int64_t(3) * cus / std::max(rows, 1))));
 }
 
 size_t logprob_workspace_bytes(int32_t rows, int32_t top, int splits) {
@@ -753,9 +781,9 @@ hipError_t launch_logprobs(const LogprobRows& r, int splits, void* workspace, hi
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits <= 1) return e;
   if (r.f32)
-    hipExtLaunchKernelGGL(logprob_merge_kernel<float>, grid_of(r.rows), dim3(64), 0, stream, nullptr, ev_stop, 0, a);
+    hipExtLaunchKernelGGL(logprob_merge_kernel<float>, grid_of(r.rows), block, 0, stream, nullptr, ev_stop, 0, a);
   else
-    hipExtLaunchKernelGGL(logprob_merge_kernel<uint16_t>, grid_of(r.rows), dim3(64), 0, stream, nullptr, ev_stop, 0, a);
+    hipExtLaunchKernelGGL(logprob_merge_kernel<uint16_t>, grid_of(r.rows), block, 0, stream, nullptr, ev_stop, 0, a);
   return hipGetLastError();
 }
 

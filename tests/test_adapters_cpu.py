@@ -74,7 +74,7 @@ def test_rows_hold_every_tile(tokens, n):
 def test_workspace():
     f = ppas.adapter_workspace_bytes
     assert f(0, 128, 16, 4) == 0 and f(8, 0, 16, 4) == 0 and f(8, 128, 129, 4) == 0 and f(8, 128, 16, 0) == 0
-    assert f(1, 2048, 16, 8) == 8 * 64 and f(16384, 2048, 64, 4) % (16384 * 256) == 0
+    assert f(1, 2048, 16, 8) == 4 * 64 and f(16384, 2048, 64, 4) % (16384 * 256) == 0
 
 
 def test_binding_refusals(monkeypatch):

@@ -136,6 +136,18 @@ def test_orders_and_ties(lib, dtype, workspace, top, order):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("top", [3, 64])
+@pytest.mark.parametrize("order", ["normal", "ascending", "equal", "one split"])
+def test_most_splits(lib, dtype, top, order):
+    """A row in 64 splits: its best in all of them, or all in one, which leaves the merge many candidates."""
+    V = 600003
+    i = np.arange(V)
+    v = {"normal": 3.0 * I.rng(12).normal(size=V), "ascending": i / 10000.0, "equal": np.zeros(V),
+         "one split": np.where((i > 300000) & (i < 300900), 2.0 + i % 7, i % 3)}[order]
+    case(lib, v[None], dtype, tokens=[300500], top=top, label=order)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("vocab", [200, 33000])
 @pytest.mark.parametrize("workspace", ["full", "none"])
 def test_masks(lib, dtype, vocab, workspace):

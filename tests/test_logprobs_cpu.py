@@ -42,7 +42,7 @@ def test_workspace():
     f = ppas.logprobs_workspace_bytes
     assert f(0, 1000) == 0 and f(-1, 1000) == 0 and f(4, 0) == 0 and f(4, 1000, 65) == 0 and f(4, (1 << 30) + 1) == 0
     assert f(1, 1000) == 0 and f(4096, 131072) == 0                            # too short, or rows enough, to be split
-    assert f(1, 131072, 0) == 64 * 16 and f(1, 131072, 20) == 64 * (16 + 160)
+    assert f(1, 131072, 0) == 16 * 16 and f(1, 131072, 20) == 16 * (16 + 160) and f(1, 1 << 30, 1) == 64 * 24
     assert f(64, 131072, 5) % 64 == 0 and f(64, 131072, 5) > 0
 
 
