@@ -400,7 +400,8 @@ ppas_status run_qkv_append(const ppas_step_plan& p, const RopeTable& table, cons
   r.hq = p.shape.n_q_heads;
   r.hkv = p.shape.n_kv_heads;
   const hipError_t e =
-      norms ? launch_norm_rope_qkv_append(r, norm_of(*norms->q), norm_of(*norms->k), table, stream, ev_of(ev, 0), ev_of(ev, 1))
+      norms ? launch_norm_rope_qkv_append(r, norm_of(*norms->q), norm_of(*norms->k), table, stream, ev_of(ev, 0),
+                                          ev_of(ev, 1))
             : launch_rope_qkv_append(r, table, stream, ev_of(ev, 0), ev_of(ev, 1));
   // a list by request travels in the kernel's arguments: no buffer is read
   const bool noted = p.n_desc > 0 || note_use(p.buf, stream);
@@ -1001,10 +1002,17 @@ ppas_status ppas_logprobs(const void* logits, int32_t type, int64_t row_stride, 
     if (row_stride > (int64_t(1) << 60) / n_rows) return PPAS_ERANGE;
     const LogprobRows r{logits,          row_stride,   tokens_dev,    out->logprob,      out->rank,
                         out->entropy,    top_k ? out->top_ids : nullptr, top_k ? out->top_logprobs : nullptr,
-                        scale,           n_rows,       vocab,         out->top_ids || out->top_logprobs ? top_k : 0, type == PPAS_F32};
+                        scale,           n_rows,       vocab,         out->top_ids || out->top_logprobs ? top_k : 0,
+                        type == PPAS_F32};
     if ((r.logprob || r.rank) && !r.tokens) return PPAS_EINVAL;
     if (off(logits, type == PPAS_F32 ? 4 : 2) || off(r.tokens, 4) || off(r.logprob, 4) || off(r.rank, 4) ||
         off(r.entropy, 4) || off(r.top_ids, 4) || off(r.top_logprobs, 4) || off(workspace, 16))
+      return PPAS_EINVAL;
+    // the rows are read until the last result is written
+    const uint64_t logit_bytes = span_bytes(n_rows, row_stride, vocab) * (r.f32 ? 2 : 1), n = uint64_t(n_rows);
+    if (overlap(logits, logit_bytes, r.logprob, 4 * n) || overlap(logits, logit_bytes, r.rank, 4 * n) ||
+        overlap(logits, logit_bytes, r.entropy, 4 * n) || overlap(logits, logit_bytes, r.top_ids, 4 * n * r.top) ||
+        overlap(logits, logit_bytes, r.top_logprobs, 4 * n * r.top))
       return PPAS_EINVAL;
     if (!r.logprob && !r.rank && !r.entropy && !r.top) return PPAS_OK;
     const DeviceInfo dev = current_device();

@@ -348,11 +348,16 @@ struct Given {       // the row's token
 
 // One row's results from its sums.
 __device__ __forceinline__ bool has_distribution(const RowStats& s) { return s.S > 0.f && s.S < __builtin_inff(); }
+// scale (x - ref); a difference of finite logits past fp32 is taken of their halves.
+__device__ __forceinline__ float over_ref(const Args& a, float x, float ref) {
+  const float d = x - ref;
+  return fabsf(d) < __builtin_inff() ? a.r.scale * d : 2.f * a.r.scale * (0.5f * x - 0.5f * ref);
+}
 __device__ __forceinline__ void write_row(const Args& a, int64_t row, const RowStats& s, const Given& g) {
   const bool ok = has_distribution(s);
   const float nan = __builtin_nanf(""), ln = logf(s.S);
   if (a.r.entropy) a.r.entropy[row] = ok ? fmaxf(ln - kLn2 * (s.U / s.S), 0.f) : nan;
-  if (a.r.logprob) a.r.logprob[row] = ok && g.id >= 0 ? a.r.scale * (g.x - s.ref) - ln : nan;
+  if (a.r.logprob) a.r.logprob[row] = ok && g.id >= 0 ? over_ref(a, g.x, s.ref) - ln : nan;
   if (a.r.rank) a.r.rank[row] = ok && g.id >= 0 && g.x > -__builtin_inff() ? s.above : -1;
 }
 // Place i of its top alternatives (key 0: none).
@@ -361,7 +366,7 @@ __device__ __forceinline__ void write_top(const Args& a, int64_t row, const RowS
   const int64_t at = row * a.r.top + i;
   if (a.r.top_ids) a.r.top_ids[at] = ok && key ? id_of(key) : -1;
   if (a.r.top_logprobs)
-    a.r.top_logprobs[at] = !ok ? __builtin_nanf("") : key ? a.r.scale * (value_of(key) - s.ref) - logf(s.S) : -__builtin_inff();
+    a.r.top_logprobs[at] = !ok ? __builtin_nanf("") : key ? over_ref(a, value_of(key), s.ref) - logf(s.S) : -__builtin_inff();
 }
 
 // Loads that are known to be from global memory: those that might be from LDS are waited for

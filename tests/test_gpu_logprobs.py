@@ -283,3 +283,15 @@ def test_rows_past_32_bit_offsets(lib):
     x.copy_(torch.randn(2, V, device="cuda"))
     got = run(lib, x, [3, 4], 9)
     check(got, x.double().cpu().numpy(), [3, 4], 9, 1.0, "far")
+
+
+@pytest.mark.parametrize("V", [777, 40000])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_differences_past_fp32(lib, dtype, V):
+    """Logits whose differences pass fp32's range, at scales that bring them back into it."""
+    x = np.zeros((4, V))
+    x[:2, 5], x[:2, 100], x[1, 400] = -2.0 ** 127.5, 2.0 ** 127.9, -np.inf
+    x[2:, 7], x[2, 300], x[3] = 2.0 ** 127, -2.0 ** 127.9, -2.0 ** 127.9
+    x[3, 9] = 2.0 ** 127.9
+    case(lib, x, dtype, tokens=[5, 400, 300, 11], top=64, scale=2.0 ** -100)
+    case(lib, x, dtype, tokens=[5, 5, 300, 11], top=3, scale=2.0 ** -60)

@@ -24,7 +24,8 @@ def test_refusals():
                dict(vocab=-3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
                dict(scale=2.0 ** -101), dict(scale=2.0 ** 101), dict(tokens=None), dict(top=-1), dict(ws_bytes=64), dict(ws=P + 8),
                dict(ev=ctypes.byref(half)), dict(logits=(1 << 24) + 1), dict(logits=(1 << 24) + 2, type=1), dict(tokens=P + 2),
-               dict(out=None), *(dict(out=ppas.LogprobOut(*[P + 2 * (i == j) for j in range(5)])) for i in range(5))):
+               dict(out=None), dict(type=1, out=ppas.LogprobOut(None, None, (1 << 24) + 4 * 3999)),
+               dict(out=ppas.LogprobOut(P, P, P, P, (1 << 24) - 4)), *(dict(out=ppas.LogprobOut(*[P + 2 * (i == j) for j in range(5)])) for i in range(5))):
         assert call(**kw) == E, kw
     assert call(top=65) == U
     assert call(vocab=(1 << 30) + 1, stride=1 << 31) == R
