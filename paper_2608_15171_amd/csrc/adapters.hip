@@ -125,7 +125,8 @@ __global__ __launch_bounds__(kSortThreads) void adapter_rows_kernel(const int32_
     if (!s.valid) continue;
     const int before = int(__popcll(s.same & ((uint64_t(1) << lane) - 1)));
     const int base = count[wave][s.g];
-    order[first[s.g] + base + before] = int32_t(t + lane);
+    // (inside the order also if someone changes the rows' adapters meanwhile)
+    order[min(first[s.g] + base + before, o.T - 1)] = int32_t(t + lane);
     // behind every lane's read: a wave's accesses to LDS are in order
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (before == 0) count[wave][s.g] = base + int(__popcll(s.same));
@@ -167,8 +168,8 @@ struct AdapterArgs {
 __device__ __forceinline__ bool tile_of(const AdapterArgs& a, int64_t i, int height, AdapterTile& t) {
   const int64_t n = height == 16 ? a.head->tiles16 : a.head->tiles64;   // both asked for at once
   t = a.tiles[min(i, a.slots - 1)];
-  return i < min(n, a.slots) && t.adapter >= -1 && t.adapter < a.c.adapters && t.count >= 1 && t.count <= height && t.first >= 0 &&
-         t.first <= a.c.T - t.count;
+  return i < min(n, a.slots) && t.adapter >= -1 && t.adapter < a.c.adapters && t.count >= 1 && t.count <= height &&
+         t.first >= 0 && t.first <= a.c.T - t.count && t.row >= -1 && t.row <= a.c.T - t.count;
 }
 __device__ __forceinline__ int32_t row_of(const AdapterArgs& a, const AdapterTile& t, int local) {
   const int at = min(local, t.count - 1);   // rows past the tile's are its last one again

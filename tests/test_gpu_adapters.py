@@ -308,3 +308,32 @@ def test_binding_refusals(lib):
             (ppas.adapter_act if kw.get("act") else ppas.adapter_add)(s, x, y, kw.get("out", out), o, kw.get("ws", ws))
     with pytest.raises(ValueError):
         ppas.adapters(t(n, r, H).transpose(1, 2), t(n, N, H))
+
+
+@pytest.mark.parametrize("T,n", [(3, 2), (70, 1)])
+def test_rows_past_32_bit_offsets(lib, T, n):
+    """Rows of x, y and out behind 2^32 elements of others, in tiles of 16 and of 64."""
+    ppas, step, torch = lib
+    H, N, r = 64, 72, 16
+    stride = 2 ** 32 // (T - 1) // 8 * 8 + 64
+    g = I.rng(21, T)
+    rows = np.arange(T) % n
+    (xb, x), (yb, y), (ab, a), (bb, b) = (bf16(g, s) for s in ((T, H), (T, N), (n, r, H), (n, N, r)))
+    xv, yv = (torch.empty(stride * (T - 1) + cols, dtype=torch.int16, device="cuda").as_strided((T, cols), (stride, 1))
+              for cols in (H, N))
+    to = lambda bits: torch.from_numpy(bits.view(np.int16)).cuda()              # noqa: E731
+    xv.copy_(to(xb))
+    yv.copy_(to(yb))
+    bf = torch.bfloat16
+    s, order = ppas.adapters(to(ab).view(bf), to(bb).view(bf)), ppas.AdapterRows(T, n)
+    order.sort(torch.from_numpy(rows.astype(np.int32)).cuda())
+    ws = torch.empty(ppas.adapter_workspace_bytes(T, H, r, n), dtype=torch.uint8, device="cuda")
+    out = torch.empty(T, N, dtype=bf, device="cuda")
+    ppas.adapter_add(s, xv.view(bf), yv.view(bf), out, order, ws)
+    z = y + A.share(x, a, b, None, rows)
+    tol = 2.0 ** -8 * np.abs(z) + bounds(x, a, b, None, rows, z) + 2.0 ** -133
+    assert (np.abs(R.bf16_bits_to_f64(step.bits_of(out)) - z) <= tol).all()
+    ppas.adapter_add(s, xv.view(bf), yv.view(bf), yv.view(bf), order, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(yv, out.view(torch.int16))
+    assert torch.equal(xv, to(xb))
