@@ -393,11 +393,12 @@ def _rope_rows_args(x, positions, y):
     """The pointers and strides of rows to turn, their positions and sizes."""
     xp, xs = _heads(x, "x")
     yp, ys = (xp, xs) if y is x else _heads(y, "y")
-    if x.shape != y.shape or positions.dim() != 1 or positions.shape[0] != x.shape[0]:
+    shape = x.shape
+    if y.shape != shape or positions.shape != shape[:1]:
         raise ValueError(f"shapes x {tuple(x.shape)}, y {tuple(y.shape)}, positions {tuple(positions.shape)} do not match")
     if positions.dtype != torch.int32:
         raise ValueError("positions must be int32")
-    return xp, xs, yp, ys, _dev(positions, "positions"), *x.shape
+    return xp, xs, yp, ys, _dev(positions, "positions"), *shape
 
 
 def rope_rows(rope: Rope, x, positions, y, transposed: bool = False, events: Events | None = None, stream=None) -> None:
@@ -429,7 +430,7 @@ def head_norm(weight=None, eps: float = 1e-6, offset: float = 0.0, center: bool 
 def _norm(norm: HeadNorm, name, heads: int, dim: int):
     """Refuses a norm whose weights are not of such heads; its weights' tensor (or None)."""
     w = norm.tensor
-    if w is not None and (w.shape[-1] != dim or (w.dim() == 2 and w.shape[0] != heads)):
+    if w is not None and w.shape != (dim,) and w.shape != (heads, dim):
         raise ValueError(f"{name}'s weight must be [{dim}] or [{heads}, {dim}], got {tuple(w.shape)}")
     return w
 
@@ -437,7 +438,7 @@ def _norm(norm: HeadNorm, name, heads: int, dim: int):
 def norm_rope_rows(norm: HeadNorm, rope: Rope, x, positions, y, events: Events | None = None, stream=None) -> None:
     """rope_rows of normalised heads."""
     args = _rope_rows_args(x, positions, y)
-    w = _norm(norm, "norm", x.shape[1], x.shape[2])
+    w = _norm(norm, "norm", *args[-2:])
     hs = _here(stream, x, y, positions, w)
     st = _lib.ppas_norm_rope_rows(ctypes.byref(norm), ctypes.byref(rope), *args,
                                   None if events is None else ctypes.byref(events), hs)
@@ -706,14 +707,15 @@ class AdapterRows:
         if size == 0 and self.n_tokens != 0:
             raise ValueError(f"no rows of {self.n_tokens} tokens and {self.n_adapters} adapters")
         self.buf = torch.empty(max(size, 16), dtype=torch.uint8, device=device)
+        self._at = self.buf.data_ptr(), self.buf.numel()   # as the calls take it
 
     def sort(self, row_adapter, events: Events | None = None, stream=None) -> None:
         """row_adapter: int32 [n_tokens], the rows' adapters (-1: none)."""
-        if row_adapter.dtype != torch.int32 or tuple(row_adapter.shape) != (self.n_tokens,):
+        if row_adapter.dtype != torch.int32 or row_adapter.shape != (self.n_tokens,):
             raise ValueError(f"row_adapter must be int32 [{self.n_tokens}], got {row_adapter.dtype} {tuple(row_adapter.shape)}")
-        p, q = _dev(row_adapter, "row_adapter"), _dev(self.buf, "rows")
+        p = _dev(row_adapter, "row_adapter")
         hs = _here(stream, row_adapter, self.buf)
-        st = _lib.ppas_adapter_rows(p, self.n_tokens, self.n_adapters, q, self.buf.numel(),
+        st = _lib.ppas_adapter_rows(p, self.n_tokens, self.n_adapters, *self._at,
                                     None if events is None else ctypes.byref(events), hs)
         _check(st, "ppas_adapter_rows")
         self.sorted = True
@@ -740,13 +742,14 @@ def adapter_workspace_bytes(n_tokens: int, hidden: int, rank: int, n_adapters: i
 
 def _packed_rows(t, name, rows: int, cols: int):
     """The pointer and row stride of a device tensor [rows, cols] of bf16 with packed rows at any stride."""
-    if t.dim() != 2 or t.dtype not in _BF16 or tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols) or t.dtype not in _BF16:
         raise ValueError(f"{name} must be bf16 [{rows}, {cols}], got {tuple(t.shape)} {t.dtype}")
-    if cols > 1 and t.stride(1) != 1:
+    row, one = t.stride()
+    if one != 1 and cols > 1:
         raise ValueError(f"the rows of {name} must be packed")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    return t.data_ptr(), row if rows > 1 else max(row, cols)
 
 
 def _adapt(fn, what, adapters, x, y, out, rows, per, workspace, events, stream):
@@ -763,8 +766,8 @@ def _adapt(fn, what, adapters, x, y, out, rows, per, workspace, events, stream):
     ptrs = (*_packed_rows(x, "x", T, adapters.hidden), *_packed_rows(y, "y", T, N), *_packed_rows(out, "out", T, N // per))
     ws = _dev(workspace, "workspace")
     hs = _here(stream, x, y, out, workspace, rows.buf, *adapters.tensors)
-    st = fn(ctypes.byref(adapters), *ptrs, T, rows.buf.data_ptr(), rows.buf.numel(), ws,
-            workspace.numel() * workspace.element_size(), None if events is None else ctypes.byref(events), hs)
+    st = fn(ctypes.byref(adapters), *ptrs, T, *rows._at, ws, workspace.nbytes,
+            None if events is None else ctypes.byref(events), hs)
     _check(st, what)
 
 
@@ -787,7 +790,7 @@ def _result(t, name, dtype, *shape):
     """The pointer of an optional result of that type and shape."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != shape:
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
     return _dev(t, name)
 
@@ -812,8 +815,7 @@ def logprobs(logits, tokens=None, logprob=None, rank=None, entropy=None, top_ids
     hs = _here(stream, logits, tokens, logprob, rank, entropy, top_ids, top_logprobs, workspace)
     st = _lib.ppas_logprobs(logits.data_ptr(), int(logits.dtype == f32), logits.stride(0) if R > 1 else max(logits.stride(0), V),
                             R, V, float(scale), tp, k, ctypes.byref(out), ws,
-                            0 if workspace is None else workspace.numel() * workspace.element_size(),
-                            None if events is None else ctypes.byref(events), hs)
+                            0 if workspace is None else workspace.nbytes, None if events is None else ctypes.byref(events), hs)
     _check(st, "ppas_logprobs")
 
 
@@ -924,15 +926,19 @@ class StepPlan:
 
     def _qkv_append(self, fn, what, norms, rope, q, k_pages, v_pages, q_new, k_new, v_new, bt_dev, events, stream) -> None:
         bt = self._bt(bt_dev)
-        if not _is_table(bt) or bt.shape[0] < len(self.desc):
+        if (bt.dtype != torch.int32 and not _is_table(bt)) or bt.shape[0] < len(self.desc):
             _check_buffers(self.shape, self.desc, bt_dev=bt)
-        x = _qkv(q_new, k_new, v_new, self._n_rows, *self._heads)
+        hq, hkv, dim = self._heads
+        x = _qkv(q_new, k_new, v_new, self._n_rows, hq, hkv, dim)
         ptrs = (_buffer(q, "q", self._q_bytes), _buffer(k_pages, "k_pages", self._pool_bytes),
                 _buffer(v_pages, "v_pages", self._pool_bytes), _dev(bt, "block_table"))
-        hq, hkv, dim = self._heads
-        weights = [_norm(n, name, h, dim) for n, name, h in zip(norms, ("q_norm", "k_norm"), (hq, hkv))]
+        weights, refs = (), ()
+        if norms:
+            qn, kn = norms
+            weights = _norm(qn, "q_norm", hq, dim), _norm(kn, "k_norm", hkv, dim)
+            refs = ctypes.byref(qn), ctypes.byref(kn)
         hs = _here(stream, q, k_pages, v_pages, q_new, k_new, v_new, bt, *weights)
-        st = fn(self._h, *map(ctypes.byref, norms), ctypes.byref(rope), ctypes.byref(x), *ptrs,
+        st = fn(self._h, *refs, ctypes.byref(rope), ctypes.byref(x), *ptrs,
                 None if events is None else ctypes.byref(events), hs)
         _check(st, what)
 
