@@ -982,7 +982,9 @@ ppas_status check_logprobs(int32_t n_rows, int32_t vocab, int32_t top_k) {
 size_t ppas_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t top_k) {
   if (check_logprobs(n_rows, vocab, top_k) != PPAS_OK || n_rows == 0) return 0;
   try {
-    return logprob_workspace_bytes(n_rows, top_k, logprob_splits(n_rows, vocab, current_device().cus));
+    const int cus = current_device().cus;
+    return std::max(logprob_workspace_bytes(n_rows, top_k, logprob_split(n_rows, vocab, false, cus).splits),
+                    logprob_workspace_bytes(n_rows, top_k, logprob_split(n_rows, vocab, true, cus).splits));
   } catch (...) {
     return 0;
   }
@@ -1017,9 +1019,10 @@ ppas_status ppas_logprobs(const void* logits, int32_t type, int64_t row_stride, 
     if (!r.logprob && !r.rank && !r.entropy && !r.top) return PPAS_OK;
     const DeviceInfo dev = current_device();
     if (!dev.gfx950) return PPAS_EUNSUPPORTED;
-    int splits = logprob_splits(n_rows, vocab, dev.cus);
-    while (splits > 1 && logprob_workspace_bytes(n_rows, r.top, splits) > workspace_bytes) --splits;
-    const hipError_t e = launch_logprobs(r, splits, workspace, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
+    LogprobSplit split = logprob_split(n_rows, vocab, r.f32, dev.cus);
+    for (; split.splits > 1 && logprob_workspace_bytes(n_rows, r.top, split.splits) > workspace_bytes; --split.splits)
+      split.held = 0;   // longer parts than lanes hold
+    const hipError_t e = launch_logprobs(r, split, workspace, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
                                          ev_of(events, 1));
     return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
   } catch (...) {

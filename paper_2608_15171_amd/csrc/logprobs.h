@@ -25,10 +25,14 @@ struct LogprobRows {
   bool f32;
 };
 // Workgroups of a row on a device with `cus` compute units, the workspace that they share
-// their results in (none for one), and the launch.
-int logprob_splits(int32_t rows, int32_t vocab, int cus);
+// their results in (none for one), and the launch. `held`: 16-byte vectors that each of their
+// lanes keeps (0: they read past parts of any length, and the few that matter again).
+struct LogprobSplit {
+  int splits, held;
+};
+LogprobSplit logprob_split(int32_t rows, int32_t vocab, bool f32, int cus);
 size_t logprob_workspace_bytes(int32_t rows, int32_t top, int splits);
-hipError_t launch_logprobs(const LogprobRows& r, int splits, void* workspace, hipStream_t stream, hipEvent_t ev_start,
-                           hipEvent_t ev_stop);
+hipError_t launch_logprobs(const LogprobRows& r, LogprobSplit split, void* workspace, hipStream_t stream,
+                           hipEvent_t ev_start, hipEvent_t ev_stop);
 
 }  // namespace ppas

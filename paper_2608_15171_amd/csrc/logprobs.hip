@@ -7,22 +7,28 @@
 // Every lane keeps S and U of its logits relative to a reference of its own, which it
 // moves when a logit comes whose t is more than 2 (U would lose digits against ln S
 // otherwise), and the lanes' sums are brought to the largest reference at the
-// end. Sums are fp32, of eight logits at a time; logits more than 150 below the reference
+// end. Sums are fp32, of a few vectors at a time; logits more than 150 below the reference
 // count as probability 0 (2^-150 is below fp32's least), so that masked tokens, whether
 // -inf or the type's lowest value, add nothing.
 //
-// The top k (largest first, equal logits by lower token) come from the same pass and a few
-// vectors read again. In the pass every lane notes the largest logit of each quarter of its
-// vectors, and the vector that has it first. Then the k-th best of each wave's lanes is a
-// bound that k logits reach, the best such bound of the waves holds for the row, and only
-// the quarters whose note reaches it, k of them and some more, can hold logits that do: they
-// are read once more, by all lanes, and what reaches the bound is ordered by counting. Notes
-// are ordered as the logits are (value, then vector), so that rows of equal logits end in as
-// few candidates as others.
+// The top k (largest first, equal logits by lower token) come from the same pass. Every lane
+// notes its largest logit and the vector that has it first; a search over the bits of the
+// workgroup's notes gives a bound that k logits reach and few more do, and what reaches it is
+// ordered by counting. Notes are ordered as the logits are (value, then vector), so that rows
+// of equal logits end in as few candidates as others. Two kernels:
+//   parts of a row that its workgroup's registers hold (up to 16,384 bf16 logits): all loads
+//   at once, and the candidates are still there;
+//   longer ones, two vectors ahead: notes for each quarter, and the quarters whose note
+//   reaches the bound are read once more.
+// Parts of a row meet in a second launch.
 //
-// What bounds it: reading the logits, and for bf16 as much the vector unit: an unpacking,
-// an fma, an exponential (four slots), a sum, an fma, two maxima and a comparison per
-// logit are about 10 slots, 2 bytes.
+// What bounds it: reading the logits, and for bf16 as much the vector unit: an unpacking, an
+// fma, an exponential (four slots), a sum, an fma, two maxima and a comparison per logit are
+// about 10 slots, 2 bytes (2,048 rows of 131,072 bf16 logits with 5 alternatives: 99 us,
+// 5.4 TB/s; a read of as many bytes 76). Few rows are a chain of small steps: a row takes a
+// workgroup 12,500 cycles, of which the loads 2,700, the sums 3,100, the bound 2,100 and the
+// order of its candidates 3,700, and 8,000 the launch that joins 16 of them (one row 10.4 us
+// on the device, 48 of 100,003 13.5, 64 fp32 ones 17.3).
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
@@ -40,6 +46,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kAhead = 2;        // vectors that a lane has in flight
+constexpr int kHeld = 8;         // vectors that a lane holds of a short part
 constexpr float kNone = -3.402823466e38f;   // a reference below every logit
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -103,9 +110,6 @@ __device__ __forceinline__ float over_wave(float v, float none, Op op) {
 }
 __device__ __forceinline__ float wave_max(float v) {
   return over_wave(v, -__builtin_inff(), [](float x, float y) { return fmaxf(x, y); });
-}
-__device__ __forceinline__ float wave_min(float v) {
-  return over_wave(v, __builtin_inff(), [](float x, float y) { return fminf(x, y); });
 }
 __device__ __forceinline__ float wave_sum(float v) {
   return over_wave(v, 0.f, [](float x, float y) { return x + y; });
@@ -204,26 +208,6 @@ static_assert(kCap >= kLogprobsMaxTop + 64 * 8, "the kept ones and a whole vecto
 // LDS that the lanes of one wave exchange: in order as it is, but not for the compiler.
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// The k-th largest of the lanes' values (k <= 64; equal ones counted each): a few by taking
-// the largest away, more by counting for each lane (12 instructions for each of the k
-// against 200).
-__device__ __forceinline__ float kth_value(float v, int k) {
-  if (k <= 16) {
-    float m = wave_max(v);
-    for (int i = 1; i < k; ++i) {
-      const uint64_t b = __ballot(v == m);
-      if (!b) return -__builtin_inff();   // NaNs only
-      if (int(threadIdx.x & 63) == int(__ffsll((unsigned long long)b)) - 1) v = -__builtin_inff();
-      m = wave_max(v);
-    }
-    return m;
-  }
-  int above = 0;
-#pragma unroll 16
-  for (int j = 0; j < 64; ++j) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), j)) > v;
-  return wave_min(above < k ? v : __builtin_inff());
-}
-
 // A lane's largest logit and the first vector that has it (-infinity: none).
 struct Note {
   float x = -__builtin_inff();
@@ -231,29 +215,50 @@ struct Note {
 };
 __device__ __forceinline__ uint64_t key_of(const Note& n) { return n.x > -__builtin_inff() ? key_of(n.x, n.v) : 0; }
 
-// The key of the k-th best note of the lanes, 0 where fewer have one.
-__device__ __forceinline__ uint64_t kth_note(const Note& n, int k) {
-  const float x = kth_value(n.x, k);
-  if (!(x > -__builtin_inff())) return 0;
-  uint64_t equal = __ballot(n.x == x);
-  // of equal ones as many as are left, from the first vector on
-  int left = k - int(__popcll(__ballot(n.x > x)));
-  if (int(__popcll(equal)) > left) {
-    int32_t v = -1;
-    bool in = n.x == x;
-    for (; left > 0; --left) {
-      v = in ? n.v : INT32_MAX;
+// A bound that k to `enough` of a wave's keys reach (N of each lane; 0: fewer than k are not
+// 0), bit by bit from the top: of the value while it leaves too many, then of the numbers
+// below `past`.
+template <int N>
+__device__ __forceinline__ uint64_t bound_of(const uint64_t (&key)[N], int k, int enough, int32_t past) {
+  const int bits = 32 - __builtin_clz(uint32_t(max(past, 1)));
+  uint32_t hi = 0, lo = ~uint32_t(0) << bits;
+  int n = INT32_MAX;
+  for (uint32_t bit = 1u << 31; bit && n > enough; bit >>= 1) {
+    int c = 0;
 #pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) v = min(v, __shfl_xor(v, d));
-      in = in && n.v != v;
+    for (int i = 0; i < N; ++i) c += int(__popcll(__ballot(uint32_t(key[i] >> 32) >= (hi | bit))));
+    if (c >= k) {
+      hi |= bit;
+      n = c;
     }
-    return key_of(x, v);
   }
-  int32_t v = 0;
-  for (; equal; equal &= equal - 1)
-    v = max(v, int32_t(__builtin_amdgcn_readlane(n.v, int(__ffsll((unsigned long long)equal)) - 1)));
-  return key_of(x, v);
+  if (hi == 0) return 0;
+  if (n <= enough) return uint64_t(hi) << 32;
+  for (uint32_t bit = 1u << (bits - 1); bit && n > enough; bit >>= 1) {
+    const uint64_t some = (uint64_t(hi) << 32) | lo | bit;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) c += int(__popcll(__ballot(key[i] >= some)));
+    if (c >= k) {
+      lo |= bit;
+      n = c;
+    }
+  }
+  return (uint64_t(hi) << 32) | lo;
 }
+// Whether a logit of a vector reaches it: above its value, or equal and of a vector up to its one.
+struct Bound {
+  float x = -__builtin_inff();
+  uint32_t end = 0;   // vectors below it
+  __device__ __forceinline__ explicit Bound(uint64_t key) {
+    if (key) {
+      const uint32_t lo = uint32_t(key);
+      x = value_of(key);
+      end = lo ? 0u - lo : 0xffffffffu;
+    }
+  }
+  __device__ __forceinline__ bool reached(float y, int32_t v) const { return y > x || (y == x && uint32_t(v) < end); }
+};
 
 // How many of n keys in LDS are above one; eight reads at a time.
 __device__ __forceinline__ int before_of(const uint64_t* keys, int n, uint64_t key) {
@@ -325,7 +330,7 @@ struct RowStats {   // of a split
 struct Args {
   LogprobRows r;
   float c;                 // scale log2 e
-  int32_t splits;
+  int32_t splits, per;     // per: vectors of a split (0: an equal share)
   RowStats* stats;         // [rows][splits], with more than one
   uint64_t* keys;          // [rows][splits][top]
 };
@@ -360,13 +365,13 @@ __device__ __forceinline__ void write_row(const Args& a, int64_t row, const RowS
   if (a.r.logprob) a.r.logprob[row] = ok && g.id >= 0 ? over_ref(a, g.x, s.ref) - ln : nan;
   if (a.r.rank) a.r.rank[row] = ok && g.id >= 0 && g.x > -__builtin_inff() ? s.above : -1;
 }
-// Place i of its top alternatives (key 0: none).
-__device__ __forceinline__ void write_top(const Args& a, int64_t row, const RowStats& s, int i, uint64_t key) {
+// Place i of its top alternatives (key 0: none); ln: of s.S.
+__device__ __forceinline__ void write_top(const Args& a, int64_t row, const RowStats& s, float ln, int i, uint64_t key) {
   const bool ok = has_distribution(s);
   const int64_t at = row * a.r.top + i;
   if (a.r.top_ids) a.r.top_ids[at] = ok && key ? id_of(key) : -1;
   if (a.r.top_logprobs)
-    a.r.top_logprobs[at] = !ok ? __builtin_nanf("") : key ? over_ref(a, value_of(key), s.ref) - logf(s.S) : -__builtin_inff();
+    a.r.top_logprobs[at] = !ok ? __builtin_nanf("") : key ? over_ref(a, value_of(key), s.ref) - ln : -__builtin_inff();
 }
 
 // Loads that are known to be from global memory: those that might be from LDS are waited for
@@ -390,160 +395,125 @@ __device__ __forceinline__ Given given_token(const Args& a, int64_t row) {
   return g;
 }
 
-constexpr int kQuarters = 4;
+// n keys in LDS to their places among the first `top`, put(place, key), and 0 to those that
+// are left over. Up to 64 by all waves, each against its part of them.
+template <typename Put>
+__device__ __forceinline__ void order_keys(const uint64_t* keys, int n, int top, int (*counts)[64], Put put) {
+  if (n <= 64) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const uint64_t key = lane < n ? keys[lane] : 0;
+    int before = 0;
+    for (int j = wave; j < n; j += 8 * kWaves) {
+      uint64_t some[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) some[i] = keys[min(j + i * kWaves, n - 1)];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) before += j + i * kWaves < n && some[i] > key;
+    }
+    counts[wave][lane] = before;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) before += counts[w][lane];
+    if (lane >= n) before = lane;   // fewer than asked for
+    if (before < top) put(before, key);
+    return;
+  }
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const uint64_t key = keys[i];
+    const int before = before_of(keys, n, key);
+    if (before < top) put(before, key);
+  }
+}
 
-template <typename T, bool kTop>
-__global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
-  constexpr int W = Type<T>::kW, kBatch = kAhead * kThreads;
-  __shared__ uint64_t lists[kTop ? kWaves * kCap : 1];
-  __shared__ uint64_t notes[kTop ? kQuarters * kThreads : 1];
-  __shared__ uint16_t pairs[kTop ? kQuarters * kThreads : 1];
-  __shared__ RowStats parts[kWaves];
-  __shared__ uint64_t bounds[kWaves];
-  __shared__ int counts[kWaves], n_pairs, n_best;
-  const int64_t block = block_of();
-  const int64_t row = block / a.splits;
-  if (row >= a.r.rows) return;
-  const int split = int(block % a.splits);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  const T* x0 = static_cast<const T*>(a.r.logits) + row * a.r.stride;
-  // vectors of W logits on 16 bytes; vector v holds tokens v W - shift .. + W - 1, the
-  // whole ones are v0 .. v1 - 1
-  const int shift = int(reinterpret_cast<uintptr_t>(x0) / sizeof(T) % W);
-  const T* base = x0 - shift;
-  const int32_t v0 = shift ? 1 : 0, v1 = (shift + a.r.vocab) / W;
-  const int32_t whole = max(v1 - v0, 0);
-  const int32_t per = (whole + a.splits - 1) / a.splits;
-  const int32_t lo = v0 + min(split * per, whole), hi = v0 + min((split + 1) * per, whole);
-  // batches of kAhead vectors for each lane; the last one is broken
-  const int32_t batches = (hi - lo) / kBatch, quarter = batches / kQuarters + 1;
+// A workgroup's part of a row in vectors of W logits on 16 bytes: vector v holds tokens
+// v W - shift .. + W - 1, the row's whole ones are v0 .. v1 - 1, the part's lo .. hi - 1.
+template <typename T>
+struct Part {
+  static constexpr int W = Type<T>::kW;
+  int64_t row;
+  int split, shift;
+  const T *x0, *base;
+  int32_t v1, lo, hi;
+  bool head, tail;   // it has the row's broken vector before, or behind, the whole ones
+
+  __device__ __forceinline__ Part(const Args& a, int64_t block) {
+    row = block / a.splits;
+    split = int(block % a.splits);
+    x0 = static_cast<const T*>(a.r.logits) + row * a.r.stride;
+    shift = int(reinterpret_cast<uintptr_t>(x0) / sizeof(T) % W);
+    base = x0 - shift;
+    const int32_t v0 = shift ? 1 : 0;
+    v1 = (shift + a.r.vocab) / W;
+    const int32_t whole = max(v1 - v0, 0), per = a.per ? a.per : (whole + a.splits - 1) / a.splits;
+    lo = v0 + min(split * per, whole);
+    hi = v0 + min((split + 1) * per, whole);
+    head = split == 0 && shift != 0;
+    tail = split == a.splits - 1 && (shift + a.r.vocab) % W != 0 && (shift == 0 || v1 > 0);
+  }
   // the pass asks the caches not to keep it: 2,048 rows of 131,072 bf16 logits 97 us against 90
-  auto stream = [&](int32_t v) {
+  __device__ __forceinline__ u32x4 stream(int32_t v) const {
     typedef const __attribute__((address_space(1))) u32x4* Global;
     return __builtin_nontemporal_load((Global)(reinterpret_cast<uintptr_t>(base + int64_t(v) * W)));
-  };
-  auto load = [&](int32_t v) { return from_global(reinterpret_cast<const u32x4*>(base + int64_t(v) * W)); };
-  u32x4 next[kAhead];
-  auto load_some = [&](int32_t v) {
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      next[j][0] = next[j][1] = next[j][2] = next[j][3] = Type<T>::kMasked;
-      if (v + j * kThreads < hi) next[j] = load(v + j * kThreads);
-    }
-  };
-  if (batches > 0) {
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) next[j] = stream(lo + j * kThreads + int(threadIdx.x));
-  } else {
-    load_some(lo + int(threadIdx.x));
   }
+  __device__ __forceinline__ u32x4 load(int32_t v) const {
+    return from_global(reinterpret_cast<const u32x4*>(base + int64_t(v) * W));
+  }
+  // Its broken vectors, in lanes 0 and 1 of a wave (what they lack, and the other lanes', is masked).
+  __device__ __forceinline__ int32_t edge_vector() const { return (threadIdx.x & 63) == 0 ? 0 : v1; }
+  __device__ __forceinline__ u32x4 edge(int32_t vocab) const {
+    const int lane = threadIdx.x & 63;
+    const bool has = lane == 0 ? head : lane == 1 && tail;
+    uint32_t one[W];
+#pragma unroll
+    for (int e = 0; e < W; ++e) {   // all asked for at once, where there is none another of the row
+      const int32_t id = min(max(edge_vector() * W - shift + e, 0), vocab - 1);
+      if constexpr (sizeof(T) == 2) one[e] = from_global(x0 + id);
+      else one[e] = __float_as_uint(from_global(x0 + id));
+    }
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      const int32_t id = edge_vector() * W - shift + e;
+      const uint32_t x = has && id >= 0 && id < vocab ? one[e] : Type<T>::kMasked & (sizeof(T) == 2 ? 0xffffu : 0xffffffffu);
+      if constexpr (sizeof(T) == 2) v[e / 2] = e % 2 ? v[e / 2] | (x << 16) : x;
+      else v[e] = x;
+    }
+    return v;
+  }
+};
 
-  const Given g = given_token<T>(a, row);
-  const int32_t given_at = g.id >= 0 ? (g.id + shift) / W : -1;
-  const float not_below = below(g.x);
-  if (kTop && threadIdx.x == 0) n_pairs = n_best = 0;
-  Sums sums;
-  bool masked = false;
+// The largest of a vector's logits.
+template <int W>
+__device__ __forceinline__ float largest(const float (&x)[W]) {
+  float t = -__builtin_inff();
+#pragma unroll
+  for (int e = 0; e < W; e += 2) t = fmaxf(fmaxf(t, x[e]), x[e + 1]);
+  return t;
+}
+
+// How many logits of a wave's vectors (at: each lane's) come before the given token.
+template <int W>
+__device__ __forceinline__ int count_above(const float (&x)[W], int32_t at, const Given& g, float not_below, int32_t given_at,
+                                           int shift) {
+  const float past = at < given_at ? not_below : g.x;
   int above = 0;
-  Note best, note;   // of the lane, and of its quarter
-
-  // N vectors of the lane, v and each kThreads behind the other; their largest logit
-  auto stats = [&](const auto& raw, int32_t v, auto size) {
-    constexpr int N = decltype(size)::value;
-    float x[N][W], top = -__builtin_inff();
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      Type<T>::unpack(raw[j], x[j]);
-      float t = -__builtin_inff();
+  for (int e = 0; e < W; ++e) above += int(__popcll(__ballot(x[e] > past)));
+  if (__any(at == given_at)) {
 #pragma unroll
-      for (int e = 0; e < W; e += 2) t = fmaxf(fmaxf(t, x[j][e]), x[j][e + 1]);
-      top = fmaxf(top, t);
-      if (kTop && N > 1) {
-        const bool more = t > note.x;
-        note.x = more ? t : note.x;
-        note.v = more ? v + j * kThreads : note.v;
-      }
-    }
-    add<N, W>(sums, masked, x, top, a.c);
-    if (a.r.rank && __any(top > not_below)) {
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const int32_t at = v + j * kThreads;
-        const float past = at < given_at ? not_below : g.x;
-#pragma unroll
-        for (int e = 0; e < W; ++e) above += int(__popcll(__ballot(x[j][e] > past)));
-        if (__any(at == given_at)) {
-#pragma unroll
-          for (int e = 0; e < W; ++e)
-            above += int(__popcll(__ballot(at == given_at && x[j][e] == g.x && at * W - shift + e < g.id)));
-        }
-      }
-    }
-    return top;
-  };
-  auto end_quarter = [&](int q) {
-    if (!kTop) return;
-    notes[q * kThreads + threadIdx.x] = key_of(note);
-    if (note.x > best.x) best = note;
-    note = Note{};
-  };
-
-  int q = 0;
-  int32_t left = quarter;   // batches of the quarter
-  for (int32_t i = 0; i < batches; ++i) {
-    const int32_t v = lo + i * kBatch + int(threadIdx.x);
-    u32x4 raw[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) raw[j] = next[j];
-    // behind the last batch it is asked for again: loads under a condition would all be waited for
-    const int32_t ahead = i + 1 < batches ? v + kBatch : v;
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) next[j] = stream(ahead + j * kThreads);
-    stats(raw, v, Size<kAhead>{});
-    if (kTop && --left == 0) {
-      end_quarter(q++);
-      left = quarter;
-    }
+    for (int e = 0; e < W; ++e)
+      above += int(__popcll(__ballot(at == given_at && x[e] == g.x && at * W - shift + e < g.id)));
   }
-  if (int32_t v = lo + batches * kBatch + int(threadIdx.x); v - lane < hi) {   // whole waves
-    if (batches > 0) load_some(v);
-    stats(next, v, Size<kAhead>{});
-  }
-  if (kTop)
-    for (; q < kQuarters; ++q) end_quarter(q);
-  // the row's broken vectors, before and behind the whole ones, by lanes 0 and 1 of a wave
-  const bool head = split == 0 && shift != 0, tail = split == a.splits - 1 && (shift == 0 || v1 > 0);
-  u32x4 edge[1];
-  edge[0][0] = edge[0][1] = edge[0][2] = edge[0][3] = Type<T>::kMasked;
-  const int32_t edge_v = lane == 0 ? 0 : v1;
-  float edge_top = -__builtin_inff();
-  if (wave == 0 && (head || tail)) {
-    if (lane == 0 ? head : lane == 1 && tail) {
-#pragma unroll
-      for (int e = 0; e < W; ++e) {
-        const int32_t id = edge_v * W - shift + e;
-        if (id >= 0 && id < a.r.vocab) {
-          if constexpr (sizeof(T) == 2) {
-            const uint32_t b = from_global(x0 + id);
-            edge[0][e / 2] = e % 2 ? (edge[0][e / 2] & 0xffffu) | (b << 16) : (edge[0][e / 2] & 0xffff0000u) | b;
-          } else {
-            edge[0][e] = __float_as_uint(from_global(x0 + id));
-          }
-        }
-      }
-    }
-    edge_top = stats(edge, edge_v, Size<1>{});
-  }
+  return above;
+}
 
-  // the wave's sums, then the workgroup's
+// The workgroup's sums from its waves' (a barrier).
+__device__ __forceinline__ RowStats workgroup_sums(Sums& sums, int above, RowStats* parts, float c) {
   const float ref = wave_max(sums.ref);
-  sums.move(ref, a.c, true);
+  sums.move(ref, c, true);
   RowStats s{ref, wave_sum(sums.S), wave_sum(sums.U), above};
-  if (kTop) {
-    const uint64_t bound = kth_note(best, a.r.top);
-    if (lane == 0) bounds[wave] = bound;
-  }
-  if (lane == 0) parts[wave] = s;
+  if ((threadIdx.x & 63) == 0) parts[threadIdx.x / 64] = s;
   __syncthreads();
   float to = parts[0].ref;
 #pragma unroll
@@ -552,90 +522,34 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     Sums one{parts[w].ref, parts[w].S, parts[w].U};
-    one.move(to, a.c, true);
+    one.move(to, c, true);
     s.S += one.S;
     s.U += one.U;
     s.above += parts[w].above;
   }
-  if (threadIdx.x == 0) {
-    if (a.splits > 1) a.stats[block] = s;
-    else write_row(a, row, s, g);
-  }
-  if (!kTop) return;
-  // Any wave's bound holds for the row, and so does the k-th best of the lanes that reach the
-  // best of them (each wave's alone is about the 3 k-th of the row's).
-  uint64_t bound = bounds[0];
+  return s;
+}
+
+// The bound of the workgroup's notes, by each of its waves.
+__device__ __forceinline__ uint64_t row_bound(const uint64_t* notes, int k, int32_t past) {
+  const int lane = threadIdx.x & 63;
+  uint64_t key[kWaves];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) bound = max(bound, bounds[w]);
-  if (bound) {
-    const uint64_t mine = key_of(best);
-    if (mine >= bound) lists[atomicAdd(&n_best, 1)] = mine;
-    __syncthreads();
-    const int n = n_best;
-    if (int(threadIdx.x) < n) {
-      const uint64_t key = lists[threadIdx.x];
-      if (before_of(lists, n, key) == a.r.top - 1) bounds[0] = key;
-    }
-    __syncthreads();
-    bound = bounds[0];
-  }
-  for (int i = 0; i < kQuarters; ++i) {
-    const uint64_t key = notes[i * kThreads + threadIdx.x];
-    const bool in = key != 0 && key >= bound;
-    const uint64_t b = __ballot(in);
-    if (!b) continue;
-    int at = 0;
-    if (lane == 0) at = atomicAdd(&n_pairs, int(__popcll(b)));
-    at = __builtin_amdgcn_readfirstlane(at);
-    if (in) pairs[at + int(__popcll(b & lanes_below()))] = uint16_t(i * kThreads + threadIdx.x);
-  }
-  __syncthreads();
-  // their vectors: logits that the bound's vector has come in it or before it
-  const float bound_x = bound ? value_of(bound) : -__builtin_inff();
-  const int32_t bound_v = bound ? id_of(bound) : INT32_MAX;
-  List list{lists + wave * kCap, 0, a.r.top, bound_x};
-  const int32_t each = quarter * kAhead;   // vectors of a quarter
-  auto find = [&](const u32x4& raw, int32_t v, bool in) {
-    float x[W];
-    Type<T>::unpack(raw, x);
-    bool some = false;
-#pragma unroll
-    for (int e = 0; e < W; ++e) some = some || x[e] >= list.bound;
-    if (__any(in && some))
-      list.push<W>(x, v * W - shift, [&](int e) {
-        return in && x[e] >= list.bound && x[e] > -__builtin_inff() && (x[e] > bound_x || v <= bound_v);
-      });
-  };
-  const uint32_t items = uint32_t(n_pairs) * uint32_t(each);   // below 2^28: 1,024 of at most 2^18
-  for (uint32_t i = 64 * wave; i < items; i += 2 * kThreads) {
-    u32x4 raw[2];
-    int32_t at[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t item = min(i + j * kThreads + lane, items - 1);   // past the end the last one, not taken
-      const uint32_t p = item / uint32_t(each), n = item - p * uint32_t(each);
-      const uint32_t pair = pairs[p], batch = pair / kThreads * quarter + n / kAhead;
-      at[j] = lo + int32_t((batch * kAhead + n % kAhead) * kThreads + pair % kThreads);
-      // a quarter's last vectors may lie past the split
-      if (at[j] >= hi || i + j * kThreads + lane >= items) at[j] = -1;
-      raw[j] = load(at[j] < 0 ? lo : at[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-      if (i + j * kThreads < items) find(raw[j], at[j], at[j] >= 0);
-  }
-  if (wave == 0 && __any(edge_top >= bound_x && edge_top > -__builtin_inff())) {
-    // before or behind all others, so that the bound's vector does not count
-    float x[W];
-    Type<T>::unpack(edge[0], x);
-    list.push<W>(x, edge_v * W - shift, [&](int e) { return x[e] >= bound_x && x[e] > -__builtin_inff(); });
-  }
+  for (int w = 0; w < kWaves; ++w) key[w] = notes[64 * w + lane];
+  return bound_of(key, k, k + k / 4 + 4, past);
+}
+
+// The first of the waves' candidates in order, to the workspace or the results.
+__device__ __forceinline__ void write_first(const Args& a, int64_t block, int64_t row, const RowStats& s, const List& list,
+                                            const uint64_t* lists, int* counts) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   if (lane == 0) counts[wave] = list.count;
   __syncthreads();
   uint64_t* out = a.splits > 1 ? a.keys + block * a.r.top : nullptr;
+  const float ln = logf(s.S);
   auto put = [&](int i, uint64_t key) {
     if (out) out[i] = key;
-    else write_top(a, row, s, i, key);
+    else write_top(a, row, s, ln, i, key);
   };
   int n = 0;
 #pragma unroll
@@ -668,35 +582,349 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   }
 }
 
+constexpr int kVectors = 512, kKeys = 1024;   // of a workgroup that may be candidates
+static_assert(2 * kVectors + kKeys <= kWaves * kCap, "both in the lists' place");
+
+// A part of at most N vectors for each lane, which hold them until its candidates are found:
+// all loads at once, one reference and one bound.
+template <typename T, bool kTop, int N>
+__global__ __launch_bounds__(kThreads, 4) void logprob_held_kernel(Args a) {
+  constexpr int W = Type<T>::kW;
+  __shared__ __attribute__((aligned(16))) uint64_t lists[kTop ? kWaves * kCap : 1];
+  __shared__ uint64_t notes[kTop ? kThreads : 1];
+  __shared__ int32_t at[kTop ? kVectors : 1];
+  __shared__ RowStats parts[kWaves];
+  __shared__ int places[kTop ? kWaves : 1][64], counts[kWaves], n_vectors, n_keys;
+  const int64_t block = block_of();
+  if (block / a.splits >= a.r.rows) return;
+  const Part<T> p(a, block);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  const int32_t token = a.r.tokens ? from_global(a.r.tokens + p.row) : -1;
+  u32x4 raw[N];
+  if (p.hi > p.lo) {   // past the end its last one, masked below
+#pragma unroll
+    for (int j = 0; j < N; ++j) raw[j] = p.stream(min(p.lo + int(threadIdx.x) + j * kThreads, p.hi - 1));
+  }
+  const bool edges = wave == 0 && (p.head || p.tail);
+  u32x4 edge[1];
+  if (edges) edge[0] = p.edge(a.r.vocab);
+  Given g{0.f, -1};
+  if (token >= 0 && token < a.r.vocab) g = Given{Type<T>::one(from_global(p.x0 + token)), token};
+  const int32_t given_at = g.id >= 0 ? (g.id + p.shift) / W : -1;
+  const float not_below = below(g.x);
+  if (kTop && threadIdx.x == 0) n_vectors = n_keys = 0;
+  Sums sums;
+  int above = 0;
+  float tops[N], top = -__builtin_inff();
+  Note best;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int32_t v = p.lo + int(threadIdx.x) + j * kThreads;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) raw[j][w] = v < p.hi ? raw[j][w] : Type<T>::kMasked;
+    float x[W];
+    Type<T>::unpack(raw[j], x);
+    tops[j] = largest(x);
+    if (kTop && tops[j] > best.x) best = Note{tops[j], v};
+    top = fmaxf(top, tops[j]);
+  }
+  constexpr int kPair = N < 2 ? N : 2;
+  bool masked = false;
+#pragma unroll
+  for (int j0 = 0; j0 < N; j0 += kPair) {
+    if (p.lo + j0 * kThreads >= p.hi) break;
+    float x[kPair][W];
+#pragma unroll
+    for (int j = 0; j < kPair; ++j) {
+      // unpacked again: kept from above, they are 64 registers more
+#pragma unroll
+      for (int w = 0; w < 4; ++w) asm volatile("" : "+v"(raw[j0 + j][w]));
+      Type<T>::unpack(raw[j0 + j], x[j]);
+    }
+    add<kPair, W>(sums, masked, x, top, a.c);
+    if (a.r.rank) {
+#pragma unroll
+      for (int j = 0; j < kPair; ++j)
+        if (__any(tops[j0 + j] > not_below))
+          above += count_above(x[j], p.lo + int(threadIdx.x) + (j0 + j) * kThreads, g, not_below, given_at, p.shift);
+    }
+  }
+  float edge_top = -__builtin_inff();
+  if (edges) {
+    float x[1][W];
+    Type<T>::unpack(edge[0], x[0]);
+    edge_top = largest(x[0]);
+    masked = true;
+    add<1, W>(sums, masked, x, edge_top, a.c);
+    if (a.r.rank && __any(edge_top > not_below))
+      above += count_above(x[0], p.edge_vector(), g, not_below, given_at, p.shift);
+  }
+  if (kTop) notes[threadIdx.x] = key_of(best);
+  const RowStats s = workgroup_sums(sums, above, parts, a.c);
+  if (threadIdx.x == 0) {
+    if (a.splits > 1) a.stats[block] = s;
+    else write_row(a, p.row, s, g);
+  }
+  if (!kTop) return;
+  // the vectors that reach the bound, then their logits, go to LDS
+  const Bound bound(row_bound(notes, a.r.top, p.v1));
+  auto reaches = [&](float x, int32_t v) { return bound.reached(x, v); };
+  u32x4* vectors = reinterpret_cast<u32x4*>(lists);
+  uint64_t* keys = lists + 2 * kVectors;
+  uint64_t in[N + 1];
+  int found = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    in[j] = __ballot(reaches(tops[j], p.lo + int(threadIdx.x) + j * kThreads));
+    found += int(__popcll(in[j]));
+  }
+  in[N] = __ballot(edges && reaches(edge_top, p.edge_vector()));
+  found += int(__popcll(in[N]));
+  if (found) {
+    int n = 0;
+    if (lane == 0) n = atomicAdd(&n_vectors, found);
+    n = __builtin_amdgcn_readfirstlane(n);
+#pragma unroll
+    for (int j = 0; j <= N; ++j) {
+      const int to = n + int(__popcll(in[j] & lanes_below()));
+      if ((in[j] >> lane & 1) && to < kVectors) {
+        vectors[to] = j < N ? raw[j < N ? j : 0] : edge[0];
+        at[to] = j < N ? p.lo + int(threadIdx.x) + j * kThreads : p.edge_vector();
+      }
+      n += int(__popcll(in[j]));
+    }
+  }
+  __syncthreads();
+  const int nv = n_vectors;
+  if (nv <= kVectors) {
+    for (int i = threadIdx.x; i < nv * W; i += kThreads) {
+      const int32_t v = at[i / W];
+      const float x = Type<T>::one(reinterpret_cast<const T*>(lists)[i]);
+      if (!reaches(x, v)) continue;
+      const int n = atomicAdd(&n_keys, 1);
+      if (n < kKeys) keys[n] = key_of(x, v * W - p.shift + i % W);
+    }
+    __syncthreads();
+    const int n = n_keys;
+    if (n <= kKeys) {
+      uint64_t* out = a.splits > 1 ? a.keys + block * a.r.top : nullptr;
+      const float ln = logf(s.S);
+      auto put = [&](int i, uint64_t key) {
+        if (out) out[i] = key;
+        else write_top(a, p.row, s, ln, i, key);
+      };
+      order_keys(keys, n, a.r.top, places, put);
+      return;
+    }
+    __syncthreads();
+  }
+  // more than there is room for (many equal logits): each wave its own, the best of them kept
+  List list{lists + wave * kCap, 0, a.r.top, bound.x};
+  auto push = [&](const u32x4& raw_v, float top, int32_t v) {
+    if (!__any(reaches(top, v))) return;
+    float x[W];
+    Type<T>::unpack(raw_v, x);
+    list.push<W>(x, v * W - p.shift, [&](int e) { return x[e] >= list.bound && reaches(x[e], v); });
+  };
+#pragma unroll
+  for (int j = 0; j < N; ++j) push(raw[j], tops[j], p.lo + int(threadIdx.x) + j * kThreads);
+  if (edges) push(edge[0], edge_top, p.edge_vector());
+  write_first(a, block, p.row, s, list, lists, counts);
+}
+
+constexpr int kQuarters = 4;
+
+template <typename T, bool kTop>
+__global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
+  constexpr int W = Type<T>::kW, kBatch = kAhead * kThreads;
+  __shared__ uint64_t lists[kTop ? kWaves * kCap : 1];
+  __shared__ uint64_t notes[kTop ? kQuarters * kThreads : 1];
+  __shared__ uint16_t pairs[kTop ? kQuarters * kThreads : 1];
+  __shared__ RowStats parts[kWaves];
+  __shared__ int counts[kWaves], n_pairs;
+  const int64_t block = block_of();
+  if (block / a.splits >= a.r.rows) return;
+  const Part<T> p(a, block);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, shift = p.shift;
+  const int64_t row = p.row;
+  const int32_t lo = p.lo, hi = p.hi;
+  // batches of kAhead vectors for each lane; the last one is broken
+  const int32_t batches = (hi - lo) / kBatch, quarter = batches / kQuarters + 1;
+  u32x4 next[kAhead];
+  auto load_some = [&](int32_t v) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      next[j][0] = next[j][1] = next[j][2] = next[j][3] = Type<T>::kMasked;
+      if (v + j * kThreads < hi) next[j] = p.load(v + j * kThreads);
+    }
+  };
+  if (batches > 0) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) next[j] = p.stream(lo + j * kThreads + int(threadIdx.x));
+  } else {
+    load_some(lo + int(threadIdx.x));
+  }
+
+  const Given g = given_token<T>(a, row);
+  const int32_t given_at = g.id >= 0 ? (g.id + shift) / W : -1;
+  const float not_below = below(g.x);
+  if (kTop && threadIdx.x == 0) n_pairs = 0;
+  Sums sums;
+  bool masked = false;
+  int above = 0;
+  Note best, note;   // of the lane, and of its quarter
+
+  // N vectors of the lane, v and each kThreads behind the other; their largest logit
+  auto stats = [&](const auto& raw, int32_t v, auto size) {
+    constexpr int N = decltype(size)::value;
+    float x[N][W], top = -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      Type<T>::unpack(raw[j], x[j]);
+      const float t = largest(x[j]);
+      top = fmaxf(top, t);
+      if (kTop && N > 1) {
+        const bool more = t > note.x;
+        note.x = more ? t : note.x;
+        note.v = more ? v + j * kThreads : note.v;
+      }
+    }
+    add<N, W>(sums, masked, x, top, a.c);
+    if (a.r.rank && __any(top > not_below)) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) above += count_above(x[j], v + j * kThreads, g, not_below, given_at, shift);
+    }
+    return top;
+  };
+  auto end_quarter = [&](int q) {
+    if (!kTop) return;
+    notes[q * kThreads + threadIdx.x] = key_of(note);
+    if (note.x > best.x) best = note;
+    note = Note{};
+  };
+
+  int q = 0;
+  int32_t left = quarter;   // batches of the quarter
+  for (int32_t i = 0; i < batches; ++i) {
+    const int32_t v = lo + i * kBatch + int(threadIdx.x);
+    u32x4 raw[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) raw[j] = next[j];
+    // behind the last batch it is asked for again: loads under a condition would all be waited for
+    const int32_t ahead = i + 1 < batches ? v + kBatch : v;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) next[j] = p.stream(ahead + j * kThreads);
+    stats(raw, v, Size<kAhead>{});
+    if (kTop && --left == 0) {
+      end_quarter(q++);
+      left = quarter;
+    }
+  }
+  if (int32_t v = lo + batches * kBatch + int(threadIdx.x); v - lane < hi) {   // whole waves
+    if (batches > 0) load_some(v);
+    stats(next, v, Size<kAhead>{});
+  }
+  if (kTop)
+    for (; q < kQuarters; ++q) end_quarter(q);
+  u32x4 edge[1];
+  const int32_t edge_v = p.edge_vector();
+  float edge_top = -__builtin_inff();
+  if (wave == 0 && (p.head || p.tail)) {
+    edge[0] = p.edge(a.r.vocab);
+    edge_top = stats(edge, edge_v, Size<1>{});
+  }
+
+  if (kTop) lists[threadIdx.x] = key_of(best);
+  const RowStats s = workgroup_sums(sums, above, parts, a.c);
+  if (threadIdx.x == 0) {
+    if (a.splits > 1) a.stats[block] = s;
+    else write_row(a, row, s, g);
+  }
+  if (!kTop) return;
+  const uint64_t key_bound = row_bound(lists, a.r.top, p.v1);
+  const Bound bound(key_bound);
+  for (int i = 0; i < kQuarters; ++i) {
+    const uint64_t key = notes[i * kThreads + threadIdx.x];
+    const bool in = key != 0 && key >= key_bound;
+    const uint64_t b = __ballot(in);
+    if (!b) continue;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&n_pairs, int(__popcll(b)));
+    at = __builtin_amdgcn_readfirstlane(at);
+    if (in) pairs[at + int(__popcll(b & lanes_below()))] = uint16_t(i * kThreads + threadIdx.x);
+  }
+  __syncthreads();
+  // their vectors: logits that the bound's vector has come in it or before it
+  List list{lists + wave * kCap, 0, a.r.top, bound.x};
+  const int32_t each = quarter * kAhead;   // vectors of a quarter
+  auto find = [&](const u32x4& raw, int32_t v, bool in) {
+    float x[W];
+    Type<T>::unpack(raw, x);
+    bool some = false;
+#pragma unroll
+    for (int e = 0; e < W; ++e) some = some || x[e] >= list.bound;
+    if (__any(in && some))
+      list.push<W>(x, v * W - shift, [&](int e) {
+        return in && x[e] >= list.bound && bound.reached(x[e], v);
+      });
+  };
+  const uint32_t items = uint32_t(n_pairs) * uint32_t(each);   // below 2^28: 1,024 of at most 2^18
+  for (uint32_t i = 64 * wave; i < items; i += 2 * kThreads) {
+    u32x4 raw[2];
+    int32_t at[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t item = min(i + j * kThreads + lane, items - 1);   // past the end the last one, not taken
+      const uint32_t nth = item / uint32_t(each), n = item - nth * uint32_t(each);
+      const uint32_t pair = pairs[nth], batch = pair / kThreads * quarter + n / kAhead;
+      at[j] = lo + int32_t((batch * kAhead + n % kAhead) * kThreads + pair % kThreads);
+      // a quarter's last vectors may lie past the split
+      if (at[j] >= hi || i + j * kThreads + lane >= items) at[j] = -1;
+      raw[j] = p.load(at[j] < 0 ? lo : at[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (i + j * kThreads < items) find(raw[j], at[j], at[j] >= 0);
+  }
+  if (wave == 0 && __any(bound.reached(edge_top, edge_v))) {
+    float x[W];
+    Type<T>::unpack(edge[0], x);
+    list.push<W>(x, edge_v * W - shift, [&](int e) { return x[e] >= list.bound && bound.reached(x[e], edge_v); });
+  }
+  write_first(a, block, row, s, list, lists, counts);
+}
+
 // The splits of a row. As in a split, a bound that enough keys reach, of the first (or, of
 // few splits, later) places of their lists, leaves few to be ordered by counting; where it
 // leaves many (ascending logits: all the best in one split), a wave takes them one by one,
 // each lane the next of a split's (tokens ascend with the splits, so that the first of equal
-// lanes is next).
+// lanes is next). The last wave joins the sums meanwhile.
 constexpr int kFew = 512;
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void logprob_merge_kernel(Args a) {
   __shared__ uint64_t keys[kLogprobsMaxSplits * kLogprobsMaxTop];
-  __shared__ uint64_t heads[kLogprobsMaxSplits], few[kFew], bound;
+  __shared__ uint64_t few[kFew];
   __shared__ RowStats total;
-  __shared__ int n_few;
+  __shared__ float total_ln;
+  __shared__ int places[kWaves][64], n_few;
   const int64_t row = block_of();
   if (row >= a.r.rows) return;
-  const int tid = threadIdx.x, top = a.r.top, n = a.splits * top;
-  const uint64_t* from = a.keys + row * n;
-  constexpr int kAtOnce = kLogprobsMaxSplits * kLogprobsMaxTop / kThreads;
-#pragma unroll
-  for (int j = 0; j < kAtOnce; ++j)
-    if (tid + j * kThreads < n) keys[tid + j * kThreads] = from_global(from + tid + j * kThreads);
-  if (tid == 0) {
-    n_few = 0;
-    bound = 0;
+  constexpr int kRest = kThreads - 64;
+  const int tid = threadIdx.x, lane = tid & 63, top = a.r.top, n = a.splits * top;
+  RowStats s{kNone, 0.f, 0.f, 0};
+  Given g{0.f, -1};
+  if (tid >= kRest) {
+    if (lane < a.splits) s = a.stats[row * a.splits + lane];
+    g = given_token<T>(a, row);
+  } else {
+    const uint64_t* from = a.keys + row * n;
+#pragma unroll 4
+    for (int i = tid; i < n; i += kRest) keys[i] = from_global(from + i);
+    if (tid == 0) n_few = 0;
   }
-  if (tid < 64) {
-    RowStats s{kNone, 0.f, 0.f, 0};
-    if (tid < a.splits) s = a.stats[row * a.splits + tid];
-    const Given g = given_token<T>(a, row);
+  __syncthreads();
+  if (tid >= kRest) {
     Sums sums{s.ref, s.S, s.U};
     const float ref = wave_max(s.ref);
     sums.move(ref, a.c, true);
@@ -704,33 +932,28 @@ __global__ __launch_bounds__(kThreads) void logprob_merge_kernel(Args a) {
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) above += __shfl_xor(above, d);
     s = RowStats{ref, wave_sum(sums.S), wave_sum(sums.U), above};
-    if (tid == 0) {
+    if (lane == 0) {
       total = s;
+      total_ln = logf(s.S);
       write_row(a, row, s, g);
+    }
+  } else if (top > 0) {
+    // `lists` of the places 0 .. place hold top keys or more
+    const int place = (top - 1) / a.splits, lists = (top + place) / (place + 1);
+    const uint64_t head[1] = {lane < a.splits ? keys[lane * top + place] : 0};
+    const uint64_t bound = max(bound_of(head, lists, lists + (a.splits - lists) / 4, a.r.vocab), uint64_t(1));
+    for (int i = tid; i < n; i += kRest) {
+      const uint64_t key = keys[i];
+      if (key < bound) continue;
+      const int at = atomicAdd(&n_few, 1);
+      if (at < kFew) few[at] = key;
     }
   }
   if (top == 0) return;
   __syncthreads();
-  // `lists` of the places 0 .. place hold top keys or more
-  const int place = (top - 1) / a.splits, lists = (top + place) / (place + 1);
-  if (tid < a.splits) heads[tid] = keys[tid * top + place];
-  __syncthreads();
-  if (tid < a.splits && heads[tid] != 0 && before_of(heads, a.splits, heads[tid]) == lists - 1) bound = heads[tid];
-  __syncthreads();
-  for (int i = tid; i < n; i += kThreads) {
-    const uint64_t key = keys[i];
-    if (key == 0 || key < bound) continue;
-    const int at = atomicAdd(&n_few, 1);
-    if (at < kFew) few[at] = key;
-  }
-  __syncthreads();
   const int m = n_few;
   if (m <= kFew) {
-    for (int i = tid; i < m; i += kThreads) {
-      const int before = before_of(few, m, few[i]);
-      if (before < top) write_top(a, row, total, before, few[i]);
-    }
-    for (int i = m + tid; i < top; i += kThreads) write_top(a, row, total, i, 0);
+    order_keys(few, m, top, places, [&](int i, uint64_t key) { write_top(a, row, total, total_ln, i, key); });
     return;
   }
   if (tid >= 64) return;
@@ -745,43 +968,68 @@ __global__ __launch_bounds__(kThreads) void logprob_merge_kernel(Args a) {
     if (tid == i) mine = won;
     if (tid == winner) key = ++next < top ? keys[tid * top + next] : 0;
   }
-  if (tid < top) write_top(a, row, total, tid, mine);
+  if (tid < top) write_top(a, row, total, total_ln, tid, mine);
 }
 
 }  // namespace
 
-// Splits of a row: about three workgroups per compute unit (64 fp32 rows of 131,072 tokens with
-// 20 alternatives 21.4 us with two, 22.6 with three, 23.5 with four; 128 bf16 rows with 5 19.6,
-// 20.1, 19.1; 300 33.9, 29.3, 28.9), each of 8,192 tokens at least (8 rows 17.4 us, of 2,048
-// tokens 19.9).
-int logprob_splits(int32_t rows, int32_t vocab, int cus) {
-  const int64_t vectors = (int64_t(vocab) + 7) / 8;
-  const int64_t most = std::min<int64_t>(kLogprobsMaxSplits, (vectors + 1023) / 1024);
-  return int(std::max<int64_t>(1, std::min(most, int64_t(3) * cus / std::max(rows, 1))));
+// Parts that lanes hold: a row of up to eight vectors a lane in one workgroup (500 bf16 rows of
+// 16,000 tokens with 20 alternatives 11.7 us, in two of four vectors 15.1), others with four
+// vectors a lane or more (a row of 131,072 12.0 us with one or two, 11.6 with four, 12.8 with
+// eight; 48 rows of 100,003 14.4, 14.3, 13.9, 16.3) in up to about four workgroups per compute
+// unit (128 rows of 131,072 19.8 us in 4, 22.4 in 6, 20.9 read past; 200 of 100,000 22.9, 27.3).
+// Longer ones are read past: three workgroups per compute unit, of 8,192 tokens or more (300 rows
+// 28.0 us with three or four, 33.9 with two).
+LogprobSplit logprob_split(int32_t rows, int32_t vocab, bool f32, int cus) {
+  const int64_t vectors = int64_t(vocab) / (f32 ? 4 : 8), row = (vectors + kThreads - 1) / kThreads;   // of a lane
+  const int64_t lanes = int64_t(4) * cus * kThreads, fair = (vectors * rows + lanes - 1) / lanes;
+  const int64_t held = row <= kHeld ? std::max<int64_t>(1, row) : std::max<int64_t>(4, fair);
+  const int64_t parts = std::max<int64_t>(1, (row + held - 1) / held);
+  if (held <= kHeld && parts <= kLogprobsMaxSplits) return {int(parts), int(held)};
+  const int64_t most = std::min<int64_t>(kLogprobsMaxSplits, ((int64_t(vocab) + 7) / 8 + 1023) / 1024);
+  return {int(std::max<int64_t>(1, std::min(most, int64_t(3) * cus / std::max(rows, 1)))), 0};
 }
 
 size_t logprob_workspace_bytes(int32_t rows, int32_t top, int splits) {
   return splits <= 1 ? 0 : size_t(rows) * size_t(splits) * (sizeof(RowStats) + size_t(top) * sizeof(uint64_t));
 }
 
-hipError_t launch_logprobs(const LogprobRows& r, int splits, void* workspace, hipStream_t stream, hipEvent_t ev_start,
-                           hipEvent_t ev_stop) {
+namespace {
+
+template <typename T, bool kTop>
+void launch_rows(const Args& a, int held, dim3 grid, hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop) {
+  const dim3 block(kThreads);
+  if (held == 0) hipExtLaunchKernelGGL((logprob_kernel<T, kTop>), grid, block, 0, stream, ev_start, ev_stop, 0, a);
+  else if (held <= 2)
+    hipExtLaunchKernelGGL((logprob_held_kernel<T, kTop, 2>), grid, block, 0, stream, ev_start, ev_stop, 0, a);
+  else if (held <= 4)
+    hipExtLaunchKernelGGL((logprob_held_kernel<T, kTop, 4>), grid, block, 0, stream, ev_start, ev_stop, 0, a);
+  else
+    hipExtLaunchKernelGGL((logprob_held_kernel<T, kTop, kHeld>), grid, block, 0, stream, ev_start, ev_stop, 0, a);
+}
+
+}  // namespace
+
+hipError_t launch_logprobs(const LogprobRows& r, LogprobSplit split, void* workspace, hipStream_t stream,
+                           hipEvent_t ev_start, hipEvent_t ev_stop) {
   if (r.rows <= 0) return hipSuccess;
-  if (r.top > kLogprobsMaxTop || splits > kLogprobsMaxSplits) return hipErrorInvalidValue;
+  const int splits = split.splits;
+  if (r.top > kLogprobsMaxTop || splits > kLogprobsMaxSplits || split.held > kHeld) return hipErrorInvalidValue;
   Args a;
   a.r = r;
   a.c = r.scale * kLog2e;
   a.splits = splits;
+  a.per = split.held * kThreads;
   a.stats = static_cast<RowStats*>(workspace);
   a.keys = reinterpret_cast<uint64_t*>(a.stats + (splits > 1 ? int64_t(r.rows) * splits : 0));
   const dim3 grid = grid_of(int64_t(r.rows) * splits), block(kThreads);
   hipEvent_t main_stop = splits > 1 ? nullptr : ev_stop;
   if (r.f32) {
-    if (r.top) hipExtLaunchKernelGGL((logprob_kernel<float, true>), grid, block, 0, stream, ev_start, main_stop, 0, a);
-    else hipExtLaunchKernelGGL((logprob_kernel<float, false>), grid, block, 0, stream, ev_start, main_stop, 0, a);
+    if (r.top) launch_rows<float, true>(a, split.held, grid, stream, ev_start, main_stop);
+    else launch_rows<float, false>(a, split.held, grid, stream, ev_start, main_stop);
   } else {
-    if (r.top) hipExtLaunchKernelGGL((logprob_kernel<uint16_t, true>), grid, block, 0, stream, ev_start, main_stop, 0, a);
-    else hipExtLaunchKernelGGL((logprob_kernel<uint16_t, false>), grid, block, 0, stream, ev_start, main_stop, 0, a);
+    if (r.top) launch_rows<uint16_t, true>(a, split.held, grid, stream, ev_start, main_stop);
+    else launch_rows<uint16_t, false>(a, split.held, grid, stream, ev_start, main_stop);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits <= 1) return e;

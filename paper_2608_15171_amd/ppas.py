@@ -787,12 +787,14 @@ def logprobs_workspace_bytes(n_rows: int, vocab: int, top_k: int = 0) -> int:
 
 
 def _result(t, name, dtype, *shape):
-    """The pointer of an optional result of that type and shape."""
+    """The pointer of an optional result of that type and shape (its device is _here's to check)."""
     if t is None:
         return None
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
-    return _dev(t, name)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 def logprobs(logits, tokens=None, logprob=None, rank=None, entropy=None, top_ids=None, top_logprobs=None, scale: float = 1.0,
@@ -800,12 +802,16 @@ def logprobs(logits, tokens=None, logprob=None, rank=None, entropy=None, top_ids
     """Log probabilities from logits [R, V] (bf16 or fp32, any row stride), times `scale`: into logprob (fp32 [R]) and rank
     (int32 [R]) those of tokens (int32 [R]), into entropy (fp32 [R]) the rows', into top_ids (int32 [R, k]) and top_logprobs
     (fp32 [R, k]) the top k tokens. Results that are None are left out. workspace: see logprobs_workspace_bytes, or None."""
-    if logits.dim() != 2 or (logits.dtype not in _BF16 and logits.dtype != torch.float32) or \
-            (logits.shape[1] > 1 and logits.stride(1) != 1):
+    f32, i32 = torch.float32, torch.int32
+    wide = logits.dtype == f32
+    if logits.dim() != 2 or not (wide or logits.dtype in _BF16):
         raise ValueError(f"logits must be 2-D bf16 or fp32 rows, got {tuple(logits.shape)} {logits.dtype}")
     R, V = logits.shape
-    k = next((t.shape[-1] for t in (top_ids, top_logprobs) if t is not None and t.dim() > 0), 0)
-    f32, i32 = torch.float32, torch.int32
+    row, one = logits.stride()
+    if one != 1 and V > 1:
+        raise ValueError("the rows of logits must be packed")
+    top = top_logprobs if top_ids is None else top_ids
+    k = top.shape[-1] if top is not None and top.dim() > 0 else 0
     tp = _result(tokens, "tokens", i32, R)
     out = LogprobOut(_result(logprob, "logprob", f32, R), _result(rank, "rank", i32, R), _result(entropy, "entropy", f32, R),
                      _result(top_ids, "top_ids", i32, R, k), _result(top_logprobs, "top_logprobs", f32, R, k))
@@ -813,8 +819,8 @@ def logprobs(logits, tokens=None, logprob=None, rank=None, entropy=None, top_ids
         raise ValueError("logits must be a device tensor")
     ws = _dev(workspace, "workspace")
     hs = _here(stream, logits, tokens, logprob, rank, entropy, top_ids, top_logprobs, workspace)
-    st = _lib.ppas_logprobs(logits.data_ptr(), int(logits.dtype == f32), logits.stride(0) if R > 1 else max(logits.stride(0), V),
-                            R, V, float(scale), tp, k, ctypes.byref(out), ws,
+    st = _lib.ppas_logprobs(logits.data_ptr(), int(wide), row if R > 1 else max(row, V), R, V, float(scale), tp, k,
+                            ctypes.byref(out), ws,
                             0 if workspace is None else workspace.nbytes, None if events is None else ctypes.byref(events), hs)
     _check(st, "ppas_logprobs")
 

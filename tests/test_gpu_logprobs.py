@@ -295,3 +295,32 @@ def test_differences_past_fp32(lib, dtype, V):
     x[3, 9] = 2.0 ** 127.9
     case(lib, x, dtype, tokens=[5, 400, 300, 11], top=64, scale=2.0 ** -100)
     case(lib, x, dtype, tokens=[5, 5, 300, 11], top=3, scale=2.0 ** -60)
+
+
+@pytest.mark.parametrize("dtype,V", [("bf16", 16384), ("fp32", 8192), ("bf16", 131072), ("fp32", 131072), ("bf16", 20003)])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_crowded_lanes(lib, dtype, V, top):
+    """All of a few lanes' logits above all others: more candidates than a workgroup has room for."""
+    W = 8 if dtype == "bf16" else 4
+    g = I.rng(13, V)
+    high = np.arange(V) // W % 256 < 80
+    x = np.where(high, 5.0 + g.random((3, V)), -g.random((3, V)))
+    x[1] = np.where(high, 5.0, -1.0)
+    case(lib, x, dtype, top=top)
+    case(lib, np.where(np.arange(V) % 7 == 3, x, -np.inf), dtype, top=top, shift=5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,V", [(1, 8191), (2, 8193), (3, 16385), (1, 262144), (200, 40000), (700, 8000), (90, 65537), (1100, 5000)])
+def test_parts(lib, dtype, rows, V):
+    """Rows about as long as a workgroup holds, and in as many parts as rows and lengths make."""
+    x = 2.0 * I.rng(14, rows, V).normal(size=(rows, V))
+    some = I.rng(15).permutation(rows)[:7]
+    case(lib, x[some], dtype, top=33)
+    if rows > 7:                      # all of them at once: the same, by the 7 that are looked at
+        ppas, step, torch = lib
+        t, exact = logits(lib, x, dtype)
+        tokens = I.rng(16).integers(0, V, rows)
+        got = run(lib, t, tokens, 20)
+        check({k: v[some] for k, v in got.items()}, exact[some], tokens[some], 20, 1.0, f"{rows} rows",
+              width=8 if dtype == "bf16" else 4)

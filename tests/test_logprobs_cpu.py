@@ -43,7 +43,8 @@ def test_workspace():
     f = ppas.logprobs_workspace_bytes
     assert f(0, 1000) == 0 and f(-1, 1000) == 0 and f(4, 0) == 0 and f(4, 1000, 65) == 0 and f(4, (1 << 30) + 1) == 0
     assert f(1, 1000) == 0 and f(4096, 131072) == 0                            # too short, or rows enough, to be split
-    assert f(1, 131072, 0) == 16 * 16 and f(1, 131072, 20) == 16 * (16 + 160) and f(1, 1 << 30, 1) == 64 * 24
+    # parts of 1,024 vectors, of fp32 logits here: half as many tokens
+    assert f(1, 131072, 0) == 32 * 16 and f(1, 131072, 20) == 32 * (16 + 160) and f(1, 1 << 30, 1) == 64 * 24
     assert f(64, 131072, 5) % 64 == 0 and f(64, 131072, 5) > 0
 
 
