@@ -305,6 +305,15 @@ __device__ __forceinline__ void halves(const float (&v)[8], u32x4& hi, u32x4& lo
   }
 }
 
+// g / (1 + e^-g) by t = e^-|g|, whose denominator is within [1, 2]: a reciprocal of one unit
+// in the last place instead of a division's eleven instructions. t is taken 2^32 up, so that
+// it underflows where g t is far below bf16's least.
+__device__ __forceinline__ float silu(float g) {
+  const float up = __builtin_amdgcn_exp2f(fmaf(fabsf(g), -1.4426950408889634f, 32.f)), t = up * 0x1p-32f;
+  const float r = g * __builtin_amdgcn_rcpf(1.f + t);
+  return g < 0.f ? r * t : r;
+}
+
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
@@ -326,13 +335,13 @@ __device__ __forceinline__ void row_store(uint16_t* row, int n, int lim, bool ve
 
 // out = y + (s v) B^T. A workgroup takes a tile and a block of columns; a wave 16 rows and 64
 // columns at a time: of a tile of 64 rows each wave its own rows and all the same columns,
-// whose rows of B they share in LDS, two steps in turn with one barrier each (kWide); of a
-// tile of 16 each wave its own columns and B. The share goes through LDS into the order of
+// whose rows of B they share in LDS (kWide; of up to 32 ranks two steps in turn, with one
+// barrier each); of a tile of 16 each wave its own columns and B. The share goes through LDS into the order of
 // memory, 128 bytes of a row to eight lanes. With the activation a step is 64 gate columns
 // and the up columns of the same features. Up to rank 16 (RS = 0) one instruction takes both
 // numbers of s v against the same B; else RS of 32 ranks each take B once for two.
-// Loads come back in the order in which they were asked for: a step's y and then its B are
-// asked for behind the results of the step before.
+// Loads come back in the order in which they were asked for: the first step's B and y before
+// the share's sums, then a step's y and its B behind the results of the step before.
 constexpr int kSharePitch = 68;   // floats of a row of 64 in LDS
 
 // A barrier that waits for this wave's LDS accesses, but not for its loads and stores.
@@ -346,7 +355,10 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a) {
   constexpr int S = RS ? RS : 1, kParts = RS ? 2 : 1, kHalves = kAct ? 2 : 1;
   constexpr int kChunks = RS ? 4 * RS : 2;      // of eight ranks, in a row of B
   constexpr int kPitch = 8 * kChunks + 8;       // elements of such a row in LDS
-  constexpr int kBufs = kWide ? 2 : 4, kStep = kWide ? 64 : 256;
+    // shared B of more ranks leaves too few workgroups with two buffers (us with two and one: 2,023
+  // rows, rank 128 with the activation 93 and 68, 64 79 and 65; 16,384 of rank 64 309 and 304)
+  constexpr bool kTwice = RS < 2;
+  constexpr int kBufs = kWide ? (kTwice ? 2 : 1) : 4, kStep = kWide ? 64 : 256;
   constexpr int kThreads = kWide ? 256 : 64, kItems = kHalves * 64 * kChunks, kLoads = (kItems + kThreads - 1) / kThreads;
   // a wave's own B is in registers before its share takes its place
   constexpr bool kOver = !kWide && !kAct;
@@ -389,29 +401,6 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a) {
       if (i < kItems) *reinterpret_cast<u32x4*>(&b_stage[buf][i / kChunks * kPitch + 8 * (i % kChunks)]) = raw[j];
     }
   };
-  if (n0 < n1) bring(n0);
-  u32x4 v[S][kParts];
-  if (b) {
-    const float scale = a.c.scale ? a.c.scale[t.adapter] : 1.f;
-    constexpr int kPart = RS ? 32 * RS : 16;
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const int r0 = RS ? 32 * s + 8 * g : 8 * (g & 1);
-      const float* p = a.c.part + (int64_t(t.first) + min(wave_row + col, t.count - 1)) * kPart + r0;
-      f32x4 sum[2] = {};
-      for (int i = 0; i < a.splits; ++i) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) sum[h] += *reinterpret_cast<const f32x4*>(p + int64_t(i) * a.c.T * kPart + 4 * h);
-      }
-      float f[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = r0 + e < R ? scale * sum[e / 4][e % 4] : 0.f;
-      u32x4 hi, lo;
-      halves(f, hi, lo);
-      v[s][0] = RS || g < 2 ? hi : lo;
-      if (RS) v[s][kParts - 1] = lo;
-    }
-  }
   u32x4 old[2][kHalves];
   auto fetch = [&](int i, int n) {
     if (8 * i + sub >= count || n + at >= lim) return;
@@ -419,8 +408,50 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a) {
     old[i][0] = row_load(y, n + at, lim, a.rows_vec);
     if (kAct) old[i][kHalves - 1] = row_load(y + half, n + at, lim, a.rows_vec);
   };
+  if (n0 < n1) bring(n0);
 #pragma unroll
   for (int i = 0; i < 2; ++i) fetch(i, n0);
+  u32x4 v[S][kParts];
+  if (b) {
+    const float scale = a.c.scale ? a.c.scale[t.adapter] : 1.f;
+    constexpr int kPart = RS ? 32 * RS : 16;
+    // several splits' at once: one after the other they wait for each (323 rows of 5,504, rank
+    // 128, 26.8 us against 22.9)
+    constexpr int kAtOnce = S == 1 ? 8 : S == 2 ? 4 : 2;
+    const float* p0 = a.c.part + (int64_t(t.first) + min(wave_row + col, t.count - 1)) * kPart;
+    const int64_t next = int64_t(a.c.T) * kPart;
+    f32x4 sum[S][2] = {};
+    for (int i0 = 0; i0 < a.splits; i0 += kAtOnce) {
+      f32x4 some[kAtOnce][S][2];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            some[i][s][h] = *reinterpret_cast<const f32x4*>(p0 + min(i0 + i, a.splits - 1) * next +
+                                                            (RS ? 32 * s + 8 * g : 8 * (g & 1)) + 4 * h);
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        if (i0 + i >= a.splits) break;
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) sum[s][h] += some[i][s][h];
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const int r0 = RS ? 32 * s + 8 * g : 8 * (g & 1);
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = r0 + e < R ? scale * sum[s][e / 4][e % 4] : 0.f;
+      u32x4 hi, lo;
+      halves(f, hi, lo);
+      v[s][0] = RS || g < 2 ? hi : lo;
+      if (RS) v[s][kParts - 1] = lo;
+    }
+  }
   int buf = kWide ? 0 : wave;
   if (kWide) {
     stage(0);
@@ -477,8 +508,8 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a) {
           for (int w = 0; w < 4; ++w) {
             float x0 = f[0][i][2 * w], x1 = f[0][i][2 * w + 1];
             if (kAct) {
-              x0 = silu_f32(x0) * f[kHalves - 1][i][2 * w];
-              x1 = silu_f32(x1) * f[kHalves - 1][i][2 * w + 1];
+              x0 = silu(x0) * f[kHalves - 1][i][2 * w];
+              x1 = silu(x1) * f[kHalves - 1][i][2 * w + 1];
             }
             done[w] = pack_bf16x2(x0, x1);
           }
@@ -488,7 +519,8 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a) {
       }
     }
     if (kWide && b) {
-      buf ^= 1;
+      if (kTwice) buf ^= 1;
+      else lds_barrier();
       if (n + kStep < n1) stage(buf);
       if (n + 2 * kStep < n1) bring(n + 2 * kStep);
       lds_barrier();
