@@ -625,7 +625,11 @@ hipError_t launch_adapters(const AdapterCall& c, bool act, int cus, hipStream_t 
   // 16,384 of rank 64 439, 315 and 336; 56 decode rows 17.4 at 256, 13.7 at 512
   const int32_t cols = act ? c.n_out / 2 : c.n_out, step = height == 16 ? 256 : 64;
   const int64_t each = int64_t(cols) * a.slots / (4 * int64_t(cus)) / step * step;
-  a.block = int32_t(std::min<int64_t>(std::max<int64_t>(step, each), height == 64 && c.rank <= 16 ? 256 : 512));
+  // more where the start reads more than four such steps' rows of partial sums, but one
+  // workgroup per compute unit (2,023 rows of 11,008 features onto 2,048 columns, rank 64: 40.7 and 35.3)
+  const int64_t start = int64_t(a.splits) * 16 * rank_frags(c.rank) / 4;
+  const int64_t least = std::min<int64_t>(start, int64_t(cols) * a.slots / cus) / step * step;
+  a.block = int32_t(std::min<int64_t>(std::max<int64_t>({step, each, least}), height == 64 && c.rank <= 16 ? 256 : 512));
   a.blocks = int32_t((int64_t(cols) + a.block - 1) / a.block);
   a.rows_vec = on16(c.y) && on16(c.out) && c.y_stride % 8 == 0 && c.out_stride % 8 == 0 && (!act || cols % 8 == 0);
   a.in_place = !act && c.y == c.out && c.y_stride == c.out_stride;
