@@ -699,9 +699,9 @@ size_t ppas_adapter_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t ra
  * token out of range (-1: none given) has logprob NaN and rank -1. Sums are fp32: up to 2^18
  * tokens, a log probability is within 1e-5 plus 2^-21 of the spread of the row's l_i. The
  * order is that of the logits themselves, before any rounding. Outputs may each be NULL, and
- * must not overlap the logits (PPAS_EINVAL) or each other; logprob and rank need tokens_dev. top_k is 0..64
- * (PPAS_EUNSUPPORTED above); scale is 2^-100..2^100; vocab at most 2^30 (PPAS_ERANGE).
- * Few rows are split over workgroups that meet in the workspace
+ * must not overlap the logits (PPAS_EINVAL) or each other; logprob and rank need
+ * tokens_dev. top_k is 0..64 (PPAS_EUNSUPPORTED above); scale is 2^-100..2^100; vocab at
+ * most 2^30 (PPAS_ERANGE). Few rows are split over workgroups that meet in the workspace
  * (ppas_logprobs_workspace_bytes, 16-byte aligned; a smaller one, NULL with 0 bytes
  * included, gives fewer splits), by which the sums' rounding, but no id or rank, may
  * differ. Nothing is allocated or kept; a call may be captured into a HIP graph, and calls

@@ -16,8 +16,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libppas.so")
 
 SOURCES = ["api.cpp", "plan.cpp", "attn_step.hip", "kv_append.hip", "rope_append.hip", "rope.cpp", "rope_rows.hip",
-           "norm_rope.hip", "logprobs.hip", "adapters.hip", "noalloc.hip", "gateup.hip", "gateup_any.hip", "gateup_i8.hip", "int8.hip",
-           "stream_read.hip"]
+           "norm_rope.hip", "logprobs.hip", "adapters.hip", "noalloc.hip", "gateup.hip", "gateup_any.hip",
+           "gateup_i8.hip", "int8.hip", "stream_read.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -14,7 +14,10 @@
 //
 // What bounds them: x for the first, y in and out for the second at many rows (a rank of
 // 16 is 64 operations per element of y); at few rows the adapters' weights, and at one the
-// two launches.
+// two launches. Measured: 16,384 rows of rank 64 from 2,048 features onto 22,016 304 us, 5.0
+// TB/s (the second product 290, a copy of as many bytes 288); 2,056 of rank 32 with the
+// activation 48.5 (136 MB in 39-43, a round of workgroups whose waves wait for their rows 68 %
+// of the time); 64 decode rows with 24 adapters 13.1, one row 8.2 behind its order's 3.6.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
@@ -196,8 +199,7 @@ __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_A
 // Both products bring their operands as 16-byte pieces of whole 128-byte lines, eight lanes
 // to a row, and turn them into operand order in LDS, as they turn the share into the order
 // of y's memory. Straight in the order of the matrix instructions, 64 bytes of a row at a
-// time, 16,384 rows of rank 64 onto 22,016 columns took 754 us where this takes 312 (a copy
-// of as many bytes 288).
+// time, 16,384 rows of rank 64 onto 22,016 columns took 754 us where this takes 304.
 
 // v = x A^T. A workgroup takes a tile of 16 MF rows (half of one of 64), 16 RF ranks and a
 // split of hidden; its waves take 64 features of every 256 and add up through LDS. Each wave
@@ -359,7 +361,8 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a) {
   // rows, rank 128 with the activation 93 and 68, 64 79 and 65; 16,384 of rank 64 309 and 304)
   constexpr bool kTwice = RS < 2;
   constexpr int kBufs = kWide ? (kTwice ? 2 : 1) : 4, kStep = kWide ? 64 : 256;
-  constexpr int kThreads = kWide ? 256 : 64, kItems = kHalves * 64 * kChunks, kLoads = (kItems + kThreads - 1) / kThreads;
+  constexpr int kThreads = kWide ? 256 : 64, kItems = kHalves * 64 * kChunks;
+  constexpr int kLoads = (kItems + kThreads - 1) / kThreads;
   // a wave's own B is in registers before its share takes its place
   constexpr bool kOver = !kWide && !kAct;
   constexpr int kB = kHalves * 64 * kPitch, kShare = 16 * kSharePitch * 2;
@@ -591,8 +594,9 @@ hipError_t launch_adapter_rows(const int32_t* row_adapter, AdapterOrder o, void*
 }
 
 // About two workgroups per compute unit, each of 512 features at least, eight splits at most:
-// every workgroup of the second product adds them up (155 rows of 11,008, rank 64: 31 us with
-// 2, 23 with 4 or 8, 28 with 16, 44 with 32; 2,056 rows of 2,048, rank 32: 54 with 8, 50 with 4).
+// every workgroup of the second product adds them up (155 rows of 11,008, rank 64: 17.8 us with
+// up to 8, 19.9 with 16, 22.4 with 24; 700 of rank 8 15.2, 17.2, 19.0; 2,056 of 2,048 features,
+// rank 32, 50.1 with 4, 53.9 with 8).
 int adapter_splits(int32_t T, int32_t hidden, int32_t adapters, int cus) {
   const int64_t tiles = AdapterOrder{T, adapters}.slots(tile_height(T, adapters));
   const int64_t most = std::min<int64_t>(8, (int64_t(hidden) + 511) / 512);
@@ -621,8 +625,9 @@ hipError_t launch_adapters(const AdapterCall& c, bool act, int cus, hipStream_t 
   a.per = int32_t(((int64_t(c.hidden) + a.splits - 1) / a.splits + 255) / 256 * 256);
   // blocks of columns: whole steps, about four workgroups per compute unit where that leaves
   // as many, up to 512 columns (256 of a small rank, whose B and share cost a start less):
-  // 2,056 rows with the activation take 71 us a step of 64 at a time, 53 at 512, 76 at 1,024;
-  // 16,384 of rank 64 439, 315 and 336; 56 decode rows 17.4 at 256, 13.7 at 512
+  // when the rest was not yet what it is, 2,056 rows with the activation took 71 us a step of
+  // 64 at a time, 53 at 512, 76 at 1,024; 16,384 of rank 64 439, 315 and 336; 56 decode rows
+  // 17.4 at 256, 13.7 at 512
   const int32_t cols = act ? c.n_out / 2 : c.n_out, step = height == 16 ? 256 : 64;
   const int64_t each = int64_t(cols) * a.slots / (4 * int64_t(cus)) / step * step;
   // more where the start reads more than four such steps' rows of partial sums, but one

@@ -475,7 +475,8 @@ struct Part {
 #pragma unroll
     for (int e = 0; e < W; ++e) {
       const int32_t id = edge_vector() * W - shift + e;
-      const uint32_t x = has && id >= 0 && id < vocab ? one[e] : Type<T>::kMasked & (sizeof(T) == 2 ? 0xffffu : 0xffffffffu);
+      constexpr uint32_t none = sizeof(T) == 2 ? Type<T>::kMasked & 0xffffu : Type<T>::kMasked;
+      const uint32_t x = has && id >= 0 && id < vocab ? one[e] : none;
       if constexpr (sizeof(T) == 2) v[e / 2] = e % 2 ? v[e / 2] | (x << 16) : x;
       else v[e] = x;
     }
@@ -494,8 +495,8 @@ __device__ __forceinline__ float largest(const float (&x)[W]) {
 
 // How many logits of a wave's vectors (at: each lane's) come before the given token.
 template <int W>
-__device__ __forceinline__ int count_above(const float (&x)[W], int32_t at, const Given& g, float not_below, int32_t given_at,
-                                           int shift) {
+__device__ __forceinline__ int count_above(const float (&x)[W], int32_t at, const Given& g, float not_below,
+                                           int32_t given_at, int shift) {
   const float past = at < given_at ? not_below : g.x;
   int above = 0;
 #pragma unroll
@@ -540,8 +541,8 @@ __device__ __forceinline__ uint64_t row_bound(const uint64_t* notes, int k, int3
 }
 
 // The first of the waves' candidates in order, to the workspace or the results.
-__device__ __forceinline__ void write_first(const Args& a, int64_t block, int64_t row, const RowStats& s, const List& list,
-                                            const uint64_t* lists, int* counts) {
+__device__ __forceinline__ void write_first(const Args& a, int64_t block, int64_t row, const RowStats& s,
+                                            const List& list, const uint64_t* lists, int* counts) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   if (lane == 0) counts[wave] = list.count;
   __syncthreads();

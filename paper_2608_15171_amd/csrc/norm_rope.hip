@@ -11,7 +11,9 @@
 // held by a group of 1 to 64 lanes of one wave, each with the pairs that it turns: its
 // loads are all in flight before the first sum, the sums go over the group by lane
 // exchanges, and every feature is read and written by one lane only, so that rows may be
-// done in place.
+// done in place. 16,384 rows of a step (16 query and 2 KV heads of 128) take 37.3 us, 4.5 TB/s
+// with the vector units busy 48 % (without norms 33; a copy of as many bytes 33); one row of
+// each of 64 requests 4.6 us on the device.
 //
 // A sum of squares that passes fp32 (features from 1e18 on) is taken again of features
 // times 2^-70, so that every finite head has its finite norm; a head with an infinity or
@@ -310,7 +312,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_rows_kernel(NormRowsArgs a
 // ---------------------------------------------------------------------------
 // A step's rows on their way into the pages, in the workgroups of rope_qkv_append_kernel:
 // for y = 0 the keys and for y = 1 the values of a page's new slots, else the queries of
-// four of them.
+// four of them. (One workgroup for keys and values was the last to end: 16,384 rows 41.5 us.)
 // Keys pass through LDS, two heads at a time: their norm needs a head's lanes side by side,
 // the page's layout (16 slots of each chunk of eight features) the slots.
 // ---------------------------------------------------------------------------
