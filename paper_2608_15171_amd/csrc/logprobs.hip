@@ -896,8 +896,8 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
 }
 
 // The splits of a row. As in a split, a bound that enough keys reach, of the first (or, of
-// few splits, later) places of their lists, leaves few to be ordered by counting; where it
-// leaves many (ascending logits: all the best in one split), a wave takes them one by one,
+// few splits, later) places of their lists, leaves few, and one of their own fewer, to be
+// ordered by counting; where the first leaves many (ascending logits: all the best in one split), a wave takes them one by one,
 // each lane the next of a split's (tokens ascend with the splits, so that the first of equal
 // lanes is next). The last wave joins the sums meanwhile.
 constexpr int kFew = 512;
@@ -908,7 +908,7 @@ __global__ __launch_bounds__(kThreads) void logprob_merge_kernel(Args a) {
   __shared__ uint64_t few[kFew];
   __shared__ RowStats total;
   __shared__ float total_ln;
-  __shared__ int places[kWaves][64], n_few;
+  __shared__ int places[kWaves][64], n_few, n_fewer;
   const int64_t row = block_of();
   if (row >= a.r.rows) return;
   constexpr int kRest = kThreads - 64;
@@ -922,7 +922,7 @@ __global__ __launch_bounds__(kThreads) void logprob_merge_kernel(Args a) {
     const uint64_t* from = a.keys + row * n;
 #pragma unroll 4
     for (int i = tid; i < n; i += kRest) keys[i] = from_global(from + i);
-    if (tid == 0) n_few = 0;
+    if (tid == 0) n_few = n_fewer = 0;
   }
   __syncthreads();
   if (tid >= kRest) {
@@ -942,7 +942,9 @@ __global__ __launch_bounds__(kThreads) void logprob_merge_kernel(Args a) {
     // `lists` of the places 0 .. place hold top keys or more
     const int place = (top - 1) / a.splits, lists = (top + place) / (place + 1);
     const uint64_t head[1] = {lane < a.splits ? keys[lane * top + place] : 0};
-    const uint64_t bound = max(bound_of(head, lists, lists + (a.splits - lists) / 4, a.r.vocab), uint64_t(1));
+    uint64_t bound = 1;
+    if (lists < a.splits) bound = max(bound_of(head, lists, lists + (a.splits - lists) / 4, a.r.vocab), bound);
+    else if (n > kFew) bound = max(bound_of(head, lists, 0, a.r.vocab), bound);   // the least of the heads
     for (int i = tid; i < n; i += kRest) {
       const uint64_t key = keys[i];
       if (key < bound) continue;
@@ -953,8 +955,22 @@ __global__ __launch_bounds__(kThreads) void logprob_merge_kernel(Args a) {
   if (top == 0) return;
   __syncthreads();
   const int m = n_few;
-  if (m <= kFew) {
-    order_keys(few, m, top, places, [&](int i, uint64_t key) { write_top(a, row, total, total_ln, i, key); });
+  auto put = [&](int i, uint64_t key) { write_top(a, row, total, total_ln, i, key); };
+  if (m <= 64) {
+    order_keys(few, m, top, places, put);
+    return;
+  }
+  if (m <= kFew) {   // a bound of their own first (58 rows of 75,816 tokens with
+    // 30 alternatives 17.0 us, without 28)
+    uint64_t some[kFew / 64];
+#pragma unroll
+    for (int i = 0; i < kFew / 64; ++i) some[i] = lane + 64 * i < m ? few[lane + 64 * i] : 0;
+    const uint64_t bound = bound_of(some, top, min(top + top / 4 + 4, 64), a.r.vocab);
+#pragma unroll
+    for (int i = 0; i < kFew / 64; ++i)
+      if (tid == lane + 64 * (i % kWaves) && some[i] >= max(bound, uint64_t(1))) keys[atomicAdd(&n_fewer, 1)] = some[i];
+    __syncthreads();
+    order_keys(keys, n_fewer, top, places, put);
     return;
   }
   if (tid >= 64) return;
@@ -978,7 +994,8 @@ __global__ __launch_bounds__(kThreads) void logprob_merge_kernel(Args a) {
 // 16,000 tokens with 20 alternatives 11.7 us, in two of four vectors 15.1), others with four
 // vectors a lane or more (a row of 131,072 12.0 us with one or two, 11.6 with four, 12.8 with
 // eight; 48 rows of 100,003 14.4, 14.3, 13.9, 16.3) in up to about four workgroups per compute
-// unit (128 rows of 131,072 19.8 us in 4, 22.4 in 6, 20.9 read past; 200 of 100,000 22.9, 27.3).
+// unit (128 rows of 131,072 19.8 us in 4, 22.4 in 6, 20.9 read past; 200 of 100,000 22.9, 27.3;
+// 551 of 24,522, two parts of which would be more than that, 24.0 and, read past, 14.8).
 // Longer ones are read past: three workgroups per compute unit, of 8,192 tokens or more (300 rows
 // 28.0 us with three or four, 33.9 with two).
 LogprobSplit logprob_split(int32_t rows, int32_t vocab, bool f32, int cus) {
@@ -986,7 +1003,8 @@ LogprobSplit logprob_split(int32_t rows, int32_t vocab, bool f32, int cus) {
   const int64_t lanes = int64_t(4) * cus * kThreads, fair = (vectors * rows + lanes - 1) / lanes;
   const int64_t held = row <= kHeld ? std::max<int64_t>(1, row) : std::max<int64_t>(4, fair);
   const int64_t parts = std::max<int64_t>(1, (row + held - 1) / held);
-  if (held <= kHeld && parts <= kLogprobsMaxSplits) return {int(parts), int(held)};
+  if (held <= kHeld && parts <= kLogprobsMaxSplits && (parts == 1 || parts * rows <= int64_t(4) * cus))
+    return {int(parts), int(held)};
   const int64_t most = std::min<int64_t>(kLogprobsMaxSplits, ((int64_t(vocab) + 7) / 8 + 1023) / 1024);
   return {int(std::max<int64_t>(1, std::min(most, int64_t(3) * cus / std::max(rows, 1)))), 0};
 }

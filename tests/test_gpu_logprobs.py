@@ -324,3 +324,16 @@ def test_parts(lib, dtype, rows, V):
         got = run(lib, t, tokens, 20)
         check({k: v[some] for k, v in got.items()}, exact[some], tokens[some], 20, 1.0, f"{rows} rows",
               width=8 if dtype == "bf16" else 4)
+
+
+@pytest.mark.parametrize("V", [75816, 131072, 300000])
+@pytest.mark.parametrize("top", [2, 30, 64])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_join(lib, dtype, top, V):
+    """Parts whose lists hold the first ones in every way: at random, all in one of them, equal ones, few of them not masked."""
+    g = I.rng(17, V)
+    x = np.stack([2.0 * g.normal(size=V), np.arange(V) / V, -np.arange(V) / V, np.full(V, -3.0),
+                  np.where(g.random(V) < 0.5, 2.0 * g.normal(size=V), -np.inf),
+                  np.where(np.arange(V) % (V // 11) == 5, g.normal(size=V), -np.inf),
+                  np.round(2.0 * g.normal(size=V))])
+    case(lib, x, dtype, top=top, scale=0.5)
