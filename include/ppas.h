@@ -625,9 +625,8 @@ size_t ppas_gateup_act_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int3
  * row t with adapter a gets
  *   out[t] = y[t] + scale[a] (x[t] A_a^T) B_a^T
  * on top of the projection's output y (any projection of this library or another, bf16),
- * and a row of no adapter out[t] = y[t]. The product with A is summed in fp32, taken on with
- * 16 bits, summed in fp32 with y and rounded once to bf16 nearest-even. Weights have to be
- * finite.
+ * and a row of no adapter out[t] = y[t]. The product with A is fp32, so is that with B
+ * and its sum with y, which is rounded once to bf16 nearest-even. Weights have to be finite.
  *
  * Rows of one adapter may lie anywhere in a step: ppas_adapter_rows brings the row numbers
  * into the order of their adapters once per step, for every layer and projection that uses

@@ -8,9 +8,9 @@
 // rows of one adapter are what the two products work on:
 //   v = x A^T, fp32 (bf16 matrix instructions, x and A straight from memory in operand
 //     order), split over hidden where tiles are few;
-//   out = y + (s v) B^T: s v is taken as two bf16 numbers, its rounding and the rest, so
-//     that it keeps 16 bits where B's product needs bf16 operands (2^-17 of v; the second
-//     instruction costs nothing beside the rows' bytes).
+//   out = y + (s v) B^T: s v is taken as three bf16 numbers, each the rounding of what the
+//     ones before leave, so that it keeps its 24 bits where B's product needs bf16 operands
+//     (the further instructions cost next to nothing beside the rows' bytes).
 //
 // What bounds them: x for the first, y in and out for the second at many rows (a rank of
 // 16 is 64 operations per element of y); at few rows the adapters' weights, and at one the
@@ -298,19 +298,22 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs a) {
   }
 }
 
-// Two bf16 numbers that are a float but for 2^-17 of it: its rounding, and that of the rest
-// (0 where the first is not finite).
-__device__ __forceinline__ void halves(const float (&v)[8], u32x4& hi, u32x4& lo) {
+// Three bf16 numbers whose sum is a float: its rounding, that of the rest, and the last
+// eight bits (0 and 0 where the first is not finite). Two alone leave 2^-17 of it, which
+// changes the rounding of one result in some thousands against the sum in fp32.
+__device__ __forceinline__ void thirds(const float (&v)[8], u32x4 (&p)[3]) {
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    hi[w] = pack_bf16x2(v[2 * w], v[2 * w + 1]);
-    float rest[2];
+    float rest[2] = {v[2 * w], v[2 * w + 1]};
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float top = __uint_as_float(e ? hi[w] & 0xffff0000u : hi[w] << 16);
-      rest[e] = fabsf(top) < __builtin_inff() ? v[2 * w + e] - top : 0.f;
+    for (int i = 0; i < 3; ++i) {
+      p[i][w] = pack_bf16x2(rest[0], rest[1]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float top = __uint_as_float(e ? p[i][w] & 0xffff0000u : p[i][w] << 16);
+        rest[e] = fabsf(top) < __builtin_inff() ? rest[e] - top : 0.f;
+      }
     }
-    lo[w] = pack_bf16x2(rest[0], rest[1]);
   }
 }
 
@@ -351,8 +354,8 @@ __device__ __forceinline__ void row_store(uint16_t* row, int n, int lim, u32x4 p
 // whose rows of B they share in LDS (kWide; of up to 32 ranks two steps in turn, with one
 // barrier each); of a tile of 16 each wave its own columns and B. The share goes through LDS into the order of
 // memory, 128 bytes of a row to eight lanes. With the activation a step is 64 gate columns
-// and the up columns of the same features. Up to rank 16 (RS = 0) one instruction takes both
-// numbers of s v against the same B; else RS of 32 ranks each take B once for two.
+// and the up columns of the same features. Up to rank 16 (RS = 0) one instruction takes two
+// of the three numbers of s v against the same B; else RS of 32 ranks each take B once for three.
 // Loads come back in the order in which they were asked for: the first step's B and y before
 // the share's sums, then a step's y and its B behind the results of the step before.
 constexpr int kSharePitch = 68;   // floats of a row of 64 in LDS
@@ -363,9 +366,16 @@ __device__ __forceinline__ void lds_barrier() {
   bare_barrier();
 }
 
+// Waves of a SIMD that the compiler has to leave registers for: one more than it does by itself
+// where the three numbers' 24 or 48 registers would cost a wave (16,384 rows of rank 64 319 us
+// without, 308 with; 8,192 of rank 128 onto 22,016 columns 268 and 252). Nothing spills.
+constexpr int up_waves(bool wide, int RS, bool vec, bool act) {
+  return wide && vec && !act ? (RS == 2 ? 5 : RS == 4 ? 4 : 1) : 1;
+}
+
 template <bool kWide, int RS, bool kVec, bool kAct>
-__global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a) {
-  constexpr int S = RS ? RS : 1, kParts = RS ? 2 : 1, kHalves = kAct ? 2 : 1;
+__global__ __launch_bounds__(256, up_waves(kWide, RS, kVec, kAct)) void adapter_up_kernel(AdapterArgs a) {
+  constexpr int S = RS ? RS : 1, kParts = RS ? 3 : 2, kHalves = kAct ? 2 : 1;
   constexpr int kChunks = RS ? 4 * RS : 2;      // of eight ranks, in a row of B
   constexpr int kPitch = 8 * kChunks + 8;       // elements of such a row in LDS
     // shared B of more ranks leaves too few workgroups with two buffers (us with two and one: 2,023
@@ -460,10 +470,15 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a) {
       float f[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = r0 + e < R ? scale * sum[s][e / 4][e % 4] : 0.f;
-      u32x4 hi, lo;
-      halves(f, hi, lo);
-      v[s][0] = RS || g < 2 ? hi : lo;
-      if (RS) v[s][kParts - 1] = lo;
+      u32x4 p[3];
+      thirds(f, p);
+      if (RS) {
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) v[s][i] = p[i];
+      } else {
+        v[s][0] = g < 2 ? p[0] : p[1];
+        v[s][1] = g < 2 ? p[2] : u32x4{0, 0, 0, 0};
+      }
     }
   }
   int buf = kWide ? 0 : wave;
