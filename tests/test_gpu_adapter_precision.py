@@ -78,3 +78,30 @@ def test_the_share_keeps_fp32(lib, act, rank, T, n):
     err = np.abs(got - exact)
     print(f"  worst/tol={float((err / tol).max()):.3f}", flush=True)
     assert (err <= tol).all()
+
+
+@pytest.mark.parametrize("T", [16, 80])
+def test_the_activation_of_every_gate(lib, T):
+    """Rows without an adapter: g and u are y's, exact. silu(g) is within 7 u of its value (its exponent's rounding 1 u of
+    the result, the exponential 2 u, 1 + t 1 u, the reciprocal 2 u and the last product 1 u), the product with u rounds once
+    more, and then bf16's grid decides: a result is off by half of its step at most, and by 8 u of the value beside that.
+    Below 2^-126 fp32's own grid adds to it: e^-|g| is off by up to 2^-150, which |g| < 2^7 and u < 2 bring to 2^-142, and
+    two products' roundings are 2^-150 times u and 2^-150."""
+    gate = np.arange(0x10000, dtype=np.uint16)
+    gate = gate[(gate & 0x7fff) < 0x7f80]                                      # every finite one
+    N = len(gate)
+    u = (0x3f80 + np.arange(T) * (128 // 16) % 128 + np.arange(T) // 16).astype(np.uint16)   # in [1, 2): many roundings of each
+    y = np.concatenate((np.tile(gate, (T, 1)), np.repeat(u[:, None], N, 1)), 1)
+    z = np.zeros
+    print(f"every gate: T={T}", flush=True)
+    got = run(lib, z((T, 8), np.uint16), z((1, 8, 8), np.uint16), z((1, 2 * N, 8), np.uint16), np.ones(1, np.float32), y,
+              np.full(T, -1), N, True)
+    exact = A.silu_gate(R.bf16_bits_to_f64(y))
+    assert np.isfinite(exact).all()
+    big = np.abs(exact) >= 2.0 ** 128 * (1 - 2.0 ** -9)                        # rounds to an infinity
+    assert (np.abs(got[big]) == np.inf).all() and (np.sign(got[big]) == np.sign(exact[big])).all()
+    step = 2.0 ** (np.maximum(np.frexp(exact)[1] - 1, -126) - 7)               # between bf16 numbers at that size
+    lim = step / 2 + 8 * U * np.abs(exact) + 2.0 ** -141
+    err = np.where(big, 0.0, np.abs(np.where(big, 0.0, got) - np.where(big, 0.0, exact)))
+    print(f"  beyond half a step, in u of the value: {float(((err - step / 2) / (U * np.abs(exact) + 2.0 ** -144)).max()):.2f}", flush=True)
+    assert (err <= lim).all(), int((err > lim).sum())
