@@ -160,9 +160,13 @@ __device__ __forceinline__ void normalise(const Raw<kMode>& r, const Head& h, co
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < n; ++i) s += f[i];
-      const float mu = group_sum(s, l.lanes) * per;
+      // A true division, and what its rounding leaves of the sum: features that are near one
+      // another have an exact sum, and then as good as exact differences (equal ones zeros, of
+      // any number; with the sum times a rounded 1 / D, up to 1 for 112 features).
+      const float sum = group_sum(s, l.lanes), mu = sum / float(h.dim);
+      const float rest = fmaf(-mu, float(h.dim), sum) * per;
 #pragma unroll
-      for (int i = 0; i < n; ++i) f[i] = mine(i) ? f[i] - mu : 0.f;
+      for (int i = 0; i < n; ++i) f[i] = mine(i) ? (f[i] - mu) - rest : 0.f;
     }
     float s = 0.f;
 #pragma unroll
