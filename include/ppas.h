@@ -655,12 +655,15 @@ ppas_status ppas_adapter_rows(const int32_t* row_adapter_dev, int32_t n_tokens, 
  * [n_tokens][hidden]; strides are elements between rows, so that parts of fused rows may be
  * given. out may be y with the same stride: rows without an adapter are then not touched;
  * otherwise it must not overlap y, nor ever x (PPAS_EINVAL, as for strides below a row's
- * features). `workspace` is device memory of ppas_adapter_workspace_bytes() on 16 bytes (a
- * smaller one is PPAS_ENOSPACE). Bases and strides on 16 bytes with hidden, rank and n_out
+ * features). `workspace` is device memory of ppas_adapter_workspace_bytes() on 16 bytes. That is
+ * not the largest for the most rows: few rows split hidden further. A smaller one gives
+ * fewer splits (one made for a server's largest step serves all of them), down to n_tokens
+ * times the rank, rounded up to 16, 32, 64 or 128, in fp32; below that PPAS_ENOSPACE. Bases and strides on 16 bytes with hidden, rank and n_out
  * that are multiples of 8 are faster. Two launches (events: start on the first, stop on the
  * last); nothing is allocated or kept, and calls may be captured into a HIP graph; calls
  * that share a workspace must not run at once. A row's result may differ in the rounding
- * of its sums with n_tokens and n_adapters, on which the split of hidden depends.
+ * of its sums with n_tokens, n_adapters and the workspace, on which the split of hidden
+ * depends.
  * n_tokens == 0 is a no-op, above 2^24 PPAS_ERANGE.
  */
 ppas_status ppas_adapter_add(const ppas_adapters* set, const void* x, int64_t x_stride, const void* y, int64_t y_stride,
@@ -678,6 +681,7 @@ ppas_status ppas_adapter_act(const ppas_adapters* set, const void* x, int64_t x_
                              void* out, int64_t out_stride, int32_t n_tokens, const void* rows, size_t rows_bytes,
                              void* workspace, size_t workspace_bytes, const ppas_events* events, void* hip_stream);
 
+/* The most workspace that such a call can use on the current device. */
 size_t ppas_adapter_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t rank, int32_t n_adapters);
 
 /*

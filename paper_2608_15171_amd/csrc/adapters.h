@@ -49,9 +49,11 @@ struct AdapterCall {
   int32_t T, hidden, n_out, rank, adapters;
   const void* rows;
   float* part;          // the rows' products with A: [splits][T][rank, padded]
+  int32_t splits;       // of hidden: up to adapter_splits
 };
+// Splits that are the fastest, and the workspace of so many.
 int adapter_splits(int32_t T, int32_t hidden, int32_t adapters, int cus);
-size_t adapter_workspace_bytes(int32_t T, int32_t hidden, int32_t rank, int32_t adapters, int cus);
+size_t adapter_workspace_bytes(int32_t T, int32_t rank, int splits);
 hipError_t launch_adapters(const AdapterCall& c, bool act, int cus, hipStream_t stream, hipEvent_t ev_start,
                            hipEvent_t ev_stop);
 

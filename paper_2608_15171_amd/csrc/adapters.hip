@@ -631,14 +631,15 @@ int adapter_splits(int32_t T, int32_t hidden, int32_t adapters, int cus) {
   return int(std::max<int64_t>(1, std::min<int64_t>(most, 2 * int64_t(cus) / tiles)));
 }
 
-size_t adapter_workspace_bytes(int32_t T, int32_t hidden, int32_t rank, int32_t adapters, int cus) {
-  return size_t(adapter_splits(T, hidden, adapters, cus)) * size_t(T) * size_t(16 * rank_frags(rank)) * sizeof(float);
+size_t adapter_workspace_bytes(int32_t T, int32_t rank, int splits) {
+  return size_t(splits) * size_t(T) * size_t(16 * rank_frags(rank)) * sizeof(float);
 }
 
 hipError_t launch_adapters(const AdapterCall& c, bool act, int cus, hipStream_t stream, hipEvent_t ev_start,
                            hipEvent_t ev_stop) {
   if (c.T <= 0) return hipSuccess;
-  if (c.rank < 1 || c.rank > kAdapterMaxRank || c.adapters < 1 || c.adapters > kAdaptersMax) return hipErrorInvalidValue;
+  if (c.rank < 1 || c.rank > kAdapterMaxRank || c.adapters < 1 || c.adapters > kAdaptersMax || c.splits < 1)
+    return hipErrorInvalidValue;
   const AdapterOrder o{c.T, c.adapters};
   const int height = tile_height(c.T, c.adapters);
   AdapterArgs a;
@@ -649,7 +650,7 @@ hipError_t launch_adapters(const AdapterCall& c, bool act, int cus, hipStream_t 
   a.tiles = height == 16 ? tiles16 : tiles64;
   a.order = reinterpret_cast<const int32_t*>(tiles64 + o.slots64());
   a.slots = o.slots(height);
-  a.splits = adapter_splits(c.T, c.hidden, c.adapters, cus);
+  a.splits = c.splits;
   a.per = int32_t(((int64_t(c.hidden) + a.splits - 1) / a.splits + 255) / 256 * 256);
   // blocks of columns: whole steps, about four workgroups per compute unit where that leaves
   // as many, up to 512 columns (256 of a small rank, whose B and share cost a start less):

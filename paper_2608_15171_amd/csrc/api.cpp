@@ -896,14 +896,16 @@ ppas_status adapter_call(const ppas_adapters* set, const void* x, int64_t x_stri
       overlap(out, out_bytes, x, span_bytes(n_tokens, x_stride, set->hidden)))
     return PPAS_EINVAL;
   if (rows_bytes < AdapterOrder{n_tokens, set->n_adapters}.bytes()) return PPAS_ENOSPACE;
+  // a buffer that is kept for steps of any size may hold fewer splits than this one would take
+  const size_t fit = workspace_bytes / adapter_workspace_bytes(n_tokens, set->rank, 1);
+  if (fit == 0) return PPAS_ENOSPACE;
   const DeviceInfo dev = current_device();
   if (!dev.gfx950) return PPAS_EUNSUPPORTED;
-  if (workspace_bytes < adapter_workspace_bytes(n_tokens, set->hidden, set->rank, set->n_adapters, dev.cus))
-    return PPAS_ENOSPACE;
+  const int splits = int(std::min<size_t>(fit, size_t(adapter_splits(n_tokens, set->hidden, set->n_adapters, dev.cus))));
   const AdapterCall c{static_cast<const uint16_t*>(set->a), static_cast<const uint16_t*>(set->b), set->scale,
                       static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(y), static_cast<uint16_t*>(out),
                       x_stride, y_stride, out_stride, n_tokens, set->hidden, set->n_out, set->rank, set->n_adapters,
-                      rows, static_cast<float*>(workspace)};
+                      rows, static_cast<float*>(workspace), splits};
   const hipError_t e = launch_adapters(c, act, dev.cus, static_cast<hipStream_t>(hip_stream), ev_of(events, 0),
                                        ev_of(events, 1));
   return e == hipSuccess ? PPAS_OK : PPAS_EHIP;
@@ -938,7 +940,7 @@ ppas_status ppas_adapter_rows(const int32_t* row_adapter_dev, int32_t n_tokens, 
 size_t ppas_adapter_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t rank, int32_t n_adapters) {
   if (check_adapter_sizes(n_tokens, hidden, rank, n_adapters) != PPAS_OK || n_tokens == 0) return 0;
   try {
-    return adapter_workspace_bytes(n_tokens, hidden, rank, n_adapters, current_device().cus);
+    return adapter_workspace_bytes(n_tokens, rank, adapter_splits(n_tokens, hidden, n_adapters, current_device().cus));
   } catch (...) {
     return 0;
   }

@@ -773,7 +773,8 @@ def _adapt(fn, what, adapters, x, y, out, rows, per, workspace, events, stream):
 
 def adapter_add(adapters: Adapters, x, y, out, rows: AdapterRows, workspace, events: Events | None = None, stream=None) -> None:
     """out = y with the adapters' share of its rows: x [T, hidden] the projection's input, y and out [T, n_out] (bf16 rows at
-    any stride; out may be y). workspace: a device buffer of adapter_workspace_bytes."""
+    any stride; out may be y). workspace: a device buffer of adapter_workspace_bytes; one made for a larger step serves a
+    smaller one too."""
     _adapt(_lib.ppas_adapter_add, "ppas_adapter_add", adapters, x, y, out, rows, 1, workspace, events, stream)
 
 

@@ -77,6 +77,14 @@ def test_workspace():
     assert f(1, 2048, 16, 8) == 4 * 64 and f(16384, 2048, 64, 4) % (16384 * 256) == 0
 
 
+@pytest.mark.parametrize("act", [False, True])
+@pytest.mark.parametrize("rank,padded", [(1, 16), (16, 16), (17, 32), (33, 64), (65, 128), (128, 128)])
+def test_workspace_holds_a_split(act, rank, padded):
+    """The least that a call takes: the rows' products with A once."""
+    assert call(act, adapters=make(rank=rank), ws_bytes=8 * padded * 4 - 1) == N
+    assert call(act, adapters=make(rank=rank), ws_bytes=0) == N
+
+
 def test_binding_refusals(monkeypatch):
     t, BF = torch.zeros, torch.bfloat16
     monkeypatch.setattr(ppas, "_dev", lambda v, name: None if v is None else 64)
