@@ -302,8 +302,8 @@ typedef struct ppas_head_norm {
 /*
  * As ppas_rope_rows (without `transposed`) and ppas_rope_qkv_append, of normalised
  * heads: the rows' heads, or a step's queries and keys, each with their norm. Values are
- * copied as they are. PPAS_EINVAL also for a norm that is NULL or out of range; the
- * outputs must not overlap the weights. Weights on 16 bytes with a head_stride that is a
+ * copied as they are. PPAS_EINVAL also for a norm that is NULL or out of range, and for
+ * outputs (the pools whole) that overlap the weights. Weights on 16 bytes with a head_stride that is a
  * multiple of 8 are faster.
  */
 ppas_status ppas_norm_rope_rows(const ppas_head_norm* norm, const ppas_rope* rope, const void* x, int64_t x_stride,
@@ -632,7 +632,7 @@ size_t ppas_gateup_act_i8_workspace_bytes(int32_t n_tokens, int32_t hidden, int3
  * into the order of their adapters once per step, for every layer and projection that uses
  * as many adapters. row_adapter_dev [n_tokens] holds the rows' adapters; -1, like every
  * number outside 0..n_adapters - 1, is a row without one. `rows` is device memory of
- * ppas_adapter_rows_bytes(n_tokens, n_adapters) on 16 bytes; the calls that read it have to
+ * ppas_adapter_rows_bytes(n_tokens, n_adapters) on 16 bytes, not over row_adapter_dev; the calls that read it have to
  * be given the n_tokens and adapters it was made for (others' results are undefined, but
  * stay inside the call's rows) and must come behind it on their stream.
  */
@@ -654,8 +654,8 @@ ppas_status ppas_adapter_rows(const int32_t* row_adapter_dev, int32_t n_tokens, 
  * The adapters' share added to y [n_tokens][n_out], x being the projection's input
  * [n_tokens][hidden]; strides are elements between rows, so that parts of fused rows may be
  * given. out may be y with the same stride: rows without an adapter are then not touched;
- * otherwise it must not overlap y, nor ever x (PPAS_EINVAL, as for strides below a row's
- * features). `workspace` is device memory of ppas_adapter_workspace_bytes() on 16 bytes. That is
+ * otherwise it must not overlap y, nor ever x, the set or `rows`; the workspace must not
+ * overlap any of these (PPAS_EINVAL, as for strides below a row's features). `workspace` is device memory of ppas_adapter_workspace_bytes() on 16 bytes. That is
  * not the largest for the most rows: few rows split hidden further. A smaller one gives
  * fewer splits (one made for a server's largest step serves all of them), down to n_tokens
  * times the rank, rounded up to 16, 32, 64 or 128, in fp32; below that PPAS_ENOSPACE. Bases and strides on 16 bytes with hidden, rank and n_out

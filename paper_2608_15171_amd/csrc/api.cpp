@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <utility>
@@ -334,6 +335,18 @@ bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
   return x < y ? y - x < a_bytes : x - y < b_bytes;
 }
 
+// Memory that a call reads or writes; of a pointer that is NULL, none.
+struct Span {
+  const void* at;
+  uint64_t bytes;
+};
+bool over_any(const Span& s, std::initializer_list<Span> others) {
+  if (!s.at || s.bytes == 0) return false;
+  for (const Span& o : others)
+    if (o.at && o.bytes > 0 && overlap(s.at, s.bytes, o.at, o.bytes)) return true;
+  return false;
+}
+
 bool off(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
 
 // T: the step's token rows.
@@ -369,6 +382,10 @@ ppas_status check_norm(const ppas_head_norm* n, int64_t heads, int32_t head_dim)
   if (!n->weight) return PPAS_OK;
   if (off(n->weight, 2) || (n->head_stride != 0 && n->head_stride < head_dim)) return PPAS_EINVAL;
   return n->head_stride > (int64_t(1) << 61) / heads ? PPAS_ERANGE : PPAS_OK;
+}
+
+Span weights_of(const ppas_head_norm& n, int64_t heads, int32_t head_dim) {
+  return {n.weight, span_bytes(heads, n.head_stride, head_dim)};
 }
 
 HeadNorm norm_of(const ppas_head_norm& n) {
@@ -590,6 +607,17 @@ ppas_status check_norms(const Norms* norms, const ppas_shape& s) {
   return st != PPAS_OK ? st : check_norm(norms->k, s.n_kv_heads, kHeadDim);
 }
 
+// A step's outputs over the weights of its norms.
+bool over_weights(const Norms* norms, const ppas_shape& s, const void* q_out, const void* k_pages, const void* v_pages,
+                  int64_t T) {
+  if (!norms) return false;
+  const uint64_t pool = 2 * uint64_t(s.num_pages) * uint64_t(s.n_kv_heads) * uint64_t(s.page_size) * uint64_t(s.head_dim);
+  const uint64_t q_row = uint64_t(s.n_q_heads) * uint64_t(s.head_dim);
+  const Span q{q_out, 2 * uint64_t(T) * q_row}, k{k_pages, pool}, v{v_pages, pool};
+  return over_any(weights_of(*norms->q, s.n_q_heads, s.head_dim), {q, k, v}) ||
+         over_any(weights_of(*norms->k, s.n_kv_heads, s.head_dim), {q, k, v});
+}
+
 ppas_status qkv_append_planned(const ppas_step_plan* plan, const Norms* norms, const ppas_rope* rope,
                                const ppas_qkv* rows, void* q_out, void* k_pages, void* v_pages,
                                const int32_t* block_table_dev, const ppas_events* events, void* hip_stream) {
@@ -603,6 +631,7 @@ ppas_status qkv_append_planned(const ppas_step_plan* plan, const Norms* norms, c
     if (plan->n_seqs == 0) return rope_table(rope, kHeadDim, table);
     st = check_qkv(plan->shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, plan->n_rows, table);
     if (st != PPAS_OK) return st;
+    if (over_weights(norms, plan->shape, q_out, k_pages, v_pages, plan->n_rows)) return PPAS_EINVAL;
     if (capturing(hip_stream)) return PPAS_EUNSUPPORTED;
     return run_qkv_append(*plan, table, norms, *rows, q_out, k_pages, v_pages, block_table_dev, events, hip_stream);
   } catch (...) {
@@ -900,8 +929,16 @@ ppas_status adapter_call(const ppas_adapters* set, const void* x, int64_t x_stri
   const size_t fit = workspace_bytes / adapter_workspace_bytes(n_tokens, set->rank, 1);
   if (fit == 0) return PPAS_ENOSPACE;
   const DeviceInfo dev = current_device();
-  if (!dev.gfx950) return PPAS_EUNSUPPORTED;
   const int splits = int(std::min<size_t>(fit, size_t(adapter_splits(n_tokens, set->hidden, set->n_adapters, dev.cus))));
+  const uint64_t n = uint64_t(set->n_adapters), r = uint64_t(set->rank);
+  const Span weights_a{set->a, 2 * n * r * uint64_t(set->hidden)}, weights_b{set->b, 2 * n * r * uint64_t(set->n_out)},
+      scale{set->scale, 4 * n}, order{rows, AdapterOrder{n_tokens, set->n_adapters}.bytes()},
+      work{workspace, adapter_workspace_bytes(n_tokens, set->rank, splits)}, result{out, out_bytes};
+  if (over_any(result, {weights_a, weights_b, scale, order, work}) ||
+      over_any(work, {weights_a, weights_b, scale, order, {x, span_bytes(n_tokens, x_stride, set->hidden)},
+                      {y, span_bytes(n_tokens, y_stride, set->n_out)}}))
+    return PPAS_EINVAL;
+  if (!dev.gfx950) return PPAS_EUNSUPPORTED;
   const AdapterCall c{static_cast<const uint16_t*>(set->a), static_cast<const uint16_t*>(set->b), set->scale,
                       static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(y), static_cast<uint16_t*>(out),
                       x_stride, y_stride, out_stride, n_tokens, set->hidden, set->n_out, set->rank, set->n_adapters,
@@ -928,6 +965,7 @@ ppas_status ppas_adapter_rows(const int32_t* row_adapter_dev, int32_t n_tokens, 
     if (!row_adapter_dev || !rows || off(row_adapter_dev, 4) || off(rows, 16)) return PPAS_EINVAL;
     const AdapterOrder o{n_tokens, n_adapters};
     if (rows_bytes < o.bytes()) return PPAS_ENOSPACE;
+    if (overlap(rows, o.bytes(), row_adapter_dev, 4 * uint64_t(n_tokens))) return PPAS_EINVAL;   // read twice
     if (!current_device().gfx950) return PPAS_EUNSUPPORTED;
     const hipError_t e = launch_adapter_rows(row_adapter_dev, o, rows, static_cast<hipStream_t>(hip_stream),
                                              ev_of(events, 0), ev_of(events, 1));
@@ -1129,6 +1167,7 @@ ppas_status rope_rows_call(const ppas_head_norm* norm, const ppas_rope* rope, co
     if (!(x == y && x_stride == y_stride) &&
         overlap(x, span_bytes(n_rows, x_stride, row), y, span_bytes(n_rows, y_stride, row)))
       return PPAS_EINVAL;
+    if (norm && over_any(weights_of(*norm, n_heads, head_dim), {{y, span_bytes(n_rows, y_stride, row)}})) return PPAS_EINVAL;
     if (!current_device().gfx950) return PPAS_EUNSUPPORTED;
     const RopeRows r{static_cast<const uint16_t*>(x), static_cast<uint16_t*>(y), x_stride, y_stride, positions_dev,
                      n_rows, n_heads, head_dim, transposed};
@@ -1176,6 +1215,7 @@ ppas_status qkv_append(const ppas_shape* shape, const Norms* norms, const ppas_r
     const int64_t T = int64_t(seqs[n_seqs - 1].query_start) + seqs[n_seqs - 1].n_query;
     st = check_qkv(*shape, rope, rows, q_out, k_pages, v_pages, block_table_dev, T, table);
     if (st != PPAS_OK) return st;
+    if (over_weights(norms, *shape, q_out, k_pages, v_pages, T)) return PPAS_EINVAL;
     if (capturing(hip_stream)) return PPAS_EUNSUPPORTED;
     // validated above; build only the page-write list
     st = build_plan(p, shape, seqs, n_seqs, nullptr, bt_stride, nullptr, kWantInline, false);

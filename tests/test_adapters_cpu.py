@@ -45,6 +45,22 @@ def test_refusals(act):
     assert call(act, rows_bytes=ppas._lib.ppas_adapter_rows_bytes(8, 4) - 1) == N
 
 
+@pytest.mark.parametrize("act", [False, True])
+def test_results_and_workspace_over_what_is_read(act):
+    """The set at P (a of 16,384 bytes, b of 32,768, four scales), its order, and the workspace's one split of 512 bytes at least."""
+    rows, ws, x, y, out = 1 << 21, 1 << 22, 1 << 24, 1 << 26, 1 << 28
+    order = ppas._lib.ppas_adapter_rows_bytes(8, 4)
+    far = 1 << 30
+    for kw in (dict(out=P), dict(out=P + 32766), dict(adapters=make(b=far, scale=far), out=P + 16382),
+               dict(adapters=make(a=far, b=far), out=P + 14), dict(out=P - 2), dict(out=rows), dict(out=rows + (order - 1) // 2 * 2),
+               dict(out=ws), dict(out=ws + 510), dict(ws=P), dict(ws=P + 32752), dict(ws=rows), dict(ws=x), dict(ws=x + 2 * 1008),
+               dict(ws=x - 496), dict(ws=y + 2 * 2032), dict(ws=out), dict(rows=ws)):
+        assert call(act, **kw) == E, kw
+    f = ppas._lib.ppas_adapter_rows
+    assert f(rows, 8, 4, rows, 1 << 20, None, None) == E and f(rows + order - 4, 8, 4, rows, 1 << 20, None, None) == E
+    assert f(rows - 28, 8, 4, rows, 1 << 20, None, None) == E
+
+
 def test_only_the_activation_needs_halves():
     assert call(True, adapters=make(out=255)) == E
     # in place is for the sum

@@ -71,6 +71,21 @@ def test_append_refusals():
     assert f(None, ref(ok), ref(ok), ref(ppas.rope()), None, None, None, None, None, None, None) == E
 
 
+def test_outputs_over_the_weights():
+    """Rows: y of 4 rows of 256 features at 1 << 30. A step: q_out of 21 rows of 2,048, pools of 100 pages of 4,096."""
+    y = 1 << 30
+    for stride, at in ((0, y), (0, y - 254), (0, y + 2 * 1023), (128, y - 510), (1000, y - 2254)):
+        assert rows_call(ppas.HeadNorm(at, stride, 1e-6, 0.0, 0)) == E, (stride, at)
+    ok = ppas.HeadNorm(W, 0, 1e-6, 0.0, 0)
+    q, kp, vp = 1 << 30, 1 << 31, 1 << 32
+    pool = 100 * 4096 * 2
+    for at in (q, q - 254, q + 2 * (21 * 2048 - 1), kp, kp + pool - 2, kp - 2, vp, vp + pool - 2):
+        bad = ppas.HeadNorm(at, 0, 1e-6, 0.0, 0)
+        assert append_call(bad, ok) == E and append_call(ok, bad) == E, at
+    assert append_call(ppas.HeadNorm(q - 16 * 256, 128, 1e-6, 0.0, 0), ok, q_out=q - 2) == E
+    assert append_call(ok, ppas.HeadNorm(kp - 2 * 1024 - 254, 1024, 1e-6, 0.0, 0)) == E
+
+
 def test_binding_takes_bf16_weights(monkeypatch):
     for w in (torch.zeros(128), torch.zeros(128, dtype=torch.float16), torch.zeros((2, 2, 128), dtype=BF),
               torch.zeros((128, 2), dtype=BF).t(), torch.zeros(256, dtype=BF)[::2], torch.zeros((), dtype=BF)):
