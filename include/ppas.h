@@ -700,8 +700,9 @@ size_t ppas_adapter_workspace_bytes(int32_t n_tokens, int32_t hidden, int32_t ra
  * A logit of -infinity has probability 0 and adds nothing. A row with a NaN, a +infinity or
  * nothing but -infinity has no distribution: its results are NaN, its ids and ranks -1. A
  * token out of range (-1: none given) has logprob NaN and rank -1. Sums are fp32: up to 2^18
- * tokens, a log probability is within 1e-5 plus 2^-21 of the spread of the row's l_i. The
- * order is that of the logits themselves, before any rounding. Outputs may each be NULL, and
+ * tokens, a log probability is within 2e-5 + 2^-20 D + 2^-22 of its own size, D the spread of
+ * the row's l_i that are not masked, counted up to 104 (what is further down adds nothing).
+ * The order is that of the logits themselves, before any rounding. Outputs may each be NULL, and
  * must not overlap the logits (PPAS_EINVAL) or each other; logprob and rank need
  * tokens_dev. top_k is 0..64 (PPAS_EUNSUPPORTED above); scale is 2^-100..2^100; vocab at
  * most 2^30 (PPAS_ERANGE). Few rows are split over workgroups that meet in the workspace
