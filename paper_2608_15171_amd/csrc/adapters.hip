@@ -14,10 +14,12 @@
 //
 // What bounds them: x for the first, y in and out for the second at many rows (a rank of
 // 16 is 64 operations per element of y); at few rows the adapters' weights, and at one the
-// two launches. Measured: 16,384 rows of rank 64 from 2,048 features onto 22,016 304 us, 5.0
-// TB/s (the second product 290, a copy of as many bytes 288); 2,056 of rank 32 with the
-// activation 48.5 (136 MB in 39-43, a round of workgroups whose waves wait for their rows 68 %
-// of the time); 64 decode rows with 24 adapters 13.1, one row 8.2 behind its order's 3.6.
+// two launches. Measured: 16,384 rows of rank 64 from 2,048 features onto 22,016 308-311 us, 4.9
+// TB/s (the second product 293-308, a copy of as many bytes 288); 2,056 of rank 32 with the
+// activation 50.5 (136 MB in 43-46: waves wait for their rows 65 % of the time, and of 1,131
+// workgroups a compute unit holds four, so that a tenth of them start when others end); 64
+// decode rows with 24 adapters 13.4, one row 8.2 behind its order's 3.6. Orders of 16,384
+// rows take 29 us where they lie in runs of one adapter, up to 374 where 1,024 adapters mix.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
@@ -180,7 +182,7 @@ __device__ __forceinline__ int32_t row_of(const AdapterArgs& a, const AdapterTil
 
 // Sixteen bytes from any element on: global memory needs no alignment, and rows of odd lengths
 // and strides are as fast as others but for the lines that they cross (5,933
-// rows onto 3,247 columns, rank 32, 58 us, element by element 92; onto 9,235, rank 114, 229 and 469).
+// rows onto 3,247 columns, rank 32, 56 us, element by element 92; 6,181 onto 9,235, rank 114, 206 and 469).
 typedef u32x4 AnyVec __attribute__((aligned(2)));
 
 // Eight elements of a row of n, from element k on: zeros past its end. kVec: n is a multiple of 8.
@@ -206,7 +208,7 @@ __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_A
 // Both products bring their operands as 16-byte pieces of whole 128-byte lines, eight lanes
 // to a row, and turn them into operand order in LDS, as they turn the share into the order
 // of y's memory. Straight in the order of the matrix instructions, 64 bytes of a row at a
-// time, 16,384 rows of rank 64 onto 22,016 columns took 754 us where this takes 304.
+// time, 16,384 rows of rank 64 onto 22,016 columns took 754 us where this takes 310.
 
 // v = x A^T. A workgroup takes a tile of 16 MF rows (half of one of 64), 16 RF ranks and a
 // split of hidden; its waves take 64 features of every 256 and add up through LDS. Each wave
@@ -382,8 +384,8 @@ __global__ __launch_bounds__(256, up_waves(kWide, RS, kVec, kAct)) void adapter_
   constexpr int S = RS ? RS : 1, kParts = RS ? 3 : 2, kHalves = kAct ? 2 : 1;
   constexpr int kChunks = RS ? 4 * RS : 2;      // of eight ranks, in a row of B
   constexpr int kPitch = 8 * kChunks + 8;       // elements of such a row in LDS
-    // shared B of more ranks leaves too few workgroups with two buffers (us with two and one: 2,023
-  // rows, rank 128 with the activation 93 and 68, 64 79 and 65; 16,384 of rank 64 309 and 304)
+  // shared B of more ranks leaves too few workgroups with two buffers (us with two and one: 2,023
+  // rows, rank 128 with the activation 99 and 70, 64 81 and 66; 16,384 of rank 64 318 and 310)
   constexpr bool kTwice = RS < 2;
   constexpr int kBufs = kWide ? (kTwice ? 2 : 1) : 4, kStep = kWide ? 64 : 256;
   constexpr int kThreads = kWide ? 256 : 64, kItems = kHalves * 64 * kChunks;
@@ -443,8 +445,8 @@ __global__ __launch_bounds__(256, up_waves(kWide, RS, kVec, kAct)) void adapter_
   if (b) {
     const float scale = a.c.scale ? a.c.scale[t.adapter] : 1.f;
     constexpr int kPart = RS ? 32 * RS : 16;
-    // several splits' at once: one after the other they wait for each (323 rows of 5,504, rank
-    // 128, 26.8 us against 22.9)
+    // several splits' loads at once (no difference measured at 323 rows of 5,504, rank 128: 23.4
+    // us, and one split after the other as long)
     constexpr int kAtOnce = S == 1 ? 8 : S == 2 ? 4 : 2;
     const float* p0 = a.c.part + (int64_t(t.first) + min(wave_row + col, t.count - 1)) * kPart;
     const int64_t next = int64_t(a.c.T) * kPart;
@@ -561,7 +563,9 @@ __global__ __launch_bounds__(256, up_waves(kWide, RS, kVec, kAct)) void adapter_
   }
 }
 
-// Rows per tile: 64 where an adapter has 32 or more on average.
+// Rows per tile: 64 where an adapter has 32 or more on average, by the adapters that the set
+// holds: the host does not know which of them a step uses. Few in use of a large set go by 16
+// rows where 64 would do (16,384 rows of rank 64 on one adapter of 1,024 442 us, of four 310).
 int tile_height(int32_t T, int32_t adapters) { return T / adapters >= 32 ? 64 : 16; }
 
 // Frags of 16 ranks that the first product computes: 1, 2, 4 or 8.
@@ -660,7 +664,7 @@ hipError_t launch_adapters(const AdapterCall& c, bool act, int cus, hipStream_t 
   const int32_t cols = act ? c.n_out / 2 : c.n_out, step = height == 16 ? 256 : 64;
   const int64_t each = int64_t(cols) * a.slots / (4 * int64_t(cus)) / step * step;
   // more where the start reads more than four such steps' rows of partial sums, but one
-  // workgroup per compute unit (2,023 rows of 11,008 features onto 2,048 columns, rank 64: 40.7 and 35.3)
+  // workgroup per compute unit (2,023 rows of 11,008 features onto 2,048 columns, rank 64: 41.3 and 36.0)
   const int64_t start = int64_t(a.splits) * 16 * rank_frags(c.rank) / 4;
   const int64_t least = std::min<int64_t>(start, int64_t(cols) * a.slots / cus) / step * step;
   a.block = int32_t(std::min<int64_t>(std::max<int64_t>({step, each, least}), height == 64 && c.rank <= 16 ? 256 : 512));

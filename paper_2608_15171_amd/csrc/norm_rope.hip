@@ -246,7 +246,9 @@ __device__ __forceinline__ void norm_rows(int n_rows, int heads, const Head& h, 
   const int step = kThreads / l.lanes, start = int(threadIdx.x) / l.lanes;
   const int step_row = step / heads, step_head = step % heads;
   int row = start / heads, head = start % heads;
-  // weights of all heads are brought once, those of each with its features
+  // weights of all heads are brought once, those of each where they are used, behind the
+  // store of the head before (16,384 rows of 18 heads 33.0 and 33.9 us, interleaved 33.4 and
+  // 34.6; without weights 32.5, the turn alone 29.7 and 32.6)
   const bool by_head = norm.weight && norm.head_stride != 0;
   Raw<kMode> w;
   if (norm.weight && !by_head) w = fetch_weights<kMode>(norm.weight, h, l);
