@@ -303,8 +303,8 @@ typedef struct ppas_head_norm {
  * As ppas_rope_rows (without `transposed`) and ppas_rope_qkv_append, of normalised
  * heads: the rows' heads, or a step's queries and keys, each with their norm. Values are
  * copied as they are. PPAS_EINVAL also for a norm that is NULL or out of range, and for
- * outputs (the pools whole) that overlap the weights. Weights on 16 bytes with a head_stride that is a
- * multiple of 8 are faster.
+ * outputs (the pools whole) that overlap the weights. Weights on 16 bytes with a
+ * head_stride that is a multiple of 8 are faster.
  */
 ppas_status ppas_norm_rope_rows(const ppas_head_norm* norm, const ppas_rope* rope, const void* x, int64_t x_stride,
                                 void* y, int64_t y_stride, const int32_t* positions_dev, int32_t n_rows,
